@@ -343,6 +343,136 @@ starkv_status starkv_step(starkv_state* st, const starkv_seq* seqs, int32_t nseq
 starkv_status starkv_step_host(starkv_state* st, const starkv_seq* seqs, int32_t nseq,
                                void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Paged cache: many sequences' caches in one pool of pages, where they are
+ * branched, appended to, compressed and attended over.  (The paper has no
+ * counterpart; its compressed caches are what a model decodes over.)
+ *
+ * A page holds page_size tokens of every layer and KV head under one number:
+ *     k, v   bf16  [layer][page][G][page_size][d]   strides of layer and page below
+ * Row r of the table is one sequence of len[r] tokens: token j lies in page
+ * table[r][j / page_size], slot j % page_size.  refs[p] is the number of rows
+ * that hold page p; a page with refs 0 is free.  Entries of a row behind its
+ * pages are neither read nor written.
+ *
+ * Conventions of the calls on it, besides those at the top of this file:
+ * - The caller owns pool, table, lengths and counts (DEVICE memory) and starts
+ *   them with starkv_pages_reset.  They change in stream order: calls that may
+ *   overlap on the GPU must not touch one pool, except that any number may read.
+ * - Rows, counts and lengths are read on the device when the call runs, so that a
+ *   captured call replays with what the arrays hold then.  `rows` may be NULL for
+ *   rows 0 .. n - 1.  A call takes at most 1024 rows (STARKV_ERR_UNSUPPORTED).
+ * - What only the device can see is checked there, latched in the device error
+ *   word (STARKV_ERR_DEVICE from starkv_check_device_error) and leaves memory
+ *   intact.  extend, fork, free and compact are then not carried out at all: too
+ *   few free pages, a row out of range or named twice, a length that does not fit.  A sequence of store or load that does not fit is
+ *   passed over; one of the attention calls has zero outputs and lse -inf.
+ * - Supported: page_size 16, 32, 64, 128 or 256; 1 <= n_pages <= 2^20;
+ *   1 <= n_rows <= 65536; max_pages * page_size <= 2^24.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  void* k;                /* bf16, 16-byte aligned                                      */
+  void* v;
+  int64_t layer_stride;   /* elements between layers, and between the pages of a layer: */
+  int64_t page_stride;    /* multiples of 8; a page of a layer is G * page_size * d     */
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_rows;
+  int32_t max_pages;      /* entries of a table row                                     */
+  int32_t* table;         /* [n_rows][max_pages]                                        */
+  int32_t* len;           /* [n_rows]                                                   */
+  int32_t* refs;          /* [n_pages]                                                  */
+} starkv_pages;
+
+/* Tokens outside the pages: for sequence i of n, the last n_tokens[i] tokens of
+ * its row, token t of layer l and KV head g at k + i seq_stride + l layer_stride +
+ * t token_stride + g head_stride (elements, multiples of 8, not negative), d
+ * contiguous elements; v the same. */
+typedef struct {
+  void* k;                   /* bf16, 16-byte aligned                                  */
+  void* v;                   /* or NULL: keys only                                     */
+  const int32_t* rows;       /* [n] or NULL                                            */
+  const int32_t* n_tokens;   /* [n], 0 .. T, or NULL = T each                          */
+  int32_t n, T;
+  int64_t seq_stride, layer_stride, token_stride, head_stride;
+} starkv_tokens;
+
+/* Queries of the attention calls: for sequence i of n, its row's last n_tokens[i]
+ * tokens, token t and head h at q + i q_seq_stride + t q_token_stride + h
+ * q_head_stride (elements, multiples of 8, not negative), d contiguous elements;
+ * o the same.  What belongs to t >= n_tokens[i] is neither read nor written. */
+typedef struct {
+  const void* q;             /* bf16, 16-byte aligned, post-RoPE                       */
+  void* o;                   /* bf16, 16-byte aligned                                  */
+  float* lse;                /* f32 [n][T][H] natural-log normaliser, or NULL          */
+  const uint64_t* mask;      /* [n][T], tree attention only                            */
+  const int32_t* rows;       /* [n] or NULL                                            */
+  const int32_t* n_tokens;   /* [n], 0 .. T, or NULL = T each                          */
+  int32_t n, T;
+  int64_t q_seq_stride, q_token_stride, q_head_stride;
+  int64_t o_seq_stride, o_token_stride, o_head_stride;
+} starkv_queries;
+
+/* Bytes of workspace for any call below over at most n rows (sequences), and at
+ * most T queries of each. */
+starkv_status starkv_pages_workspace_bytes(const starkv_state* st, const starkv_pages* pages, int32_t n, int32_t T,
+                                           size_t* bytes);
+
+/* Every row empty, every page free. */
+starkv_status starkv_pages_reset(starkv_state* st, const starkv_pages* pages, void* stream);
+
+/* Makes room for n_new[i] >= 0 more tokens of rows[i] (i32 device arrays [n]):
+ * len += n_new.  New pages are the free ones with the lowest numbers, in the order
+ * of the call's rows.  A last page that is partly filled and that another row
+ * holds too (when the call begins) is first copied, its filled slots in every
+ * layer.  The new slots hold what they held; starkv_pages_store fills them. */
+starkv_status starkv_pages_extend(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const int32_t* n_new,
+                                  int32_t n, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Branches: dst[i], an empty row, becomes a copy of src[i] as it is when the call
+ * begins.  deep = 0: it shares src's pages.  deep = 1: it gets pages of its own
+ * (numbers as for extend) and their filled slots are copied. */
+starkv_status starkv_pages_fork(starkv_state* st, const starkv_pages* pages, const int32_t* src, const int32_t* dst, int32_t n,
+                                int32_t deep, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Empties rows: len = 0, and one holder less for each of their pages. */
+starkv_status starkv_pages_free(starkv_state* st, const starkv_pages* pages, const int32_t* rows, int32_t n, void* stream);
+
+/* starkv_compact of every layer where the cache lies: rows[i] (L = seqs[i].L
+ * tokens, which must be its length) keeps the tokens idx and the last w, in that
+ * order, in pages of its own (numbers as for extend, taken before the old pages
+ * are let go; other holders of those keep them): len = B + w.  Reads idx, L,
+ * budget, meta and its strides of seqs, writes meta_out where meta is given; the
+ * other buffers may be NULL.  In the per-KV-head mode group g keeps idx[g]. */
+starkv_status starkv_pages_compact(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const starkv_seq* seqs,
+                                   int32_t nseq, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bit copies of tokens into the pages (store) or out of them (load), layers
+ * [layer0, layer0 + n_layers).  A page that more than one row holds is not
+ * written to (device error). */
+starkv_status starkv_pages_store(starkv_state* st, const starkv_pages* pages, int32_t layer0, int32_t n_layers,
+                                 const starkv_tokens* tokens, void* stream);
+starkv_status starkv_pages_load(starkv_state* st, const starkv_pages* pages, int32_t layer0, int32_t n_layers,
+                                const starkv_tokens* tokens, void* stream);
+
+/* Attention of drafted tokens over a row's cache, one layer.  The last n =
+ * n_tokens[i] <= 64 tokens of the row (L tokens, the drafted ones stored) are a
+ * tree: query t sees the keys j < L - n, and drafted token b where bit b of
+ * mask[i][t] is set (its own bit too, if it is to see itself; bits from n on are
+ * not looked at).  With z_j = q . K[g(h), j] / sqrt(d) over the keys seen,
+ *   o = sum_j softmax_j(z) V[g(h), j],   lse = log sum_j exp(z_j);
+ * a query that sees none has o = 0 and lse = -inf.  K and V that a query does not
+ * see do not reach its output, whatever they hold.  H / G <= 128. */
+starkv_status starkv_tree_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same with a sliding window and sinks: query t, the token at position i = L -
+ * n + t of its row, sees the keys j <= i with j < n_sink or j > i - window
+ * (n_sink, window >= 0; window >= L is plain causal attention).  T = 1 is decoding,
+ * larger T a chunk of a prompt (T <= 1024 * floor(128 / (H / G))). */
+starkv_status starkv_sink_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
+                                    int32_t n_sink, int32_t window, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Reads and clears the state's device error word (synchronises `stream`).
  * Returns STARKV_OK, STARKV_ERR_DEVICE or STARKV_ERR_TIMEOUT. */
 starkv_status starkv_check_device_error(starkv_state* st, void* stream);
@@ -374,7 +504,12 @@ enum {
   STARKV_KERNEL_COMPACT = 4,      /* KV gather (Eq. 11)                                    */
   STARKV_KERNEL_ATTENTION = 5,    /* window-row attention over the past keys (pieces)      */
   STARKV_KERNEL_ATTN_COMBINE = 6, /* merge of its pieces into attn_o / attn_lse            */
-  STARKV_NUM_KERNELS = 7
+  STARKV_KERNEL_PAGE_BOOK = 7,    /* paged cache: tables, counts, free pages               */
+  STARKV_KERNEL_PAGE_COPY = 8,    /* its page copies (extend, deep fork)                   */
+  STARKV_KERNEL_PAGE_GATHER = 9,  /* its compaction (Eq. 11 on pages)                      */
+  STARKV_KERNEL_PAGE_MOVE = 10,   /* tokens into and out of pages                          */
+  STARKV_KERNEL_PAGED_ATTENTION = 11,  /* tree and sink attention                          */
+  STARKV_NUM_KERNELS = 12
 };
 
 /* Kernel timing, a profiling aid.  While `on` is non-zero every kernel launch

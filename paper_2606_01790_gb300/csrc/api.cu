@@ -17,6 +17,8 @@
 #include "attn.cuh"
 #include "common.cuh"
 #include "compact.cuh"
+#include "paged_attn.cuh"
+#include "pages.cuh"
 #include "score.cuh"
 #include "select.cuh"
 
@@ -138,6 +140,11 @@ const char* kernel_range_name(int kind) {
     case STARKV_KERNEL_COMPACT: return "starkv: compaction";
     case STARKV_KERNEL_ATTENTION: return "starkv: window attention (pieces)";
     case STARKV_KERNEL_ATTN_COMBINE: return "starkv: window attention (combine)";
+    case STARKV_KERNEL_PAGE_BOOK: return "starkv: page tables";
+    case STARKV_KERNEL_PAGE_COPY: return "starkv: page copies";
+    case STARKV_KERNEL_PAGE_GATHER: return "starkv: page compaction";
+    case STARKV_KERNEL_PAGE_MOVE: return "starkv: tokens and pages";
+    case STARKV_KERNEL_PAGED_ATTENTION: return "starkv: paged attention";
     default: return "starkv: kernel";
   }
 }
@@ -624,6 +631,7 @@ starkv_status starkv_init_state(const starkv_config* cfg, starkv_state** out, vo
   if (e == cudaSuccess) e = score_configure();
   if (e == cudaSuccess) e = select_configure();
   if (e == cudaSuccess) e = attn_configure();
+  if (e == cudaSuccess) e = pages_configure();
   if (e != cudaSuccess) {
     delete st;
     return set_error(STARKV_ERR_CUDA, "device setup failed: %s", cudaGetErrorString(e));
@@ -1020,6 +1028,9 @@ starkv_status starkv_check_device_error(starkv_state* st, void* stream) {
   if (h & kErrTimeout) return set_error(STARKV_ERR_TIMEOUT, "a bounded device wait ran out");
   if (h & kErrMeta) return set_error(STARKV_ERR_DEVICE, "token metadata outside the patch grid");
   if (h & kErrIndex) return set_error(STARKV_ERR_DEVICE, "a kept index outside the past tokens reached the gather");
+  if (h & kErrRow)
+    return set_error(STARKV_ERR_DEVICE, "a page-table row, length or page number did not fit a paged call");
+  if (h & kErrPool) return set_error(STARKV_ERR_DEVICE, "not enough free pages");
   return STARKV_OK;
 }
 
@@ -1107,3 +1118,380 @@ extern "C" starkv_status starkv_score_layer_noalloc(starkv_state* st, int32_t la
   return run_stages(st, seqs, nseq, layer, 1, kScore | kPool, st->noalloc_scratch, kNoAllocScratchBytes,
                     static_cast<cudaStream_t>(stream));
 }
+
+// ---------------------------------------------------------------------------
+// The paged cache (pages.cu) and the attention over it (paged_attn.cu).
+
+namespace {
+
+starkv_status validate_pages(const starkv_state* st, const starkv_pages* pg) {
+  if (!st) return set_error(STARKV_ERR_INVALID_ARG, "state is NULL");
+  if (!pg) return set_error(STARKV_ERR_INVALID_ARG, "pages is NULL");
+  if (!pg->k || !pg->v || !aligned16(pg->k) || !aligned16(pg->v))
+    return set_error(STARKV_ERR_INVALID_ARG, "pages: k or v NULL or not 16-byte aligned");
+  if (!pg->table || !pg->len || !pg->refs || !aligned4(pg->table) || !aligned4(pg->len) || !aligned4(pg->refs))
+    return set_error(STARKV_ERR_INVALID_ARG, "pages: table, len or refs NULL or not 4-byte aligned");
+  if (pg->n_pages < 1 || pg->n_rows < 1 || pg->max_pages < 1)
+    return set_error(STARKV_ERR_INVALID_ARG, "pages: n_pages, n_rows and max_pages must be >= 1");
+  const int P = pg->page_size;
+  if (P != 16 && P != 32 && P != 64 && P != 128 && P != 256)
+    return set_error(STARKV_ERR_UNSUPPORTED, "pages: page_size must be 16, 32, 64, 128 or 256");
+  if (pg->n_pages > kMaxPages) return set_error(STARKV_ERR_UNSUPPORTED, "pages: n_pages > 2^20");
+  if (pg->n_rows > kMaxTableRows) return set_error(STARKV_ERR_UNSUPPORTED, "pages: n_rows > 65536");
+  if (static_cast<int64_t>(pg->max_pages) * P > (1 << 24))
+    return set_error(STARKV_ERR_UNSUPPORTED, "pages: max_pages * page_size > 2^24");
+  const int64_t one = static_cast<int64_t>(st->cfg.n_kv_heads) * P * kHeadDim, nl = st->cfg.n_layers;
+  const int64_t lim = int64_t(1) << 38;   // (element strides of a TMA map: bytes below 2^40)
+  if (pg->layer_stride < 0 || pg->page_stride < 0 || (pg->layer_stride & 7) || (pg->page_stride & 7) ||
+      pg->page_stride >= lim || pg->layer_stride >= (int64_t(1) << 48))
+    return set_error(STARKV_ERR_INVALID_ARG, "pages: strides must be multiples of 8 elements, not negative");
+  // a page of a layer must not reach into another: layers outside pages, or pages outside layers
+  const bool pages_inside = pg->page_stride >= one && (nl == 1 || pg->layer_stride >= (pg->n_pages - 1) * pg->page_stride + one);
+  const bool layers_inside = (nl == 1 || pg->layer_stride >= one) &&
+                             (pg->n_pages == 1 || pg->page_stride >= (nl - 1) * pg->layer_stride + one);
+  if (!pages_inside && !layers_inside)
+    return set_error(STARKV_ERR_INVALID_ARG, "pages: layer_stride and page_stride let pages overlap");
+  return STARKV_OK;
+}
+
+starkv_status check_rows(int32_t n) {
+  if (n < 0) return set_error(STARKV_ERR_INVALID_ARG, "n is negative");
+  if (n > kMaxCallRows) return set_error(STARKV_ERR_UNSUPPORTED, "more than 1024 rows in one call");
+  return STARKV_OK;
+}
+
+PagesView view_of(const starkv_state* st, const starkv_pages& p) {
+  PagesView v;
+  v.k = static_cast<__nv_bfloat16*>(p.k);
+  v.v = static_cast<__nv_bfloat16*>(p.v);
+  v.layer_stride = p.layer_stride;
+  v.page_stride = p.page_stride;
+  v.table = p.table;
+  v.len = p.len;
+  v.refs = p.refs;
+  v.n_pages = p.n_pages;
+  v.n_rows = p.n_rows;
+  v.max_pages = p.max_pages;
+  v.shift = 0;
+  while ((1 << v.shift) < p.page_size) ++v.shift;
+  v.n_layers = st->cfg.n_layers;
+  v.G = st->cfg.n_kv_heads;
+  return v;
+}
+
+// Workspace of the bookkeeping calls: the plan, then the copy list (a copy needs a
+// new page, so there are never more than pages) or the rows' old
+// pages.
+struct BookWs {
+  size_t list, total;
+};
+
+BookWs book_ws(const starkv_pages& p, int n) {
+  const size_t copies = std::max<size_t>(n, std::min<size_t>(static_cast<size_t>(n) * p.max_pages, p.n_pages));
+  const size_t old_rows = static_cast<size_t>(n) * p.max_pages;
+  BookWs w;
+  w.list = 256;
+  w.total = w.list + align256(std::max(copies * sizeof(int4), old_rows * sizeof(int32_t)));
+  return w;
+}
+
+BookParams book_params(starkv_state* st, const starkv_pages& p, const int32_t* rows, int n, char* ws) {
+  BookParams b;
+  memset(&b, 0, sizeof(b));
+  b.pg = view_of(st, p);
+  b.rows = rows;
+  b.n = n;
+  b.err = st->dev.err;
+  if (ws) {
+    b.plan = reinterpret_cast<PagePlan*>(ws);
+    b.copies = reinterpret_cast<int4*>(ws + 256);
+    b.old_table = reinterpret_cast<int32_t*>(ws + 256);
+  }
+  return b;
+}
+
+starkv_status validate_tokens(const starkv_state* st, int layer0, int nl, const starkv_tokens* t) {
+  if (!t) return set_error(STARKV_ERR_INVALID_ARG, "tokens is NULL");
+  starkv_status s = check_rows(t->n);
+  if (s != STARKV_OK) return s;
+  if (t->T < 0) return set_error(STARKV_ERR_INVALID_ARG, "tokens: T is negative");
+  if (t->T > (1 << 24)) return set_error(STARKV_ERR_UNSUPPORTED, "tokens: T > 2^24");
+  if (layer0 < 0 || nl < 0 || layer0 > st->cfg.n_layers - nl)
+    return set_error(STARKV_ERR_INVALID_ARG, "layer range out of range");
+  if (t->n == 0 || t->T == 0 || nl == 0) return STARKV_OK;
+  if (!t->k || !aligned16(t->k) || !aligned16(t->v))
+    return set_error(STARKV_ERR_INVALID_ARG, "tokens: k NULL, or k or v not 16-byte aligned");
+  if (!aligned4(t->rows) || !aligned4(t->n_tokens))
+    return set_error(STARKV_ERR_INVALID_ARG, "tokens: rows or n_tokens not 4-byte aligned");
+  for (int64_t x : {t->seq_stride, t->layer_stride, t->token_stride, t->head_stride})
+    if (x < 0 || (x & 7)) return set_error(STARKV_ERR_INVALID_ARG, "tokens: strides must be multiples of 8 elements, not negative");
+  return STARKV_OK;
+}
+
+starkv_status move_tokens(starkv_state* st, bool store, const starkv_pages* pages, int32_t layer0, int32_t nl,
+                          const starkv_tokens* t, void* stream) {
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = validate_tokens(st, layer0, nl, t)) != STARKV_OK) return s;
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if (t->n == 0 || t->T == 0 || nl == 0) return STARKV_OK;
+  TokensView v;
+  v.k = static_cast<__nv_bfloat16*>(t->k);
+  v.v = static_cast<__nv_bfloat16*>(t->v);
+  v.rows = t->rows;
+  v.n_tokens = t->n_tokens;
+  v.n = t->n;
+  v.T = t->T;
+  v.layer0 = layer0;
+  v.nlayers = nl;
+  v.seq_stride = t->seq_stride;
+  v.layer_stride = t->layer_stride;
+  v.token_stride = t->token_stride;
+  v.head_stride = t->head_stride;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_MOVE, cs, [&] {
+    return page_move_launch(store, view_of(st, *pages), v, st->num_sms, st->dev.err, cs);
+  }));
+  return STARKV_OK;
+}
+
+constexpr int kMaxRowBlocks = 1024;   // 128-row blocks of one sequence's queries
+
+starkv_status validate_queries(const starkv_state* st, int layer, const starkv_queries* q, bool tree) {
+  if (!q) return set_error(STARKV_ERR_INVALID_ARG, "queries is NULL");
+  starkv_status s = check_rows(q->n);
+  if (s != STARKV_OK) return s;
+  const starkv_config& c = st->cfg;
+  if (layer < 0 || layer >= c.n_layers) return set_error(STARKV_ERR_INVALID_ARG, "layer out of range");
+  const int hg = c.n_heads / c.n_kv_heads;
+  if (hg > 128) return set_error(STARKV_ERR_UNSUPPORTED, "paged attention takes n_heads / n_kv_heads <= 128");
+  if (q->T < 0) return set_error(STARKV_ERR_INVALID_ARG, "queries: T is negative");
+  if (tree && q->T > kMaxDraft) return set_error(STARKV_ERR_UNSUPPORTED, "tree attention takes T <= 64");
+  if (q->T > kMaxRowBlocks * (128 / hg)) return set_error(STARKV_ERR_UNSUPPORTED, "queries: T > 1024 * floor(128 / (H / G))");
+  if (q->n == 0 || q->T == 0) return STARKV_OK;
+  if (!q->q || !q->o || !aligned16(q->q) || !aligned16(q->o))
+    return set_error(STARKV_ERR_INVALID_ARG, "queries: q or o NULL or not 16-byte aligned");
+  if (!aligned4(q->lse) || !aligned4(q->rows) || !aligned4(q->n_tokens))
+    return set_error(STARKV_ERR_INVALID_ARG, "queries: lse, rows or n_tokens not 4-byte aligned");
+  if (tree && (!q->mask || (reinterpret_cast<uintptr_t>(q->mask) & 7)))
+    return set_error(STARKV_ERR_INVALID_ARG, "queries: mask NULL or not 8-byte aligned");
+  for (int64_t x : {q->q_seq_stride, q->q_token_stride, q->q_head_stride, q->o_seq_stride, q->o_token_stride, q->o_head_stride})
+    if (x < 0 || (x & 7)) return set_error(STARKV_ERR_INVALID_ARG, "queries: strides must be multiples of 8 elements, not negative");
+  if ((q->n > 1 && q->o_seq_stride < kHeadDim) || (q->T > 1 && q->o_token_stride < kHeadDim) ||
+      (c.n_heads > 1 && q->o_head_stride < kHeadDim))
+    return set_error(STARKV_ERR_INVALID_ARG, "queries: strides of o let its rows overlap");
+  return STARKV_OK;
+}
+
+size_t paged_attn_ws_bytes(const starkv_state*, int, int) { return 0; }
+
+starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* q, bool tree,
+                              int32_t n_sink, int32_t window, void* workspace, size_t workspace_bytes, void* stream) {
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = validate_queries(st, layer, q, tree)) != STARKV_OK) return s;
+  if (n_sink < 0 || window < 0) return set_error(STARKV_ERR_INVALID_ARG, "n_sink and window must be >= 0");
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if (q->n == 0 || q->T == 0) return STARKV_OK;
+  if ((s = check_ws(st, workspace, workspace_bytes, paged_attn_ws_bytes(st, q->n, q->T))) != STARKV_OK) return s;
+  const starkv_config& c = st->cfg;
+  const PagesView pg = view_of(st, *pages);
+  PagedAttnParams p;
+  memset(&p, 0, sizeof(p));
+  p.k = pg.k + layer * pg.layer_stride;
+  p.v = pg.v + layer * pg.layer_stride;
+  p.page_stride = pg.page_stride;
+  p.table = pg.table;
+  p.len = pg.len;
+  p.n_pages = pg.n_pages;
+  p.n_rows = pg.n_rows;
+  p.max_pages = pg.max_pages;
+  p.shift = pg.shift;
+  p.q = static_cast<const __nv_bfloat16*>(q->q);
+  p.o = static_cast<__nv_bfloat16*>(q->o);
+  p.lse = q->lse;
+  p.mask = q->mask;
+  p.rows = q->rows;
+  p.n_tokens = q->n_tokens;
+  p.n = q->n;
+  p.T = q->T;
+  p.q_seq = q->q_seq_stride;
+  p.q_token = q->q_token_stride;
+  p.q_head = q->q_head_stride;
+  p.o_seq = q->o_seq_stride;
+  p.o_token = q->o_token_stride;
+  p.o_head = q->o_head_stride;
+  p.H = c.n_heads;
+  p.G = c.n_kv_heads;
+  p.tree = tree;
+  p.n_sink = std::min(n_sink, 1 << 25);   // (more than any length)
+  p.window = std::min(window, 1 << 25);
+  p.scale2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kHeadDim)));
+  p.err = st->dev.err;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_ATTENTION, cs, [&] { return paged_attn_launch(p, st->num_sms, cs); }));
+  return STARKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+starkv_status starkv_pages_workspace_bytes(const starkv_state* st, const starkv_pages* pages, int32_t n, int32_t T,
+                                           size_t* bytes) {
+  if (!bytes) return set_error(STARKV_ERR_INVALID_ARG, "bytes is NULL");
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = check_rows(n)) != STARKV_OK) return s;
+  if (T < 0) return set_error(STARKV_ERR_INVALID_ARG, "T is negative");
+  *bytes = std::max(book_ws(*pages, n).total, paged_attn_ws_bytes(st, n, T));
+  return STARKV_OK;
+}
+
+starkv_status starkv_pages_reset(starkv_state* st, const starkv_pages* pages, void* stream) {
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  CUDA_TRY(cudaMemsetAsync(pages->len, 0, static_cast<size_t>(pages->n_rows) * sizeof(int32_t), cs));
+  CUDA_TRY(cudaMemsetAsync(pages->refs, 0, static_cast<size_t>(pages->n_pages) * sizeof(int32_t), cs));
+  return STARKV_OK;
+}
+
+starkv_status starkv_pages_extend(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const int32_t* n_new,
+                                  int32_t n, void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange range("starkv_pages_extend");
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = check_rows(n)) != STARKV_OK) return s;
+  if (n > 0 && (!n_new || !aligned4(n_new) || !aligned4(rows)))
+    return set_error(STARKV_ERR_INVALID_ARG, "n_new NULL, or n_new or rows not 4-byte aligned");
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if ((s = check_ws(st, workspace, workspace_bytes, book_ws(*pages, n).total)) != STARKV_OK) return s;
+  if (n == 0) return STARKV_OK;
+  BookParams b = book_params(st, *pages, rows, n, static_cast<char*>(workspace));
+  b.n_new = n_new;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_BOOK, cs, [&] { return book_launch(kBookExtend, b, nullptr, cs); }));
+  CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_COPY, cs, [&] {
+    return page_copy_launch(b.pg, b.plan, b.copies, n, st->num_sms, cs);
+  }));
+  return STARKV_OK;
+}
+
+starkv_status starkv_pages_fork(starkv_state* st, const starkv_pages* pages, const int32_t* src, const int32_t* dst, int32_t n,
+                                int32_t deep, void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange range("starkv_pages_fork");
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = check_rows(n)) != STARKV_OK) return s;
+  if (n > 0 && (!src || !dst || !aligned4(src) || !aligned4(dst)))
+    return set_error(STARKV_ERR_INVALID_ARG, "src or dst NULL or not 4-byte aligned");
+  if (deep != 0 && deep != 1) return set_error(STARKV_ERR_INVALID_ARG, "deep must be 0 or 1");
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if ((s = check_ws(st, workspace, workspace_bytes, book_ws(*pages, n).total)) != STARKV_OK) return s;
+  if (n == 0) return STARKV_OK;
+  BookParams b = book_params(st, *pages, dst, n, static_cast<char*>(workspace));
+  b.src = src;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_BOOK, cs, [&] { return book_launch(deep ? kBookForkDeep : kBookFork, b, nullptr, cs); }));
+  if (deep) {
+    const int64_t most = std::min<int64_t>(static_cast<int64_t>(n) * pages->max_pages, pages->n_pages);
+    CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_COPY, cs, [&] {
+      return page_copy_launch(b.pg, b.plan, b.copies, most, st->num_sms, cs);
+    }));
+  }
+  return STARKV_OK;
+}
+
+starkv_status starkv_pages_free(starkv_state* st, const starkv_pages* pages, const int32_t* rows, int32_t n, void* stream) {
+  NvtxRange range("starkv_pages_free");
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = check_rows(n)) != STARKV_OK) return s;
+  if (!aligned4(rows)) return set_error(STARKV_ERR_INVALID_ARG, "rows not 4-byte aligned");
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if (n == 0) return STARKV_OK;
+  const BookParams b = book_params(st, *pages, rows, n, nullptr);
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_BOOK, cs, [&] { return book_launch(kBookFree, b, nullptr, cs); }));
+  return STARKV_OK;
+}
+
+starkv_status starkv_pages_compact(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const starkv_seq* seqs,
+                                   int32_t nseq, void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange range("starkv_pages_compact");
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = check_rows(nseq)) != STARKV_OK) return s;
+  if (!aligned4(rows)) return set_error(STARKV_ERR_INVALID_ARG, "rows not 4-byte aligned");
+  if ((s = validate_seqs(st, seqs, nseq, kNeedIdx)) != STARKV_OK) return s;
+  for (int i = 0; i < nseq; ++i) {
+    if (!seqs[i].meta) continue;
+    if (!seqs[i].meta_out) return set_error(STARKV_ERR_INVALID_ARG, "seq %d: meta without meta_out", i);
+    if ((s = validate_seqs(st, seqs + i, 1, kNeedMeta)) != STARKV_OK) return s;
+  }
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if ((s = check_ws(st, workspace, workspace_bytes, book_ws(*pages, nseq).total)) != STARKV_OK) return s;
+  const starkv_config& c = st->cfg;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  if (nseq == 0) return STARKV_OK;
+  const BookParams b = book_params(st, *pages, rows, nseq, static_cast<char*>(workspace));
+  static thread_local BookLens lens;   // 8 KB: kept off the stack
+  for (int i = 0; i < nseq; ++i) {
+    lens.L[i] = seqs[i].L;
+    lens.kept[i] = seqs[i].budget + c.window;
+  }
+  CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_BOOK, cs, [&] { return book_launch(kBookCompact, b, &lens, cs); }));
+  for (int i0 = 0; i0 < nseq; i0 += kMaxBatch) {
+    SeqBatch batch;
+    memset(&batch, 0, sizeof(batch));
+    batch.nseq = std::min(nseq - i0, kMaxBatch);
+    batch.nlayers = c.n_layers;
+    int rows_out = 0;
+    for (int i = 0; i < batch.nseq; ++i) {
+      const starkv_seq& q = seqs[i0 + i];
+      SeqView& v = batch.s[i];
+      v.meta = q.meta;
+      v.meta_layer_stride = q.meta_layer_stride;
+      v.meta_group_stride = q.meta_group_stride;
+      v.L = q.L;
+      v.Lp = q.L - c.window;
+      v.budget = q.budget;
+      v.meta_out = q.meta_out;
+      v.idx = q.idx;
+      rows_out = std::max(rows_out, q.budget + c.window);
+    }
+    CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_GATHER, cs, [&] {
+      return page_gather_launch(b.pg, batch, rows, i0, c.window, c.select_mode == STARKV_SELECT_PER_HEAD, b.plan, b.old_table,
+                                rows_out, st->dev.err, cs);
+    }));
+  }
+  return STARKV_OK;
+}
+
+starkv_status starkv_pages_store(starkv_state* st, const starkv_pages* pages, int32_t layer0, int32_t n_layers,
+                                 const starkv_tokens* tokens, void* stream) {
+  NvtxRange range("starkv_pages_store");
+  return move_tokens(st, true, pages, layer0, n_layers, tokens, stream);
+}
+
+starkv_status starkv_pages_load(starkv_state* st, const starkv_pages* pages, int32_t layer0, int32_t n_layers,
+                                const starkv_tokens* tokens, void* stream) {
+  NvtxRange range("starkv_pages_load");
+  return move_tokens(st, false, pages, layer0, n_layers, tokens, stream);
+}
+
+starkv_status starkv_tree_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange range("starkv_tree_attention");
+  return paged_attention(st, pages, layer, queries, true, 0, 0, workspace, workspace_bytes, stream);
+}
+
+starkv_status starkv_sink_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
+                                    int32_t n_sink, int32_t window, void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange range("starkv_sink_attention");
+  return paged_attention(st, pages, layer, queries, false, n_sink, window, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

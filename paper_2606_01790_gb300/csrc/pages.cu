@@ -1,0 +1,552 @@
+// The paged cache: page tables, reference counts and the copies they call for.
+//
+// A token's keys and values of every layer and KV head lie under one page
+// number; row r of the table lists the pages of a sequence in order and refs[p]
+// counts the rows that hold page p (0: free).  Sharing a page is counting it once
+// more, so that a branch costs a table row; what a row may write it holds alone
+// (the last page is copied before tokens are added to a shared one).
+//
+// k_book: one cluster of eight 1024-thread CTAs.  Every CTA reads the call's rows
+// (at most one per thread), checks them and adds up their needs, so that all come
+// to the same verdict; its eighth of the counts becomes one bit per page.  After
+// the only exchange, the number of free pages per CTA, the a-th free page
+// (lowest number first) belongs to the a-th need: results do not depend on the
+// order in which threads run.  The call is carried out as a whole or not at all.
+//
+// The copies move 256-byte rows (d = 128 bf16) as k_compact does: a warp task is
+// 32 rows, whose places its lanes resolve; 16-byte accesses, eight per lane in
+// flight, past L1.
+#include "common.cuh"
+#include "pages.cuh"
+#include "ptx.cuh"
+
+namespace starkv {
+
+namespace {
+
+constexpr int kBookThreads = 1024;
+constexpr int kBookCtas = 8;
+constexpr int kSliceWords = kMaxPages / 32 / kBookCtas;   // free-page words of a CTA, at most
+constexpr uint32_t kFull = 0xffffffffu;
+
+struct BookSmem {
+  int off[kMaxCallRows + 1];    // new pages before row i
+  int held[kMaxCallRows + 1];   // pages held before row i
+  int row[kMaxCallRows];
+  int from[kMaxCallRows];       // fork: the row it branches from
+  int pos[kMaxCallRows];        // table position of the row's first new page
+  int len[kMaxCallRows];        // tokens before the call (fork: of the row branched from)
+  uint32_t bits[kSliceWords];   // free pages of this CTA's part
+  int before[kSliceWords];      // free pages before a word, in this CTA's part
+  uint32_t seen[kMaxTableRows / 32];   // rows named so far
+  int warp_sum[32];
+  int count[kBookCtas];         // free pages of each CTA's part
+  int bad;
+};
+
+// Exclusive sum over the block; every thread gets the total in *total.
+__device__ int block_scan(int v, int* warp_sum, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int inc = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(kFull, inc, o);
+    if (lane >= o) inc += u;
+  }
+  if (lane == 31) warp_sum[warp] = inc;
+  __syncthreads();
+  if (warp == 0) {
+    int s = warp_sum[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(kFull, s, o);
+      if (lane >= o) s += u;
+    }
+    warp_sum[lane] = s;
+  }
+  __syncthreads();
+  const int base = warp ? warp_sum[warp - 1] : 0;
+  *total = warp_sum[31];
+  __syncthreads();   // warp_sum is free again
+  return base + inc - v;
+}
+
+// Last i in [0, n) with off[i] <= a (rows that need nothing are passed over).
+__device__ __forceinline__ int row_of(const int* off, int n, int a) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (off[mid] <= a) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
+}
+
+__device__ __forceinline__ void st_stream(uint4* p, const uint4& v) {
+  asm volatile("st.global.cs.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+               : "memory");
+}
+
+}  // namespace
+
+struct NoLens {};
+
+template <int OP, typename Lens>
+__global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads, 1)
+    k_book(const __grid_constant__ BookParams p, const __grid_constant__ Lens lens) {
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  BookSmem& s = *reinterpret_cast<BookSmem*>(smem_raw);
+  constexpr bool kTakes = OP == kBookExtend || OP == kBookForkDeep || OP == kBookCompact;
+  constexpr bool kForks = OP == kBookFork || OP == kBookForkDeep;
+  const PagesView& pg = p.pg;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = blockIdx.x;
+  const int P = 1 << pg.shift;
+  const int64_t room = static_cast<int64_t>(pg.max_pages) << pg.shift;
+  for (int i = tid; i < kMaxTableRows / 32; i += kBookThreads) s.seen[i] = 0;
+  if (tid == 0) s.bad = 0;
+  __syncthreads();
+  griddep_launch_dependents();
+  griddep_wait();
+
+  // ---- the call's rows
+  const int i = tid;
+  int need = 0, held = 0, L = 0, after = 0, fill = 0;
+  bool copies = false;
+  if (i < p.n) {
+    bool bad = false;
+    const int row = p.rows ? p.rows[i] : i;
+    int from = row;
+    if (row < 0 || row >= pg.n_rows) bad = true;
+    else if (atomicOr(&s.seen[row >> 5], 1u << (row & 31)) & (1u << (row & 31))) bad = true;   // named twice
+    if (kForks) {
+      from = p.src[i];
+      bad = bad || from < 0 || from >= pg.n_rows;
+    }
+    if (!bad) {
+      L = pg.len[from];
+      bad = L < 0 || L > room;
+      if (kForks) bad = bad || pg.len[row] != 0;   // a branch starts in an empty row
+      if constexpr (OP == kBookCompact) bad = bad || L != lens.L[i];
+    }
+    if (!bad) {
+      held = (L + P - 1) >> pg.shift;
+      fill = L & (P - 1);
+      int pos = 0;
+      after = kForks ? L : 0;
+      if (OP == kBookExtend) {
+        const int nn = p.n_new[i];
+        if (nn < 0 || static_cast<int64_t>(L) + nn > room) bad = true;
+        else {
+          after = L + nn;
+          if (fill && nn) {
+            const int last = pg.table[static_cast<int64_t>(row) * pg.max_pages + held - 1];
+            if (last < 0 || last >= pg.n_pages) bad = true;
+            else copies = pg.refs[last] > 1;   // somebody else holds it too
+          }
+          need = ((after + P - 1) >> pg.shift) - held + copies;
+          pos = held - copies;
+        }
+      }
+      if (OP == kBookForkDeep) need = held;
+      if constexpr (OP == kBookCompact) {
+        after = lens.kept[i];
+        need = (after + P - 1) >> pg.shift;
+        bad = need > pg.max_pages;
+      }
+      s.pos[i] = pos;
+    }
+    s.row[i] = row;
+    s.from[i] = from;
+    s.len[i] = L;
+    if (bad) {
+      s.bad = 1;
+      need = held = 0;
+    }
+  }
+  int total, held_total;
+  const int off = block_scan(need, s.warp_sum, &total);
+  const int held_off = block_scan(held, s.warp_sum, &held_total);
+  if (i < p.n) {
+    s.off[i] = off;
+    s.held[i] = held_off;
+  }
+  __syncthreads();
+  const bool bad = s.bad != 0;
+
+  // ---- the free pages of this CTA's part, one bit each
+  const int words = (pg.n_pages + 31) >> 5;
+  const int per = (words + kBookCtas - 1) / kBookCtas;
+  const int w0 = min(rank * per, words), nw = min(per, words - w0);
+  int mine = 0;   // free pages of the part
+  if (kTakes) {
+    for (int w = warp; w < nw; w += kBookThreads / 32) {
+      const int page = ((w0 + w) << 5) + lane;
+      const uint32_t m = __ballot_sync(kFull, page < pg.n_pages && pg.refs[page] == 0);
+      if (lane == 0) s.bits[w] = m;
+    }
+    __syncthreads();
+    int base = 0;
+    for (int c = 0; c < nw; c += kBookThreads) {
+      const int w = c + tid;
+      int sum;
+      const int b = block_scan(w < nw ? __popc(s.bits[w]) : 0, s.warp_sum, &sum);
+      if (w < nw) s.before[w] = base + b;
+      base += sum;
+    }
+    mine = base;
+    if (tid < kBookCtas) dsmem_st_u32(dsmem_map(&s.count[rank], tid), static_cast<uint32_t>(mine));
+  }
+  if (OP == kBookCompact && !bad) {   // the gather reads the pages that the table is about to lose
+    for (int a = rank * kBookThreads + tid; a < held_total; a += kBookCtas * kBookThreads) {
+      const int r = row_of(s.held, p.n, a), j = a - s.held[r];
+      p.old_table[static_cast<int64_t>(r) * pg.max_pages + j] = pg.table[static_cast<int64_t>(s.row[r]) * pg.max_pages + j];
+    }
+  }
+  cluster_sync();   // from here on lengths, tables and counts change
+
+  int before = 0, avail = 0;
+  if (kTakes)
+    for (int c = 0; c < kBookCtas; ++c) {
+      if (c < rank) before += s.count[c];
+      avail += s.count[c];
+    }
+  const bool ok = !bad && (!kTakes || total <= avail);
+  if (rank == 0 && tid == 0) {
+    if (!ok) atomicOr(p.err, bad ? kErrRow : kErrPool);
+    if (p.plan) {
+      p.plan->ok = ok;
+      p.plan->n_copies = !ok ? 0 : OP == kBookExtend ? p.n : OP == kBookForkDeep ? total : 0;
+    }
+  }
+  if (!ok) return;
+
+  // ---- free page number a goes to need number a
+  if (kTakes)
+    for (int w = warp; w < nw; w += kBookThreads / 32) {
+      if (before + s.before[w] >= total) break;   // the words after it come later still
+      const uint32_t m = s.bits[w];
+      const int a = before + s.before[w] + __popc(m & ((1u << lane) - 1));
+      if (!(m >> lane & 1) || a >= total) continue;
+      const int page = ((w0 + w) << 5) + lane;
+      const int r = row_of(s.off, p.n, a), j = a - s.off[r];
+      int32_t* entry = pg.table + static_cast<int64_t>(s.row[r]) * pg.max_pages + s.pos[r] + j;
+      if (OP == kBookExtend && j == 0) {
+        const int f = s.len[r] & (P - 1);
+        if (s.pos[r] < (s.len[r] + P - 1) >> pg.shift) {   // in the place of a shared last page
+          p.copies[r] = make_int4(*entry, page, f, 0);
+          atomicSub(&pg.refs[*entry], 1);
+        }
+      }
+      if (OP == kBookForkDeep) {
+        const int from = pg.table[static_cast<int64_t>(s.from[r]) * pg.max_pages + j];
+        const bool good = from >= 0 && from < pg.n_pages;
+        if (!good) atomicOr(p.err, kErrRow);
+        p.copies[a] = make_int4(good ? from : -1, page, min(P, s.len[r] - (j << pg.shift)), 0);
+      }
+      *entry = page;
+      pg.refs[page] = 1;
+    }
+
+  // ---- pages that change hands without moving
+  if (OP == kBookFork || OP == kBookFree || OP == kBookCompact)
+    for (int a = rank * kBookThreads + tid; a < held_total; a += kBookCtas * kBookThreads) {
+      const int r = row_of(s.held, p.n, a), j = a - s.held[r];
+      const int32_t* entry = OP == kBookCompact ? p.old_table + static_cast<int64_t>(r) * pg.max_pages + j
+                                                : pg.table + static_cast<int64_t>(s.from[r]) * pg.max_pages + j;
+      const int page = *entry;
+      if (page < 0 || page >= pg.n_pages) {
+        atomicOr(p.err, kErrRow);
+        continue;
+      }
+      if (OP == kBookFork) {
+        atomicAdd(&pg.refs[page], 1);
+        pg.table[static_cast<int64_t>(s.row[r]) * pg.max_pages + j] = page;
+      } else if (atomicSub(&pg.refs[page], 1) <= 0) {   // held by nobody: a table that is not this pool's
+        atomicAdd(&pg.refs[page], 1);
+        atomicOr(p.err, kErrRow);
+      }
+    }
+  if (rank == 0 && i < p.n) {
+    pg.len[s.row[i]] = after;
+    if (OP == kBookExtend && !copies) p.copies[i] = make_int4(-1, 0, 0, 0);
+  }
+}
+
+namespace {
+
+using BookKernel = void (*)(BookParams, NoLens);
+
+BookKernel book_kernel(BookOp op) {
+  switch (op) {
+    case kBookExtend: return k_book<kBookExtend, NoLens>;
+    case kBookFork: return k_book<kBookFork, NoLens>;
+    case kBookForkDeep: return k_book<kBookForkDeep, NoLens>;
+    default: return k_book<kBookFree, NoLens>;
+  }
+}
+
+}  // namespace
+
+cudaError_t pages_configure() {
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  for (BookOp op : {kBookExtend, kBookFork, kBookForkDeep, kBookFree}) {
+    const cudaError_t e = cudaFuncSetAttribute(book_kernel(op), attr, sizeof(BookSmem));
+    if (e != cudaSuccess) return e;
+  }
+  return cudaFuncSetAttribute(k_book<kBookCompact, BookLens>, attr, sizeof(BookSmem));
+}
+
+cudaError_t book_launch(BookOp op, const BookParams& p, const BookLens* lens, cudaStream_t stream) {
+  if (p.n <= 0) return cudaSuccess;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kBookCtas);
+  cfg.blockDim = dim3(kBookThreads);
+  cfg.dynamicSmemBytes = sizeof(BookSmem);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (op == kBookCompact) return cudaLaunchKernelEx(&cfg, k_book<kBookCompact, BookLens>, p, *lens);
+  return cudaLaunchKernelEx(&cfg, book_kernel(op), p, NoLens{});
+}
+
+// ---------------------------------------------------------------- copies
+
+namespace {
+
+constexpr int kMoveThreads = 256;
+constexpr int kMoveWarps = kMoveThreads / 32;
+constexpr int kTaskRows = 32;   // rows of a warp task
+constexpr int kInFlight = 8;    // 16-byte accesses per lane in flight (16 rows per warp)
+constexpr int kMoveBlocksPerSm = 4;
+constexpr int kRow4 = kHeadDim / 8;   // 16-byte units of a row
+
+// 32 rows, row i from in + src(i) to out + dst(i) (16-byte units), where lane i
+// holds its own row's `from` and `to` words and a word below 0 skips the row.
+template <typename Src, typename Dst>
+__device__ __forceinline__ void move_rows(const uint4* in, uint4* out, int from, int to, Src src, Dst dst) {
+  const int lane = threadIdx.x & 31, half = lane >> 4, hl = lane & 15;
+#pragma unroll
+  for (int j0 = 0; j0 < kTaskRows; j0 += 2 * kInFlight) {
+    uint4 v[kInFlight];
+#pragma unroll
+    for (int k = 0; k < kInFlight; ++k) {
+      const int f = __shfl_sync(kFull, from, j0 + 2 * k + half);
+      if (f >= 0) v[k] = ld_stream(in + src(f) + hl);
+    }
+#pragma unroll
+    for (int k = 0; k < kInFlight; ++k) {
+      const int row = j0 + 2 * k + half;
+      const int f = __shfl_sync(kFull, from, row), t = __shfl_sync(kFull, to, row);
+      if (f >= 0) st_stream(out + dst(t) + hl, v[k]);
+    }
+  }
+}
+
+cudaLaunchConfig_t move_config(cudaLaunchAttribute* attr, dim3 grid, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kMoveThreads);
+  cfg.stream = stream;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // starts under the previous kernel's tail
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cfg;
+}
+
+// Place of a token word (page << shift | slot) in one KV head of a layer, in 16-byte units.
+struct PagePlace {
+  int64_t page4;   // page stride
+  int head4;       // of the KV head
+  int shift;
+  __device__ __forceinline__ int64_t operator()(int word) const {
+    return static_cast<int64_t>(word >> shift) * page4 + head4 + (word & ((1 << shift) - 1)) * kRow4;
+  }
+};
+
+}  // namespace
+
+// Warp tasks: (copy, layer, tensor, KV head, 32 rows of the page).
+__global__ void __launch_bounds__(kMoveThreads, kMoveBlocksPerSm)
+    k_page_copy(const __grid_constant__ PagesView pg, const PagePlan* plan, const int4* copies) {
+  griddep_launch_dependents();
+  griddep_wait();
+  const int lane = threadIdx.x & 31;
+  const int blocks = max(1, (1 << pg.shift) / kTaskRows);
+  const int per = blocks * pg.G * 2 * pg.n_layers;   // tasks of a copy
+  const int64_t ntask = static_cast<int64_t>(plan->n_copies) * per;
+  for (int64_t task = static_cast<int64_t>(blockIdx.x) * kMoveWarps + (threadIdx.x >> 5); task < ntask;
+       task += static_cast<int64_t>(gridDim.x) * kMoveWarps) {
+    const int c = static_cast<int>(task / per);
+    int rem = static_cast<int>(task - static_cast<int64_t>(c) * per);
+    const int b = rem % blocks;
+    rem /= blocks;
+    const int g = rem % pg.G;
+    rem /= pg.G;
+    const int layer = rem >> 1;
+    const int4 e = copies[c];
+    const int slot = b * kTaskRows + lane;
+    const bool live = e.x >= 0 && slot < e.z;
+    if (!__any_sync(kFull, live)) continue;
+    __nv_bfloat16* pool = (rem & 1 ? pg.v : pg.k) + layer * pg.layer_stride;
+    const PagePlace place{pg.page_stride / 8, (g << pg.shift) * kRow4, pg.shift};
+    move_rows(reinterpret_cast<const uint4*>(pool), reinterpret_cast<uint4*>(pool), live ? e.x << pg.shift | slot : -1,
+              live ? e.y << pg.shift | slot : -1, place, place);
+  }
+}
+
+cudaError_t page_copy_launch(const PagesView& pg, const PagePlan* plan, const int4* copies, int64_t max_copies, int num_sms,
+                             cudaStream_t stream) {
+  const int64_t tasks = max_copies * max(1, (1 << pg.shift) / kTaskRows) * pg.G * 2 * pg.n_layers;
+  if (tasks <= 0) return cudaSuccess;
+  const int64_t blocks = (tasks + kMoveWarps - 1) / kMoveWarps;
+  cudaLaunchAttribute attr[1];
+  cudaLaunchConfig_t cfg = move_config(attr, dim3(static_cast<unsigned>(min(blocks, static_cast<int64_t>(num_sms) * kMoveBlocksPerSm))), stream);
+  return cudaLaunchKernelEx(&cfg, k_page_copy, pg, plan, copies);
+}
+
+// grid: (blocks, layers, sequences).  Tasks of one (sequence, layer): 2 tensors x
+// G x ceil((B + w) / 32) row blocks, one per warp.
+__global__ void __launch_bounds__(kMoveThreads, kMoveBlocksPerSm)
+    k_page_gather(const __grid_constant__ PagesView pg, const __grid_constant__ SeqBatch b, const int32_t* rows, int row0, int w,
+                  int per_head, const PagePlan* plan, const int32_t* old_table, uint32_t* err) {
+  griddep_launch_dependents();
+  griddep_wait();
+  if (!plan->ok) return;
+  const SeqView& sv = b.s[blockIdx.z];
+  const int seq = blockIdx.z, layer = blockIdx.y;
+  const int B = sv.budget, Lp = sv.Lp;
+  const int rows_out = B + w;
+  const int lane = threadIdx.x & 31;
+  const int sets = per_head ? pg.G : 1;
+  const int row = rows ? rows[row0 + seq] : row0 + seq;
+  const int32_t* idx_l = sv.idx + static_cast<int64_t>(layer) * sets * B;
+  const uint32_t* meta_l = sv.meta ? sv.meta + static_cast<int64_t>(layer) * sv.meta_layer_stride : nullptr;
+  uint32_t* meta_out_l = sv.meta_out + static_cast<int64_t>(layer) * sets * rows_out;
+  const int32_t* was = old_table + static_cast<int64_t>(row0 + seq) * pg.max_pages;
+  const int32_t* is = pg.table + static_cast<int64_t>(row) * pg.max_pages;
+  const int nblk = ceil_div(rows_out, kTaskRows);
+  const int ntask = 2 * pg.G * nblk;
+  for (int task = blockIdx.x * kMoveWarps + (threadIdx.x >> 5); task < ntask; task += gridDim.x * kMoveWarps) {
+    const int tensor = task / (pg.G * nblk);
+    const int rem = task - tensor * pg.G * nblk;
+    const int g = rem / nblk, r = (rem - g * nblk) * kTaskRows + lane;
+    const int set = per_head ? g : 0;
+    int from = -1, to = -1;
+    if (r < rows_out) {
+      int src = r < B ? idx_l[static_cast<int64_t>(set) * B + r] : Lp + (r - B);
+      if (src < 0 || src >= (r < B ? Lp : sv.L)) {   // a kept index must name a past token: report, copy row 0
+        atomicOr(err, kErrIndex);
+        src = 0;
+      }
+      if (meta_l && tensor == 0 && g == set)
+        meta_out_l[static_cast<int64_t>(set) * rows_out + r] = meta_l[set * sv.meta_group_stride + src];
+      const int page = was[src >> pg.shift];
+      to = is[r >> pg.shift] << pg.shift | (r & ((1 << pg.shift) - 1));
+      if (page >= 0 && page < pg.n_pages) from = page << pg.shift | (src & ((1 << pg.shift) - 1));   // (else reported)
+    }
+    __nv_bfloat16* pool = (tensor == 0 ? pg.k : pg.v) + layer * pg.layer_stride;
+    const PagePlace place{pg.page_stride / 8, (g << pg.shift) * kRow4, pg.shift};
+    move_rows(reinterpret_cast<const uint4*>(pool), reinterpret_cast<uint4*>(pool), from, to, place, place);
+  }
+}
+
+cudaError_t page_gather_launch(const PagesView& pg, const SeqBatch& b, const int32_t* rows, int row0, int w, int per_head,
+                               const PagePlan* plan, const int32_t* old_table, int rows_out_max, uint32_t* err,
+                               cudaStream_t stream) {
+  if (rows_out_max <= 0) return cudaSuccess;
+  const int ntask = 2 * pg.G * ceil_div(rows_out_max, kTaskRows);
+  cudaLaunchAttribute attr[1];
+  cudaLaunchConfig_t cfg = move_config(attr, dim3(static_cast<unsigned>(ceil_div(ntask, kMoveWarps)), b.nlayers, b.nseq), stream);
+  return cudaLaunchKernelEx(&cfg, k_page_gather, pg, b, rows, row0, w, per_head, plan, old_table, err);
+}
+
+// Warp tasks: (sequence, layer, tensor, 32 of the T * G rows, the KV heads of a
+// token together).  The tokens are the last n_tokens of their row.
+template <bool STORE>
+__global__ void __launch_bounds__(kMoveThreads, kMoveBlocksPerSm)
+    k_page_move(const __grid_constant__ PagesView pg, const __grid_constant__ TokensView t, uint32_t* err) {
+  griddep_launch_dependents();
+  griddep_wait();
+  const int lane = threadIdx.x & 31;
+  const int nblk = static_cast<int>((static_cast<int64_t>(t.T) * pg.G + kTaskRows - 1) / kTaskRows);
+  const int tensors = t.v ? 2 : 1;
+  const int64_t per_seq = static_cast<int64_t>(nblk) * tensors * t.nlayers;
+  const int64_t ntask = per_seq * t.n;
+  for (int64_t task = static_cast<int64_t>(blockIdx.x) * kMoveWarps + (threadIdx.x >> 5); task < ntask;
+       task += static_cast<int64_t>(gridDim.x) * kMoveWarps) {
+    const int seq = static_cast<int>(task / per_seq);
+    int64_t rem = task - seq * per_seq;
+    const int blk = static_cast<int>(rem % nblk);
+    rem /= nblk;
+    const int tensor = tensors == 2 ? static_cast<int>(rem & 1) : 0;
+    const int l = static_cast<int>(tensors == 2 ? rem >> 1 : rem);
+    const int row = t.rows ? t.rows[seq] : seq;
+    const int count = t.n_tokens ? t.n_tokens[seq] : t.T;
+    const bool row_ok = row >= 0 && row < pg.n_rows;
+    const int L = row_ok ? pg.len[row] : 0;
+    if (!row_ok || count < 0 || count > t.T || count > L || L > static_cast<int64_t>(pg.max_pages) << pg.shift) {
+      if (lane == 0) atomicOr(err, kErrRow);
+      continue;
+    }
+    const int64_t r = static_cast<int64_t>(blk) * kTaskRows + lane;
+    const int tok = static_cast<int>(r / pg.G), g = static_cast<int>(r - static_cast<int64_t>(tok) * pg.G);
+    int word = -1;   // the token's place in the pages
+    if (tok < count) {
+      const int at = L - count + tok;
+      const int page = pg.table[static_cast<int64_t>(row) * pg.max_pages + (at >> pg.shift)];
+      // a page that others hold too is not written to
+      if (page < 0 || page >= pg.n_pages || (STORE && pg.refs[page] != 1)) atomicOr(err, kErrRow);
+      else word = page << pg.shift | (at & ((1 << pg.shift) - 1));
+    }
+    __nv_bfloat16* pool = (tensor ? pg.v : pg.k) + (t.layer0 + l) * pg.layer_stride;
+    __nv_bfloat16* flat = (tensor ? t.v : t.k) + seq * t.seq_stride + l * t.layer_stride;
+    const int half = lane >> 4, hl = lane & 15;
+#pragma unroll
+    for (int j0 = 0; j0 < kTaskRows; j0 += 2 * kInFlight) {
+      uint4 v[kInFlight];
+      uint4* dst[kInFlight];
+#pragma unroll
+      for (int k = 0; k < kInFlight; ++k) {
+        const int i = j0 + 2 * k + half;
+        const int wd = __shfl_sync(kFull, word, i);
+        const int tk = __shfl_sync(kFull, tok, i), gg = __shfl_sync(kFull, g, i);
+        dst[k] = nullptr;
+        if (wd >= 0) {
+          const PagePlace place{pg.page_stride / 8, (gg << pg.shift) * kRow4, pg.shift};
+          uint4* in_pool = reinterpret_cast<uint4*>(pool) + place(wd) + hl;
+          uint4* in_flat = reinterpret_cast<uint4*>(flat + tk * t.token_stride + gg * t.head_stride) + hl;
+          v[k] = ld_stream(STORE ? in_flat : in_pool);
+          dst[k] = STORE ? in_pool : in_flat;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kInFlight; ++k)
+        if (dst[k]) st_stream(dst[k], v[k]);
+    }
+  }
+}
+
+cudaError_t page_move_launch(bool store, const PagesView& pg, const TokensView& t, int num_sms, uint32_t* err,
+                             cudaStream_t stream) {
+  const int64_t tasks = ((static_cast<int64_t>(t.T) * pg.G + kTaskRows - 1) / kTaskRows) * (t.v ? 2 : 1) * t.nlayers * t.n;
+  if (tasks <= 0) return cudaSuccess;
+  const int64_t blocks = (tasks + kMoveWarps - 1) / kMoveWarps;
+  cudaLaunchAttribute attr[1];
+  cudaLaunchConfig_t cfg = move_config(attr, dim3(static_cast<unsigned>(min(blocks, static_cast<int64_t>(num_sms) * kMoveBlocksPerSm))), stream);
+  return cudaLaunchKernelEx(&cfg, store ? k_page_move<true> : k_page_move<false>, pg, t, err);
+}
+
+}  // namespace starkv

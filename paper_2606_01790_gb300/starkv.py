@@ -29,9 +29,13 @@ ABI_FUNCTIONS = [
     "starkv_last_error",
     "starkv_score_layer_noalloc", "starkv_selftest_wait", "starkv_slot_state_bytes", "starkv_export_slot",
     "starkv_import_slot", "starkv_window_attention",
+    "starkv_pages_workspace_bytes", "starkv_pages_reset", "starkv_pages_extend", "starkv_pages_fork",
+    "starkv_pages_free", "starkv_pages_compact", "starkv_pages_store", "starkv_pages_load",
+    "starkv_tree_attention", "starkv_sink_attention",
 ]
 
-KERNELS = ["score_lse", "score_accum", "pool", "calibrate", "compact", "attention", "attn_combine"]
+KERNELS = ["score_lse", "score_accum", "pool", "calibrate", "compact", "attention", "attn_combine",
+           "page_book", "page_copy", "page_gather", "page_move", "paged_attention"]
 
 
 SELECT_GLOBAL, SELECT_PER_HEAD = 0, 1   # starkv_config.select_mode
@@ -60,6 +64,25 @@ class CSeq(C.Structure):
                 ("S", C.c_void_p), ("score", C.c_void_p), ("stats", C.c_void_p),
                 ("meta_group_stride", C.c_int64), ("lse", C.c_void_p), ("attn_o", C.c_void_p),
                 ("attn_lse", C.c_void_p)]
+
+
+class CPages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("layer_stride", C.c_int64), ("page_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_rows", C.c_int32), ("max_pages", C.c_int32),
+                ("table", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p)]
+
+
+class CTokens(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("rows", C.c_void_p), ("n_tokens", C.c_void_p),
+                ("n", C.c_int32), ("T", C.c_int32), ("seq_stride", C.c_int64), ("layer_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class CQueries(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("o", C.c_void_p), ("lse", C.c_void_p), ("mask", C.c_void_p),
+                ("rows", C.c_void_p), ("n_tokens", C.c_void_p), ("n", C.c_int32), ("T", C.c_int32),
+                ("q_seq_stride", C.c_int64), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("o_seq_stride", C.c_int64), ("o_token_stride", C.c_int64), ("o_head_stride", C.c_int64)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -112,6 +135,17 @@ def lib() -> C.CDLL:
         L.starkv_set_timing.argtypes = [st, C.c_int32]
         L.starkv_kernel_times.argtypes = [st, C.POINTER(C.c_int64), C.POINTER(C.c_float)]
         L.starkv_backward_launches.argtypes = [st, C.POINTER(C.c_int64)]
+        pg, ws = C.POINTER(CPages), [C.c_void_p, C.c_size_t, C.c_void_p]
+        L.starkv_pages_workspace_bytes.argtypes = [st, pg, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        L.starkv_pages_reset.argtypes = [st, pg, C.c_void_p]
+        L.starkv_pages_extend.argtypes = [st, pg, C.c_void_p, C.c_void_p, C.c_int32] + ws
+        L.starkv_pages_fork.argtypes = [st, pg, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32] + ws
+        L.starkv_pages_free.argtypes = [st, pg, C.c_void_p, C.c_int32, C.c_void_p]
+        L.starkv_pages_compact.argtypes = [st, pg, C.c_void_p, C.POINTER(CSeq), C.c_int32] + ws
+        for name in ("starkv_pages_store", "starkv_pages_load"):
+            getattr(L, name).argtypes = [st, pg, C.c_int32, C.c_int32, C.POINTER(CTokens), C.c_void_p]
+        L.starkv_tree_attention.argtypes = [st, pg, C.c_int32, C.POINTER(CQueries)] + ws
+        L.starkv_sink_attention.argtypes = [st, pg, C.c_int32, C.POINTER(CQueries), C.c_int32, C.c_int32] + ws
         L.starkv_last_error.argtypes = []
         L.starkv_last_error.restype = C.c_char_p
         for name in ABI_FUNCTIONS:
@@ -433,3 +467,220 @@ def backward_launches(st: State) -> int:
     n = C.c_int64(0)
     _check(lib().starkv_backward_launches(st.handle, C.byref(n)))
     return int(n.value)
+
+
+# ---------------------------------------------------------------- paged cache
+
+@dataclass
+class Pages:
+    """A paged cache (``starkv_pages``): pool, page table, lengths and page counts, all the caller's."""
+
+    k: torch.Tensor       # bf16 [n_layers][n_pages][G][page_size][d], the last three contiguous
+    v: torch.Tensor       # the same, with k's strides
+    table: torch.Tensor   # i32 [n_rows][max_pages]
+    len: torch.Tensor     # i32 [n_rows]
+    refs: torch.Tensor    # i32 [n_pages]
+
+    def to_c(self) -> CPages:
+        k, v = self.k, self.v
+        if k.dim() != 5 or v.shape != k.shape or v.stride() != k.stride():
+            raise ValueError("pages: k and v are [n_layers, n_pages, G, page_size, d] with the same strides")
+        nl, n_pages, G, P, d = k.shape
+        if k.stride()[2:] != (P * d, d, 1):
+            raise ValueError("pages: a page of a layer must be contiguous")
+        _expect(torch.bfloat16, k, v)
+        _expect(torch.int32, self.table, self.len, self.refs)
+        if self.table.dim() != 2 or self.len.numel() != self.table.shape[0] or self.refs.numel() != n_pages:
+            raise ValueError("pages: table is [n_rows, max_pages], len [n_rows], refs [n_pages]")
+        if len({t.device for t in (k, v, self.table, self.len, self.refs)}) != 1:
+            raise ValueError("pages: tensors on more than one device")
+        return CPages(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), n_pages, P, *self.table.shape,
+                      _ptr(self.table), _ptr(self.len), _ptr(self.refs))
+
+
+@dataclass
+class Tokens:
+    """Tokens outside the pages (``starkv_tokens``): the last n_tokens[i] of row rows[i]."""
+
+    k: torch.Tensor                          # bf16 [n][layers][T][G][d], any strides with d contiguous
+    v: Optional[torch.Tensor] = None         # the same, or None: keys only
+    rows: Optional[torch.Tensor] = None      # i32 [n], or None: rows 0, 1, ...
+    n_tokens: Optional[torch.Tensor] = None  # i32 [n], or None: T each
+
+
+@dataclass
+class Queries:
+    """Queries of ``tree_attention`` and ``sink_attention`` (``starkv_queries``)."""
+
+    q: torch.Tensor                          # bf16 [n][T][H][d], any strides with d contiguous
+    o: torch.Tensor                          # bf16, the same shape
+    lse: Optional[torch.Tensor] = None       # f32 [n][T][H]
+    mask: Optional[torch.Tensor] = None      # i64 [n][T] (the bits of the u64 words), tree attention only
+    rows: Optional[torch.Tensor] = None      # i32 [n], or None: rows 0, 1, ...
+    n_tokens: Optional[torch.Tensor] = None  # i32 [n], or None: T each
+
+
+def _expect(dtype: torch.dtype, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and t.dtype != dtype:
+            raise ValueError(f"expected {dtype}, got {t.dtype}")
+
+
+def _on(pages: Pages, *tensors: Optional[torch.Tensor]) -> None:
+    """The call's tensors lie where its pages do, on the current CUDA device."""
+    dev = pages.k.device
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise ValueError(f"pages on {dev}: the paged calls take tensors of the current CUDA device")
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError(f"a tensor on {t.device}, pages on {dev}")
+
+
+def _ids(t: Optional[torch.Tensor], n: int, what: str) -> int:
+    if t is None:
+        return 0
+    _expect(torch.int32, t)
+    if t.numel() != n:
+        raise ValueError(f"{what}: {t.numel()} entries for {n} sequences")
+    return _ptr(t)
+
+
+def _strides(t: torch.Tensor):
+    """Element strides; those of axes of one entry, which are never stepped along, as if contiguous."""
+    out, step = list(t.stride()), t.shape[-1]
+    for i in range(t.dim() - 2, -1, -1):
+        if t.shape[i] == 1:
+            out[i] = step
+        step = max(step, out[i] * t.shape[i])
+    return out
+
+
+def _c_tokens(st: State, pages: Pages, tok: Tokens) -> CTokens:
+    k, v = tok.k, tok.v
+    if k.dim() != 5 or k.shape[3:] != (st.cfg.n_kv_heads, st.cfg.head_dim) or k.stride(4) != 1:
+        raise ValueError("tokens: k is [n, layers, T, G, d] with d contiguous")
+    if v is not None and (v.shape != k.shape or v.stride() != k.stride()):
+        raise ValueError("tokens: v has k's shape and strides")
+    _expect(torch.bfloat16, k, v)
+    _on(pages, k, v, tok.rows, tok.n_tokens)
+    n, _, T = k.shape[:3]
+    s = _strides(k)
+    return CTokens(k.data_ptr(), 0 if v is None else v.data_ptr(), _ids(tok.rows, n, "rows"),
+                   _ids(tok.n_tokens, n, "n_tokens"), n, T, s[0], s[1], s[2], s[3])
+
+
+def _c_queries(st: State, pages: Pages, qs: Queries) -> CQueries:
+    q, o = qs.q, qs.o
+    if q.dim() != 4 or q.shape[2:] != (st.cfg.n_heads, st.cfg.head_dim) or q.stride(3) != 1:
+        raise ValueError("queries: q is [n, T, H, d] with d contiguous")
+    if o.shape != q.shape or o.stride(3) != 1:
+        raise ValueError("queries: o has q's shape, with d contiguous")
+    n, T, H, _ = q.shape
+    _expect(torch.bfloat16, q, o)
+    _on(pages, q, o, qs.lse, qs.mask, qs.rows, qs.n_tokens)
+    if qs.lse is not None:
+        _expect(torch.float32, qs.lse)
+        if qs.lse.shape != (n, T, H):
+            raise ValueError("queries: lse is [n, T, H]")
+    if qs.mask is not None:
+        _expect(torch.int64, qs.mask)
+        if qs.mask.shape != (n, T):
+            raise ValueError("queries: mask is [n, T]")
+    return CQueries(q.data_ptr(), o.data_ptr(), _ptr(qs.lse), _ptr(qs.mask), _ids(qs.rows, n, "rows"),
+                    _ids(qs.n_tokens, n, "n_tokens"), n, T, *_strides(q)[:3], *_strides(o)[:3])
+
+
+def _c_pages(st: State, pages: Pages) -> CPages:
+    c = pages.to_c()
+    if (pages.k.shape[0], pages.k.shape[2], pages.k.shape[4]) != (st.cfg.n_layers, st.cfg.n_kv_heads, st.cfg.head_dim):
+        raise ValueError("pages: k is not of the state's layers, KV heads and head dimension")
+    return c
+
+
+def make_pages(st: State, n_pages: int, page_size: int, n_rows: int, max_pages: int, device=None, stream=None) -> Pages:
+    """An empty paged cache in newly allocated tensors."""
+    dev = device or torch.device("cuda", torch.cuda.current_device())
+    shape = (st.cfg.n_layers, n_pages, st.cfg.n_kv_heads, page_size, st.cfg.head_dim)
+    pages = Pages(k=torch.empty(shape, dtype=torch.bfloat16, device=dev),
+                  v=torch.empty(shape, dtype=torch.bfloat16, device=dev),
+                  table=torch.zeros((n_rows, max_pages), dtype=torch.int32, device=dev),
+                  len=torch.empty(n_rows, dtype=torch.int32, device=dev),
+                  refs=torch.empty(n_pages, dtype=torch.int32, device=dev))
+    pages_reset(st, pages, stream)
+    return pages
+
+
+def pages_workspace(st: State, pages: Pages, n: int, T: int = 1) -> torch.Tensor:
+    """Workspace for the paged calls over at most ``n`` rows and ``T`` queries of each."""
+    b = C.c_size_t()
+    _check(lib().starkv_pages_workspace_bytes(st.handle, C.byref(_c_pages(st, pages)), n, T, C.byref(b)))
+    return torch.empty(int(b.value), dtype=torch.uint8, device=pages.k.device)
+
+
+def pages_reset(st: State, pages: Pages, stream=None) -> None:
+    c = _c_pages(st, pages)
+    _on(pages)
+    _check(lib().starkv_pages_reset(st.handle, C.byref(c), _stream(stream)))
+
+
+def pages_extend(st: State, pages: Pages, rows: Optional[torch.Tensor], n_new: torch.Tensor, ws: torch.Tensor,
+                 stream=None) -> None:
+    """Room for ``n_new[i]`` more tokens of ``rows[i]``; shared last pages are copied first."""
+    c, n = _c_pages(st, pages), n_new.numel()
+    _on(pages, rows, n_new, ws)
+    _check(lib().starkv_pages_extend(st.handle, C.byref(c), _ids(rows, n, "rows"), _ids(n_new, n, "n_new"), n,
+                                     ws.data_ptr(), ws.numel(), _stream(stream)))
+
+
+def pages_fork(st: State, pages: Pages, src: torch.Tensor, dst: torch.Tensor, ws: torch.Tensor, deep: bool = False,
+               stream=None) -> None:
+    """Row ``dst[i]`` becomes a copy of ``src[i]``, sharing its pages (``deep``: with pages of its own)."""
+    c, n = _c_pages(st, pages), dst.numel()
+    _on(pages, src, dst, ws)
+    _check(lib().starkv_pages_fork(st.handle, C.byref(c), _ids(src, n, "src"), _ids(dst, n, "dst"), n, int(deep),
+                                   ws.data_ptr(), ws.numel(), _stream(stream)))
+
+
+def pages_free(st: State, pages: Pages, rows: torch.Tensor, stream=None) -> None:
+    """Empties rows; pages that no row holds any more are free."""
+    c, n = _c_pages(st, pages), rows.numel()
+    _on(pages, rows)
+    _check(lib().starkv_pages_free(st.handle, C.byref(c), _ids(rows, n, "rows"), n, _stream(stream)))
+
+
+def pages_compact(st: State, pages: Pages, rows: Optional[torch.Tensor], seqs: Sequence[Seq], ws: torch.Tensor,
+                  stream=None) -> None:
+    """Every layer of ``rows[i]`` keeps the tokens ``seqs[i].idx`` and the window (``starkv_compact`` on pages)."""
+    c = _c_pages(st, pages)
+    _on(pages, rows, ws, *(t for s in seqs for t in (s.idx, s.meta, s.meta_out)))
+    _check(lib().starkv_pages_compact(st.handle, C.byref(c), _ids(rows, len(seqs), "rows"), _seq_array(seqs), len(seqs),
+                                      ws.data_ptr(), ws.numel(), _stream(stream)))
+
+
+def pages_store(st: State, pages: Pages, layer0: int, tokens: Tokens, stream=None) -> None:
+    """``tokens`` into the last places of their rows, layers layer0, layer0 + 1, ..."""
+    c, tok = _c_pages(st, pages), _c_tokens(st, pages, tokens)
+    _check(lib().starkv_pages_store(st.handle, C.byref(c), layer0, tokens.k.shape[1], C.byref(tok), _stream(stream)))
+
+
+def pages_load(st: State, pages: Pages, layer0: int, tokens: Tokens, stream=None) -> None:
+    """The last tokens of their rows into ``tokens``."""
+    c, tok = _c_pages(st, pages), _c_tokens(st, pages, tokens)
+    _check(lib().starkv_pages_load(st.handle, C.byref(c), layer0, tokens.k.shape[1], C.byref(tok), _stream(stream)))
+
+
+def tree_attention(st: State, pages: Pages, layer: int, queries: Queries, ws: torch.Tensor, stream=None) -> None:
+    """Attention of each row's last (drafted) tokens over its cache; ``queries.mask`` names the drafted ones seen."""
+    c, q = _c_pages(st, pages), _c_queries(st, pages, queries)
+    _on(pages, ws)
+    _check(lib().starkv_tree_attention(st.handle, C.byref(c), layer, C.byref(q), ws.data_ptr(), ws.numel(),
+                                       _stream(stream)))
+
+
+def sink_attention(st: State, pages: Pages, layer: int, queries: Queries, n_sink: int, window: int, ws: torch.Tensor,
+                   stream=None) -> None:
+    """Causal attention over the first ``n_sink`` tokens and the last ``window``."""
+    c, q = _c_pages(st, pages), _c_queries(st, pages, queries)
+    _on(pages, ws)
+    _check(lib().starkv_sink_attention(st.handle, C.byref(c), layer, C.byref(q), n_sink, window, ws.data_ptr(),
+                                       ws.numel(), _stream(stream)))

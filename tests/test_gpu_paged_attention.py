@@ -1,0 +1,364 @@
+"""Attention over the paged cache on the GPU against the fp64 definition: trees of
+drafted tokens, sliding windows with sinks, and what must not reach an output."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as O
+from paper_2606_01790_gb300 import starkv as sk
+
+import paged_harness as PH
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("needs a CUDA device", allow_module_level=True)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    import __graft_entry__
+    __graft_entry__.build()
+
+
+def filled(lens, P=64, heads=28, kv_heads=4, layers=1, seed=0, page_major=False, spare=3):
+    """Rows of the given lengths in shuffled pages."""
+    st = PH.state(layers=layers, heads=heads, kv_heads=kv_heads, window=1)
+    need = [-(-n // P) for n in lens]
+    c = PH.Pair(st, n_pages=sum(need) + spare, P=P, n_rows=len(lens), max_pages=max(max(need), 1) + 1, seed=seed,
+                page_major=page_major)
+    order = np.random.default_rng(seed + 1).permutation(sum(need) + spare)
+    at = 0
+    for r, (n, m) in enumerate(zip(lens, need)):
+        c.ref.table[r, :m] = order[at:at + m]
+        c.ref.refs[order[at:at + m]] = 1
+        c.ref.len[r] = n
+        at += m
+    for x, y in ((c.pages.table, c.ref.table), (c.pages.len, c.ref.len), (c.pages.refs, c.ref.refs)):
+        x.copy_(torch.from_numpy(y))
+    return c
+
+
+def queries(c, n, T, seed=0, scale=1.0, **over):
+    H = c.st.cfg.n_heads
+    q = torch.from_numpy(np.random.default_rng(seed).standard_normal((n, T, H, PH.D), dtype=np.float32) * scale)
+    return sk.Queries(q=q.to(torch.bfloat16).cuda(), o=torch.full((n, T, H, PH.D), 9.0, dtype=torch.bfloat16, device="cuda"),
+                      lse=torch.full((n, T, H), 9.0, device="cuda"), **over)
+
+
+def random_tree(rng, T):
+    mask = []
+    for j in range(T):
+        up = int(rng.integers(-1, j)) if j else -1
+        mask.append((mask[up] if up >= 0 else 0) | 1 << j)
+    return mask
+
+
+def words(masks, T):
+    out = np.zeros((len(masks), T), np.uint64)
+    for i, m in enumerate(masks):
+        out[i, :len(m)] = [x & (1 << 64) - 1 for x in m]
+    return torch.from_numpy(out.view(np.int64)).cuda()
+
+
+def verify(c, qs, seen_of, rows, counts, layer=0, errors=True):
+    """Every sequence against the oracle; what lies behind its queries is untouched."""
+    torch.cuda.synchronize()
+    if errors:
+        sk.check_device_error(c.st)
+    o, lse, q = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy(), qs.q.float().cpu().numpy()
+    for i, (r, n) in enumerate(zip(rows, counts)):
+        k, v = c.cache(r, layer)
+        PH.check_attention(o[i, :n], lse[i, :n], q[i, :n], k, v, seen_of(i, int(c.ref.len[r]), n), what=f"seq {i}")
+        assert np.all(o[i, n:] == 9.0) and np.all(lse[i, n:] == 9.0), i
+
+
+@pytest.mark.parametrize("P", [16, 64, 256])
+@pytest.mark.parametrize("heads,kv_heads", [(28, 4), (8, 8), (12, 1), (40, 8)])
+@pytest.mark.parametrize("T", [1, 5, 19, 64])
+def test_trees(P, heads, kv_heads, T):
+    lens = [T, T + 1, 63 + T, 64 + T, 200 + T, 517]
+    c = filled(lens, P=P, heads=heads, kv_heads=kv_heads, seed=T)
+    rng = np.random.default_rng(T)
+    rows = [int(r) for r in rng.permutation(6)]
+    counts = [T if i % 2 else int(rng.integers(1, T + 1)) for i in range(6)]
+    masks = [random_tree(rng, n) for n in counts]
+    qs = queries(c, 6, T, mask=words(masks, T), rows=c.ids(rows), n_tokens=c.ids(counts))
+    sk.tree_attention(c.st, c.pages, 0, qs, c.ws)
+    verify(c, qs, lambda i, L, n: O.seen_tree(L, n, masks[i]), rows, counts)
+    c.st.close()
+
+
+@pytest.mark.parametrize("P", [16, 64, 128])
+@pytest.mark.parametrize("n_sink,window", [(0, 1), (4, 64), (64, 100), (1, 1 << 20), (70, 37), (3, 0), (0, 0), (100000, 5), (0, 2**31 - 1)])
+@pytest.mark.parametrize("T", [1, 3, 40])
+def test_windows_and_sinks(P, n_sink, window, T):
+    lens = [T, T + 7, 64 + T, 128, 391, 640]
+    c = filled(lens, P=P, seed=window % 97)
+    rng = np.random.default_rng(n_sink + T)
+    rows = [int(r) for r in rng.permutation(6)]
+    counts = [int(rng.integers(0, T + 1)) if i == 2 else T for i in range(6)]
+    qs = queries(c, 6, T, rows=c.ids(rows), n_tokens=c.ids(counts))
+    sk.sink_attention(c.st, c.pages, 0, qs, n_sink, window, c.ws)
+    verify(c, qs, lambda i, L, n: O.seen_sink(L, n, n_sink, window), rows, counts)
+    c.st.close()
+
+
+def test_a_prompt_from_its_first_token():
+    """T = L: every query sees what precedes it, the first only itself."""
+    c = filled([300, 131], P=32)
+    qs = queries(c, 2, 300, rows=None, n_tokens=c.ids([300, 131]))
+    sk.sink_attention(c.st, c.pages, 0, qs, 2, 50, sk.pages_workspace(c.st, c.pages, 2, 300))
+    verify(c, qs, lambda i, L, n: O.seen_sink(L, n, 2, 50), [0, 1], [300, 131])
+    c.st.close()
+
+
+def test_a_long_cache_many_pieces():
+    c = filled([9001, 70, 4099], P=16)
+    qs = queries(c, 3, 2)
+    sk.sink_attention(c.st, c.pages, 0, qs, 4, 1 << 20, c.ws)
+    verify(c, qs, lambda i, L, n: O.seen_sink(L, n, 4, 1 << 20), [0, 1, 2], [2, 2, 2])
+    c.st.close()
+
+
+def test_layers_strides_and_page_major_pools():
+    """A query part of a fused projection, outputs head-major, layer 2 of a page-major pool."""
+    c = filled([100, 333], P=16, layers=3, page_major=True)
+    n, T, H = 2, 7, 28
+    fused = torch.randn((T, n, H + 8, PH.D), device="cuda").to(torch.bfloat16)
+    out = torch.full((H, n, T + 1, PH.D), 9.0, dtype=torch.bfloat16, device="cuda")
+    qs = sk.Queries(q=fused[:, :, 4:H + 4].transpose(0, 1), o=out[:, :, :T].permute(1, 2, 0, 3),
+                    lse=torch.empty((n, T, H), device="cuda"))
+    sk.sink_attention(c.st, c.pages, 2, qs, 4, 90, c.ws)
+    verify(c, qs, lambda i, L, m: O.seen_sink(L, m, 4, 90), [0, 1], [T, T], layer=2)
+    assert torch.all(out[:, :, T] == 9.0)
+    qs.lse = None      # optional
+    before = qs.o.clone()
+    out.zero_()
+    sk.sink_attention(c.st, c.pages, 2, qs, 4, 90, c.ws)
+    assert torch.equal(qs.o, before)
+    c.st.close()
+
+
+def test_masks_that_leave_queries_empty():
+    T = 6
+    c = filled([T, 80], P=16)
+    masks = [[0, 1, 0, 0b1000, 0, 0b111111], [0] * T]
+    qs = queries(c, 2, T, mask=words(masks, T))
+    sk.tree_attention(c.st, c.pages, 0, qs, c.ws)
+    verify(c, qs, lambda i, L, n: O.seen_tree(L, n, masks[i]), [0, 1], [T, T])
+    assert torch.all(qs.o[0, 0] == 0) and torch.all(torch.isneginf(qs.lse[0, 0]))
+    c.st.close()
+
+
+@pytest.mark.parametrize("scale", [30.0, 300.0])
+def test_logits_over_a_wide_range(scale):
+    """Row references that move again and again, and weights that underflow."""
+    c = filled([700, 450], P=64)
+    qs = queries(c, 2, 3, scale=scale)
+    sk.sink_attention(c.st, c.pages, 0, qs, 0, 600, c.ws)
+    verify(c, qs, lambda i, L, n: O.seen_sink(L, n, 0, 600), [0, 1], [3, 3])
+    c.st.close()
+
+
+def test_values_of_every_magnitude():
+    """Values far above and below fp16's range."""
+    for scale in (1e30, 1e-30):
+        c = filled([300], P=64)
+        v = c.pages.v.float() * scale
+        c.pages.v.copy_(v)
+        c.ref.v[:] = c.pages.v.view(torch.int16).cpu().numpy()
+        qs = queries(c, 1, 3)
+        sk.sink_attention(c.st, c.pages, 0, qs, 0, 600, c.ws)
+        verify(c, qs, lambda i, L, n: O.seen_sink(L, n, 0, 600), [0], [3])
+        c.st.close()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_what_is_not_seen_does_not_reach_an_output(bad):
+    """Slots behind the last token, free pages and tokens outside a window or a branch hold `bad`."""
+    T, L = 8, 203
+    c = filled([L, 90], P=64)
+    mask = [[1 << j for j in range(T)], [1 << j | 1 for j in range(T)]]     # token 5 of row 0 is seen by itself only
+    k0, v0 = c.cache(0, 0)
+    k1, v1 = c.cache(1, 0)
+    clean_k, clean_v = c.pages.k.clone(), c.pages.v.clone()
+    for x in (c.pages.k, c.pages.v):
+        held = torch.zeros(x.shape[1], dtype=torch.bool)
+        for r, n in ((0, L), (1, 90)):
+            for j in range(-(-n // 64)):
+                p = int(c.ref.table[r, j])
+                held[p] = True
+                if j == n // 64:
+                    x[0, p, :, n % 64:] = bad
+        x[0, ~held.cuda()] = bad
+        at = L - T + 5
+        x[0, int(c.ref.table[0, at // 64]), :, at % 64] = bad
+    qs = queries(c, 2, T, mask=words(mask, T))
+    sk.tree_attention(c.st, c.pages, 0, qs, c.ws)
+    torch.cuda.synchronize()
+    sk.check_device_error(c.st)
+    o, lse, q = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy(), qs.q.float().cpu().numpy()
+    for i, (k, v, n) in enumerate(((k0, v0, L), (k1, v1, 90))):
+        seen = O.seen_tree(n, T, mask[i])
+        for t in range(T):
+            if i == 0 and t == 5:
+                continue
+            PH.check_attention(o[i, t:t + 1], lse[i, t:t + 1], q[i, t:t + 1], k, v, seen[t:t + 1], what=f"{i} {t}")
+    assert not np.isfinite(o[0, 5]).any()
+    # and under a window: everything before it but the sinks
+    c.pages.k.copy_(clean_k)
+    c.pages.v.copy_(clean_v)
+    W, S = 70, 3
+    for x in (c.pages.k, c.pages.v):
+        for j in range(S, L - 4 - W + 1):
+            x[0, int(c.ref.table[0, j // 64]), :, j % 64] = bad
+    qs = queries(c, 2, 4)
+    sk.sink_attention(c.st, c.pages, 0, qs, S, W, c.ws)
+    verify(c, qs, lambda i, n, m: O.seen_sink(n, m, S, W), [0, 1], [4, 4])
+    # a token that only the first of the queries still sees
+    j = L - 4 - W + 1
+    for x in (c.pages.v,):
+        x[0, int(c.ref.table[0, j // 64]), :, j % 64] = bad
+    sk.sink_attention(c.st, c.pages, 0, qs, S, W, c.ws)
+    torch.cuda.synchronize()
+    o, lse, q = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy(), qs.q.float().cpu().numpy()
+    assert not np.isfinite(o[0, 0]).any()
+    seen = O.seen_sink(L, 4, S, W)
+    for t in (1, 2, 3):
+        PH.check_attention(o[0, t:t + 1], lse[0, t:t + 1], q[0, t:t + 1], k0, v0, seen[t:t + 1], what=f"window {t}")
+    c.st.close()
+
+
+def test_a_seen_value_that_is_not_finite_marks_its_column_only():
+    T, L = 4, 150
+    c = filled([L], P=64)
+    at = L - T + 2
+    c.pages.v[0, int(c.ref.table[0, at // 64]), 1, at % 64, 17] = float("inf")
+    mask = [[0b0001, 0b0011, 0b0101, 0b1101]]
+    qs = queries(c, 1, T, mask=words(mask, T))
+    sk.tree_attention(c.st, c.pages, 0, qs, c.ws)
+    o = qs.o.float().cpu()
+    for t in range(T):
+        for h in range(28):
+            want_inf = t >= 2 and h // 7 == 1
+            assert bool(torch.isinf(o[0, t, h, 17])) == want_inf, (t, h)
+            assert torch.isfinite(torch.cat((o[0, t, h, :17], o[0, t, h, 18:]))).all(), (t, h)
+    c.st.close()
+
+
+def test_sequences_that_do_not_fit_are_reported_and_empty():
+    c = filled([40, 90, 50], P=16)
+    for rows, counts, reported in (([0, 7, 2], [3, 3, 3], 1), ([0, -1, 2], [3, 3, 3], 1), ([1, 0, 2], [3, 41, 3], 1)):
+        T = max(counts)
+        qs = queries(c, 3, T, rows=c.ids(rows), n_tokens=c.ids(counts))
+        sk.sink_attention(c.st, c.pages, 0, qs, 2, 30, c.ws)
+        torch.cuda.synchronize()
+        assert sk.device_error_status(c.st) == sk.ERR_DEVICE
+        n = counts[1]
+        assert torch.all(qs.o[1, :n] == 0) and torch.all(torch.isneginf(qs.lse[1, :n]))
+        for i in (0, 2):
+            k, v = c.cache(rows[i], 0)
+            PH.check_attention(qs.o[i, :3].float().cpu().numpy(), qs.lse[i, :3].cpu().numpy(), qs.q[i, :3].float().cpu().numpy(),
+                               k, v, O.seen_sink(k.shape[1], 3, 2, 30), what=f"seq {i}")
+    for counts in ([3, 4, 3], [3, -2, 3]):      # more queries than the call has room for, or fewer than none
+        qs = queries(c, 3, 3, n_tokens=c.ids(counts))
+        sk.sink_attention(c.st, c.pages, 0, qs, 2, 30, c.ws)
+        torch.cuda.synchronize()
+        assert sk.device_error_status(c.st) == sk.ERR_DEVICE
+        assert torch.all(qs.o[1] == 9.0)
+    # a page number that is not one
+    c.pages.table[1, 2] = 1 << 28
+    qs = queries(c, 3, 3)
+    sk.sink_attention(c.st, c.pages, 0, qs, 0, 1000, c.ws)
+    torch.cuda.synchronize()
+    assert sk.device_error_status(c.st) == sk.ERR_DEVICE
+    c.st.close()
+
+
+def test_a_captured_call_replays_as_the_cache_grows():
+    c = filled([60, 125], P=64, spare=8)
+    qs = queries(c, 2, 1)
+    rows, one = c.ids([0, 1]), c.ids([1, 1])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        sk.pages_extend(c.st, c.pages, rows, one, c.ws)
+        sk.sink_attention(c.st, c.pages, 0, qs, 4, 100, c.ws)
+    for step in range(8):      # over the end of a page
+        qs.q.copy_(torch.randn_like(qs.q))
+        g.replay()
+        c.ref.extend([0, 1], [1, 1])
+        verify(c, qs, lambda i, L, n: O.seen_sink(L, n, 4, 100), [0, 1], [1, 1])
+    c.check()
+    c.st.close()
+
+
+def test_the_same_bits_every_time():
+    c = filled([3001, 500, 1700], P=32)
+    qs = queries(c, 3, 9)
+    sk.sink_attention(c.st, c.pages, 0, qs, 4, 1500, c.ws)
+    first = qs.o.clone(), qs.lse.clone()
+    for _ in range(5):
+        c.ws.fill_(0xAB)
+        sk.sink_attention(c.st, c.pages, 0, qs, 4, 1500, c.ws)
+        assert torch.equal(qs.o, first[0]) and torch.equal(qs.lse, first[1])
+    c.st.close()
+
+
+def test_a_decoding_loop_over_a_compressed_cache():
+    """The operators as they are used: prompts go into pages, are scored and selected from a contiguous copy of
+    their keys, compressed where they are, branched, and each branch checks drafted tokens and keeps those it
+    accepts.  The pool and every output are the oracle's."""
+    w, nl = 8, 2
+    st = sk.init_state(sk.Config(n_layers=nl, n_heads=28, n_kv_heads=4, window=w, grid_rows=8, grid_cols=8, max_seqs=2,
+                                 n_warmup=0, n_ramp=0))
+    c = PH.Pair(st, n_pages=60, P=16, n_rows=6, max_pages=20, seed=3)
+    lens, B = [201, 137], 60
+    c.extend([0, 1], lens)
+    rng = np.random.default_rng(0)
+    seqs = []
+    for i, L in enumerate(lens):
+        kv = torch.from_numpy(rng.standard_normal((2, 1, nl, L, 4, PH.D), dtype=np.float32)).to(torch.bfloat16).cuda()
+        sk.pages_store(st, c.pages, 0, sk.Tokens(k=kv[0], v=kv[1], rows=c.ids([i])))
+        for l in range(nl):
+            for x, part in ((c.ref.k, kv[0]), (c.ref.v, kv[1])):
+                c.ref.store(i, l, x, part[0, l].view(torch.int16).cpu().numpy())
+        flat = torch.empty((1, nl, 4, L, PH.D), dtype=torch.bfloat16, device="cuda")
+        sk.pages_load(st, c.pages, 0, sk.Tokens(k=flat.transpose(2, 3), rows=c.ids([i])))
+        assert torch.equal(flat.transpose(2, 3), kv[0])
+        q = torch.from_numpy(rng.standard_normal((nl, 28, w, PH.D), dtype=np.float32)).to(torch.bfloat16).cuda()
+        meta = sk.meta_tensor(sk.pack_meta(np.arange(L) < 64, np.zeros(L), np.arange(L) // 8 % 8, np.arange(L) % 8)).cuda()
+        seqs.append(sk.Seq(k=flat[0], q=q, meta=meta, L=L, budget=B, slot=i, S=torch.empty((nl, 4, L - w), device="cuda"),
+                           idx=torch.empty((nl, 1, B), dtype=torch.int32, device="cuda"),
+                           meta_out=torch.empty((nl, 1, B + w), dtype=torch.int32, device="cuda")))
+    ws = sk.workspace(st, seqs)
+    for l in range(nl):
+        sk.score_layer(st, l, seqs, ws)
+        sk.select(st, l, seqs, ws)
+    sk.pages_compact(st, c.pages, c.ids([0, 1]), seqs, c.ws)
+    c.ref.compact([0, 1], lens, [s.idx.cpu().numpy() for s in seqs], w)
+    c.check()
+    c.fork([0, 0, 1], [2, 4, 5])
+    rows, T = [0, 2, 4, 5], 7
+    for step in range(3):
+        c.extend(rows, [T] * 4)
+        masks = [random_tree(rng, T) for _ in rows]
+        kv = torch.from_numpy(rng.standard_normal((2, 4, nl, T, 4, PH.D), dtype=np.float32)).to(torch.bfloat16).cuda()
+        sk.pages_store(st, c.pages, 0, sk.Tokens(k=kv[0], v=kv[1], rows=c.ids(rows)))
+        for i, r in enumerate(rows):
+            for l in range(nl):
+                for x, part in ((c.ref.k, kv[0]), (c.ref.v, kv[1])):
+                    c.ref.store(r, l, x, part[i, l].view(torch.int16).cpu().numpy())
+        for l in range(nl):
+            qs = queries(c, 4, T, seed=10 * step + l, mask=words(masks, T), rows=c.ids(rows))
+            sk.tree_attention(st, c.pages, l, qs, c.ws)
+            verify(c, qs, lambda i, L, n: O.seen_tree(L, n, masks[i]), rows, [T] * 4, layer=l)
+            qs = queries(c, 4, T, seed=10 * step + l, rows=c.ids(rows))
+            sk.sink_attention(st, c.pages, l, qs, 4, 40, c.ws)
+            verify(c, qs, lambda i, L, n: O.seen_sink(L, n, 4, 40), rows, [T] * 4, layer=l)
+        c.check()
+    c.free([0, 2, 4, 5, 1])
+    c.check()
+    assert int(c.pages.refs.sum()) == 0
+    st.close()
