@@ -509,7 +509,8 @@ enum {
   STARKV_KERNEL_PAGE_GATHER = 9,  /* its compaction (Eq. 11 on pages)                      */
   STARKV_KERNEL_PAGE_MOVE = 10,   /* tokens into and out of pages                          */
   STARKV_KERNEL_PAGED_ATTENTION = 11,  /* tree and sink attention                          */
-  STARKV_NUM_KERNELS = 12
+  STARKV_KERNEL_PAGED_COMBINE = 12,    /* merge of its parts                               */
+  STARKV_NUM_KERNELS = 13
 };
 
 /* Kernel timing, a profiling aid.  While `on` is non-zero every kernel launch

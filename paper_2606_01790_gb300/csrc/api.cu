@@ -145,6 +145,7 @@ const char* kernel_range_name(int kind) {
     case STARKV_KERNEL_PAGE_GATHER: return "starkv: page compaction";
     case STARKV_KERNEL_PAGE_MOVE: return "starkv: tokens and pages";
     case STARKV_KERNEL_PAGED_ATTENTION: return "starkv: paged attention";
+    case STARKV_KERNEL_PAGED_COMBINE: return "starkv: paged attention (combine)";
     default: return "starkv: kernel";
   }
 }
@@ -632,6 +633,7 @@ starkv_status starkv_init_state(const starkv_config* cfg, starkv_state** out, vo
   if (e == cudaSuccess) e = select_configure();
   if (e == cudaSuccess) e = attn_configure();
   if (e == cudaSuccess) e = pages_configure();
+  if (e == cudaSuccess) e = paged_attn_configure();
   if (e != cudaSuccess) {
     delete st;
     return set_error(STARKV_ERR_CUDA, "device setup failed: %s", cudaGetErrorString(e));
@@ -1255,8 +1257,6 @@ starkv_status move_tokens(starkv_state* st, bool store, const starkv_pages* page
   return STARKV_OK;
 }
 
-constexpr int kMaxRowBlocks = 1024;   // 128-row blocks of one sequence's queries
-
 starkv_status validate_queries(const starkv_state* st, int layer, const starkv_queries* q, bool tree) {
   if (!q) return set_error(STARKV_ERR_INVALID_ARG, "queries is NULL");
   starkv_status s = check_rows(q->n);
@@ -1264,10 +1264,10 @@ starkv_status validate_queries(const starkv_state* st, int layer, const starkv_q
   const starkv_config& c = st->cfg;
   if (layer < 0 || layer >= c.n_layers) return set_error(STARKV_ERR_INVALID_ARG, "layer out of range");
   const int hg = c.n_heads / c.n_kv_heads;
-  if (hg > 128) return set_error(STARKV_ERR_UNSUPPORTED, "paged attention takes n_heads / n_kv_heads <= 128");
+  if (hg > kPagedRows) return set_error(STARKV_ERR_UNSUPPORTED, "paged attention takes n_heads / n_kv_heads <= 128");
   if (q->T < 0) return set_error(STARKV_ERR_INVALID_ARG, "queries: T is negative");
   if (tree && q->T > kMaxDraft) return set_error(STARKV_ERR_UNSUPPORTED, "tree attention takes T <= 64");
-  if (q->T > kMaxRowBlocks * (128 / hg)) return set_error(STARKV_ERR_UNSUPPORTED, "queries: T > 1024 * floor(128 / (H / G))");
+  if (q->T > kPagedItems * (kPagedRows / hg)) return set_error(STARKV_ERR_UNSUPPORTED, "queries: T > 1024 * floor(128 / (H / G))");
   if (q->n == 0 || q->T == 0) return STARKV_OK;
   if (!q->q || !q->o || !aligned16(q->q) || !aligned16(q->o))
     return set_error(STARKV_ERR_INVALID_ARG, "queries: q or o NULL or not 16-byte aligned");
@@ -1283,7 +1283,35 @@ starkv_status validate_queries(const starkv_state* st, int layer, const starkv_q
   return STARKV_OK;
 }
 
-size_t paged_attn_ws_bytes(const starkv_state*, int, int) { return 0; }
+// Workspace of the attention: two parts and one record per CTA.
+struct PagedWs {
+  size_t ml, o, total;
+};
+
+PagedWs paged_attn_ws(const starkv_state* st) {
+  const size_t parts = 2 * static_cast<size_t>(st->num_sms) * kPagedRows;
+  PagedWs w;
+  w.ml = align256(static_cast<size_t>(st->num_sms) * sizeof(PagedSplit));
+  w.o = w.ml + align256(parts * sizeof(float2));
+  w.total = w.o + align256(parts * kHeadDim * sizeof(float));
+  return w;
+}
+
+// The pages of one layer as a 4-D bf16 map, 128-byte swizzle, box (64, min(P, 64), 1, 1), zeros out of bounds.
+starkv_status encode_pages(CUtensorMap* map, const void* base, const PagesView& pg) {
+  const cuuint64_t P = cuuint64_t(1) << pg.shift;
+  cuuint64_t dims[4] = {kHeadDim, P, static_cast<cuuint64_t>(pg.G), static_cast<cuuint64_t>(pg.n_pages)};
+  // (one page: its stride is never stepped along, and may be any)
+  cuuint64_t strides[3] = {kHeadDim * 2, P * kHeadDim * 2,
+                           pg.n_pages > 1 ? static_cast<cuuint64_t>(pg.page_stride) * 2 : P * kHeadDim * 2 * pg.G};
+  cuuint32_t box[4] = {64, static_cast<cuuint32_t>(std::min<cuuint64_t>(P, kPagedUnitKeys)), 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return set_error(STARKV_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+  return STARKV_OK;
+}
 
 starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* q, bool tree,
                               int32_t n_sink, int32_t window, void* workspace, size_t workspace_bytes, void* stream) {
@@ -1293,12 +1321,16 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
   if (n_sink < 0 || window < 0) return set_error(STARKV_ERR_INVALID_ARG, "n_sink and window must be >= 0");
   if ((s = check_device(st)) != STARKV_OK) return s;
   if (q->n == 0 || q->T == 0) return STARKV_OK;
-  if ((s = check_ws(st, workspace, workspace_bytes, paged_attn_ws_bytes(st, q->n, q->T))) != STARKV_OK) return s;
+  const PagedWs w = paged_attn_ws(st);
+  if ((s = check_ws(st, workspace, workspace_bytes, w.total)) != STARKV_OK) return s;
+  if ((s = get_encoder()) != STARKV_OK) return s;
   const starkv_config& c = st->cfg;
   const PagesView pg = view_of(st, *pages);
+  char* ws = static_cast<char*>(workspace);
   PagedAttnParams p;
   memset(&p, 0, sizeof(p));
-  p.k = pg.k + layer * pg.layer_stride;
+  if ((s = encode_pages(&p.tmk, pg.k + layer * pg.layer_stride, pg)) != STARKV_OK) return s;
+  if ((s = encode_pages(&p.tmv, pg.v + layer * pg.layer_stride, pg)) != STARKV_OK) return s;
   p.v = pg.v + layer * pg.layer_stride;
   p.page_stride = pg.page_stride;
   p.table = pg.table;
@@ -1307,13 +1339,6 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
   p.n_rows = pg.n_rows;
   p.max_pages = pg.max_pages;
   p.shift = pg.shift;
-  p.q = static_cast<const __nv_bfloat16*>(q->q);
-  p.o = static_cast<__nv_bfloat16*>(q->o);
-  p.lse = q->lse;
-  p.mask = q->mask;
-  p.rows = q->rows;
-  p.n_tokens = q->n_tokens;
-  p.n = q->n;
   p.T = q->T;
   p.q_seq = q->q_seq_stride;
   p.q_token = q->q_token_stride;
@@ -1323,13 +1348,38 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
   p.o_head = q->o_head_stride;
   p.H = c.n_heads;
   p.G = c.n_kv_heads;
+  p.hg = p.H / p.G;
+  p.tb = kPagedRows / p.hg;
+  p.nblk = (p.T + p.tb - 1) / p.tb;
   p.tree = tree;
   p.n_sink = std::min(n_sink, 1 << 25);   // (more than any length)
   p.window = std::min(window, 1 << 25);
   p.scale2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kHeadDim)));
+  p.stages = paged_attn_stages();
+  p.split = reinterpret_cast<PagedSplit*>(ws);
+  p.part_ml = reinterpret_cast<float2*>(ws + w.ml);
+  p.part_o = reinterpret_cast<float*>(ws + w.o);
   p.err = st->dev.err;
+  p.wait_ns = st->wait_ns;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_ATTENTION, cs, [&] { return paged_attn_launch(p, st->num_sms, cs); }));
+  // as many sequences a launch as it has room for query blocks
+  const int per_launch = kPagedItems / p.nblk;
+  const int64_t max_units = (static_cast<int64_t>(pg.max_pages) << pg.shift) / kPagedUnitKeys + 2;
+  for (int i0 = 0; i0 < q->n; i0 += per_launch) {
+    p.n = std::min(q->n - i0, per_launch);
+    p.items = p.n * p.nblk;
+    p.q = static_cast<const __nv_bfloat16*>(q->q) + i0 * p.q_seq;
+    p.o = static_cast<__nv_bfloat16*>(q->o) + i0 * p.o_seq;
+    const int64_t first = static_cast<int64_t>(i0) * p.T;
+    p.lse = q->lse ? q->lse + first * p.H : nullptr;
+    p.mask = q->mask ? q->mask + first : nullptr;
+    p.rows = q->rows ? q->rows + i0 : nullptr;
+    p.n_tokens = q->n_tokens ? q->n_tokens + i0 : nullptr;
+    p.row0 = i0;
+    p.grid = static_cast<int>(std::min<int64_t>(st->num_sms, p.items * max_units * p.G));
+    CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_ATTENTION, cs, [&] { return paged_attn_launch(p, cs); }));
+    CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_COMBINE, cs, [&] { return paged_combine_launch(p, cs); }));
+  }
   return STARKV_OK;
 }
 
@@ -1344,7 +1394,7 @@ starkv_status starkv_pages_workspace_bytes(const starkv_state* st, const starkv_
   if (s != STARKV_OK) return s;
   if ((s = check_rows(n)) != STARKV_OK) return s;
   if (T < 0) return set_error(STARKV_ERR_INVALID_ARG, "T is negative");
-  *bytes = std::max(book_ws(*pages, n).total, paged_attn_ws_bytes(st, n, T));
+  *bytes = std::max(book_ws(*pages, n).total, paged_attn_ws(st).total);
   return STARKV_OK;
 }
 

@@ -107,19 +107,6 @@ __device__ __forceinline__ bool warp_wait(const AttnCtl* ctl, uint64_t* bar, uin
   return __all_sync(kFull, mbar_wait(bar, parity, limit_ns) && !aborted);
 }
 
-// Shared-memory descriptor of an MN-major operand in 128-byte swizzled rows
-// (TMA SWIZZLE_128B of a [K][MN] tile, MN contiguous): 64-element MN groups
-// `lbo` bytes apart, 8-row K groups `sbo` bytes apart.
-__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr >> 4) & 0x3FFFu);
-  d |= static_cast<uint64_t>((lbo >> 4) & 0x3FFFu) << 16;
-  d |= static_cast<uint64_t>((sbo >> 4) & 0x3FFFu) << 32;
-  d |= static_cast<uint64_t>(1) << 46;   // descriptor version (tcgen05)
-  d |= static_cast<uint64_t>(2) << 61;   // swizzle mode: 128 B
-  return d;
-}
-
 // Instruction descriptor of tcgen05.mma kind::f16 with fp16 A (K-major) and
 // fp16 B (MN-major), fp32 accumulator, shape M x N.
 __host__ __device__ constexpr uint32_t idesc_f16_bmn(int M, int N) {
@@ -128,38 +115,6 @@ __host__ __device__ constexpr uint32_t idesc_f16_bmn(int M, int N) {
          | (static_cast<uint32_t>(N >> 3) << 17)
          | (static_cast<uint32_t>(M >> 4) << 24);
 }
-
-// D[tmem] (+)= A[tmem] * B[smem]: A with M = 128 rows on TMEM lanes and its
-// K elements as fp16 pairs, lower index in the low half of each 32-bit column.
-__device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                           uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
-// 8 consecutive 32-bit columns of this warp's 32 TMEM lanes, stored.
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};\n" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-      : "memory");
-}
-
-// 16 consecutive fp32 columns of this warp's 32 TMEM lanes, stored.
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t pack_half2(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);

@@ -5,10 +5,19 @@
 
 namespace starkv {
 
-constexpr int kMaxDraft = 64;   // drafted tokens of a tree (bits of a mask word)
+constexpr int kMaxDraft = 64;        // drafted tokens of a tree (bits of a mask word)
+constexpr int kPagedRows = 128;      // query rows of a block: (token, head of the group)
+constexpr int kPagedUnitKeys = 64;   // keys per pipeline unit
+constexpr int kPagedItems = 1024;    // query blocks of a launch
+
+// The piece that a CTA leaves unfinished: blocks c0 .. c1 hold parts of it.
+struct PagedSplit {
+  int64_t total;   // units of the launch
+  int valid, item, g, c1;
+};
 
 struct PagedAttnParams {
-  const __nv_bfloat16* k;   // the layer's pages
+  CUtensorMap tmk, tmv;     // the layer's pages: dims (d, P, G, n_pages), box (64, min(P, 64), 1, 1), 128B swizzle
   const __nv_bfloat16* v;
   int64_t page_stride;      // elements
   const int32_t* table;
@@ -19,17 +28,27 @@ struct PagedAttnParams {
   __nv_bfloat16* o;
   float* lse;               // [n][T][H], or NULL
   const uint64_t* mask;     // tree: [n][T]
-  const int32_t* rows;      // [n], or NULL
+  const int32_t* rows;      // [n], or NULL = row0, row0 + 1, ...
   const int32_t* n_tokens;  // [n], or NULL
-  int n, T;
+  int row0, n, T;
   int64_t q_seq, q_token, q_head, o_seq, o_token, o_head;
-  int H, G;
+  int H, G, hg;             // hg = H / G
+  int tb, nblk, items;      // tokens of a block (floor(128 / hg)), blocks of a sequence, n * nblk
   int tree;                 // 1: mask, 0: n_sink and window
   int n_sink, window;
   float scale2;             // log2(e) / sqrt(d)
+  int grid;                 // CTAs of the main kernel
+  int stages;               // depth of the K and V rings
+  PagedSplit* split;        // [grid]
+  float2* part_ml;          // [2 * grid][128] reference and sum of a part
+  float* part_o;            // [2 * grid][128][128] unnormalised output of a part
   uint32_t* err;
+  uint64_t wait_ns;
 };
 
-cudaError_t paged_attn_launch(const PagedAttnParams& p, int num_sms, cudaStream_t stream);
+cudaError_t paged_attn_configure();
+int paged_attn_stages();
+cudaError_t paged_attn_launch(const PagedAttnParams& p, cudaStream_t stream);
+cudaError_t paged_combine_launch(const PagedAttnParams& p, cudaStream_t stream);
 
 }  // namespace starkv

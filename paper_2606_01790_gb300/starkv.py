@@ -35,7 +35,7 @@ ABI_FUNCTIONS = [
 ]
 
 KERNELS = ["score_lse", "score_accum", "pool", "calibrate", "compact", "attention", "attn_combine",
-           "page_book", "page_copy", "page_gather", "page_move", "paged_attention"]
+           "page_book", "page_copy", "page_gather", "page_move", "paged_attention", "paged_combine"]
 
 
 SELECT_GLOBAL, SELECT_PER_HEAD = 0, 1   # starkv_config.select_mode
