@@ -462,14 +462,14 @@ starkv_status starkv_pages_load(starkv_state* st, const starkv_pages* pages, int
  * not looked at).  With z_j = q . K[g(h), j] / sqrt(d) over the keys seen,
  *   o = sum_j softmax_j(z) V[g(h), j],   lse = log sum_j exp(z_j);
  * a query that sees none has o = 0 and lse = -inf.  K and V that a query does not
- * see do not reach its output, whatever they hold.  H / G <= 128. */
+ * see do not reach its output, whatever they hold. */
 starkv_status starkv_tree_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
                                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* The same with a sliding window and sinks: query t, the token at position i = L -
  * n + t of its row, sees the keys j <= i with j < n_sink or j > i - window
  * (n_sink, window >= 0; window >= L is plain causal attention).  T = 1 is decoding,
- * larger T a chunk of a prompt (T <= 1024 * floor(128 / (H / G))). */
+ * larger T a chunk of a prompt (T * H / G <= 2^17). */
 starkv_status starkv_sink_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
                                     int32_t n_sink, int32_t window, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -1264,10 +1264,10 @@ starkv_status validate_queries(const starkv_state* st, int layer, const starkv_q
   const starkv_config& c = st->cfg;
   if (layer < 0 || layer >= c.n_layers) return set_error(STARKV_ERR_INVALID_ARG, "layer out of range");
   const int hg = c.n_heads / c.n_kv_heads;
-  if (hg > kPagedRows) return set_error(STARKV_ERR_UNSUPPORTED, "paged attention takes n_heads / n_kv_heads <= 128");
   if (q->T < 0) return set_error(STARKV_ERR_INVALID_ARG, "queries: T is negative");
   if (tree && q->T > kMaxDraft) return set_error(STARKV_ERR_UNSUPPORTED, "tree attention takes T <= 64");
-  if (q->T > kPagedItems * (kPagedRows / hg)) return set_error(STARKV_ERR_UNSUPPORTED, "queries: T > 1024 * floor(128 / (H / G))");
+  if (static_cast<int64_t>(q->T) * hg > kPagedItems * kPagedRows)
+    return set_error(STARKV_ERR_UNSUPPORTED, "queries: T * (H / G) > 2^17");
   if (q->n == 0 || q->T == 0) return STARKV_OK;
   if (!q->q || !q->o || !aligned16(q->q) || !aligned16(q->o))
     return set_error(STARKV_ERR_INVALID_ARG, "queries: q or o NULL or not 16-byte aligned");
@@ -1349,13 +1349,11 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
   p.H = c.n_heads;
   p.G = c.n_kv_heads;
   p.hg = p.H / p.G;
-  p.tb = kPagedRows / p.hg;
-  p.nblk = (p.T + p.tb - 1) / p.tb;
+  p.nblk = (p.T * p.hg + kPagedRows - 1) / kPagedRows;
   p.tree = tree;
   p.n_sink = std::min(n_sink, 1 << 25);   // (more than any length)
   p.window = std::min(window, 1 << 25);
   p.scale2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kHeadDim)));
-  p.stages = paged_attn_stages();
   p.split = reinterpret_cast<PagedSplit*>(ws);
   p.part_ml = reinterpret_cast<float2*>(ws + w.ml);
   p.part_o = reinterpret_cast<float*>(ws + w.o);

@@ -6,7 +6,7 @@
 namespace starkv {
 
 constexpr int kMaxDraft = 64;        // drafted tokens of a tree (bits of a mask word)
-constexpr int kPagedRows = 128;      // query rows of a block: (token, head of the group)
+constexpr int kPagedRows = 128;      // query rows of a block: (token, head of the group) pairs
 constexpr int kPagedUnitKeys = 64;   // keys per pipeline unit
 constexpr int kPagedItems = 1024;    // query blocks of a launch
 
@@ -33,12 +33,11 @@ struct PagedAttnParams {
   int row0, n, T;
   int64_t q_seq, q_token, q_head, o_seq, o_token, o_head;
   int H, G, hg;             // hg = H / G
-  int tb, nblk, items;      // tokens of a block (floor(128 / hg)), blocks of a sequence, n * nblk
+  int nblk, items;          // blocks of a sequence, n * nblk
   int tree;                 // 1: mask, 0: n_sink and window
   int n_sink, window;
   float scale2;             // log2(e) / sqrt(d)
   int grid;                 // CTAs of the main kernel
-  int stages;               // depth of the K and V rings
   PagedSplit* split;        // [grid]
   float2* part_ml;          // [2 * grid][128] reference and sum of a part
   float* part_o;            // [2 * grid][128][128] unnormalised output of a part
@@ -47,7 +46,6 @@ struct PagedAttnParams {
 };
 
 cudaError_t paged_attn_configure();
-int paged_attn_stages();
 cudaError_t paged_attn_launch(const PagedAttnParams& p, cudaStream_t stream);
 cudaError_t paged_combine_launch(const PagedAttnParams& p, cudaStream_t stream);
 
