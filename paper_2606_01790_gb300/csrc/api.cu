@@ -1350,6 +1350,9 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
   p.G = c.n_kv_heads;
   p.hg = p.H / p.G;
   p.nblk = (p.T * p.hg + kPagedRows - 1) / kPagedRows;
+  auto reciprocal = [](int n) { return n > 1 ? static_cast<uint32_t>(((uint64_t(1) << 32) + n - 1) / n) : 0u; };
+  p.inv_hg = reciprocal(p.hg);
+  p.inv_nblk = reciprocal(p.nblk);
   p.tree = tree;
   p.n_sink = std::min(n_sink, 1 << 25);   // (more than any length)
   p.window = std::min(window, 1 << 25);
@@ -1365,7 +1368,6 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
   const int64_t max_units = (static_cast<int64_t>(pg.max_pages) << pg.shift) / kPagedUnitKeys + 2;
   for (int i0 = 0; i0 < q->n; i0 += per_launch) {
     p.n = std::min(q->n - i0, per_launch);
-    p.items = p.n * p.nblk;
     p.q = static_cast<const __nv_bfloat16*>(q->q) + i0 * p.q_seq;
     p.o = static_cast<__nv_bfloat16*>(q->o) + i0 * p.o_seq;
     const int64_t first = static_cast<int64_t>(i0) * p.T;
@@ -1374,7 +1376,7 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
     p.rows = q->rows ? q->rows + i0 : nullptr;
     p.n_tokens = q->n_tokens ? q->n_tokens + i0 : nullptr;
     p.row0 = i0;
-    p.grid = static_cast<int>(std::min<int64_t>(st->num_sms, p.items * max_units * p.G));
+    p.grid = static_cast<int>(std::min<int64_t>(st->num_sms, p.n * p.nblk * max_units * p.G));
     CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_ATTENTION, cs, [&] { return paged_attn_launch(p, cs); }));
     CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_COMBINE, cs, [&] { return paged_combine_launch(p, cs); }));
   }

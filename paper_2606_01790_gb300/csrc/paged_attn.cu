@@ -26,12 +26,19 @@
 // and V covers where a block's rows are few.  (fp16 weights would need V in fp16, which
 // holds neither its range nor its small values.)
 //
-// Even and odd units are two lines with a softmax warpgroup each, which keep a
-// reference m, a sum l and an O of their own: nothing passes between them until a
-// piece's end, where both read both O and write half of the columns.  With one
-// warpgroup for all units the chain S -> registers -> exp2 -> P took 1,900 to 2,100 cycles
-// a unit, more than the stream (1,490) and the products (850).  Three S / P places go
-// round, so that S of a line's next unit is ready when its last P is written.
+// Even and odd units go to two softmax warpgroups.  A unit's way from its first product
+// to the end of its last (S 300 cycles, P V 540, arithmetic and the barriers between)
+// takes about 4,000 cycles, so five units are under way, each in a place of its own in
+// tensor memory.  Both warpgroups weigh against one reference m per row, which passes
+// from unit to unit in order through shared memory (warp to warp); it moves only when a
+// unit's maximum lies more than 15 above it, which rescales the row's O.  Measured, us,
+// chunk of 2,704 tokens / four 56k caches with 64 drafted tokens: one warpgroup 278 / 344, two
+// with an O each and three places 185 / 232.
+//
+// Query blocks of one drafted tree read the same keys.  Where most sequences have as
+// many blocks, a gang of CTAs, one per block, goes through a range of keys at the same
+// time, so that the second reader finds them in L2; the flat order, whose readers come
+// apart, reads them from memory again.
 //
 // Pages come by TMA, a box per page (or 64 of its rows); a page number that is none
 // lies outside the map and reads as zeros.  Units that not every row of the block sees
@@ -44,7 +51,6 @@
 // Warp roles: 0 loads K, 3 loads V, 1 issues S and owns tensor memory, 2 issues P V,
 // 4..7 and 8..11 softmax.
 #include <algorithm>
-#include <type_traits>
 
 #include "common.cuh"
 #include "paged_attn.cuh"
@@ -59,15 +65,17 @@ constexpr int kStages = 4;                         // depth of the K ring and of
 constexpr int kUnitBytes = kPagedUnitKeys * 256;   // 64 keys x 128 bf16: 16 KB (K or V)
 constexpr int kHalfBytes = kPagedUnitKeys * 128;   // one 64-column half of a unit
 constexpr int kTmemCols = 512;
-constexpr int kSoftWarps = 8;                      // four a line
+constexpr int kStageO = 32 * 64 * 4;                // a softmax warp's half of O: 32 rows x 64 columns
+constexpr int kSoftWarps = 8;                      // four a line (even or odd units)
 constexpr uint32_t kFull = 0xffffffffu;
-constexpr float kMoveThreshold = 15.f;             // log2 units that a row may rise above its reference
+constexpr float kSumLimit = 16384.f;               // largest sum of a unit's 64 weights against a row's reference ...
+constexpr float kMoveThreshold = 8.f;              // ... a larger one holds a weight above 2^8
 constexpr uint64_t kDrainWaitNs = 2000000000ull;
 constexpr uint64_t kAll = ~uint64_t(0);
 
-// Tensor memory, in columns: O 2 x 128, S or P 3 x 64 (P: 32 hi, 32 lo), Q 64.
-constexpr int kPlaces = 3;
-constexpr uint32_t kColO = 0, kColS = 256, kColQ = 448;
+// Tensor memory, in columns: O 128, S or P 5 x 64 (P: 32 hi, 32 lo), Q 64.
+constexpr int kPlaces = 5;
+constexpr uint32_t kColO = 0, kColS = 128, kColQ = 448;
 
 __device__ __forceinline__ uint64_t drain_limit(uint64_t wait_ns) {
   return wait_ns > kDrainWaitNs ? wait_ns : kDrainWaitNs;
@@ -81,6 +89,7 @@ struct Ctl {
   uint64_t k_full[kStages], k_empty[kStages];
   uint64_t v_full[kStages], v_empty[kStages];
   uint64_t s_full[kPlaces], p_full[kPlaces], p_empty[kPlaces];   // S is there; P is; the product that reads P is done
+  uint64_t ref[2][4];               // [line][warp]: the references after its unit are in `m`
   uint64_t qt_full;                 // a piece's queries are in tensor memory
   uint64_t ml_full;                 // both lines' m and l of a piece are in `ml`
   uint64_t o_empty;                 // a piece's O has been read
@@ -89,33 +98,55 @@ struct Ctl {
   volatile int abort;
   volatile int poison[8];           // [piece & 7]: piece + 1 if the piece met such elements
   int warp_sum[kThreads / 32];
+  int items;                        // of the launch: sequences in gangs, else query blocks
+  int gang;                         // CTAs of a gang (1: none)
+  int64_t sum[2];                   // units, and units times blocks
+  volatile float m[1 + kPagedRows]; // [1 + row]: the rows' references, as they pass from unit to unit
   float2 ml[2][2][kPagedRows];      // [piece & 1][line]
   int before[kPagedItems + 1];      // units before an item (one KV group)
   Item item[kPagedItems];
 };
 
-// Unit u of a CTA uses place u % 3 and the stages u % kStages for the (u / 3)-th or
-// (u / kStages)-th time, which gives the parities of their barriers.
-__device__ __forceinline__ int place_of(uint32_t u) { return static_cast<int>(u % kPlaces); }
-__device__ __forceinline__ uint32_t place_par(uint32_t u) { return u / kPlaces & 1; }
+// Where a unit stands in a ring of N barriers: its place and the parity of its use.
+template <int N>
+struct Ring {
+  int at = 0;
+  uint32_t par = 0;
+  __device__ __forceinline__ void next() {
+    if (++at == N) at = 0, par ^= 1;
+  }
+};
 
 __device__ __forceinline__ void fail(Ctl* ctl, uint32_t* err) {
   ctl->abort = 1;
   atomicOr(err, kErrTimeout);
 }
 
-// A wait of a warp-wide role: true when every lane's barrier completed and no role
-// had failed before it.  The one place where these roles learn of a failure, so
-// that a warp's lanes leave together (`abort` is read ahead of the wait, where it
-// costs nothing).
+// A wait of a warp-wide role: true when every lane's barrier completed and, where that
+// took time, no role had failed.  The one place where these roles learn of a failure, so
+// that a warp's lanes leave together: a barrier that a failed role should have
+// completed does not complete.
 __device__ __forceinline__ bool warp_wait(const Ctl* ctl, uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
+  if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
   const bool aborted = ctl->abort;
   return __all_sync(kFull, mbar_wait(bar, parity, limit_ns) && !aborted);
+}
+
+// Two of them, at the price of one where both are complete.
+__device__ __forceinline__ bool warp_wait2(const Ctl* ctl, uint64_t* a, uint32_t pa, uint64_t* b, uint32_t pb, uint64_t limit_ns) {
+  const bool ra = mbar_try_wait(a, pa), rb = mbar_try_wait(b, pb);
+  if (__all_sync(kFull, ra && rb)) return true;
+  return warp_wait(ctl, a, pa, limit_ns) && warp_wait(ctl, b, pb, limit_ns);
 }
 
 // Instruction descriptor of tcgen05.mma kind::f16 with bf16 A (K-major) and bf16 B
 // (MN-major), fp32 accumulator, shape M x N.
 __host__ __device__ constexpr uint32_t idesc_bf16_bmn(int M, int N) { return idesc_bf16(M, N) | (1u << 16); }
+
+// x / n by its reciprocal ceil(2^32 / n) (0 for n = 1), for x n < 2^32
+__device__ __forceinline__ int quotient(int x, uint32_t inv) {
+  return inv ? static_cast<int>(__umulhi(static_cast<uint32_t>(x), inv)) : x;
+}
 
 // ---------------------------------------------------------------- what is seen
 
@@ -130,6 +161,8 @@ __device__ __forceinline__ uint64_t shifted(uint64_t m, int s) {
 struct Seen {
   int first, lo, hi, ctx;
   uint64_t bits;
+  // all of the keys k0 .. k0 + 63 (apart from drafted tokens)
+  __device__ __forceinline__ bool whole(int k0) const { return k0 + 64 <= first || (k0 >= lo && k0 + 64 <= hi); }
   // of the keys k0 .. k0 + 63
   __device__ __forceinline__ uint64_t operator()(int k0) const {
     return below(first - k0) | (below(hi - k0) & ~below(lo - k0)) | (bits ? shifted(bits, ctx - k0) : 0);
@@ -143,12 +176,11 @@ struct Block {
   int L, n;
   int sinks, win0;     // units of the sinks before the window's first unit; that unit
 
-  __device__ __forceinline__ Block(const PagedAttnParams& p, const Item& it, int item) : L(it.L), n(it.n) {
-    seq = item / p.nblk;
-    row0 = (item - seq * p.nblk) * kPagedRows;
+  __device__ __forceinline__ Block(const PagedAttnParams& p, const Item& it, int seq_, int b) : seq(seq_), L(it.L), n(it.n) {
+    row0 = b * kPagedRows;
     nrows = min(kPagedRows, n * p.hg - row0);
-    tf = row0 / p.hg;
-    tl = (row0 + max(nrows, 1) - 1) / p.hg;
+    tf = quotient(row0, p.inv_hg);
+    tl = quotient(row0 + max(nrows, 1) - 1, p.inv_hg);
     const int lo = p.tree ? 0 : max(0, first_pos() - p.window + 1), hi = end(p);
     win0 = lo >> 6;
     sinks = p.tree ? 0 : min((min(p.n_sink, hi) + 63) >> 6, win0);
@@ -182,9 +214,56 @@ struct Block {
   }
 };
 
-// Every CTA: the items' lengths and the units before each.
+// A sequence's length and queries (read by every CTA: the call may be replayed).
+__device__ Item read_item(const PagedAttnParams& p, int seq) {
+  const int row = p.rows ? p.rows[seq] : p.row0 + seq;
+  Item it;
+  it.n = p.n_tokens ? p.n_tokens[seq] : p.T;
+  it.L = row >= 0 && row < p.n_rows ? p.len[row] : -1;
+  if (it.n < 0 || it.n > p.T) {
+    it.n = 0;
+    atomicOr(p.err, kErrRow);
+  } else if (it.L < it.n || it.L > static_cast<int64_t>(p.max_pages) << p.shift) {
+    it.L = -1;
+    if (it.n) atomicOr(p.err, kErrRow);
+  }
+  return it;
+}
+
+// Whether the launch goes in gangs, and the units before each item.
 __device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (p.tree && p.nblk > 1) {
+    // A gang of B (the most blocks of a sequence) leaves CTAs idle at sequences with fewer.
+    // A unit costs about 0.55 us of a CTA's time and 0.74 us of its share of the memory's
+    // rate, so the flat order, which reads each block's keys on its own, wins where the
+    // gangs would be busy for less than three quarters of the time.
+    int64_t units = 0, work = 0;
+    int most = 1;
+    for (int seq = tid; seq < p.n; seq += kThreads) {
+      const Item it = read_item(p, seq);
+      const int nb = (it.n * p.hg + kPagedRows - 1) / kPagedRows, u = Block(p, it, seq, 0).units(p);
+      units += u;
+      work += static_cast<int64_t>(u) * nb;
+      most = max(most, nb);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      units += __shfl_xor_sync(kFull, units, o);
+      work += __shfl_xor_sync(kFull, work, o);
+      most = max(most, __shfl_xor_sync(kFull, most, o));
+    }
+    if (lane == 0) {
+      atomicAdd(reinterpret_cast<unsigned long long*>(&ctl->sum[0]), static_cast<unsigned long long>(units));
+      atomicAdd(reinterpret_cast<unsigned long long*>(&ctl->sum[1]), static_cast<unsigned long long>(work));
+      atomicMax(&ctl->gang, most);
+    }
+    __syncthreads();
+    if (tid == 0 && (ctl->gang == 1 || 4 * ctl->sum[1] < 3 * ctl->sum[0] * ctl->gang)) ctl->gang = 1;
+    __syncthreads();
+  }
+  const bool gangs = ctl->gang > 1;
+  const int items = gangs ? p.n : p.n * p.nblk;
   constexpr int kPer = (kPagedItems + kThreads - 1) / kThreads;
   int u[kPer];
   int sum = 0;
@@ -192,21 +271,11 @@ __device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
   for (int k = 0; k < kPer; ++k) {
     const int item = tid * kPer + k;
     u[k] = 0;
-    if (item >= p.items) continue;
-    const int seq = item / p.nblk;
-    const int row = p.rows ? p.rows[seq] : p.row0 + seq;
-    Item it;
-    it.n = p.n_tokens ? p.n_tokens[seq] : p.T;
-    it.L = row >= 0 && row < p.n_rows ? p.len[row] : -1;
-    if (it.n < 0 || it.n > p.T) {
-      it.n = 0;
-      atomicOr(p.err, kErrRow);
-    } else if (it.L < it.n || it.L > static_cast<int64_t>(p.max_pages) << p.shift) {
-      it.L = -1;
-      if (it.n) atomicOr(p.err, kErrRow);
-    }
+    if (item >= items) continue;
+    const int seq = gangs ? item : quotient(item, p.inv_nblk);
+    const Item it = read_item(p, seq);
     ctl->item[item] = it;
-    u[k] = Block(p, it, item).units(p);
+    u[k] = Block(p, it, seq, gangs ? 0 : item - seq * p.nblk).units(p);
     sum += u[k];
   }
   int inc = sum;
@@ -222,26 +291,29 @@ __device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int item = tid * kPer + k;
-    if (item <= p.items) ctl->before[item] = at;
+    if (item <= items) ctl->before[item] = at;
     at += u[k];
   }
+  if (tid == 0) ctl->items = items;
   __syncthreads();
 }
 
 __device__ __forceinline__ int64_t range_begin(int64_t T, int c, int P) { return T * c / P; }
 
-// CTA whose range holds flat unit f
-__device__ __forceinline__ int cta_of(int64_t f, int64_t T, int P) { return static_cast<int>(((f + 1) * P - 1) / T); }
+// Range (of P) that holds flat unit f
+__device__ __forceinline__ int range_of(int64_t f, int64_t T, int P) { return static_cast<int>(((f + 1) * P - 1) / T); }
 
-// The pieces of a CTA's flat range [f0, f1), in order: a run of n units j0, j0 + 1,
-// ... of the nu units of one (item, group).
+// The pieces of a flat range [f0, f1), in order: a run of n units j0, j0 + 1, ... of
+// the nu units of one (item, group).  A gang's CTA number `member` has the query block
+// `member` of every sequence, and passes over the sequences that have no such block.
 struct PieceIter {
   int item, g, j0, n, nu;
+  int member;    // -1: no gangs
   int64_t rem;   // units of the range from this piece on
-  __device__ __forceinline__ PieceIter(const PagedAttnParams& p, const Ctl* ctl, int64_t f0, int64_t f1)
-      : item(0), g(0), j0(0), n(0), nu(0), rem(f1 - f0) {
+  __device__ __forceinline__ PieceIter(const PagedAttnParams& p, const Ctl* ctl, int member_, int64_t f0, int64_t f1)
+      : item(0), g(0), j0(0), n(0), nu(0), member(member_), rem(f1 - f0) {
     if (rem <= 0) return;
-    int hi = p.items;   // the last item with no more than f0 units before it (items without units are passed over)
+    int hi = ctl->items;   // the last item with no more than f0 units before it (items without units are passed over)
     while (hi - item > 1) {
       const int mid = (item + hi) >> 1;
       if (static_cast<int64_t>(ctl->before[mid]) * p.G <= f0) item = mid;
@@ -252,21 +324,50 @@ struct PieceIter {
     g = static_cast<int>(u / nu);
     j0 = static_cast<int>(u - static_cast<int64_t>(g) * nu);
     n = static_cast<int>(min(rem, static_cast<int64_t>(nu - j0)));
+    if (skipped(p, ctl)) next(p, ctl);
   }
   __device__ __forceinline__ bool valid() const { return rem > 0; }
   __device__ __forceinline__ bool whole() const { return n == nu; }
+  __device__ __forceinline__ bool skipped(const PagedAttnParams& p, const Ctl* ctl) const {
+    return member > 0 && member * kPagedRows >= ctl->item[item].n * p.hg;
+  }
+  __device__ __forceinline__ Block block(const PagedAttnParams& p, const Ctl* ctl) const {
+    const int seq = member >= 0 ? item : quotient(item, p.inv_nblk);
+    return Block(p, ctl->item[item], seq, member >= 0 ? member : item - seq * p.nblk);
+  }
   __device__ __forceinline__ void next(const PagedAttnParams& p, const Ctl* ctl) {
-    rem -= n;
-    j0 = 0;
-    if (rem <= 0) return;
-    if (++g == p.G) {
-      g = 0;
-      do {
-        ++item;
-        nu = ctl->before[item + 1] - ctl->before[item];
-      } while (nu == 0);
+    do {
+      rem -= n;
+      j0 = 0;
+      if (rem <= 0) return;
+      if (++g == p.G) {
+        g = 0;
+        do {
+          ++item;
+          nu = ctl->before[item + 1] - ctl->before[item];
+        } while (nu == 0);
+      }
+      n = static_cast<int>(min(rem, static_cast<int64_t>(nu)));
+    } while (skipped(p, ctl));
+  }
+};
+
+// A CTA's share: its place in a gang, and its range.
+struct Share {
+  int member;            // -1: no gangs
+  int range, ranges;
+  int64_t total, fb, fe;
+  __device__ __forceinline__ Share(const PagedAttnParams& p, const Ctl* ctl) {
+    const int B = ctl->gang;
+    member = B > 1 ? static_cast<int>(blockIdx.x % B) : -1;
+    range = blockIdx.x / B;
+    ranges = gridDim.x / B;
+    total = static_cast<int64_t>(ctl->before[ctl->items]) * p.G;
+    fb = fe = 0;
+    if (range < ranges) {   // (the last CTAs may be too few for a gang)
+      fb = range_begin(total, range, ranges);
+      fe = range_begin(total, range + 1, ranges);
     }
-    n = static_cast<int>(min(rem, static_cast<int64_t>(nu)));
   }
 };
 
@@ -275,7 +376,7 @@ struct PieceIter {
 // K or V loader: the units' pages into a ring.  Lane l holds the number of page
 // base + l of the row, so that the table is read once in 32 pages.
 __device__ void load_loop(const PagedAttnParams& p, Ctl* ctl, const CUtensorMap* map, uint8_t* ring, uint64_t* full,
-                          uint64_t* empty, int lane, int64_t fb, int64_t fe) {
+                          uint64_t* empty, int lane, const Share& sh) {
   const uint64_t pol = policy_evict_first();   // a single query block reads K and V once
   const bool once = p.nblk == 1;
   const int P = 1 << p.shift;
@@ -284,12 +385,11 @@ __device__ void load_loop(const PagedAttnParams& p, Ctl* ctl, const CUtensorMap*
   int stage = 0;
   uint32_t phase = 0, used = 0, last_ph = 0;   // last_ph: bit s = phase of the last load into stage s
   bool ok = true;
-  for (PieceIter c(p, ctl, fb, fe); ok && c.valid(); c.next(p, ctl)) {
-    const Item it = ctl->item[c.item];
-    const Block blk(p, it, c.item);
+  for (PieceIter c(p, ctl, sh.member, sh.fb, sh.fe); ok && c.valid(); c.next(p, ctl)) {
+    const Block blk = c.block(p, ctl);
     const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
     const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
-    const int held = it.L < 0 ? 0 : (it.L + P - 1) >> p.shift;
+    const int held = blk.L < 0 ? 0 : (blk.L + P - 1) >> p.shift;
     int base = 0, have = 0, id = 0;
     for (int j = c.j0; ok && j < c.j0 + c.n; ++j) {
       const int k0 = blk.key(j), page0 = k0 >> p.shift;
@@ -336,30 +436,33 @@ __device__ void load_loop(const PagedAttnParams& p, Ctl* ctl, const CUtensorMap*
 
 // ---------------------------------------------------------------- MMA issuers
 
-__device__ void mma_s_loop(const PagedAttnParams& p, Ctl* ctl, const uint8_t* sK, uint32_t tmem, int64_t fb, int64_t fe) {
+__device__ void mma_s_loop(const PagedAttnParams& p, Ctl* ctl, const uint8_t* sK, uint32_t tmem, const Share& sh) {
   const uint32_t idesc = idesc_bf16(kPagedRows, kPagedUnitKeys);
   const uint64_t dk0 = sdesc_k_sw128(smem_u32(sK));
+  Ring<kStages> st;
+  Ring<kPlaces> pl;
   int pc = 0;
-  uint32_t ui = 0;
   bool ok = true;
-  for (PieceIter c(p, ctl, fb, fe); ok && c.valid(); c.next(p, ctl)) {
+  for (PieceIter c(p, ctl, sh.member, sh.fb, sh.fe); ok && c.valid(); c.next(p, ctl)) {
     ok = warp_wait(ctl, &ctl->qt_full, pc & 1, p.wait_ns);
     ++pc;
-    for (int i = 0; ok && i < c.n; ++i, ++ui) {
-      const int stage = ui % kStages, pl = place_of(ui);
-      ok = warp_wait(ctl, &ctl->k_full[stage], ui / kStages & 1, p.wait_ns) &&
-           warp_wait(ctl, &ctl->p_empty[pl], place_par(ui) ^ 1, p.wait_ns);   // the place's previous P has been used
+    for (int i = 0; ok && i < c.n; ++i) {
+      // (the place's previous P has been used)
+      ok = warp_wait2(ctl, &ctl->k_full[st.at], st.par, &ctl->p_empty[pl.at], pl.par ^ 1, p.wait_ns);
       if (!ok) break;
       tc_fence_after();
-      const uint64_t dk = dk0 + static_cast<uint64_t>(stage * (kUnitBytes >> 4));
+      const uint64_t dk = dk0 + static_cast<uint64_t>(st.at * (kUnitBytes >> 4));
+      const uint32_t s = tmem + kColS + 64 * pl.at;
       if (elect_one()) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
-          mma_f16_ts(tmem + kColS + 64 * pl, tmem + kColQ + kk * 8, dk + ((kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2), idesc, kk > 0);
-        mma_commit(&ctl->s_full[pl]);
-        mma_commit(&ctl->k_empty[stage]);
+          mma_f16_ts(s, tmem + kColQ + kk * 8, dk + ((kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2), idesc, kk > 0);
+        mma_commit(&ctl->s_full[pl.at]);
+        mma_commit(&ctl->k_empty[st.at]);
       }
       __syncwarp();
+      st.next();
+      pl.next();
     }
   }
   if (!ok) fail(ctl, p.err);
@@ -369,33 +472,35 @@ __device__ void mma_s_loop(const PagedAttnParams& p, Ctl* ctl, const uint8_t* sK
   __syncwarp();
 }
 
-__device__ void mma_pv_loop(const PagedAttnParams& p, Ctl* ctl, const uint8_t* sV, uint32_t tmem, int64_t fb, int64_t fe) {
+__device__ void mma_pv_loop(const PagedAttnParams& p, Ctl* ctl, const uint8_t* sV, uint32_t tmem, const Share& sh) {
   const uint32_t idesc = idesc_bf16_bmn(kPagedRows, kHeadDim);
   const uint64_t dv0 = sdesc_mn_sw128(smem_u32(sV), kHalfBytes, 1024);
+  Ring<kStages> st;
+  Ring<kPlaces> pl;
   int pc = 0;
-  uint32_t ui = 0;
   bool ok = true;
-  for (PieceIter c(p, ctl, fb, fe); ok && c.valid(); c.next(p, ctl)) {
-    ok = warp_wait(ctl, &ctl->o_empty, (pc & 1) ^ 1, p.wait_ns);   // both O of the previous piece have been read
+  for (PieceIter c(p, ctl, sh.member, sh.fb, sh.fe); ok && c.valid(); c.next(p, ctl)) {
+    ok = warp_wait(ctl, &ctl->o_empty, (pc & 1) ^ 1, p.wait_ns);   // O of the previous piece has been read
     ++pc;
-    for (int i = 0; ok && i < c.n; ++i, ++ui) {
-      const int stage = ui % kStages, pl = place_of(ui);
-      ok = warp_wait(ctl, &ctl->v_full[stage], ui / kStages & 1, p.wait_ns) &&
-           warp_wait(ctl, &ctl->p_full[pl], place_par(ui), p.wait_ns);
+    for (int i = 0; ok && i < c.n; ++i) {
+      ok = warp_wait2(ctl, &ctl->v_full[st.at], st.par, &ctl->p_full[pl.at], pl.par, p.wait_ns);
       if (!ok) break;
       tc_fence_after();
-      const uint64_t dv = dv0 + static_cast<uint64_t>(stage * (kUnitBytes >> 4));
+      const uint64_t dv = dv0 + static_cast<uint64_t>(st.at * (kUnitBytes >> 4));
+      const uint32_t s = tmem + kColS + 64 * pl.at;
       if (elect_one()) {
 #pragma unroll
         for (int part = 0; part < 2; ++part)
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk)   // 16 keys per step: 8 columns of P, 16 rows of V; a line's first product of a piece overwrites O
-            mma_f16_ts(tmem + kColO + kHeadDim * (ui & 1), tmem + kColS + 64 * pl + 32 * part + kk * 8,
-                       dv + static_cast<uint64_t>(kk * 128), idesc, (i > 1 || part > 0 || kk > 0) ? 1u : 0u);
-        mma_commit(&ctl->p_empty[pl]);
-        mma_commit(&ctl->v_empty[stage]);
+          for (int kk = 0; kk < 4; ++kk)   // 16 keys per step: 8 columns of P, 16 rows of V; the piece's first product overwrites O
+            mma_f16_ts(tmem + kColO, s + 32 * part + kk * 8, dv + static_cast<uint64_t>(kk * 128), idesc,
+                       (i > 0 || part > 0 || kk > 0) ? 1u : 0u);
+        mma_commit(&ctl->p_empty[pl.at]);
+        mma_commit(&ctl->v_empty[st.at]);
       }
       __syncwarp();
+      st.next();
+      pl.next();
     }
   }
   if (!ok) fail(ctl, p.err);
@@ -407,16 +512,13 @@ __device__ void mma_pv_loop(const PagedAttnParams& p, Ctl* ctl, const uint8_t* s
 // ---------------------------------------------------------------- softmax
 
 // 32 keys of a unit, exp2 arguments and sums as packed pairs; p = hi + lo, hi the
-// upper 16 bits of p.  Masked keys (bits of `vis` clear) have p = 0.
-template <bool FULL>
-__device__ __forceinline__ void exp_split(const uint32_t (&z0)[16], const uint32_t (&z1)[16], uint32_t vis, float2 sc2, float2 nm2,
-                                          float2 (&acc)[4], uint32_t (&hi)[16], uint32_t (&lo)[16]) {
+// upper 16 bits of p.
+__device__ __forceinline__ void exp_split(const uint32_t (&z)[32], float2 sc2, float2 nm2, float2 (&acc)[4], uint32_t (&hi)[16],
+                                          uint32_t (&lo)[16]) {
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    const uint32_t a = i < 16 ? z0[i & 15] : z1[i & 15], b = i < 16 ? z0[(i + 1) & 15] : z1[(i + 1) & 15];
-    const float2 e = ffma2(make_float2(__uint_as_float(a), __uint_as_float(b)), sc2, nm2);
-    const float p0 = FULL || (vis >> i & 1) ? ex2_approx(e.x) : 0.f;
-    const float p1 = FULL || (vis >> (i + 1) & 1) ? ex2_approx(e.y) : 0.f;
+    const float2 e = ffma2(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), sc2, nm2);
+    const float p0 = ex2_approx(e.x), p1 = ex2_approx(e.y);
     acc[(i >> 1) & 3] = fadd2(acc[(i >> 1) & 3], make_float2(p0, p1));
     const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
     hi[i >> 1] = __byte_perm(u0, u1, 0x7632);
@@ -426,19 +528,37 @@ __device__ __forceinline__ void exp_split(const uint32_t (&z0)[16], const uint32
   }
 }
 
-template <bool FULL>
-__device__ __forceinline__ float unit_max(const uint32_t (&z)[4][16], uint64_t vis) {
-  float pm[8];   // independent partial maxima
+// What runs once or twice a piece is kept in short loops over 16 columns: code that is
+// not in the instruction cache costs about ten cycles an instruction, and unrolled over a
+// unit a masked softmax took 2,600 and a second pass 5,300 cycles.
+
+// Largest raw logit of a unit.
+__device__ __forceinline__ float unit_max(uint32_t s_addr) {
+  float mx = -INFINITY;
+#pragma unroll 1
+  for (int c = 0; c < kPagedUnitKeys; c += 16) {
+    uint32_t z[16];
+    tmem_ld16_async(s_addr + c, z);
+    tmem_wait16(z);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) pm[k] = -INFINITY;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const uint32_t bits = static_cast<uint32_t>(vis >> (16 * q));
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (FULL || (bits >> i & 1)) pm[i & 7] = fmaxf(pm[i & 7], __uint_as_float(z[q][i]));
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, __uint_as_float(z[i]));
   }
-  return fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), fmaxf(fmaxf(pm[4], pm[5]), fmaxf(pm[6], pm[7])));
+  return mx;
+}
+
+// S = -inf at the keys that this thread's row does not see (bits of `vis` clear).
+__device__ __forceinline__ void mask_s(uint32_t s_addr, uint64_t vis) {
+#pragma unroll 1
+  for (int c = 0; c < kPagedUnitKeys; c += 16) {
+    uint32_t z[16];
+    tmem_ld16_async(s_addr + c, z);
+    tmem_wait16(z);
+    const uint32_t bits = static_cast<uint32_t>(vis >> c);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = bits >> i & 1 ? z[i] : 0xFF800000u;
+    tmem_st16(s_addr + c, z);
+  }
+  tmem_wait_st();
 }
 
 // Rescales this warp's O rows by alpha (1 in lanes whose reference stays).
@@ -454,68 +574,128 @@ __device__ __forceinline__ void rescale_o(uint32_t o_addr, float alpha) {
   }
 }
 
-// One unit of a softmax warp with rows: S into registers, P in its place.  A row's
-// reference m starts at its first maximum (its O is 0 until then) and moves only when a
-// later maximum lies more than 15 above it; the move rescales its O row once the product
-// of the line's previous unit is done.  Returns false when a wait ran out.
-template <bool FULL>
-__device__ __forceinline__ bool softmax_unit(const PagedAttnParams& p, Ctl* ctl, uint64_t vis, uint32_t s_addr, uint32_t o_addr,
-                                             uint32_t ui, float& m, float& l) {
-  const float c2 = p.scale2;
-  uint32_t z[4][16];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) tmem_ld16_async(s_addr + q * 16, z[q]);
-#pragma unroll
-  for (int q = 0; q < 4; ++q) tmem_wait16(z[q]);
-  const float mx = unit_max<FULL>(z, vis) * c2;
-  const bool first = m == -INFINITY;
-  const bool move = !first && mx > m + kMoveThreshold;
-  if (__any_sync(kFull, move)) {   // rare
-    const float alpha = move ? ex2_approx(m - mx) : 1.f;
-    const uint32_t up = ui - 2;
-    if (!warp_wait(ctl, &ctl->p_empty[place_of(up)], place_par(up), p.wait_ns)) return false;
-    tc_fence_after();
-    rescale_o(o_addr, alpha);
-    l *= alpha;
-  }
-  if (first || move) m = mx;
-  const float ref = m == -INFINITY ? 0.f : m;
+// P of a unit against `ref`; returns the sum.
+__device__ __forceinline__ float weights(const uint32_t (&z)[2][32], float c2, float ref, uint32_t (&hi)[2][16], uint32_t (&lo)[2][16]) {
   const float2 sc2 = make_float2(c2, c2), nm2 = make_float2(-ref, -ref);
   float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    uint32_t hi[16], lo[16];
-    exp_split<FULL>(z[2 * k], z[2 * k + 1], static_cast<uint32_t>(vis >> (32 * k)), sc2, nm2, acc, hi, lo);
-    tmem_st16(s_addr + 16 * k, hi);
-    tmem_st16(s_addr + 32 + 16 * k, lo);
-  }
+  for (int k = 0; k < 2; ++k) exp_split(z[k], sc2, nm2, acc, hi[k], lo[k]);
   const float2 a = fadd2(fadd2(acc[0], acc[1]), fadd2(acc[2], acc[3]));
-  l += a.x + a.y;
+  return a.x + a.y;
+}
+
+__device__ __forceinline__ void load_s(uint32_t s_addr, uint32_t (&z)[2][32]) {
+  tmem_ld32_async(s_addr, z[0]);
+  tmem_ld32_async(s_addr + 32, z[1]);
+  tmem_wait32(z[0]);
+  tmem_wait32(z[1]);
+}
+
+// One unit of a softmax warp with rows: S into registers, P in its place.
+//
+// The weights are taken against the reference m that the line knows, without looking for
+// the unit's maximum.  Before they are used, the reference that holds after the unit
+// before (the other line's warp of these rows passes it on) has to be that one, and no
+// row's sum may be large: otherwise (the piece's first unit, a rising maximum) they are
+// taken again, against a reference that the unit's maximum moves where it lies more
+// than 8 above it; the row of O is rescaled once the previous unit's product is done.  (A
+// reference far above a unit's logits does no harm: the weights keep their relative
+// precision, and those below 2^-126 of the largest seen so far are nothing.)  l counts
+// against m.  `unit`: its number in the piece.  Returns false when a wait ran out.
+__device__ __forceinline__ bool softmax_unit(const PagedAttnParams& p, Ctl* ctl, uint64_t* ref_in, uint32_t ref_par, uint64_t* ref_out,
+                                             uint64_t* prev_empty, uint32_t prev_par, volatile float* slot, int lane, bool live, int unit,
+                                             bool masked, uint64_t vis, uint32_t s_addr, uint32_t o_addr, float& m, float& l) {
+  const float c2 = p.scale2;
+  if (masked) mask_s(s_addr, vis);
+  uint32_t hi[2][16], lo[2][16];
+  float sum, was = live ? -INFINITY : 0.f;   // (rows that are none weigh against 0 and never ask for more)
+  bool again = unit == 0;                    // (nothing to weigh against)
+  if (unit == 1) {                           // the line's first: nothing known yet
+    if (!warp_wait(ctl, ref_in, ref_par, p.wait_ns)) return false;
+    m = *slot;
+  }
+#pragma unroll 1
+  while (true) {
+    if (again) {
+      const float mx = unit_max(s_addr) * c2;
+      const bool first = was == -INFINITY, move = live && !first && mx > was + kMoveThreshold;
+      if (__any_sync(kFull, move)) {
+        if (!warp_wait(ctl, prev_empty, prev_par, p.wait_ns)) return false;
+        tc_fence_after();
+        rescale_o(o_addr, move ? ex2_approx(was - mx) : 1.f);
+        tmem_wait_st();
+      }
+      const float now = first || move ? mx : was;
+      l = now == m || m == -INFINITY ? l : l * ex2_approx(m - now);   // (l is 0 while m is -inf)
+      m = now;
+      *slot = now;
+      __syncwarp();
+    }
+    uint32_t z[2][32];
+    load_s(s_addr, z);
+    sum = weights(z, c2, m == -INFINITY ? 0.f : m, hi, lo);
+    if (again) break;
+    // The slot is read only once the barrier has been seen complete: its address depends
+    // on the answer (in front of row 0 lies a slot that is nobody's), since a load that
+    // merely stands behind the question may be served before it.
+    const bool in = mbar_try_wait(ref_in, ref_par);
+    was = slot[static_cast<int>(in) - 1];
+    if (!__any_sync(kFull, !in || was != m || was == -INFINITY || !(sum <= kSumLimit))) break;
+    if (!warp_wait(ctl, ref_in, ref_par, p.wait_ns)) return false;
+    was = *slot;
+    if (!__any_sync(kFull, was != m || was == -INFINITY || !(sum <= kSumLimit))) break;
+    again = true;
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    tmem_st16(s_addr + 16 * k, hi[k]);
+    tmem_st16(s_addr + 32 + 16 * k, lo[k]);
+  }
+  if (lane == 0) mbar_arrive(ref_out);
+  l += sum;
   return true;
 }
 
 __device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7F80u) == 0x7F80u; }
 
-// Adds to 16 columns of a row's O what its product left out: the elements of V that
-// are not finite, at the keys it sees in the piece's masked units.  (Their weight is
-// taken as positive: one that has underflowed to 0 gives the infinity and not a NaN.)
+// Bits 15 and 31: the lower and the upper bf16 of a word is not finite (an exponent of
+// ones carries into the sign's place).
+__device__ __forceinline__ uint32_t not_finite2(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+
+// A word with the halves that are not finite zeroed.
+__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
+  const uint32_t bad = not_finite2(w);
+  return w & ~((bad >> 15 & 1) * 0xFFFFu | (bad >> 31) * 0xFFFF0000u);
+}
+
+// 16-byte chunk c (of 16) of row i of a warp's staged half of O: rows of 64 floats, the
+// chunks in an order that depends on the row, so that neither lanes on rows nor lanes on
+// columns meet in a bank.
+__device__ __forceinline__ float4* staged(float* stage, int i, int c) {
+  return reinterpret_cast<float4*>(stage) + i * 16 + (c ^ (i & 15));
+}
+
+// Adds to a staged row of O, columns col .. col + 63, what its product left out: the
+// elements of V that are not finite, at the keys it sees in the piece's masked units.  (Their
+// weight is taken as positive: one that has underflowed to 0 gives the infinity and not a
+// NaN.)
 __device__ __noinline__ void patch_poison(const PagedAttnParams& p, const Block& blk, const Seen& see, int g, int j0, int n, int col,
-                                          float (&o)[16]) {
+                                          float* stage, int i) {
   const Seen all = blk.all(p);
   const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
   const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
   for (int j = j0; j < j0 + n; ++j) {
     const int k0 = blk.key(j);
-    if (all(k0) == kAll) continue;
+    if (all.whole(k0)) continue;
     for (uint64_t bits = see(k0); bits; bits &= bits - 1) {
       const int key = k0 + __ffsll(static_cast<long long>(bits)) - 1;
       const int page = entries[key >> p.shift];
       if (page < 0 || page >= p.n_pages) continue;
       const __nv_bfloat16* v = p.v + page * p.page_stride +
                                ((static_cast<int64_t>(g) << p.shift) + (key & ((1 << p.shift) - 1))) * kHeadDim + col;
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t b = *reinterpret_cast<const uint16_t*>(v + i);
-        if (not_finite(b)) o[i] += __uint_as_float(b << 16);
+      for (int x = 0; x < 64; ++x) {
+        const uint32_t b = *reinterpret_cast<const uint16_t*>(v + x);
+        if (not_finite(b)) reinterpret_cast<float*>(staged(stage, i, x >> 2))[x & 3] += __uint_as_float(b << 16);
       }
     }
   }
@@ -527,22 +707,19 @@ __device__ __noinline__ void patch_poison(const PagedAttnParams& p, const Block&
 __device__ __forceinline__ bool clean_v(uint4* v4, uint64_t seen, int thread) {
   bool met = false;
 #pragma unroll 1
-  for (int x = thread; x < kUnitBytes / 16; x += 128) {
-    if (!(seen >> (x >> 3 & 63) & 1)) {   // 8 chunks of 16 bytes a key and half
-      v4[x] = make_uint4(0u, 0u, 0u, 0u);
-      continue;
-    }
-    const uint4 w = v4[x];
-    uint32_t e[4] = {w.x, w.y, w.z, w.w};
-    bool bad = false;
+  for (int x0 = thread; x0 < kUnitBytes / 16; x0 += 4 * 128) {
+    uint4 w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = v4[x0 + 128 * k];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (not_finite(e[k])) e[k] &= 0xFFFF0000u, bad = true;
-      if (not_finite(e[k] >> 16)) e[k] &= 0xFFFFu, bad = true;
-    }
-    if (bad) {
-      v4[x] = make_uint4(e[0], e[1], e[2], e[3]);
-      met = true;
+      const int x = x0 + 128 * k;
+      if (!(seen >> (x >> 3 & 63) & 1)) {   // 8 chunks of 16 bytes a key and half
+        v4[x] = make_uint4(0u, 0u, 0u, 0u);
+      } else if (not_finite2(w[k].x) | not_finite2(w[k].y) | not_finite2(w[k].z) | not_finite2(w[k].w)) {
+        v4[x] = make_uint4(finite_part(w[k].x), finite_part(w[k].y), finite_part(w[k].z), finite_part(w[k].w));
+        met = true;
+      }
     }
   }
   fence_proxy_async_smem();
@@ -551,29 +728,29 @@ __device__ __forceinline__ bool clean_v(uint4* v4, uint64_t seen, int thread) {
 
 // Softmax warps of a line (0: even units, 1: odd): one thread per query row (TMEM lane
 // quad * 32 + lane).
-__device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, uint32_t tmem, uint32_t line, int quad, int lane,
-                             int64_t fb, int64_t fe) {
+__device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, float* stage_o, uint32_t tmem, int line, int quad, int lane,
+                             const Share& sh) {
   const int r = quad * 32 + lane;
   const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
-  const uint32_t o_addr = lane_base + kColO + kHeadDim * line;
+  const uint32_t o_addr = lane_base + kColO;
   uint32_t u0 = 0;   // number of the piece's first unit
   // line 0: the queries of a piece (no product reads the previous piece's any more)
   auto take_queries = [&](const PieceIter& c) {
-    const Block blk(p, ctl->item[c.item], c.item);
+    const Block blk = c.block(p, ctl);
     if (quad * 32 < blk.nrows) {
       const bool live = r < blk.nrows;
-      const int t = (blk.row0 + r) / p.hg, h = c.g * p.hg + (blk.row0 + r) % p.hg;
+      const int t = quotient(blk.row0 + r, p.inv_hg), h = c.g * p.hg + blk.row0 + r - t * p.hg;
       const uint4* src = reinterpret_cast<const uint4*>(p.q + blk.seq * p.q_seq + t * p.q_token + h * p.q_head);
+      uint4 w[16];   // every load before the first use
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = live ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+      __syncwarp();   // (`live` differs between lanes)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        uint32_t w[16];
+        uint32_t x[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 x = live ? src[4 * k + i] : make_uint4(0u, 0u, 0u, 0u);
-          w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
-        }
-        __syncwarp();   // (`live` differs between lanes)
-        tmem_st16(lane_base + kColQ + 16 * k, w);
+        for (int i = 0; i < 4; ++i) x[4 * i] = w[4 * k + i].x, x[4 * i + 1] = w[4 * k + i].y, x[4 * i + 2] = w[4 * k + i].z, x[4 * i + 3] = w[4 * k + i].w;
+        tmem_st16(lane_base + kColQ + 16 * k, x);
       }
       tmem_wait_st();
     }
@@ -583,29 +760,33 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, ui
   };
   bool ok = true;
   int pc = 0;
-  PieceIter c(p, ctl, fb, fe);
+  PieceIter c(p, ctl, sh.member, sh.fb, sh.fe);
   if (line == 0 && c.valid()) take_queries(c);
   for (; ok && c.valid(); ++pc) {
-    const Block blk(p, ctl->item[c.item], c.item);
+    const Block blk = c.block(p, ctl);
     const bool wactive = quad * 32 < blk.nrows;
     const bool live = r < blk.nrows;
-    const int t = (blk.row0 + r) / p.hg, h = c.g * p.hg + (blk.row0 + r) % p.hg;
+    const int t = quotient(blk.row0 + r, p.inv_hg), h = c.g * p.hg + blk.row0 + r - t * p.hg;
     const Seen all = blk.all(p);
     const uint64_t* masks = p.mask + static_cast<int64_t>(blk.seq) * p.T;
     Seen see = blk.row(p, blk.L - blk.n + t, p.tree && live ? masks[t] : 0);
     if (!live) see = Seen{0, 0, 0, 0, 0};
     float m = -INFINITY, l = 0.f;
-    for (uint32_t ui = u0 + ((u0 ^ line) & 1); ui < u0 + c.n; ui += 2) {
-      const int pl = place_of(ui);
+    for (int i = (u0 ^ static_cast<uint32_t>(line)) & 1; i < c.n; i += 2) {
+      const uint32_t ui = u0 + i, pl = ui % kPlaces, up = ui - 1;
       const uint32_t s_addr = lane_base + kColS + 64 * pl;
-      ok = warp_wait(ctl, &ctl->s_full[pl], place_par(ui), p.wait_ns);
+      ok = warp_wait(ctl, &ctl->s_full[pl], ui / kPlaces & 1, p.wait_ns);
       if (!ok) break;
       tc_fence_after();
-      const int k0 = blk.key(c.j0 + static_cast<int>(ui - u0));
-      if (all(k0) == kAll) {
-        if (wactive) ok = softmax_unit<true>(p, ctl, kAll, s_addr, o_addr, ui, m, l);
-      } else {
-        if (wactive) ok = softmax_unit<false>(p, ctl, see(k0), s_addr, o_addr, ui, m, l);
+      const int k0 = blk.key(c.j0 + i);
+      const bool masked = !all.whole(k0);
+      if (wactive) {
+        ok = softmax_unit(p, ctl, &ctl->ref[line ^ 1][quad], up >> 1 & 1, &ctl->ref[line][quad], &ctl->p_empty[up % kPlaces],
+                          up / kPlaces & 1, &ctl->m[1 + r], lane, live, i, masked, masked ? see(k0) : kAll, s_addr, o_addr, m, l);
+      } else if (lane == 0) {   // a warp without rows only keeps the counts
+        mbar_arrive(&ctl->ref[line][quad]);
+      }
+      if (masked) {
         if (!ok) break;
         uint64_t bits = 0;
         if (p.tree) {   // the union of the block's masks (at most 64 tokens)
@@ -625,77 +806,56 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, ui
       if (lane == 0) mbar_arrive(&ctl->p_full[pl]);
     }
     if (!ok) break;
-    const uint32_t lu = u0 + c.n - 1;
+    const uint32_t lu = u0 + c.n - 1, lpl = lu % kPlaces, lpar = lu / kPlaces & 1;
+    // both lines' references and sums, and O
+    ctl->ml[pc & 1][line][r] = make_float2(m, l);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&ctl->ml_full);
     PieceIter nx = c;
     nx.next(p, ctl);
     if (line == 0 && nx.valid()) {   // S of the next piece runs under this piece's end
-      ok = warp_wait(ctl, &ctl->s_full[place_of(lu)], place_par(lu), p.wait_ns);
+      ok = warp_wait(ctl, &ctl->s_full[lpl], lpar, p.wait_ns);
       if (!ok) break;
       tc_fence_after();
       take_queries(nx);
     }
-    // both lines' references and sums, and both O
-    ctl->ml[pc & 1][line][r] = make_float2(m, l);
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&ctl->ml_full);
-    ok = warp_wait(ctl, &ctl->ml_full, pc & 1, p.wait_ns) && warp_wait(ctl, &ctl->p_empty[place_of(lu)], place_par(lu), p.wait_ns);
+    ok = warp_wait2(ctl, &ctl->ml_full, pc & 1, &ctl->p_empty[lpl], lpar, p.wait_ns);
     if (!ok) break;
     tc_fence_after();
     if (wactive) {
       const bool whole = c.whole();
-      const bool two = c.n > 1;   // (a line without units has no O)
       const float2 other = ctl->ml[pc & 1][line ^ 1][r];
-      const float M = fmaxf(m, other.x), ref = M == -INFINITY ? 0.f : M;
-      const float w_own = exp2f(m - ref), w_other = exp2f(other.x - ref);
-      const float L = w_own * l + w_other * other.y;
+      const float M = fmaxf(m, other.x), ref = M == -INFINITY ? 0.f : M;   // (the last reference is the largest)
+      const float L = exp2f(m - ref) * l + exp2f(other.x - ref) * other.y;
       const float norm = !whole ? 1.f : L == 0.f ? 0.f : 1.f / L;
-      const float w0 = (line ? w_other : w_own) * norm, w1 = (line ? w_own : w_other) * norm;
-      const uint32_t first = lane_base + kColO + kHeadDim * (two ? 0 : u0 & 1);
-      const float wf = two || !(u0 & 1) ? w0 : w1;
-      const bool poison = ctl->poison[pc & 7] == pc + 1;
       const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (c.j0 == 0);
-      __nv_bfloat16* out = p.o + blk.seq * p.o_seq + t * p.o_token + h * p.o_head;
-      float* part = p.part_o + (slot * kPagedRows + r) * kHeadDim;
-#pragma unroll 1
-      for (int ch = 4 * line; ch < 4 * static_cast<int>(line) + 4; ++ch) {
-        uint32_t a[16], b[16];
-        tmem_ld16_async(first + ch * 16, a);
-        if (two) tmem_ld16_async(lane_base + kColO + kHeadDim + ch * 16, b);
-        tmem_wait16(a);
-        float o[16];
-        if (two) {
-          tmem_wait16(b);
+      // this line's half of the columns by way of shared memory, for rows that are written whole
+      uint32_t a[2][32];
+      load_s(o_addr + 64 * line, a);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = __uint_as_float(a[i]) * wf + __uint_as_float(b[i]) * w1;
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = __uint_as_float(a[i]) * wf;
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t* x = &a[i >> 3][4 * (i & 7)];
+        *staged(stage_o, lane, i) = make_float4(__uint_as_float(x[0]) * norm, __uint_as_float(x[1]) * norm, __uint_as_float(x[2]) * norm,
+                                                __uint_as_float(x[3]) * norm);
+      }
+      if (ctl->poison[pc & 7] == pc + 1 && live) patch_poison(p, blk, see, c.g, c.j0, c.n, 64 * line, stage_o, lane);
+      __syncwarp();
+      const int rows = min(32, blk.nrows - quad * 32);
+      if (whole) {
+        const int64_t at = blk.seq * p.o_seq + t * p.o_token + h * p.o_head + 64 * line;   // this lane's row
+#pragma unroll 4
+        for (int i = lane >> 3; i < 32; i += 4) {   // eight lanes a row, eight columns each
+          const int64_t to = __shfl_sync(kFull, at, i);
+          if (i >= rows) continue;
+          const float4 a = *staged(stage_o, i, 2 * (lane & 7)), b = *staged(stage_o, i, 2 * (lane & 7) + 1);
+          const __nv_bfloat162 x[4] = {__floats2bfloat162_rn(a.x, a.y), __floats2bfloat162_rn(a.z, a.w), __floats2bfloat162_rn(b.x, b.y),
+                                       __floats2bfloat162_rn(b.z, b.w)};
+          *reinterpret_cast<uint4*>(p.o + to + 8 * (lane & 7)) = *reinterpret_cast<const uint4*>(x);
         }
-        if (live) {
-          if (poison) {
-            float x[16];   // (a copy: the address of o would keep it out of registers)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = o[i];
-            patch_poison(p, blk, see, c.g, c.j0, c.n, ch * 16, x);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = x[i];
-          }
-          if (whole) {
-            uint32_t w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const __nv_bfloat162 x = __floats2bfloat162_rn(o[2 * i], o[2 * i + 1]);
-              w[i] = *reinterpret_cast<const uint32_t*>(&x);
-            }
-            reinterpret_cast<uint4*>(out + ch * 16)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            reinterpret_cast<uint4*>(out + ch * 16)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              reinterpret_cast<float4*>(part + ch * 16)[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-          }
-        }
-        __syncwarp();
+      } else {
+        float* part = p.part_o + (slot * kPagedRows + quad * 32) * kHeadDim + 64 * line + 4 * (lane & 15);
+#pragma unroll 4
+        for (int i = lane >> 4; i < rows; i += 2) *reinterpret_cast<float4*>(part + i * kHeadDim) = *staged(stage_o, i, lane & 15);
       }
       if (live && line == 0) {
         if (!whole) p.part_ml[slot * kPagedRows + r] = make_float2(M, L);
@@ -704,7 +864,7 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, ui
       }
     }
     tc_fence_before();
-    __syncwarp();
+    __syncwarp();   // (also: the staged rows have been read)
     if (lane == 0) mbar_arrive(&ctl->o_empty);
     u0 += c.n;
     c = nx;
@@ -719,7 +879,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sK = smem;                           // [kStages][2 halves][64 keys][128 B]
   uint8_t* sV = sK + kStages * kUnitBytes;      // the same
-  Ctl* ctl = reinterpret_cast<Ctl*>(sV + kStages * kUnitBytes);
+  float* sO = reinterpret_cast<float*>(sV + kStages * kUnitBytes);   // [8 softmax warps][32 rows][64 columns]
+  Ctl* ctl = reinterpret_cast<Ctl*>(reinterpret_cast<uint8_t*>(sO) + kStageO * kSoftWarps);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
@@ -734,12 +895,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
       mbar_init(&ctl->p_full[i], kSoftWarps / 2);
       mbar_init(&ctl->p_empty[i], 1);
     }
+    for (int i = 0; i < 8; ++i) mbar_init(&ctl->ref[i >> 2][i & 3], 1);
     mbar_init(&ctl->qt_full, kSoftWarps / 2);
     mbar_init(&ctl->ml_full, kSoftWarps);
     mbar_init(&ctl->o_empty, kSoftWarps);
     mbar_init(&ctl->drain, 2);   // one commit per MMA issuer
     ctl->abort = 0;
     for (int i = 0; i < 8; ++i) ctl->poison[i] = 0;
+    ctl->gang = 1;
+    ctl->sum[0] = ctl->sum[1] = 0;
     fence_mbar_init();
   }
   if (warp == 1) {
@@ -753,33 +917,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
   griddep_wait();
   const uint32_t tmem = ctl->tmem_base;
   count_units(p, ctl);
-  const int64_t T = static_cast<int64_t>(ctl->before[p.items]) * p.G;
-  const int64_t fb = range_begin(T, blockIdx.x, gridDim.x);
-  const int64_t fe = range_begin(T, blockIdx.x + 1, gridDim.x);
+  const Share sh(p, ctl);
 
   if (warp == 0) {
-    load_loop(p, ctl, &p.tmk, sK, ctl->k_full, ctl->k_empty, lane, fb, fe);
+    load_loop(p, ctl, &p.tmk, sK, ctl->k_full, ctl->k_empty, lane, sh);
   } else if (warp == 3) {
-    load_loop(p, ctl, &p.tmv, sV, ctl->v_full, ctl->v_empty, lane, fb, fe);
+    load_loop(p, ctl, &p.tmv, sV, ctl->v_full, ctl->v_empty, lane, sh);
   } else if (warp == 1) {
-    mma_s_loop(p, ctl, sK, tmem, fb, fe);
+    mma_s_loop(p, ctl, sK, tmem, sh);
   } else if (warp == 2) {
-    mma_pv_loop(p, ctl, sV, tmem, fb, fe);
+    mma_pv_loop(p, ctl, sV, tmem, sh);
   } else {
-    softmax_loop(p, ctl, sV, tmem, (warp - 4) >> 2, warp & 3, lane, fb, fe);
+    softmax_loop(p, ctl, sV, sO + (warp - 4) * (kStageO / 4), tmem, (warp - 4) >> 2, warp & 3, lane, sh);
   }
   if (threadIdx.x == 0) {   // what the merge has to know of this range's end
     PagedSplit s;
-    s.total = T;
+    s.total = sh.total;
     s.valid = 0;
-    if (fe > fb) {   // the piece that the range's last unit is in, if it begins here and goes on
-      const PieceIter e(p, ctl, fe - 1, fe);
-      const int64_t f0 = static_cast<int64_t>(ctl->before[e.item]) * p.G + static_cast<int64_t>(e.g) * e.nu;
-      if (f0 >= fb && f0 + e.nu > fe) {
-        s.valid = 1;
-        s.item = e.item;
-        s.g = e.g;
-        s.c1 = cta_of(f0 + e.nu - 1, T, gridDim.x);
+    s.gang = ctl->gang;
+    if (sh.fe > sh.fb) {   // the piece that the range's last unit is in, if it begins here and goes on
+      const PieceIter e(p, ctl, sh.member, sh.fe - 1, sh.fe);
+      if (e.valid()) {
+        const int64_t f0 = static_cast<int64_t>(ctl->before[e.item]) * p.G + static_cast<int64_t>(e.g) * e.nu;
+        if (f0 >= sh.fb && f0 + e.nu > sh.fe) {
+          const Block blk = e.block(p, ctl);
+          s.valid = 1;
+          s.seq = blk.seq;
+          s.row0 = blk.row0;
+          s.nrows = blk.nrows;
+          s.g = e.g;
+          s.last = range_of(f0 + e.nu - 1, sh.total, sh.ranges);
+        }
       }
     }
     p.split[blockIdx.x] = s;
@@ -793,24 +961,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
 
 // Merges the parts of the (item, group)s that ranges cut: M = max m, L = sum 2^(m - M)
 // l, O = sum 2^(m - M) O_part / L, lse = (M + log2 L) ln 2.  Block (c, y): the one that
-// CTA c began, query rows 8 y and on, a warp per row; the loads of eight parts are in
+// CTA c began, query rows 8 y and on, a warp per row; the loads of four parts are in
 // flight before the first is used (one after the other, 40 parts took 75 us).
-constexpr int kBatch = 8;
+constexpr int kBatch = 4;
 
 __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ PagedAttnParams p) {
   griddep_launch_dependents();
   griddep_wait();
-  const int c0 = blockIdx.x;
-  const PagedSplit s = p.split[c0];
+  const PagedSplit s = p.split[blockIdx.x];
   if (!s.valid) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int seq = s.item / p.nblk, row0 = (s.item - seq * p.nblk) * kPagedRows;
-  const int n = p.n_tokens ? p.n_tokens[seq] : p.T;
+  const int first = blockIdx.x / s.gang, member = blockIdx.x % s.gang, ranges = gridDim.x / s.gang;
   const int r = blockIdx.y * 8 + warp;
-  if (r >= min(kPagedRows, n * p.hg - row0)) return;
+  if (r >= s.nrows) return;
   float M = -INFINITY, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int cb = c0; cb <= s.c1; cb += kBatch) {
+  for (int cb = first; cb <= s.last; cb += kBatch) {
     float2 ml[kBatch];
     float4 o[kBatch];
 #pragma unroll
@@ -818,8 +984,8 @@ __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ P
       const int c = cb + k;
       ml[k] = make_float2(-INFINITY, 0.f);
       o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (c > s.c1 || range_begin(s.total, c, p.grid) == range_begin(s.total, c + 1, p.grid)) continue;   // (a CTA without units)
-      const int64_t at = (2 * static_cast<int64_t>(c) + (c == c0)) * kPagedRows + r;
+      if (c > s.last || range_begin(s.total, c, ranges) == range_begin(s.total, c + 1, ranges)) continue;   // (an empty range)
+      const int64_t at = (2 * (static_cast<int64_t>(c) * s.gang + member) + (c == first)) * kPagedRows + r;
       ml[k] = p.part_ml[at];
       o[k] = reinterpret_cast<const float4*>(p.part_o + at * kHeadDim)[lane];
     }
@@ -838,16 +1004,16 @@ __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ P
     }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  const int t = (row0 + r) / p.hg, h = s.g * p.hg + (row0 + r) % p.hg;
+  const int t = (s.row0 + r) / p.hg, h = s.g * p.hg + (s.row0 + r) % p.hg;
   const __nv_bfloat162 x[2] = {__floats2bfloat162_rn(acc.x * inv, acc.y * inv), __floats2bfloat162_rn(acc.z * inv, acc.w * inv)};
-  *reinterpret_cast<uint2*>(p.o + seq * p.o_seq + t * p.o_token + h * p.o_head + lane * 4) = *reinterpret_cast<const uint2*>(x);
+  *reinterpret_cast<uint2*>(p.o + s.seq * p.o_seq + t * p.o_token + h * p.o_head + lane * 4) = *reinterpret_cast<const uint2*>(x);
   if (p.lse && lane == 0)
-    p.lse[(static_cast<int64_t>(seq) * p.T + t) * p.H + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    p.lse[(static_cast<int64_t>(s.seq) * p.T + t) * p.H + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
 namespace {
 
-constexpr size_t kSmemBytes = 1024 + 2 * static_cast<size_t>(kStages) * kUnitBytes + sizeof(Ctl);
+constexpr size_t kSmemBytes = 1024 + 2 * static_cast<size_t>(kStages) * kUnitBytes + kStageO * kSoftWarps + sizeof(Ctl);
 static_assert(kSmemBytes <= 227 * 1024, "the rings and the control block fit an SM");
 
 cudaLaunchConfig_t config(cudaLaunchAttribute* attr, dim3 grid, int threads, size_t smem, cudaStream_t stream) {

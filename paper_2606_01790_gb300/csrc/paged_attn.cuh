@@ -8,12 +8,14 @@ namespace starkv {
 constexpr int kMaxDraft = 64;        // drafted tokens of a tree (bits of a mask word)
 constexpr int kPagedRows = 128;      // query rows of a block: (token, head of the group) pairs
 constexpr int kPagedUnitKeys = 64;   // keys per pipeline unit
-constexpr int kPagedItems = 1024;    // query blocks of a launch
+constexpr int kPagedItems = 1024;    // query blocks of a launch, at most
 
-// The piece that a CTA leaves unfinished: blocks c0 .. c1 hold parts of it.
+// The (query block, group) that a CTA's range begins and does not finish: the ranges up to
+// `last` hold the rest of it.
 struct PagedSplit {
   int64_t total;   // units of the launch
-  int valid, item, g, c1;
+  int valid, gang; // CTAs of a gang (1: none): range c is that of CTAs c * gang ..
+  int seq, row0, nrows, g, last, pad_;
 };
 
 struct PagedAttnParams {
@@ -33,7 +35,8 @@ struct PagedAttnParams {
   int row0, n, T;
   int64_t q_seq, q_token, q_head, o_seq, o_token, o_head;
   int H, G, hg;             // hg = H / G
-  int nblk, items;          // blocks of a sequence, n * nblk
+  int nblk;                 // query blocks of a sequence
+  uint32_t inv_hg, inv_nblk;   // ceil(2^32 / n), 0 for n = 1
   int tree;                 // 1: mask, 0: n_sink and window
   int n_sink, window;
   float scale2;             // log2(e) / sqrt(d)
