@@ -300,6 +300,16 @@ __device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
 
 __device__ __forceinline__ int64_t range_begin(int64_t T, int c, int P) { return T * c / P; }
 
+// Ranges of a launch of T units on P CTAs (or gangs): at least kMinUnits units each.  A
+// unit more costs a CTA 0.55 us, a part more costs the merge a wait for memory: one tree
+// of 8 tokens over 2,744 (172 units) 32 us with a unit a CTA.
+constexpr int kMinUnits = 4;
+
+__host__ __device__ __forceinline__ int ranges_of(int64_t T, int P) {
+  const int64_t most = (T + kMinUnits - 1) / kMinUnits;
+  return most < P ? max(static_cast<int>(most), 1) : P;
+}
+
 // Range (of P) that holds flat unit f
 __device__ __forceinline__ int range_of(int64_t f, int64_t T, int P) { return static_cast<int>(((f + 1) * P - 1) / T); }
 
@@ -361,10 +371,10 @@ struct Share {
     const int B = ctl->gang;
     member = B > 1 ? static_cast<int>(blockIdx.x % B) : -1;
     range = blockIdx.x / B;
-    ranges = gridDim.x / B;
     total = static_cast<int64_t>(ctl->before[ctl->items]) * p.G;
+    ranges = ranges_of(total, gridDim.x / B);
     fb = fe = 0;
-    if (range < ranges) {   // (the last CTAs may be too few for a gang)
+    if (range < ranges) {   // (the last CTAs may be too few for a gang, the units too few for all)
       fb = range_begin(total, range, ranges);
       fe = range_begin(total, range + 1, ranges);
     }
@@ -960,31 +970,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
 }
 
 // Merges the parts of the (item, group)s that ranges cut: M = max m, L = sum 2^(m - M)
-// l, O = sum 2^(m - M) O_part / L, lse = (M + log2 L) ln 2.  Block (c, y): the one that
-// CTA c began, query rows 8 y and on, a warp per row; the loads of four parts are in
-// flight before the first is used (one after the other, 40 parts took 75 us).
+// l, O = sum 2^(m - M) O_part / L, lse = (M + log2 L) ln 2.  Block (c, y): the one that range
+// c began, 8 / WARPS query rows from there on; the WARPS warps of a row take every
+// WARPS-th part, four at a time (their loads are in flight before the first is used), and
+// the first adds up what they found.  One warp a row where the launch has many (item,
+// group)s, so that few parts meet; four where a few of them are cut into many.
 constexpr int kBatch = 4;
 
+template <int WARPS>
 __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ PagedAttnParams p) {
+  __shared__ float2 s_ml[8];
+  __shared__ float4 s_o[8][32];
   griddep_launch_dependents();
   griddep_wait();
   const PagedSplit s = p.split[blockIdx.x];
   if (!s.valid) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int first = blockIdx.x / s.gang, member = blockIdx.x % s.gang, ranges = gridDim.x / s.gang;
-  const int r = blockIdx.y * 8 + warp;
-  if (r >= s.nrows) return;
+  const int first = blockIdx.x / s.gang, member = blockIdx.x % s.gang;
+  const int r = blockIdx.y * (8 / WARPS) + warp / WARPS;
+  const bool live = r < s.nrows;
+  if (WARPS == 1 && !live) return;
   float M = -INFINITY, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int cb = first; cb <= s.last; cb += kBatch) {
+  for (int cb = first + warp % WARPS; live && cb <= s.last; cb += kBatch * WARPS) {
     float2 ml[kBatch];
     float4 o[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const int c = cb + k;
+      const int c = cb + k * WARPS;
       ml[k] = make_float2(-INFINITY, 0.f);
       o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (c > s.last || range_begin(s.total, c, ranges) == range_begin(s.total, c + 1, ranges)) continue;   // (an empty range)
+      if (c > s.last) continue;
       const int64_t at = (2 * (static_cast<int64_t>(c) * s.gang + member) + (c == first)) * kPagedRows + r;
       ml[k] = p.part_ml[at];
       o[k] = reinterpret_cast<const float4*>(p.part_o + at * kHeadDim)[lane];
@@ -1003,8 +1019,28 @@ __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ P
       acc = make_float4(acc.x + w * o[k].x, acc.y + w * o[k].y, acc.z + w * o[k].z, acc.w + w * o[k].w);
     }
   }
+  if (WARPS > 1) {
+    s_ml[warp] = make_float2(M, L);
+    s_o[warp][lane] = acc;
+    __syncthreads();
+    if (!live || warp % WARPS != 0) return;
+    float top = M;
+#pragma unroll
+    for (int k = 1; k < WARPS; ++k) top = fmaxf(top, s_ml[warp + k].x);
+    const float ref = top == -INFINITY ? 0.f : top, keep = exp2f(M - ref);
+    M = top;
+    L *= keep;
+    acc = make_float4(acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep);
+#pragma unroll
+    for (int k = 1; k < WARPS; ++k) {
+      const float w = exp2f(s_ml[warp + k].x - ref);
+      const float4 o = s_o[warp + k][lane];
+      L += w * s_ml[warp + k].y;
+      acc = make_float4(acc.x + w * o.x, acc.y + w * o.y, acc.z + w * o.z, acc.w + w * o.w);
+    }
+  }
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  const int t = (s.row0 + r) / p.hg, h = s.g * p.hg + (s.row0 + r) % p.hg;
+  const int t = quotient(s.row0 + r, p.inv_hg), h = s.g * p.hg + s.row0 + r - t * p.hg;
   const __nv_bfloat162 x[2] = {__floats2bfloat162_rn(acc.x * inv, acc.y * inv), __floats2bfloat162_rn(acc.z * inv, acc.w * inv)};
   *reinterpret_cast<uint2*>(p.o + s.seq * p.o_seq + t * p.o_token + h * p.o_head + lane * 4) = *reinterpret_cast<const uint2*>(x);
   if (p.lse && lane == 0)
@@ -1043,8 +1079,10 @@ cudaError_t paged_attn_launch(const PagedAttnParams& p, cudaStream_t stream) {
 
 cudaError_t paged_combine_launch(const PagedAttnParams& p, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = config(attr, dim3(p.grid, (std::min(kPagedRows, p.T * p.hg) + 7) / 8), 256, 0, stream);
-  return cudaLaunchKernelEx(&cfg, k_paged_combine, p);
+  const bool many = p.n * p.nblk * p.G * 4 >= p.grid;   // (item, group)s: about four parts of each at most
+  const int rows = std::min(kPagedRows, p.T * p.hg), per = many ? 8 : 2;
+  cudaLaunchConfig_t cfg = config(attr, dim3(p.grid, (rows + per - 1) / per), 256, 0, stream);
+  return cudaLaunchKernelEx(&cfg, many ? k_paged_combine<1> : k_paged_combine<4>, p);
 }
 
 }  // namespace starkv

@@ -8,6 +8,7 @@ built, importing the first call raises.
 """
 from __future__ import annotations
 
+import builtins
 import ctypes as C
 import struct
 from dataclasses import dataclass, fields
@@ -135,7 +136,7 @@ def lib() -> C.CDLL:
         L.starkv_set_timing.argtypes = [st, C.c_int32]
         L.starkv_kernel_times.argtypes = [st, C.POINTER(C.c_int64), C.POINTER(C.c_float)]
         L.starkv_backward_launches.argtypes = [st, C.POINTER(C.c_int64)]
-        pg, ws = C.POINTER(CPages), [C.c_void_p, C.c_size_t, C.c_void_p]
+        pg, ws = C.c_void_p, [C.c_void_p, C.c_size_t, C.c_void_p]
         L.starkv_pages_workspace_bytes.argtypes = [st, pg, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
         L.starkv_pages_reset.argtypes = [st, pg, C.c_void_p]
         L.starkv_pages_extend.argtypes = [st, pg, C.c_void_p, C.c_void_p, C.c_int32] + ws
@@ -143,9 +144,9 @@ def lib() -> C.CDLL:
         L.starkv_pages_free.argtypes = [st, pg, C.c_void_p, C.c_int32, C.c_void_p]
         L.starkv_pages_compact.argtypes = [st, pg, C.c_void_p, C.POINTER(CSeq), C.c_int32] + ws
         for name in ("starkv_pages_store", "starkv_pages_load"):
-            getattr(L, name).argtypes = [st, pg, C.c_int32, C.c_int32, C.POINTER(CTokens), C.c_void_p]
-        L.starkv_tree_attention.argtypes = [st, pg, C.c_int32, C.POINTER(CQueries)] + ws
-        L.starkv_sink_attention.argtypes = [st, pg, C.c_int32, C.POINTER(CQueries), C.c_int32, C.c_int32] + ws
+            getattr(L, name).argtypes = [st, pg, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
+        L.starkv_tree_attention.argtypes = [st, pg, C.c_int32, C.c_void_p] + ws
+        L.starkv_sink_attention.argtypes = [st, pg, C.c_int32, C.c_void_p, C.c_int32, C.c_int32] + ws
         L.starkv_last_error.argtypes = []
         L.starkv_last_error.restype = C.c_char_p
         for name in ABI_FUNCTIONS:
@@ -201,7 +202,7 @@ class Config:
     @staticmethod
     def default() -> "Config":
         c = CConfig()
-        lib().starkv_default_config(C.byref(c))
+        lib().starkv_default_config(c)
         return Config(**{f.name: getattr(c, f.name) for f in fields(Config)})
 
 
@@ -471,31 +472,41 @@ def backward_launches(st: State) -> int:
 
 # ---------------------------------------------------------------- paged cache
 
-@dataclass
 class Pages:
-    """A paged cache (``starkv_pages``): pool, page table, lengths and page counts, all the caller's."""
+    """A paged cache (``starkv_pages``): pool, page table, lengths and page counts, all the
+    caller's.  The tensors are checked once, when the object is made, and stay its own.
 
-    k: torch.Tensor       # bf16 [n_layers][n_pages][G][page_size][d], the last three contiguous
-    v: torch.Tensor       # the same, with k's strides
-    table: torch.Tensor   # i32 [n_rows][max_pages]
-    len: torch.Tensor     # i32 [n_rows]
-    refs: torch.Tensor    # i32 [n_pages]
+    k, v   bf16 [n_layers][n_pages][G][page_size][d], the last three contiguous, the same strides
+    table  i32 [n_rows][max_pages];  len  i32 [n_rows];  refs  i32 [n_pages]
+    """
 
-    def to_c(self) -> CPages:
-        k, v = self.k, self.v
+    __slots__ = ("_k", "_v", "_table", "_len", "_refs", "_packed", "_shape", "_device")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, len: torch.Tensor, refs: torch.Tensor):
         if k.dim() != 5 or v.shape != k.shape or v.stride() != k.stride():
             raise ValueError("pages: k and v are [n_layers, n_pages, G, page_size, d] with the same strides")
         nl, n_pages, G, P, d = k.shape
         if k.stride()[2:] != (P * d, d, 1):
             raise ValueError("pages: a page of a layer must be contiguous")
         _expect(torch.bfloat16, k, v)
-        _expect(torch.int32, self.table, self.len, self.refs)
-        if self.table.dim() != 2 or self.len.numel() != self.table.shape[0] or self.refs.numel() != n_pages:
+        _expect(torch.int32, table, len, refs)
+        if table.dim() != 2 or len.numel() != table.shape[0] or refs.numel() != n_pages:
             raise ValueError("pages: table is [n_rows, max_pages], len [n_rows], refs [n_pages]")
-        if len({t.device for t in (k, v, self.table, self.len, self.refs)}) != 1:
+        if builtins.len({t.device for t in (k, v, table, len, refs)}) != 1:
             raise ValueError("pages: tensors on more than one device")
-        return CPages(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), n_pages, P, *self.table.shape,
-                      _ptr(self.table), _ptr(self.len), _ptr(self.refs))
+        self._k, self._v, self._table, self._len, self._refs = k, v, table, len, refs
+        self._shape, self._device = (nl, G, d), k.get_device()
+        self._packed = bytes(CPages(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), n_pages, P, *table.shape,
+                                    _ptr(table), _ptr(len), _ptr(refs)))
+
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
+    table = property(lambda self: self._table)
+    len = property(lambda self: self._len)
+    refs = property(lambda self: self._refs)
+
+    def to_c(self) -> CPages:
+        return CPages.from_buffer_copy(self._packed)
 
 
 @dataclass
@@ -528,73 +539,78 @@ def _expect(dtype: torch.dtype, *tensors: Optional[torch.Tensor]) -> None:
 
 def _on(pages: Pages, *tensors: Optional[torch.Tensor]) -> None:
     """The call's tensors lie where its pages do, on the current CUDA device."""
-    dev = pages.k.device
-    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
-        raise ValueError(f"pages on {dev}: the paged calls take tensors of the current CUDA device")
+    dev = pages._device
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"pages on {pages.k.device}: the paged calls take tensors of the current CUDA device")
     for t in tensors:
-        if t is not None and t.device != dev:
-            raise ValueError(f"a tensor on {t.device}, pages on {dev}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor on {t.device}, pages on {pages.k.device}")
 
 
 def _ids(t: Optional[torch.Tensor], n: int, what: str) -> int:
     if t is None:
         return 0
-    _expect(torch.int32, t)
+    if t.dtype is not torch.int32:
+        raise ValueError(f"expected {torch.int32}, got {t.dtype}")
     if t.numel() != n:
         raise ValueError(f"{what}: {t.numel()} entries for {n} sequences")
     return _ptr(t)
 
 
-def _strides(t: torch.Tensor):
-    """Element strides; those of axes of one entry, which are never stepped along, as if contiguous."""
-    out, step = list(t.stride()), t.shape[-1]
-    for i in range(t.dim() - 2, -1, -1):
-        if t.shape[i] == 1:
-            out[i] = step
-        step = max(step, out[i] * t.shape[i])
-    return out
+_TOKENS = struct.Struct("@4P2i4q")
+_QUERIES = struct.Struct("@6P2i6q")
+assert _TOKENS.size == C.sizeof(CTokens) and _QUERIES.size == C.sizeof(CQueries)
 
 
-def _c_tokens(st: State, pages: Pages, tok: Tokens) -> CTokens:
-    k, v = tok.k, tok.v
-    if k.dim() != 5 or k.shape[3:] != (st.cfg.n_kv_heads, st.cfg.head_dim) or k.stride(4) != 1:
+def _c_tokens(st: State, pages: Pages, tok: Tokens) -> bytes:
+    k, v, rows, count = tok.k, tok.v, tok.rows, tok.n_tokens
+    if k.dim() != 5:
+        raise ValueError("tokens: k is [n, layers, T, G, d]")
+    n, nl, T, G, d = k.shape
+    s0, s1, s2, s3, s4 = k.stride()
+    if G != st.cfg.n_kv_heads or d != st.cfg.head_dim or s4 != 1:
         raise ValueError("tokens: k is [n, layers, T, G, d] with d contiguous")
     if v is not None and (v.shape != k.shape or v.stride() != k.stride()):
         raise ValueError("tokens: v has k's shape and strides")
-    _expect(torch.bfloat16, k, v)
-    _on(pages, k, v, tok.rows, tok.n_tokens)
-    n, _, T = k.shape[:3]
-    s = _strides(k)
-    return CTokens(k.data_ptr(), 0 if v is None else v.data_ptr(), _ids(tok.rows, n, "rows"),
-                   _ids(tok.n_tokens, n, "n_tokens"), n, T, s[0], s[1], s[2], s[3])
+    if k.dtype is not torch.bfloat16 or (v is not None and v.dtype is not torch.bfloat16):
+        raise ValueError(f"tokens: expected {torch.bfloat16}")
+    _on(pages, k, v, rows, count)
+    # (an axis of one entry is never stepped along: its stride may be any)
+    return _TOKENS.pack(k.data_ptr(), 0 if v is None else v.data_ptr(), _ids(rows, n, "rows"), _ids(count, n, "n_tokens"), n, T,
+                        s0 if n > 1 else d, s1 if nl > 1 else d, s2 if T > 1 else d, s3 if G > 1 else d)
 
 
-def _c_queries(st: State, pages: Pages, qs: Queries) -> CQueries:
-    q, o = qs.q, qs.o
-    if q.dim() != 4 or q.shape[2:] != (st.cfg.n_heads, st.cfg.head_dim) or q.stride(3) != 1:
-        raise ValueError("queries: q is [n, T, H, d] with d contiguous")
-    if o.shape != q.shape or o.stride(3) != 1:
-        raise ValueError("queries: o has q's shape, with d contiguous")
-    n, T, H, _ = q.shape
-    _expect(torch.bfloat16, q, o)
-    _on(pages, q, o, qs.lse, qs.mask, qs.rows, qs.n_tokens)
-    if qs.lse is not None:
-        _expect(torch.float32, qs.lse)
-        if qs.lse.shape != (n, T, H):
-            raise ValueError("queries: lse is [n, T, H]")
-    if qs.mask is not None:
-        _expect(torch.int64, qs.mask)
-        if qs.mask.shape != (n, T):
-            raise ValueError("queries: mask is [n, T]")
-    return CQueries(q.data_ptr(), o.data_ptr(), _ptr(qs.lse), _ptr(qs.mask), _ids(qs.rows, n, "rows"),
-                    _ids(qs.n_tokens, n, "n_tokens"), n, T, *_strides(q)[:3], *_strides(o)[:3])
+def _c_queries(st: State, pages: Pages, qs: Queries) -> bytes:
+    q, o, lse, mask, rows, count = qs.q, qs.o, qs.lse, qs.mask, qs.rows, qs.n_tokens
+    if q.dim() != 4 or o.shape != q.shape:
+        raise ValueError("queries: q is [n, T, H, d], o of the same shape")
+    n, T, H, d = q.shape
+    s0, s1, s2, s3 = q.stride()
+    o0, o1, o2, o3 = o.stride()
+    if H != st.cfg.n_heads or d != st.cfg.head_dim or s3 != 1 or o3 != 1:
+        raise ValueError("queries: q and o are [n, T, H, d] with d contiguous")
+    if q.dtype is not torch.bfloat16 or o.dtype is not torch.bfloat16:
+        raise ValueError(f"queries: expected {torch.bfloat16}, got {q.dtype} and {o.dtype}")
+    _on(pages, q, o, lse, mask, rows, count)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n, T, H)):
+        raise ValueError("queries: lse is f32 [n, T, H]")
+    if mask is not None and (mask.dtype is not torch.int64 or mask.shape != (n, T)):
+        raise ValueError("queries: mask is i64 [n, T]")
+    if n < 2:      # (an axis of one entry is never stepped along: its stride may be any)
+        s0 = o0 = d
+    if T < 2:
+        s1 = o1 = d
+    if H < 2:
+        s2 = o2 = d
+    return _QUERIES.pack(q.data_ptr(), o.data_ptr(), _ptr(lse), _ptr(mask), _ids(rows, n, "rows"),
+                         _ids(count, n, "n_tokens"), n, T, s0, s1, s2, o0, o1, o2)
 
 
-def _c_pages(st: State, pages: Pages) -> CPages:
-    c = pages.to_c()
-    if (pages.k.shape[0], pages.k.shape[2], pages.k.shape[4]) != (st.cfg.n_layers, st.cfg.n_kv_heads, st.cfg.head_dim):
+def _c_pages(st: State, pages: Pages) -> bytes:
+    cfg = st.cfg
+    if pages._shape != (cfg.n_layers, cfg.n_kv_heads, cfg.head_dim):
         raise ValueError("pages: k is not of the state's layers, KV heads and head dimension")
-    return c
+    return pages._packed
 
 
 def make_pages(st: State, n_pages: int, page_size: int, n_rows: int, max_pages: int, device=None, stream=None) -> Pages:
@@ -613,14 +629,14 @@ def make_pages(st: State, n_pages: int, page_size: int, n_rows: int, max_pages: 
 def pages_workspace(st: State, pages: Pages, n: int, T: int = 1) -> torch.Tensor:
     """Workspace for the paged calls over at most ``n`` rows and ``T`` queries of each."""
     b = C.c_size_t()
-    _check(lib().starkv_pages_workspace_bytes(st.handle, C.byref(_c_pages(st, pages)), n, T, C.byref(b)))
+    _check(lib().starkv_pages_workspace_bytes(st.handle, _c_pages(st, pages), n, T, C.byref(b)))
     return torch.empty(int(b.value), dtype=torch.uint8, device=pages.k.device)
 
 
 def pages_reset(st: State, pages: Pages, stream=None) -> None:
     c = _c_pages(st, pages)
     _on(pages)
-    _check(lib().starkv_pages_reset(st.handle, C.byref(c), _stream(stream)))
+    _check(lib().starkv_pages_reset(st.handle, c, _stream(stream)))
 
 
 def pages_extend(st: State, pages: Pages, rows: Optional[torch.Tensor], n_new: torch.Tensor, ws: torch.Tensor,
@@ -628,7 +644,7 @@ def pages_extend(st: State, pages: Pages, rows: Optional[torch.Tensor], n_new: t
     """Room for ``n_new[i]`` more tokens of ``rows[i]``; shared last pages are copied first."""
     c, n = _c_pages(st, pages), n_new.numel()
     _on(pages, rows, n_new, ws)
-    _check(lib().starkv_pages_extend(st.handle, C.byref(c), _ids(rows, n, "rows"), _ids(n_new, n, "n_new"), n,
+    _check(lib().starkv_pages_extend(st.handle, c, _ids(rows, n, "rows"), _ids(n_new, n, "n_new"), n,
                                      ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
@@ -637,7 +653,7 @@ def pages_fork(st: State, pages: Pages, src: torch.Tensor, dst: torch.Tensor, ws
     """Row ``dst[i]`` becomes a copy of ``src[i]``, sharing its pages (``deep``: with pages of its own)."""
     c, n = _c_pages(st, pages), dst.numel()
     _on(pages, src, dst, ws)
-    _check(lib().starkv_pages_fork(st.handle, C.byref(c), _ids(src, n, "src"), _ids(dst, n, "dst"), n, int(deep),
+    _check(lib().starkv_pages_fork(st.handle, c, _ids(src, n, "src"), _ids(dst, n, "dst"), n, int(deep),
                                    ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
@@ -645,7 +661,7 @@ def pages_free(st: State, pages: Pages, rows: torch.Tensor, stream=None) -> None
     """Empties rows; pages that no row holds any more are free."""
     c, n = _c_pages(st, pages), rows.numel()
     _on(pages, rows)
-    _check(lib().starkv_pages_free(st.handle, C.byref(c), _ids(rows, n, "rows"), n, _stream(stream)))
+    _check(lib().starkv_pages_free(st.handle, c, _ids(rows, n, "rows"), n, _stream(stream)))
 
 
 def pages_compact(st: State, pages: Pages, rows: Optional[torch.Tensor], seqs: Sequence[Seq], ws: torch.Tensor,
@@ -653,27 +669,27 @@ def pages_compact(st: State, pages: Pages, rows: Optional[torch.Tensor], seqs: S
     """Every layer of ``rows[i]`` keeps the tokens ``seqs[i].idx`` and the window (``starkv_compact`` on pages)."""
     c = _c_pages(st, pages)
     _on(pages, rows, ws, *(t for s in seqs for t in (s.idx, s.meta, s.meta_out)))
-    _check(lib().starkv_pages_compact(st.handle, C.byref(c), _ids(rows, len(seqs), "rows"), _seq_array(seqs), len(seqs),
+    _check(lib().starkv_pages_compact(st.handle, c, _ids(rows, len(seqs), "rows"), _seq_array(seqs), len(seqs),
                                       ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def pages_store(st: State, pages: Pages, layer0: int, tokens: Tokens, stream=None) -> None:
     """``tokens`` into the last places of their rows, layers layer0, layer0 + 1, ..."""
     c, tok = _c_pages(st, pages), _c_tokens(st, pages, tokens)
-    _check(lib().starkv_pages_store(st.handle, C.byref(c), layer0, tokens.k.shape[1], C.byref(tok), _stream(stream)))
+    _check(lib().starkv_pages_store(st.handle, c, layer0, tokens.k.shape[1], tok, _stream(stream)))
 
 
 def pages_load(st: State, pages: Pages, layer0: int, tokens: Tokens, stream=None) -> None:
     """The last tokens of their rows into ``tokens``."""
     c, tok = _c_pages(st, pages), _c_tokens(st, pages, tokens)
-    _check(lib().starkv_pages_load(st.handle, C.byref(c), layer0, tokens.k.shape[1], C.byref(tok), _stream(stream)))
+    _check(lib().starkv_pages_load(st.handle, c, layer0, tokens.k.shape[1], tok, _stream(stream)))
 
 
 def tree_attention(st: State, pages: Pages, layer: int, queries: Queries, ws: torch.Tensor, stream=None) -> None:
     """Attention of each row's last (drafted) tokens over its cache; ``queries.mask`` names the drafted ones seen."""
     c, q = _c_pages(st, pages), _c_queries(st, pages, queries)
     _on(pages, ws)
-    _check(lib().starkv_tree_attention(st.handle, C.byref(c), layer, C.byref(q), ws.data_ptr(), ws.numel(),
+    _check(lib().starkv_tree_attention(st.handle, c, layer, q, ws.data_ptr(), ws.numel(),
                                        _stream(stream)))
 
 
@@ -682,5 +698,5 @@ def sink_attention(st: State, pages: Pages, layer: int, queries: Queries, n_sink
     """Causal attention over the first ``n_sink`` tokens and the last ``window``."""
     c, q = _c_pages(st, pages), _c_queries(st, pages, queries)
     _on(pages, ws)
-    _check(lib().starkv_sink_attention(st.handle, C.byref(c), layer, C.byref(q), n_sink, window, ws.data_ptr(),
+    _check(lib().starkv_sink_attention(st.handle, c, layer, q, n_sink, window, ws.data_ptr(),
                                        ws.numel(), _stream(stream)))

@@ -108,10 +108,24 @@ def test_the_binding_checks_the_tensors_of_a_call():
             sk._c_queries(st, pages, bad)
 
 
-def test_strides_of_axes_that_are_never_stepped_along():
-    x = torch.empty_strided((1, 3, 1, 128), (7, 256, 5, 1))
-    assert sk._strides(x) == [768, 256, 128, 1]
-    assert sk._strides(torch.zeros(2, 3, 4, 128)) == [1536, 512, 128, 1]
+def test_packed_calls_equal_the_ctypes_structs(monkeypatch):
+    st, pages = _State(), _pages()
+    monkeypatch.setattr(sk, "_on", lambda *a: None)
+    bf, i32 = dict(dtype=torch.bfloat16), dict(dtype=torch.int32)
+    k, rows, n = torch.zeros((3, 2, 5, 4, 128), **bf), torch.zeros(3, **i32), torch.ones(3, **i32)
+    want = sk.CTokens(k.data_ptr(), 0, rows.data_ptr(), n.data_ptr(), 3, 5, *k.stride()[:4])
+    assert sk._c_tokens(st, pages, sk.Tokens(k=k, rows=rows, n_tokens=n)) == bytes(want)
+    q, o = torch.zeros((5, 3, 8, 128), **bf).transpose(0, 1), torch.zeros((3, 5, 8, 128), **bf)
+    lse, mask = torch.zeros((3, 5, 8)), torch.zeros((3, 5), dtype=torch.int64)
+    want = sk.CQueries(q.data_ptr(), o.data_ptr(), lse.data_ptr(), mask.data_ptr(), rows.data_ptr(), 0, 3, 5, *q.stride()[:3],
+                       *o.stride()[:3])
+    assert sk._c_queries(st, pages, sk.Queries(q=q, o=o, lse=lse, mask=mask, rows=rows)) == bytes(want)
+    # an axis of one entry is never stepped along, whatever its stride
+    x = torch.empty_strided((1, 1, 8, 128), (7, 5, 256, 1), **bf)
+    got = sk.CQueries.from_buffer_copy(sk._c_queries(st, pages, sk.Queries(q=x, o=x)))
+    assert (got.q_seq_stride, got.q_token_stride, got.q_head_stride) == (128, 128, 256)
+    with pytest.raises(AttributeError):      # a pool's tensors are checked once, and stay its own
+        pages.k = k
 
 
 def test_the_definition_of_attention_against_torch():
