@@ -1252,7 +1252,7 @@ starkv_status move_tokens(starkv_state* st, bool store, const starkv_pages* page
   v.head_stride = t->head_stride;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_MOVE, cs, [&] {
-    return page_move_launch(store, view_of(st, *pages), v, st->num_sms, st->dev.err, cs);
+    return page_move_launch(store, view_of(st, *pages), v, st->dev.err, cs);
   }));
   return STARKV_OK;
 }

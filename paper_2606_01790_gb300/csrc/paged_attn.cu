@@ -132,7 +132,9 @@ __device__ __forceinline__ bool warp_wait(const Ctl* ctl, uint64_t* bar, uint32_
   return __all_sync(kFull, mbar_wait(bar, parity, limit_ns) && !aborted);
 }
 
-// Two of them, at the price of one where both are complete.
+// Two of them, at the price of one where both are complete.  They may be looked at in
+// either order: each has to be a barrier whose previous phase this warp knows to be
+// complete already (a parity cannot tell a phase from the one two before it).
 __device__ __forceinline__ bool warp_wait2(const Ctl* ctl, uint64_t* a, uint32_t pa, uint64_t* b, uint32_t pb, uint64_t limit_ns) {
   const bool ra = mbar_try_wait(a, pa), rb = mbar_try_wait(b, pb);
   if (__all_sync(kFull, ra && rb)) return true;
@@ -804,8 +806,13 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
           bits = static_cast<uint64_t>(__reduce_or_sync(kFull, static_cast<uint32_t>(bits >> 32))) << 32 |
                  __reduce_or_sync(kFull, static_cast<uint32_t>(bits));
         }
+        // V of this unit is asked for only once the stage's previous V has been used: S runs
+        // further ahead than the ring of V is deep, and a parity says nothing of a load while
+        // the one before it is still under way
+        const uint32_t before = ui - kStages;
+        if (ui >= kStages) ok = warp_wait(ctl, &ctl->p_empty[before % kPlaces], before / kPlaces & 1, p.wait_ns);
         const int stage = ui % kStages;
-        ok = warp_wait(ctl, &ctl->v_full[stage], ui / kStages & 1, p.wait_ns);
+        ok = ok && warp_wait(ctl, &ctl->v_full[stage], ui / kStages & 1, p.wait_ns);
         if (!ok) break;
         if (clean_v(reinterpret_cast<uint4*>(sV + stage * kUnitBytes), blk.any(p, bits)(k0), r)) ctl->poison[pc & 7] = pc + 1;
       }
@@ -829,7 +836,9 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
       tc_fence_after();
       take_queries(nx);
     }
-    ok = warp_wait2(ctl, &ctl->ml_full, pc & 1, &ctl->p_empty[lpl], lpar, p.wait_ns);
+    // (one after the other: until both lines are through, the last unit's place may not have
+    // come round, and its parity would speak of the use before)
+    ok = warp_wait(ctl, &ctl->ml_full, pc & 1, p.wait_ns) && warp_wait(ctl, &ctl->p_empty[lpl], lpar, p.wait_ns);
     if (!ok) break;
     tc_fence_after();
     if (wactive) {

@@ -70,7 +70,6 @@ struct TokensView {
   int64_t seq_stride, layer_stride, token_stride, head_stride;
 };
 
-cudaError_t page_move_launch(bool store, const PagesView& pg, const TokensView& t, int num_sms, uint32_t* err,
-                             cudaStream_t stream);
+cudaError_t page_move_launch(bool store, const PagesView& pg, const TokensView& t, uint32_t* err, cudaStream_t stream);
 
 }  // namespace starkv

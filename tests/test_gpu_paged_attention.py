@@ -362,3 +362,57 @@ def test_a_decoding_loop_over_a_compressed_cache():
     c.check()
     assert int(c.pages.refs.sum()) == 0
     st.close()
+
+
+def _reference(k, v, q, seen):
+    """One sequence's attention in 64 bits on the GPU: k, v [G][L][d], q [n][H][d], seen [n][L]."""
+    n, H, d = q.shape
+    G = k.shape[0]
+    z = torch.einsum("nghd,gld->nghl", q.double().view(n, G, H // G, d), k.double()) / d**0.5
+    z = z.masked_fill(~seen[:, None, None], -torch.inf)
+    p = z.softmax(-1)
+    o, size = (torch.einsum("nghl,gld->nghd", p, x).reshape(n, H, d) for x in (v.double(), v.double().abs()))
+    return o, size, torch.logsumexp(z, -1).reshape(n, H)
+
+
+@pytest.mark.parametrize("heads,kv_heads,P,n,T,most", [(32, 8, 32, 64, 1, 14033), (28, 4, 64, 32, 26, 9000), (28, 4, 16, 6, 64, 20001)])
+def test_ragged_batches_that_fill_the_gpu(heads, kv_heads, P, n, T, most):
+    """Many ranges over long rows: loads, products and softmax of many units at once, rows whose last unit ends
+    inside a page, pieces that ranges cut anywhere.  o is rounded to bf16 (2^-8 of its value), from sums that
+    carry what check_attention counts (2^-15 for the weights, and logits of up to 14 here: 4 dz < 2^-13)."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    lens = [int(x) for x in np.random.default_rng(n).integers(most // 4, most, n)]
+    lens[0] = most
+    need = [-(-x // P) for x in lens]
+    st = PH.state(heads=heads, kv_heads=kv_heads, window=1)
+    pages = sk.make_pages(st, sum(need), P, n, max(need))
+    for x in (pages.k, pages.v):
+        x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+    order, at = torch.randperm(sum(need), generator=g, device="cuda").int(), 0
+    for r, m in enumerate(need):
+        pages.table[r, :m] = order[at:at + m]
+        at += m
+    pages.len.copy_(torch.tensor(lens, dtype=torch.int32))
+    ws = sk.pages_workspace(st, pages, n, T)
+    q = (2 * torch.randn((n, T, heads, PH.D), generator=g, device="cuda")).to(torch.bfloat16)
+    o, lse = torch.empty_like(q), torch.empty((n, T, heads), device="cuda")
+    mask = torch.tensor([[(1 << t + 1) - 1 if t < 63 else -1 for t in range(T)]] * n, device="cuda")
+    for tree in (False, True):
+        for _ in range(5):
+            qs = sk.Queries(q=q, o=o, lse=lse, mask=mask)
+            if tree:
+                sk.tree_attention(st, pages, 0, qs, ws)
+            else:
+                sk.sink_attention(st, pages, 0, qs, 4, 4096, ws)
+        sk.check_device_error(st)
+        for r, L in enumerate(lens):
+            ids = pages.table[r, :need[r]].long()
+            k, v = (x[0, ids].transpose(0, 1).flatten(1, 2)[:, :L] for x in (pages.k, pages.v))
+            j, i = torch.arange(L, device="cuda"), torch.arange(L - T, L, device="cuda")[:, None]
+            seen = (j <= i) if tree else (j <= i) & ((j < 4) | (j > i - 4096))
+            ro, size, rl = _reference(k, v, q[r], seen)
+            err = (o[r].double() - ro).abs()
+            tol = 2.0**-8 * ro.abs() + (2.0**-12 + L * 2.0**-24) * size
+            assert bool((err <= tol).all()), (tree, r, float((err / tol).max()))
+            assert float((lse[r].double() - rl).abs().max()) < 1e-4, (tree, r)
+    st.close()

@@ -68,3 +68,35 @@ def test_loaders_see_every_copy_land(source, role):
         depth += line.count("{") - line.count("}")
     assert found and all(d == 0 for d, _ in found)
     assert not re.search(r"if \(ctl->abort\)\s*\{?\s*for", body)
+
+
+@pytest.mark.parametrize("role", ["load_loop", "mma_s_loop", "mma_pv_loop", "softmax_unit", "softmax_loop"])
+def test_warp_wide_paged_attention_roles_leave_together(role):
+    """As in the window attention: these roles learn of a failure through a vote only, and wait on regardless
+    for nothing but their own products and copies."""
+    body = functions("paged_attn.cu")[role]
+    assert "abort" not in body
+    assert "warp_wait(" in body
+    alone = [w for w in re.findall(r"\bmbar_wait\(([^,]*),", body)]
+    assert alone == {"load_loop": ["&full[i]"], "mma_s_loop": ["&ctl->drain"], "mma_pv_loop": ["&ctl->drain"]}.get(role, [])
+
+
+def test_paged_attention_asks_two_barriers_at_once_only_where_either_order_is_right():
+    """A parity cannot tell a phase from the one two before it, and two questions may be answered in either
+    order: only barriers whose previous phase the asking warp has waited for itself may share a vote.  The loader's
+    and the softmax's (rings that the products go round) do; a piece's end asks one after the other."""
+    f = functions("paged_attn.cu")
+    assert {name for name, body in f.items() if "warp_wait2(" in body} == {"mma_s_loop", "mma_pv_loop"}
+    assert "warp_wait2" not in f["softmax_loop"] and f["softmax_loop"].count("ml_full, pc & 1, p.wait_ns) && warp_wait(") == 1
+    clean = f["softmax_loop"].index("clean_v(")
+    assert f["softmax_loop"].index("p_empty[before % kPlaces]") < f["softmax_loop"].index("v_full[stage]") < clean
+
+
+def test_the_paged_loader_sees_every_copy_land():
+    body = functions("paged_attn.cu")["load_loop"]
+    depth, found = 0, []
+    for line in body.split("\n"):
+        if "drain_limit(" in line:
+            found.append(depth)
+        depth += line.count("{") - line.count("}")
+    assert found == [0]
