@@ -1331,6 +1331,7 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
   memset(&p, 0, sizeof(p));
   if ((s = encode_pages(&p.tmk, pg.k + layer * pg.layer_stride, pg)) != STARKV_OK) return s;
   if ((s = encode_pages(&p.tmv, pg.v + layer * pg.layer_stride, pg)) != STARKV_OK) return s;
+  p.k = pg.k + layer * pg.layer_stride;
   p.v = pg.v + layer * pg.layer_stride;
   p.page_stride = pg.page_stride;
   p.table = pg.table;

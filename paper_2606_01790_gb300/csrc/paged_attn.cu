@@ -42,11 +42,12 @@
 //
 // Pages come by TMA, a box per page (or 64 of its rows); a page number that is none
 // lies outside the map and reads as zeros.  Units that not every row of the block sees
-// whole take a masked softmax, whose warpgroup also looks after V: the rows that no
-// query sees are zeroed in shared memory (0 times what a free slot holds need not be
-// 0).  A V element that is not finite and is seen by some rows of a block only must reach
-// those alone, which the product cannot do: it is zeroed as well, and each row that sees
-// it adds it at the end (patch_poison).
+// whole take a masked softmax.  A weight of 0 does not keep out a V that is not finite: the
+// slots behind the last token, which may hold anything, are zeroed in shared memory, and a
+// piece with masked units whose O has elements that are not finite takes those rows
+// again, key by key (recompute_rows): what a row does not see then has no part in it, and
+// what it sees has its due.  (Looking through V of every masked unit beforehand took 1,500
+// cycles a unit.)
 //
 // Warp roles: 0 loads K, 3 loads V, 1 issues S and owns tensor memory, 2 issues P V,
 // 4..7 and 8..11 softmax.
@@ -96,13 +97,13 @@ struct Ctl {
   uint64_t drain;
   uint32_t tmem_base;
   volatile int abort;
-  volatile int poison[8];           // [piece & 7]: piece + 1 if the piece met such elements
   int warp_sum[kThreads / 32];
   int items;                        // of the launch: sequences in gangs, else query blocks
   int gang;                         // CTAs of a gang (1: none)
   int64_t sum[2];                   // units, and units times blocks
   volatile float m[1 + kPagedRows]; // [1 + row]: the rows' references, as they pass from unit to unit
   float2 ml[2][2][kPagedRows];      // [piece & 1][line]
+  volatile int masked[2][2];        // [piece & 1][line]: a unit of the piece was masked
   int before[kPagedItems + 1];      // units before an item (one KV group)
   Item item[kPagedItems];
 };
@@ -207,12 +208,6 @@ struct Block {
     if (L < 0) return Seen{0, 0, 0, 0, 0};
     if (p.tree) return Seen{0, 0, L - n, 0, 0};
     return Seen{min(p.n_sink, first_pos() + 1), max(0, last_pos() - p.window + 1), first_pos() + 1, 0, 0};
-  }
-  // by some row; `bits`: the union of the block's masks
-  __device__ __forceinline__ Seen any(const PagedAttnParams& p, uint64_t bits) const {
-    if (L < 0) return Seen{0, 0, 0, 0, 0};
-    if (p.tree) return Seen{0, 0, L - n, L - n, bits & below(n)};
-    return Seen{min(p.n_sink, last_pos() + 1), max(0, first_pos() - p.window + 1), last_pos() + 1, 0, 0};
   }
 };
 
@@ -668,18 +663,6 @@ __device__ __forceinline__ bool softmax_unit(const PagedAttnParams& p, Ctl* ctl,
   return true;
 }
 
-__device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7F80u) == 0x7F80u; }
-
-// Bits 15 and 31: the lower and the upper bf16 of a word is not finite (an exponent of
-// ones carries into the sign's place).
-__device__ __forceinline__ uint32_t not_finite2(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
-
-// A word with the halves that are not finite zeroed.
-__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
-  const uint32_t bad = not_finite2(w);
-  return w & ~((bad >> 15 & 1) * 0xFFFFu | (bad >> 31) * 0xFFFF0000u);
-}
-
 // 16-byte chunk c (of 16) of row i of a warp's staged half of O: rows of 64 floats, the
 // chunks in an order that depends on the row, so that neither lanes on rows nor lanes on
 // columns meet in a bank.
@@ -687,55 +670,61 @@ __device__ __forceinline__ float4* staged(float* stage, int i, int c) {
   return reinterpret_cast<float4*>(stage) + i * 16 + (c ^ (i & 15));
 }
 
-// Adds to a staged row of O, columns col .. col + 63, what its product left out: the
-// elements of V that are not finite, at the keys it sees in the piece's masked units.  (Their
-// weight is taken as positive: one that has underflowed to 0 gives the infinity and not a
-// NaN.)
-__device__ __noinline__ void patch_poison(const PagedAttnParams& p, const Block& blk, const Seen& see, int g, int j0, int n, int col,
-                                          float* stage, int i) {
-  const Seen all = blk.all(p);
-  const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
-  const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
-  for (int j = j0; j < j0 + n; ++j) {
-    const int k0 = blk.key(j);
-    if (all.whole(k0)) continue;
-    for (uint64_t bits = see(k0); bits; bits &= bits - 1) {
-      const int key = k0 + __ffsll(static_cast<long long>(bits)) - 1;
-      const int page = entries[key >> p.shift];
-      if (page < 0 || page >= p.n_pages) continue;
-      const __nv_bfloat16* v = p.v + page * p.page_stride +
-                               ((static_cast<int64_t>(g) << p.shift) + (key & ((1 << p.shift) - 1))) * kHeadDim + col;
-      for (int x = 0; x < 64; ++x) {
-        const uint32_t b = *reinterpret_cast<const uint16_t*>(v + x);
-        if (not_finite(b)) reinterpret_cast<float*>(staged(stage, i, x >> 2))[x & 3] += __uint_as_float(b << 16);
-      }
-    }
-  }
+__device__ __forceinline__ float4 bf16x4(const __nv_bfloat16* p) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                     __uint_as_float(w.y & 0xFFFF0000u));
 }
 
-// V of a unit that not every row sees whole (by the 128 threads of its line): rows that
-// no query sees (bits of `seen` clear) and elements that are not finite become zeros.
-// Returns whether this thread met one of the latter.
-__device__ __forceinline__ bool clean_v(uint4* v4, uint64_t seen, int thread) {
-  bool met = false;
-#pragma unroll 1
-  for (int x0 = thread; x0 < kUnitBytes / 16; x0 += 4 * 128) {
-    uint4 w[4];
+// Columns col .. col + 63 of the staged rows `which` (bits) of a warp's 32, from row r0 of
+// the block on, over the piece's keys: by the whole warp, one row and one key at a
+// time, skipping the keys that the row does not see.  Against the reference `top` of the
+// row (lane i: row i), times `norm` (the same).
+__device__ __noinline__ void recompute_rows(const PagedAttnParams& p, const Block& blk, int g, int j0, int n, int r0, int col, uint32_t which,
+                                            float top, float norm, float* stage) {
+  const int lane = threadIdx.x & 31;
+  const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
+  const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
+  for (; which; which &= which - 1) {
+    const int i = __ffs(which) - 1;
+    const int t = quotient(blk.row0 + r0 + i, p.inv_hg), h = g * p.hg + blk.row0 + r0 + i - t * p.hg;
+    const Seen see = blk.row(p, blk.L - blk.n + t, p.tree ? p.mask[static_cast<int64_t>(blk.seq) * p.T + t] : 0);
+    const float4 q = bf16x4(p.q + blk.seq * p.q_seq + t * p.q_token + h * p.q_head + 4 * lane);
+    const float ref = __shfl_sync(kFull, top, i), scale = __shfl_sync(kFull, norm, i);
+    float2 acc = make_float2(0.f, 0.f);
+    for (int j = j0; j < j0 + n; ++j) {
+      const int k0 = blk.key(j);
+      for (uint64_t bits = see(k0); bits;) {
+        float4 k[8];   // eight keys' loads at once: their latency is most of this path's time
+        float2 v[8];
+        bool any[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = v4[x0 + 128 * k];
+        for (int u = 0; u < 8; ++u) {
+          any[u] = bits != 0;
+          const int key = k0 + __ffsll(static_cast<long long>(bits)) - 1;
+          bits &= bits - 1;
+          k[u] = make_float4(0.f, 0.f, 0.f, 0.f);   // (a page number that is none: zeros)
+          v[u] = make_float2(0.f, 0.f);
+          const int page = any[u] ? entries[key >> p.shift] : -1;
+          if (page >= 0 && page < p.n_pages) {
+            const int64_t at = page * p.page_stride + ((static_cast<int64_t>(g) << p.shift) + (key & ((1 << p.shift) - 1))) * kHeadDim;
+            k[u] = bf16x4(p.k + at + 4 * lane);
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(p.v + at + col + 2 * lane);
+            v[u] = make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+          }
+        }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int x = x0 + 128 * k;
-      if (!(seen >> (x >> 3 & 63) & 1)) {   // 8 chunks of 16 bytes a key and half
-        v4[x] = make_uint4(0u, 0u, 0u, 0u);
-      } else if (not_finite2(w[k].x) | not_finite2(w[k].y) | not_finite2(w[k].z) | not_finite2(w[k].w)) {
-        v4[x] = make_uint4(finite_part(w[k].x), finite_part(w[k].y), finite_part(w[k].z), finite_part(w[k].w));
-        met = true;
+        for (int u = 0; u < 8; ++u) {
+          float z = q.x * k[u].x + q.y * k[u].y + q.z * k[u].z + q.w * k[u].w;
+#pragma unroll
+          for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
+          const float e = exp2f(z * p.scale2 - ref);
+          if (any[u]) acc = make_float2(acc.x + e * v[u].x, acc.y + e * v[u].y);
+        }
       }
     }
+    reinterpret_cast<float2*>(staged(stage, i, lane >> 1))[lane & 1] = make_float2(acc.x * scale, acc.y * scale);
   }
-  fence_proxy_async_smem();
-  return met;
 }
 
 // Softmax warps of a line (0: even units, 1: odd): one thread per query row (TMEM lane
@@ -775,6 +764,7 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
   PieceIter c(p, ctl, sh.member, sh.fb, sh.fe);
   if (line == 0 && c.valid()) take_queries(c);
   for (; ok && c.valid(); ++pc) {
+    bool any_masked = false;
     const Block blk = c.block(p, ctl);
     const bool wactive = quad * 32 < blk.nrows;
     const bool live = r < blk.nrows;
@@ -799,22 +789,21 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
         mbar_arrive(&ctl->ref[line][quad]);
       }
       if (masked) {
-        if (!ok) break;
-        uint64_t bits = 0;
-        if (p.tree) {   // the union of the block's masks (at most 64 tokens)
-          for (int x = blk.tf + lane; x <= blk.tl && x < blk.n; x += 32) bits |= masks[x];
-          bits = static_cast<uint64_t>(__reduce_or_sync(kFull, static_cast<uint32_t>(bits >> 32))) << 32 |
-                 __reduce_or_sync(kFull, static_cast<uint32_t>(bits));
+        any_masked = true;
+        if (ok && k0 + kPagedUnitKeys > blk.L) {
+          // The slots behind the last token.  V of this unit is asked for only once the stage's
+          // previous V has been used: S runs further ahead than the ring of V is deep, and a
+          // parity says nothing of a load while the one before it is still under way
+          const uint32_t before = ui - kStages;
+          if (ui >= kStages) ok = warp_wait(ctl, &ctl->p_empty[before % kPlaces], before / kPlaces & 1, p.wait_ns);
+          const int stage = ui % kStages;
+          ok = ok && warp_wait(ctl, &ctl->v_full[stage], ui / kStages & 1, p.wait_ns);
+          if (!ok) break;
+          uint4* v4 = reinterpret_cast<uint4*>(sV + stage * kUnitBytes);
+          for (int x = (max(blk.L, k0) - k0) * 8 + r; x < kUnitBytes / 32; x += 128)   // 8 chunks of 16 bytes a key, in each half
+            v4[x] = v4[x + kUnitBytes / 32] = make_uint4(0u, 0u, 0u, 0u);
+          fence_proxy_async_smem();
         }
-        // V of this unit is asked for only once the stage's previous V has been used: S runs
-        // further ahead than the ring of V is deep, and a parity says nothing of a load while
-        // the one before it is still under way
-        const uint32_t before = ui - kStages;
-        if (ui >= kStages) ok = warp_wait(ctl, &ctl->p_empty[before % kPlaces], before / kPlaces & 1, p.wait_ns);
-        const int stage = ui % kStages;
-        ok = ok && warp_wait(ctl, &ctl->v_full[stage], ui / kStages & 1, p.wait_ns);
-        if (!ok) break;
-        if (clean_v(reinterpret_cast<uint4*>(sV + stage * kUnitBytes), blk.any(p, bits)(k0), r)) ctl->poison[pc & 7] = pc + 1;
       }
       if (!ok) break;
       tmem_wait_st();
@@ -827,7 +816,10 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
     // both lines' references and sums, and O
     ctl->ml[pc & 1][line][r] = make_float2(m, l);
     __syncwarp();
-    if (lane == 0) mbar_arrive(&ctl->ml_full);
+    if (lane == 0) {
+      ctl->masked[pc & 1][line] = any_masked;   // (the same from each of the line's warps)
+      mbar_arrive(&ctl->ml_full);
+    }
     PieceIter nx = c;
     nx.next(p, ctl);
     if (line == 0 && nx.valid()) {   // S of the next piece runs under this piece's end
@@ -857,7 +849,13 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
         *staged(stage_o, lane, i) = make_float4(__uint_as_float(x[0]) * norm, __uint_as_float(x[1]) * norm, __uint_as_float(x[2]) * norm,
                                                 __uint_as_float(x[3]) * norm);
       }
-      if (ctl->poison[pc & 7] == pc + 1 && live) patch_poison(p, blk, see, c.g, c.j0, c.n, 64 * line, stage_o, lane);
+      if (ctl->masked[pc & 1][0] | ctl->masked[pc & 1][1]) {   // (else every row sees every key)
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sum += __uint_as_float(a[0][i]) * 0.f + __uint_as_float(a[1][i]) * 0.f;   // 0, or NaN
+        const uint32_t which = __ballot_sync(kFull, live && sum != 0.f);
+        if (which) recompute_rows(p, blk, c.g, c.j0, c.n, quad * 32, 64 * line, which, ref, norm, stage_o);
+      }
       __syncwarp();
       const int rows = min(32, blk.nrows - quad * 32);
       if (whole) {
@@ -920,7 +918,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
     mbar_init(&ctl->o_empty, kSoftWarps);
     mbar_init(&ctl->drain, 2);   // one commit per MMA issuer
     ctl->abort = 0;
-    for (int i = 0; i < 8; ++i) ctl->poison[i] = 0;
     ctl->gang = 1;
     ctl->sum[0] = ctl->sum[1] = 0;
     fence_mbar_init();

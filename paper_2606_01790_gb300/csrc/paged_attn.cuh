@@ -20,6 +20,7 @@ struct PagedSplit {
 
 struct PagedAttnParams {
   CUtensorMap tmk, tmv;     // the layer's pages: dims (d, P, G, n_pages), box (64, min(P, 64), 1, 1), 128B swizzle
+  const __nv_bfloat16* k;
   const __nv_bfloat16* v;
   int64_t page_stride;      // elements
   const int32_t* table;

@@ -416,3 +416,25 @@ def test_ragged_batches_that_fill_the_gpu(heads, kv_heads, P, n, T, most):
             assert bool((err <= tol).all()), (tree, r, float((err / tol).max()))
             assert float((lse[r].double() - rl).abs().max()) < 1e-4, (tree, r)
     st.close()
+
+
+def test_values_that_are_not_finite_in_long_rows():
+    """A NaN before the window's edge and one behind the drafted tokens of another branch, in rows of many units: the
+    queries that do not see it are what they are without it, within the wait limit."""
+    T = 20
+    c = filled([20000, 9001], P=64, seed=4)
+    clean = [c.cache(r, 0) for r in (0, 1)]
+    S, W = 2, 19000
+    j = 20000 - T - W + 1        # only the first query's window begins with it
+    c.pages.v[0, int(c.ref.table[0, j // 64]), :, j % 64, 3] = float("nan")
+    qs = queries(c, 2, T, seed=1)
+    sk.sink_attention(c.st, c.pages, 0, qs, S, W, c.ws)
+    torch.cuda.synchronize()
+    sk.check_device_error(c.st)
+    o, lse, q = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy(), qs.q.float().cpu().numpy()
+    assert np.isnan(o[0, 0, :, 3]).all() and np.isfinite(np.delete(o[0, 0], 3, axis=1)).all()
+    for r, (k, v) in enumerate(clean):
+        seen = O.seen_sink(k.shape[1], T, S, W)
+        for t in (1, 7, T - 1):
+            PH.check_attention(o[r, t:t + 1], lse[r, t:t + 1], q[r, t:t + 1], k, v, seen[t:t + 1], what=f"{r} {t}")
+    c.st.close()

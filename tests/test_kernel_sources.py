@@ -88,8 +88,8 @@ def test_paged_attention_asks_two_barriers_at_once_only_where_either_order_is_ri
     f = functions("paged_attn.cu")
     assert {name for name, body in f.items() if "warp_wait2(" in body} == {"mma_s_loop", "mma_pv_loop"}
     assert "warp_wait2" not in f["softmax_loop"] and f["softmax_loop"].count("ml_full, pc & 1, p.wait_ns) && warp_wait(") == 1
-    clean = f["softmax_loop"].index("clean_v(")
-    assert f["softmax_loop"].index("p_empty[before % kPlaces]") < f["softmax_loop"].index("v_full[stage]") < clean
+    loop = f["softmax_loop"]
+    assert loop.index("p_empty[before % kPlaces]") < loop.index("v_full[stage]") < loop.index("v4[x] =")
 
 
 def test_the_paged_loader_sees_every_copy_land():
