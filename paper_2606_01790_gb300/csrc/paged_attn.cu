@@ -21,7 +21,7 @@
 //   P           p = exp2(S c - m), l += p in fp32; p = hi + lo, two bf16 (16 bits),
 //               in the place of S in tensor memory;
 //   O += P V    M = 128, N = d = 128, K = 64 keys, once for hi and once for lo.
-// One bf16 part would round each weight by 2^-9, as much as the output's own
+// One bf16 part would round each weight by up to 2^-8, as much as the output's own
 // rounding; the second part costs four more products a unit, which the stream of K
 // and V covers where a block's rows are few.  (fp16 weights would need V in fp16, which
 // holds neither its range nor its small values.)
@@ -31,9 +31,7 @@
 // takes about 4,000 cycles, so five units are under way, each in a place of its own in
 // tensor memory.  Both warpgroups weigh against one reference m per row, which passes
 // from unit to unit in order through shared memory (warp to warp); it moves only when a
-// unit's maximum lies more than 15 above it, which rescales the row's O.  Measured, us,
-// chunk of 2,704 tokens / four 56k caches with 64 drafted tokens: one warpgroup 278 / 344, two
-// with an O each and three places 185 / 232.
+// unit's maximum lies more than 8 above it, which rescales the row's O.
 //
 // Query blocks of one drafted tree read the same keys.  Where most sequences have as
 // many blocks, a gang of CTAs, one per block, goes through a range of keys at the same
@@ -48,6 +46,17 @@
 // again, key by key (recompute_rows): what a row does not see then has no part in it, and
 // what it sees has its due.  (Looking through V of every masked unit beforehand took 1,500
 // cycles a unit.)
+//
+// What bounds it.  Few query rows: the stream of K and V (64 rows of one token, 4.2k keys
+// each in sight, 1.07 GB in 168 us: 94 % of the copy rate).  Many: shared memory and the
+// tensor pipe, which a unit keeps busy for 840 of its 1,000 cycles (K once, V twice, the
+// loads: 80 KB at some 91 B a cycle); four 56k caches with 64 drafted tokens 222 us, tensor
+// pipe 75 % busy, a chunk of 2,704 tokens under a window of 4,096 168 us, of which a sixth at
+// the ends of pieces.  Not kept: one softmax warpgroup for all units (344 and 278 us), two
+// with an O each and three places (232 and 185), one issuer for S and P V (291 and 275), waits
+// that spin (276 and 218), five or six stages (2 to 4 % slower), rows of O written by bulk copies
+// (5 % slower), range ends moved to the ends of (item, group)s (3 % faster for the chunk, 1 %
+// slower for decoding).
 //
 // Warp roles: 0 loads K, 3 loads V, 1 issues S and owns tensor memory, 2 issues P V,
 // 4..7 and 8..11 softmax.
@@ -297,15 +306,10 @@ __device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
 
 __device__ __forceinline__ int64_t range_begin(int64_t T, int c, int P) { return T * c / P; }
 
-// Ranges of a launch of T units on P CTAs (or gangs): at least kMinUnits units each.  A
-// unit more costs a CTA 0.55 us, a part more costs the merge a wait for memory: one tree
-// of 8 tokens over 2,744 (172 units) 32 us with a unit a CTA.
-constexpr int kMinUnits = 4;
-
-__host__ __device__ __forceinline__ int ranges_of(int64_t T, int P) {
-  const int64_t most = (T + kMinUnits - 1) / kMinUnits;
-  return most < P ? max(static_cast<int>(most), 1) : P;
-}
+// Ranges of a launch of T units on P CTAs (or gangs): as many, but none empty.  (Fewer and
+// longer ones for small launches: a tree of 8 tokens over 2,744, 172 units, 16.9 us with a
+// unit a CTA, 18.5 with four; one token over 577, 36 units, 11.4 and 13.8.)
+__device__ __forceinline__ int ranges_of(int64_t T, int P) { return T < P ? max(static_cast<int>(T), 1) : P; }
 
 // Range (of P) that holds flat unit f
 __device__ __forceinline__ int range_of(int64_t f, int64_t T, int P) { return static_cast<int>(((f + 1) * P - 1) / T); }
