@@ -387,7 +387,7 @@ typedef struct {
 /* Tokens outside the pages: for sequence i of n, the last n_tokens[i] tokens of
  * its row, token t of layer l and KV head g at k + i seq_stride + l layer_stride +
  * t token_stride + g head_stride (elements, multiples of 8, not negative), d
- * contiguous elements; v the same. */
+ * contiguous elements; v the same.  (starkv_pages_load: rows that do not overlap.) */
 typedef struct {
   void* k;                   /* bf16, 16-byte aligned                                  */
   void* v;                   /* or NULL: keys only                                     */
@@ -400,7 +400,8 @@ typedef struct {
 /* Queries of the attention calls: for sequence i of n, its row's last n_tokens[i]
  * tokens, token t and head h at q + i q_seq_stride + t q_token_stride + h
  * q_head_stride (elements, multiples of 8, not negative), d contiguous elements;
- * o the same.  What belongs to t >= n_tokens[i] is neither read nor written. */
+ * o the same, apart from q and with rows that do not overlap.  What belongs to t >=
+ * n_tokens[i] is neither read nor written. */
 typedef struct {
   const void* q;             /* bf16, 16-byte aligned, post-RoPE                       */
   void* o;                   /* bf16, 16-byte aligned                                  */
@@ -442,8 +443,9 @@ starkv_status starkv_pages_free(starkv_state* st, const starkv_pages* pages, con
  * tokens, which must be its length) keeps the tokens idx and the last w, in that
  * order, in pages of its own (numbers as for extend, taken before the old pages
  * are let go; other holders of those keep them): len = B + w.  Reads idx, L,
- * budget, meta and its strides of seqs, writes meta_out where meta is given; the
- * other buffers may be NULL.  In the per-KV-head mode group g keeps idx[g]. */
+ * budget, meta and its strides of seqs (host values, fixed in a captured call), writes
+ * meta_out where meta is given; the other buffers may be NULL.  In the per-KV-head mode
+ * group g keeps idx[g].  Error (device): an index outside the past tokens keeps token 0. */
 starkv_status starkv_pages_compact(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const starkv_seq* seqs,
                                    int32_t nseq, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -1212,7 +1212,7 @@ BookParams book_params(starkv_state* st, const starkv_pages& p, const int32_t* r
   return b;
 }
 
-starkv_status validate_tokens(const starkv_state* st, int layer0, int nl, const starkv_tokens* t) {
+starkv_status validate_tokens(const starkv_state* st, bool store, int layer0, int nl, const starkv_tokens* t) {
   if (!t) return set_error(STARKV_ERR_INVALID_ARG, "tokens is NULL");
   starkv_status s = check_rows(t->n);
   if (s != STARKV_OK) return s;
@@ -1227,6 +1227,9 @@ starkv_status validate_tokens(const starkv_state* st, int layer0, int nl, const 
     return set_error(STARKV_ERR_INVALID_ARG, "tokens: rows or n_tokens not 4-byte aligned");
   for (int64_t x : {t->seq_stride, t->layer_stride, t->token_stride, t->head_stride})
     if (x < 0 || (x & 7)) return set_error(STARKV_ERR_INVALID_ARG, "tokens: strides must be multiples of 8 elements, not negative");
+  if (!store && ((t->n > 1 && t->seq_stride < kHeadDim) || (nl > 1 && t->layer_stride < kHeadDim) ||
+                 (t->T > 1 && t->token_stride < kHeadDim) || (st->cfg.n_kv_heads > 1 && t->head_stride < kHeadDim)))
+    return set_error(STARKV_ERR_INVALID_ARG, "tokens: strides let the rows that are loaded overlap");
   return STARKV_OK;
 }
 
@@ -1234,7 +1237,7 @@ starkv_status move_tokens(starkv_state* st, bool store, const starkv_pages* page
                           const starkv_tokens* t, void* stream) {
   starkv_status s = validate_pages(st, pages);
   if (s != STARKV_OK) return s;
-  if ((s = validate_tokens(st, layer0, nl, t)) != STARKV_OK) return s;
+  if ((s = validate_tokens(st, store, layer0, nl, t)) != STARKV_OK) return s;
   if ((s = check_device(st)) != STARKV_OK) return s;
   if (t->n == 0 || t->T == 0 || nl == 0) return STARKV_OK;
   TokensView v;
@@ -1271,6 +1274,7 @@ starkv_status validate_queries(const starkv_state* st, int layer, const starkv_q
   if (q->n == 0 || q->T == 0) return STARKV_OK;
   if (!q->q || !q->o || !aligned16(q->q) || !aligned16(q->o))
     return set_error(STARKV_ERR_INVALID_ARG, "queries: q or o NULL or not 16-byte aligned");
+  if (q->q == q->o) return set_error(STARKV_ERR_INVALID_ARG, "queries: q and o are the same");
   if (!aligned4(q->lse) || !aligned4(q->rows) || !aligned4(q->n_tokens))
     return set_error(STARKV_ERR_INVALID_ARG, "queries: lse, rows or n_tokens not 4-byte aligned");
   if (tree && (!q->mask || (reinterpret_cast<uintptr_t>(q->mask) & 7)))

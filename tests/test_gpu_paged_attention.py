@@ -104,6 +104,32 @@ def test_windows_and_sinks(P, n_sink, window, T):
     c.st.close()
 
 
+@pytest.mark.parametrize("heads,kv_heads,T", [(160, 1, 3), (256, 1, 1), (33, 3, 12), (32, 32, 5)])
+def test_other_head_layouts(heads, kv_heads, T):
+    """More heads of a group than a query block has rows, odd numbers of them, one of each group."""
+    c = filled([150, 77, 64], P=32, heads=heads, kv_heads=kv_heads, seed=heads)
+    qs = queries(c, 3, T)
+    sk.sink_attention(c.st, c.pages, 0, qs, 2, 100, c.ws)
+    verify(c, qs, lambda i, L, n: O.seen_sink(L, n, 2, 100), [0, 1, 2], [T] * 3)
+    c.st.close()
+
+
+def test_more_query_blocks_than_a_launch_takes():
+    """1024 rows of two blocks each go in two launches; sequences on both sides of the border."""
+    n, T = 1024, 33
+    c = filled([40 + i % 90 for i in range(n)], P=16, heads=8, kv_heads=2)
+    rows = [int(r) for r in np.random.default_rng(0).permutation(n)]
+    qs = queries(c, n, T, rows=c.ids(rows))
+    sk.sink_attention(c.st, c.pages, 0, qs, 1, 60, c.ws)
+    torch.cuda.synchronize()
+    sk.check_device_error(c.st)
+    pick = [0, 1, 510, 511, 512, 513, 1022, 1023]
+    some = sk.Queries(q=qs.q[pick], o=qs.o[pick], lse=qs.lse[pick])
+    verify(c, some, lambda i, L, m: O.seen_sink(L, m, 1, 60), [rows[i] for i in pick], [T] * len(pick))
+    assert torch.isfinite(qs.o).all() and torch.isfinite(qs.lse).all()
+    c.st.close()
+
+
 def test_a_prompt_from_its_first_token():
     """T = L: every query sees what precedes it, the first only itself."""
     c = filled([300, 131], P=32)

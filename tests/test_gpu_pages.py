@@ -392,7 +392,10 @@ def test_calls_that_do_not_fit_are_refused_on_the_host():
     q = torch.zeros((2, 3, 8, PH.D), dtype=torch.bfloat16, device="cuda")
     o = torch.zeros_like(q)
     mask = torch.ones((2, 3), dtype=torch.int64, device="cuda")
-    calls = [lambda: sk.tree_attention(st, c.pages, 2, sk.Queries(q=q, o=o, mask=mask), c.ws),
+    with pytest.raises(sk.StarkvError):       # two sequences into one place
+        sk.pages_load(st, c.pages, 0, sk.Tokens(k=k[:1].expand(2, 2, 4, 4, PH.D)))
+    calls = [lambda: sk.sink_attention(st, c.pages, 0, sk.Queries(q=q, o=q), 1, 4, c.ws),
+             lambda: sk.tree_attention(st, c.pages, 2, sk.Queries(q=q, o=o, mask=mask), c.ws),
              lambda: sk.tree_attention(st, c.pages, 0, sk.Queries(q=q, o=o), c.ws),
              lambda: sk.sink_attention(st, c.pages, 0, sk.Queries(q=q, o=o), -1, 4, c.ws),
              lambda: sk.sink_attention(st, c.pages, 0, sk.Queries(q=q, o=o), 1, -4, c.ws),
