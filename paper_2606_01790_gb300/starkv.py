@@ -538,13 +538,19 @@ def _expect(dtype: torch.dtype, *tensors: Optional[torch.Tensor]) -> None:
 
 
 def _on(pages: Pages, *tensors: Optional[torch.Tensor]) -> None:
-    """The call's tensors lie where its pages do, on the current CUDA device."""
+    """The call's tensors lie where its pages do."""
     dev = pages._device
-    if dev < 0 or dev != torch.cuda.current_device():
-        raise ValueError(f"pages on {pages.k.device}: the paged calls take tensors of the current CUDA device")
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor on {t.device}, pages on {pages.k.device}")
+
+
+def _stream_on(pages: Pages, stream) -> int:
+    """The stream of a call whose pages lie on the current CUDA device."""
+    dev = pages._device
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"pages on {pages.k.device}: the paged calls take tensors of the current CUDA device")
+    return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _ids(t: Optional[torch.Tensor], n: int, what: str) -> int:
@@ -635,8 +641,7 @@ def pages_workspace(st: State, pages: Pages, n: int, T: int = 1) -> torch.Tensor
 
 def pages_reset(st: State, pages: Pages, stream=None) -> None:
     c = _c_pages(st, pages)
-    _on(pages)
-    _check(lib().starkv_pages_reset(st.handle, c, _stream(stream)))
+    _check(lib().starkv_pages_reset(st.handle, c, _stream_on(pages, stream)))
 
 
 def pages_extend(st: State, pages: Pages, rows: Optional[torch.Tensor], n_new: torch.Tensor, ws: torch.Tensor,
@@ -645,7 +650,7 @@ def pages_extend(st: State, pages: Pages, rows: Optional[torch.Tensor], n_new: t
     c, n = _c_pages(st, pages), n_new.numel()
     _on(pages, rows, n_new, ws)
     _check(lib().starkv_pages_extend(st.handle, c, _ids(rows, n, "rows"), _ids(n_new, n, "n_new"), n,
-                                     ws.data_ptr(), ws.numel(), _stream(stream)))
+                                     ws.data_ptr(), ws.numel(), _stream_on(pages, stream)))
 
 
 def pages_fork(st: State, pages: Pages, src: torch.Tensor, dst: torch.Tensor, ws: torch.Tensor, deep: bool = False,
@@ -654,14 +659,14 @@ def pages_fork(st: State, pages: Pages, src: torch.Tensor, dst: torch.Tensor, ws
     c, n = _c_pages(st, pages), dst.numel()
     _on(pages, src, dst, ws)
     _check(lib().starkv_pages_fork(st.handle, c, _ids(src, n, "src"), _ids(dst, n, "dst"), n, int(deep),
-                                   ws.data_ptr(), ws.numel(), _stream(stream)))
+                                   ws.data_ptr(), ws.numel(), _stream_on(pages, stream)))
 
 
 def pages_free(st: State, pages: Pages, rows: torch.Tensor, stream=None) -> None:
     """Empties rows; pages that no row holds any more are free."""
     c, n = _c_pages(st, pages), rows.numel()
     _on(pages, rows)
-    _check(lib().starkv_pages_free(st.handle, c, _ids(rows, n, "rows"), n, _stream(stream)))
+    _check(lib().starkv_pages_free(st.handle, c, _ids(rows, n, "rows"), n, _stream_on(pages, stream)))
 
 
 def pages_compact(st: State, pages: Pages, rows: Optional[torch.Tensor], seqs: Sequence[Seq], ws: torch.Tensor,
@@ -670,19 +675,19 @@ def pages_compact(st: State, pages: Pages, rows: Optional[torch.Tensor], seqs: S
     c = _c_pages(st, pages)
     _on(pages, rows, ws, *(t for s in seqs for t in (s.idx, s.meta, s.meta_out)))
     _check(lib().starkv_pages_compact(st.handle, c, _ids(rows, len(seqs), "rows"), _seq_array(seqs), len(seqs),
-                                      ws.data_ptr(), ws.numel(), _stream(stream)))
+                                      ws.data_ptr(), ws.numel(), _stream_on(pages, stream)))
 
 
 def pages_store(st: State, pages: Pages, layer0: int, tokens: Tokens, stream=None) -> None:
     """``tokens`` into the last places of their rows, layers layer0, layer0 + 1, ..."""
     c, tok = _c_pages(st, pages), _c_tokens(st, pages, tokens)
-    _check(lib().starkv_pages_store(st.handle, c, layer0, tokens.k.shape[1], tok, _stream(stream)))
+    _check(lib().starkv_pages_store(st.handle, c, layer0, tokens.k.shape[1], tok, _stream_on(pages, stream)))
 
 
 def pages_load(st: State, pages: Pages, layer0: int, tokens: Tokens, stream=None) -> None:
     """The last tokens of their rows into ``tokens``."""
     c, tok = _c_pages(st, pages), _c_tokens(st, pages, tokens)
-    _check(lib().starkv_pages_load(st.handle, c, layer0, tokens.k.shape[1], tok, _stream(stream)))
+    _check(lib().starkv_pages_load(st.handle, c, layer0, tokens.k.shape[1], tok, _stream_on(pages, stream)))
 
 
 def tree_attention(st: State, pages: Pages, layer: int, queries: Queries, ws: torch.Tensor, stream=None) -> None:
@@ -690,7 +695,7 @@ def tree_attention(st: State, pages: Pages, layer: int, queries: Queries, ws: to
     c, q = _c_pages(st, pages), _c_queries(st, pages, queries)
     _on(pages, ws)
     _check(lib().starkv_tree_attention(st.handle, c, layer, q, ws.data_ptr(), ws.numel(),
-                                       _stream(stream)))
+                                       _stream_on(pages, stream)))
 
 
 def sink_attention(st: State, pages: Pages, layer: int, queries: Queries, n_sink: int, window: int, ws: torch.Tensor,
@@ -699,4 +704,4 @@ def sink_attention(st: State, pages: Pages, layer: int, queries: Queries, n_sink
     c, q = _c_pages(st, pages), _c_queries(st, pages, queries)
     _on(pages, ws)
     _check(lib().starkv_sink_attention(st.handle, c, layer, q, n_sink, window, ws.data_ptr(),
-                                       ws.numel(), _stream(stream)))
+                                       ws.numel(), _stream_on(pages, stream)))
