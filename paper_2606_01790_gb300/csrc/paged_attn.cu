@@ -983,8 +983,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
 // l, O = sum 2^(m - M) O_part / L, lse = (M + log2 L) ln 2.  Block (c, y): the one that range
 // c began, 8 / WARPS query rows from there on; the WARPS warps of a row take every
 // WARPS-th part, four at a time (their loads are in flight before the first is used), and
-// the first adds up what they found.  One warp a row where the launch has many (item,
-// group)s, so that few parts meet; four where a few of them are cut into many.
+// the first adds up what they found.  (paged_combine_launch chooses WARPS.)
 constexpr int kBatch = 4;
 
 template <int WARPS>
@@ -1089,8 +1088,12 @@ cudaError_t paged_attn_launch(const PagedAttnParams& p, cudaStream_t stream) {
 
 cudaError_t paged_combine_launch(const PagedAttnParams& p, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
-  const bool many = p.n * p.nblk * p.G * 4 >= p.grid;   // (item, group)s: about four parts of each at most
-  const int rows = std::min(kPagedRows, p.T * p.hg), per = many ? 8 : 2;
+  // one warp a row, but four where few rows meet more than 16 parts: one tree of 8 tokens (56
+  // rows, 38 parts) 16.9 us so, 19.8 with one; of 18 (126 rows) 23.3 with four, 21.5 with one; four
+  // trees of 8 (10 parts) 20.1 and 18.7; one of 60 (four blocks, 10 parts) 30.3 and 24.9
+  const int rows = std::min(kPagedRows, p.T * p.hg);
+  const bool many = p.n * p.nblk * p.G * 16 >= p.grid || rows > 64;
+  const int per = many ? 8 : 2;
   cudaLaunchConfig_t cfg = config(attr, dim3(p.grid, (rows + per - 1) / per), 256, 0, stream);
   return cudaLaunchKernelEx(&cfg, many ? k_paged_combine<1> : k_paged_combine<4>, p);
 }
