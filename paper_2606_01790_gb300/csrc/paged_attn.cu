@@ -241,9 +241,10 @@ __device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (p.tree && p.nblk > 1) {
     // A gang of B (the most blocks of a sequence) leaves CTAs idle at sequences with fewer.
-    // A unit costs about 0.55 us of a CTA's time and 0.74 us of its share of the memory's
-    // rate, so the flat order, which reads each block's keys on its own, wins where the
-    // gangs would be busy for less than three quarters of the time.
+    // The flat order leaves none idle but takes about 1.2 times as long a unit, since it reads
+    // each block's keys on its own.  Busy for all of the time, gangs took 124 us where the flat order
+    // took 143 (32 trees of 36 over 6,000), for 0.76 of it 140 and 131 (ragged, 64), for 0.71 151
+    // and 145 (ragged, 26).
     int64_t units = 0, work = 0;
     int most = 1;
     for (int seq = tid; seq < p.n; seq += kThreads) {
@@ -265,7 +266,7 @@ __device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
       atomicMax(&ctl->gang, most);
     }
     __syncthreads();
-    if (tid == 0 && (ctl->gang == 1 || 4 * ctl->sum[1] < 3 * ctl->sum[0] * ctl->gang)) ctl->gang = 1;
+    if (tid == 0 && (ctl->gang == 1 || 6 * ctl->sum[1] < 5 * ctl->sum[0] * ctl->gang)) ctl->gang = 1;
     __syncthreads();
   }
   const bool gangs = ctl->gang > 1;
