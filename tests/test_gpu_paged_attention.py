@@ -464,3 +464,60 @@ def test_values_that_are_not_finite_in_long_rows():
         for t in (1, 7, T - 1):
             PH.check_attention(o[r, t:t + 1], lse[r, t:t + 1], q[r, t:t + 1], k, v, seen[t:t + 1], what=f"{r} {t}")
     c.st.close()
+
+
+def test_a_row_twice_other_streams_and_two_graphs_on_one_workspace():
+    c = filled([700, 333], P=64)
+    T = 5
+    masks = [random_tree(np.random.default_rng(i), T) for i in range(3)]
+    rows = c.ids([0, 1, 0])
+    a = queries(c, 3, T, seed=1, rows=rows, mask=words(masks, T))
+    b = queries(c, 3, T, seed=2, rows=rows)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    sk.tree_attention(c.st, c.pages, 0, a, c.ws, stream=s)      # a stream given, and a current one
+    with torch.cuda.stream(s):
+        sk.sink_attention(c.st, c.pages, 0, b, 3, 200, c.ws)
+    s.synchronize()
+    tree, sink = (lambda i, L, n: O.seen_tree(L, n, masks[i])), (lambda i, L, n: O.seen_sink(L, n, 3, 200))
+    verify(c, a, tree, [0, 1, 0], [T] * 3)
+    verify(c, b, sink, [0, 1, 0], [T] * 3)
+    graphs = []
+    for call in (lambda: sk.tree_attention(c.st, c.pages, 0, a, c.ws), lambda: sk.sink_attention(c.st, c.pages, 0, b, 3, 200, c.ws)):
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+        graphs.append(g)
+    for step in range(6):      # in turn, on one stream
+        qs, seen = ((a, tree), (b, sink))[step % 2]
+        qs.q.copy_(torch.randn_like(qs.q))
+        qs.o.fill_(9.0)
+        graphs[step % 2].replay()
+        verify(c, qs, seen, [0, 1, 0], [T] * 3)
+    c.st.close()
+
+
+def test_offsets_past_32_bits():
+    """A row in the last pages of a pool of more than 2^32 elements gives the bits that it gives in a small one."""
+    st = PH.state(heads=28, kv_heads=4, window=1)
+    L, P = 500, 128
+    per = 4 * P * PH.D
+    big = sk.make_pages(st, (1 << 32) // per + 9, P, n_rows=1, max_pages=8)
+    small = sk.make_pages(st, 5, P, n_rows=1, max_pages=8)
+    big.refs[:-5] = 1
+    ws, n = sk.pages_workspace(st, big, 1, 3), torch.tensor([L], dtype=torch.int32, device="cuda")
+    k = torch.randn((2, 1, 1, L, 4, PH.D), device="cuda").to(torch.bfloat16)
+    out = []
+    for pages in (big, small):
+        sk.pages_extend(st, pages, None, n, ws)
+        sk.pages_store(st, pages, 0, sk.Tokens(k=k[0], v=k[1]))
+        torch.manual_seed(0)
+        q = torch.randn((1, 3, 28, PH.D), device="cuda").to(torch.bfloat16)
+        o, lse = torch.empty_like(q), torch.empty((1, 3, 28), device="cuda")
+        sk.sink_attention(st, pages, 0, sk.Queries(q=q, o=o, lse=lse), 2, 300, ws)
+        out.append((o, lse))
+    sk.check_device_error(st)
+    assert int(big.table[0, 0]) == big.refs.numel() - 5 and int(small.table[0, 0]) == 0
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+    st.close()

@@ -286,6 +286,30 @@ def test_captured_calls_replay_with_what_the_arrays_hold():
     st.close()
 
 
+def test_a_captured_compaction_replays():
+    """free, fork and compact, captured once: each replay drops the branch, branches again and compresses the branch."""
+    w, B = 8, 20
+    st = PH.state(layers=2, heads=4, kv_heads=2, window=w)
+    c = PH.Pair(st, n_pages=30, P=16, n_rows=2, max_pages=8)
+    c.extend([0], [77])
+    idx = torch.arange(0, 2 * B, 2, dtype=torch.int32, device="cuda").expand(2, 1, B).contiguous()
+    seq, src, dst = sk.Seq(L=77, budget=B, idx=idx), c.ids([0]), c.ids([1])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        sk.pages_free(st, c.pages, dst)
+        sk.pages_fork(st, c.pages, src, dst, c.ws)
+        sk.pages_compact(st, c.pages, dst, [seq], c.ws)
+    for step in range(4):
+        idx += 1          # (other tokens each time: the index is read on the device)
+        g.replay()
+        c.ref.free([1])
+        c.ref.fork([0], [1])
+        c.ref.compact([1], [77], [idx.cpu().numpy()], w)
+        c.check()
+    st.close()
+
+
 def test_offsets_past_32_bits():
     """A pool of more than 2^32 elements: its last pages are stored to, copied and read back."""
     st = PH.state(heads=4, kv_heads=4)
