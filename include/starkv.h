@@ -408,7 +408,8 @@ typedef struct {
   float* lse;                /* f32 [n][T][H] natural-log normaliser, or NULL          */
   const uint64_t* mask;      /* [n][T], tree attention only                            */
   const int32_t* rows;       /* [n] or NULL                                            */
-  const int32_t* n_tokens;   /* [n], 0 .. T, or NULL = T each                          */
+  const int32_t* n_tokens;   /* [n], 0 .. T, or NULL = T each (another count: device
+                                error, and nothing of sequence i is written)           */
   int32_t n, T;
   int64_t q_seq_stride, q_token_stride, q_head_stride;
   int64_t o_seq_stride, o_token_stride, o_head_stride;
