@@ -39,36 +39,35 @@ struct BookSmem {
   uint32_t bits[kSliceWords];   // free pages of this CTA's part
   int before[kSliceWords];      // free pages before a word, in this CTA's part
   uint32_t seen[kMaxTableRows / 32];   // rows named so far
-  int warp_sum[32];
+  int2 warp_sum[32];
   int count[kBookCtas];         // free pages of each CTA's part
   int bad;
 };
 
-// Exclusive sum over the block; every thread gets the total in *total.
-__device__ int block_scan(int v, int* warp_sum, int* total) {
+// Exclusive sums over the block of two numbers at once (x, y: their sums fit 31 bits);
+// every thread gets the totals.
+__device__ int2 block_scan(int2 v, int2* warp_sum, int2* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int inc = v;
+  int2 inc = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(kFull, inc, o);
-    if (lane >= o) inc += u;
+    const int x = __shfl_up_sync(kFull, inc.x, o), y = __shfl_up_sync(kFull, inc.y, o);
+    if (lane >= o) inc.x += x, inc.y += y;
   }
   if (lane == 31) warp_sum[warp] = inc;
   __syncthreads();
-  if (warp == 0) {
-    int s = warp_sum[lane];
+  // (every warp adds up the warps' sums for itself)
+  int2 s = warp_sum[lane];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(kFull, s, o);
-      if (lane >= o) s += u;
-    }
-    warp_sum[lane] = s;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(kFull, s.x, o), y = __shfl_up_sync(kFull, s.y, o);
+    if (lane >= o) s.x += x, s.y += y;
   }
-  __syncthreads();
-  const int base = warp ? warp_sum[warp - 1] : 0;
-  *total = warp_sum[31];
+  total->x = __shfl_sync(kFull, s.x, 31);
+  total->y = __shfl_sync(kFull, s.y, 31);
+  const int bx = __shfl_sync(kFull, s.x, max(warp - 1, 0)), by = __shfl_sync(kFull, s.y, max(warp - 1, 0));
   __syncthreads();   // warp_sum is free again
-  return base + inc - v;
+  return make_int2((warp ? bx : 0) + inc.x - v.x, (warp ? by : 0) + inc.y - v.y);
 }
 
 // Last i in [0, n) with off[i] <= a (rows that need nothing are passed over).
@@ -116,6 +115,13 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
   __syncthreads();
   griddep_launch_dependents();
   griddep_wait();
+
+  // the counts of this CTA's part of the pages; a warp's first 32 on their way already
+  const int words = (pg.n_pages + 31) >> 5;
+  const int per = (words + kBookCtas - 1) / kBookCtas;
+  const int w0 = min(rank * per, words), nw = min(per, words - w0);
+  int count0 = 1;
+  if (kTakes && warp < nw && ((w0 + warp) << 5) + lane < pg.n_pages) count0 = pg.refs[((w0 + warp) << 5) + lane];
 
   // ---- the call's rows
   const int i = tid;
@@ -172,35 +178,32 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
       need = held = 0;
     }
   }
-  int total, held_total;
-  const int off = block_scan(need, s.warp_sum, &total);
-  const int held_off = block_scan(held, s.warp_sum, &held_total);
+  int2 totals;
+  const int2 off = block_scan(make_int2(need, held), s.warp_sum, &totals);
+  const int total = totals.x, held_total = totals.y;
   if (i < p.n) {
-    s.off[i] = off;
-    s.held[i] = held_off;
+    s.off[i] = off.x;
+    s.held[i] = off.y;
   }
   __syncthreads();
   const bool bad = s.bad != 0;
 
   // ---- the free pages of this CTA's part, one bit each
-  const int words = (pg.n_pages + 31) >> 5;
-  const int per = (words + kBookCtas - 1) / kBookCtas;
-  const int w0 = min(rank * per, words), nw = min(per, words - w0);
   int mine = 0;   // free pages of the part
   if (kTakes) {
     for (int w = warp; w < nw; w += kBookThreads / 32) {
       const int page = ((w0 + w) << 5) + lane;
-      const uint32_t m = __ballot_sync(kFull, page < pg.n_pages && pg.refs[page] == 0);
+      const uint32_t m = __ballot_sync(kFull, w == warp ? count0 == 0 : page < pg.n_pages && pg.refs[page] == 0);
       if (lane == 0) s.bits[w] = m;
     }
     __syncthreads();
     int base = 0;
     for (int c = 0; c < nw; c += kBookThreads) {
       const int w = c + tid;
-      int sum;
-      const int b = block_scan(w < nw ? __popc(s.bits[w]) : 0, s.warp_sum, &sum);
-      if (w < nw) s.before[w] = base + b;
-      base += sum;
+      int2 sum;
+      const int2 b = block_scan(make_int2(w < nw ? __popc(s.bits[w]) : 0, 0), s.warp_sum, &sum);
+      if (w < nw) s.before[w] = base + b.x;
+      base += sum.x;
     }
     mine = base;
     if (tid < kBookCtas) dsmem_st_u32(dsmem_map(&s.count[rank], tid), static_cast<uint32_t>(mine));
