@@ -9,7 +9,8 @@
 // k_book: one cluster of eight 1024-thread CTAs.  Every CTA reads the call's rows
 // (at most one per thread), checks them and adds up their needs, so that all come
 // to the same verdict; its eighth of the counts becomes one bit per page.  After
-// the only exchange, the number of free pages per CTA, the a-th free page
+// the only exchange, the number of free pages per CTA (written into the peers' shared
+// memory once all of them are known to run), the a-th free page
 // (lowest number first) belongs to the a-th need: results do not depend on the
 // order in which threads run.  The call is carried out as a whole or not at all.
 //
@@ -118,6 +119,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
   const int64_t room = static_cast<int64_t>(pg.max_pages) << pg.shift;
   for (int i = tid; i < kMaxTableRows / 32; i += kBookThreads) s.seen[i] = 0;
   if (tid == 0) s.bad = 0;
+  if (kTakes) cluster_arrive();   // waited for before the first write into a peer's shared memory
   __syncthreads();
   griddep_launch_dependents();
   griddep_wait();
@@ -212,6 +214,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
       base += sum.x;
     }
     mine = base;
+    cluster_wait();   // every CTA of the cluster runs: its shared memory may be written
     if (tid < kBookCtas) dsmem_st_u32(dsmem_map(&s.count[rank], tid), static_cast<uint32_t>(mine));
   }
   if (OP == kBookCompact && !bad) {   // the gather reads the pages that the table is about to lose

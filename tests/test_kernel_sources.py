@@ -100,3 +100,14 @@ def test_the_paged_loader_sees_every_copy_land():
             found.append(depth)
         depth += line.count("{") - line.count("}")
     assert found == [0]
+
+
+def test_page_bookkeeping_writes_to_peers_only_once_all_of_them_run():
+    """A peer's shared memory may be written once that CTA is known to have started, which only a cluster barrier
+    shows: every thread arrives before the call's first reads and waits before the first such write."""
+    body = functions("pages.cu")["k_book"]
+    first = body.index("dsmem_")
+    arrive, wait = body.index("cluster_arrive();"), body.index("cluster_wait();")
+    assert arrive < body.index("griddep_wait();") < wait < first < body.index("cluster_sync();")
+    assert body.count("cluster_arrive();") == body.count("cluster_wait();") == 1
+    assert "return" not in body[arrive:wait]
