@@ -365,8 +365,12 @@ starkv_status starkv_step_host(starkv_state* st, const starkv_seq* seqs, int32_t
  * - What only the device can see is checked there, latched in the device error
  *   word (STARKV_ERR_DEVICE from starkv_check_device_error) and leaves memory
  *   intact.  extend, fork, free and compact are then not carried out at all: too
- *   few free pages, a row out of range or named twice, a length that does not fit.  A sequence of store or load that does not fit is
- *   passed over; one of the attention calls has zero outputs and lse -inf.
+ *   few free pages, a row out of range or named twice, a length that does not fit, a
+ *   page to be shared, let go or copied that is none or that no row holds.  (Counts
+ *   below the number of rows that hold a page are not those of this pool; free and
+ *   compact report them and lower none below 0.)  A sequence of store or load that
+ *   does not fit is passed over; one of the attention calls has zero outputs and lse
+ *   -inf.
  * - Supported: page_size 16, 32, 64, 128 or 256; 1 <= n_pages <= 2^20;
  *   1 <= n_rows <= 65536; max_pages * page_size <= 2^24.
  * ------------------------------------------------------------------------- */

@@ -12,12 +12,15 @@
 // the only exchange, the number of free pages per CTA (written into the peers' shared
 // memory once all of them are known to run), the a-th free page
 // (lowest number first) belongs to the a-th need: results do not depend on the
-// order in which threads run.  The call is carried out as a whole or not at all.
+// order in which threads run.  The call is carried out as a whole or not at all: the
+// pages that its rows hold are looked at, an eighth of them per CTA, before anything
+// changes, and a CTA that finds a wrong one says so in the same exchange.
 //
 // What bounds it is a chain of memory waits (row, length, table, count), two sums over
-// the block and the cluster barrier (0.7 us): 2.3 us for fork and free, 4 for extend and
-// compact, up to 300,000 pages measured.
-//
+// the block and the cluster barrier (0.7 us): 3.9 us a call of 64 rows for fork and free,
+// launches one after another (0.8 of it for looking at the held pages first).  extend and
+// compact read every count, through eight SMs: extend with its copies 4.8 us in a pool of
+// 4,096 pages, 12 in 300,000, 30 in 2^20.
 // The copies move 256-byte rows (d = 128 bf16) as k_compact does: a warp task is
 // 32 rows, whose places its lanes resolve; 16-byte accesses, eight per lane in
 // flight, past L1.  Bound by HBM: 28 layers of a 2,736-token row gathered, stored or
@@ -47,7 +50,7 @@ struct BookSmem {
   int before[kSliceWords];      // free pages before a word, in this CTA's part
   uint32_t seen[kMaxTableRows / 32];   // rows named so far
   int2 warp_sum[32];
-  int count[kBookCtas];         // free pages of each CTA's part
+  int count[kBookCtas];         // free pages of each CTA's part; -1: a page there that no row can hold
   int bad;
 };
 
@@ -119,7 +122,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
   const int64_t room = static_cast<int64_t>(pg.max_pages) << pg.shift;
   for (int i = tid; i < kMaxTableRows / 32; i += kBookThreads) s.seen[i] = 0;
   if (tid == 0) s.bad = 0;
-  if (kTakes) cluster_arrive();   // waited for before the first write into a peer's shared memory
+  cluster_arrive();   // waited for before the first write into a peer's shared memory
   __syncthreads();
   griddep_launch_dependents();
   griddep_wait();
@@ -163,8 +166,9 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
           after = L + nn;
           if (fill && nn) {
             const int last = pg.table[static_cast<int64_t>(row) * pg.max_pages + held - 1];
-            if (last < 0 || last >= pg.n_pages) bad = true;
-            else copies = pg.refs[last] > 1;   // somebody else holds it too
+            const int holders = last >= 0 && last < pg.n_pages ? pg.refs[last] : 0;
+            bad = holders < 1;      // no page, or one that nobody holds
+            copies = holders > 1;   // somebody else holds it too
           }
           need = ((after + P - 1) >> pg.shift) - held + copies;
           pos = held - copies;
@@ -196,6 +200,22 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
   __syncthreads();
   const bool bad = s.bad != 0;
 
+  // ---- the pages that the rows hold, an eighth of them per CTA: each has to be one that is held.
+  // (Looked at before anything changes; a thread's first page is kept for afterwards.)
+  constexpr bool kWalks = OP != kBookExtend;
+  const int a0 = rank * kBookThreads + tid;
+  int row0 = 0, page0 = 0;
+  bool odd = false;
+  if (kWalks && !bad)
+    for (int a = a0; a < held_total; a += kBookCtas * kBookThreads) {
+      const int r = row_of(s.held, p.n, a), j = a - s.held[r];
+      const int page = pg.table[static_cast<int64_t>(s.from[r]) * pg.max_pages + j];
+      odd = odd || page < 0 || page >= pg.n_pages || pg.refs[page] < 1;
+      if (a == a0) row0 = r, page0 = page;
+      if (OP == kBookCompact) p.old_table[static_cast<int64_t>(r) * pg.max_pages + j] = page;   // what the gather reads
+    }
+  if (kWalks) odd = __syncthreads_or(odd);
+
   // ---- the free pages of this CTA's part, one bit each
   int mine = 0;   // free pages of the part
   if (kTakes) {
@@ -214,26 +234,21 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
       base += sum.x;
     }
     mine = base;
-    cluster_wait();   // every CTA of the cluster runs: its shared memory may be written
-    if (tid < kBookCtas) dsmem_st_u32(dsmem_map(&s.count[rank], tid), static_cast<uint32_t>(mine));
   }
-  if (OP == kBookCompact && !bad) {   // the gather reads the pages that the table is about to lose
-    for (int a = rank * kBookThreads + tid; a < held_total; a += kBookCtas * kBookThreads) {
-      const int r = row_of(s.held, p.n, a), j = a - s.held[r];
-      p.old_table[static_cast<int64_t>(r) * pg.max_pages + j] = pg.table[static_cast<int64_t>(s.row[r]) * pg.max_pages + j];
-    }
-  }
+  cluster_wait();   // every CTA of the cluster runs: its shared memory may be written
+  if (tid < kBookCtas) dsmem_st_u32(dsmem_map(&s.count[rank], tid), static_cast<uint32_t>(odd ? -1 : mine));
   cluster_sync();   // from here on lengths, tables and counts change
 
   int before = 0, avail = 0;
-  if (kTakes)
-    for (int c = 0; c < kBookCtas; ++c) {
-      if (c < rank) before += s.count[c];
-      avail += s.count[c];
-    }
-  const bool ok = !bad && (!kTakes || total <= avail);
+  bool wrong = bad;
+  for (int c = 0; c < kBookCtas; ++c) {
+    wrong = wrong || s.count[c] < 0;
+    if (c < rank) before += s.count[c];
+    avail += s.count[c];
+  }
+  const bool ok = !wrong && (!kTakes || total <= avail);
   if (rank == 0 && tid == 0) {
-    if (!ok) atomicOr(p.err, bad ? kErrRow : kErrPool);
+    if (!ok) atomicOr(p.err, wrong ? kErrRow : kErrPool);
     if (p.plan) {
       p.plan->ok = ok;
       p.plan->n_copies = !ok ? 0 : OP == kBookExtend ? p.n : OP == kBookForkDeep ? total : 0;
@@ -260,9 +275,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
       }
       if (OP == kBookForkDeep) {
         const int from = pg.table[static_cast<int64_t>(s.from[r]) * pg.max_pages + j];
-        const bool good = from >= 0 && from < pg.n_pages;
-        if (!good) atomicOr(p.err, kErrRow);
-        p.copies[a] = make_int4(good ? from : -1, page, min(P, s.len[r] - (j << pg.shift)), 0);
+        p.copies[a] = make_int4(from, page, min(P, s.len[r] - (j << pg.shift)), 0);
       }
       *entry = page;
       pg.refs[page] = 1;
@@ -270,19 +283,15 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
 
   // ---- pages that change hands without moving
   if (OP == kBookFork || OP == kBookFree || OP == kBookCompact)
-    for (int a = rank * kBookThreads + tid; a < held_total; a += kBookCtas * kBookThreads) {
-      const int r = row_of(s.held, p.n, a), j = a - s.held[r];
-      const int32_t* entry = OP == kBookCompact ? p.old_table + static_cast<int64_t>(r) * pg.max_pages + j
-                                                : pg.table + static_cast<int64_t>(s.from[r]) * pg.max_pages + j;
-      const int page = *entry;
-      if (page < 0 || page >= pg.n_pages) {
-        atomicOr(p.err, kErrRow);
-        continue;
-      }
+    for (int a = a0; a < held_total; a += kBookCtas * kBookThreads) {
+      const int r = a == a0 ? row0 : row_of(s.held, p.n, a), j = a - s.held[r];
+      const int page = a == a0                ? page0
+                       : OP == kBookCompact ? p.old_table[static_cast<int64_t>(r) * pg.max_pages + j]
+                                            : pg.table[static_cast<int64_t>(s.from[r]) * pg.max_pages + j];
       if (OP == kBookFork) {
         atomicAdd(&pg.refs[page], 1);
         pg.table[static_cast<int64_t>(s.row[r]) * pg.max_pages + j] = page;
-      } else if (atomicSub(&pg.refs[page], 1) <= 0) {   // held by nobody: a table that is not this pool's
+      } else if (atomicSub(&pg.refs[page], 1) <= 0) {   // fewer holders counted than the call's rows that name it
         atomicAdd(&pg.refs[page], 1);
         atomicOr(p.err, kErrRow);
       }

@@ -442,3 +442,45 @@ def test_calls_that_do_not_fit_are_refused_on_the_host():
     sk.pages_store(st, c.pages, 0, sk.Tokens(k=k[:, :, :0]))
     c.check()
     st.close()
+
+
+ON_HELD_PAGES = {
+    "fork": lambda c, r, dst: sk.pages_fork(c.st, c.pages, c.ids([r]), c.ids([dst]), c.ws),
+    "fork deep": lambda c, r, dst: sk.pages_fork(c.st, c.pages, c.ids([r]), c.ids([dst]), c.ws, deep=True),
+    "free": lambda c, r, dst: sk.pages_free(c.st, c.pages, c.ids([r])),
+    "compact": lambda c, r, dst: sk.pages_compact(c.st, c.pages, c.ids([r]), [sk.Seq(L=int(c.ref.len[r]), budget=0)], c.ws),
+}
+
+
+@pytest.mark.parametrize("at", [0, 3, 1100, 1299])
+@pytest.mark.parametrize("what", sorted(ON_HELD_PAGES))
+def test_a_call_on_a_row_with_a_wrong_page_changes_nothing(what, at):
+    """A number that is no page, or a page that no row holds, anywhere among the pages of the call's row (the first
+    1,024 are one block's): nothing is counted, moved or branched, and the branch's row keeps what it held."""
+    st = PH.state(heads=1, kv_heads=1, window=8)
+    c = PH.Pair(st, n_pages=4000, P=16, n_rows=4, max_pages=1400)
+    c.extend([2, 0, 1], [16 * 1300, 16 * 1300 - 5, 70])
+    c.free([2])                    # its entries stay behind: pages that are free now
+    good = int(c.ref.table[0, at])
+    for bad in (-1, 4000, 1 << 30, 3999):
+        c.pages.table[0, at] = bad
+        ON_HELD_PAGES[what](c, 0, 2)
+        assert _error(st) == sk.ERR_DEVICE
+        c.ref.table[0, at] = bad
+        c.check()
+        c.pages.table[0, at] = c.ref.table[0, at] = good
+        c.check()
+    ON_HELD_PAGES[what](c, 0, 2)   # and with the right one it is carried out
+    assert _error(st) == sk.OK
+    st.close()
+
+
+def test_extending_a_row_whose_last_page_nobody_holds_changes_nothing():
+    st = PH.state(heads=4, kv_heads=1, window=8)
+    c = PH.Pair(st, n_pages=13, P=16, n_rows=2, max_pages=6)
+    c.extend([0], [40])
+    c.pages.refs[2] = c.ref.refs[2] = 0
+    sk.pages_extend(st, c.pages, c.ids([0]), c.ids([3]), c.ws)
+    assert _error(st) == sk.ERR_DEVICE
+    c.check()
+    st.close()
