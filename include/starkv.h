@@ -371,6 +371,14 @@ starkv_status starkv_step_host(starkv_state* st, const starkv_seq* seqs, int32_t
  *   compact report them and lower none below 0.)  A sequence of store or load that
  *   does not fit is passed over; one of the attention calls has zero outputs and lse
  *   -inf.
+ * - What is queued behind a refused extend, fork, free or compact counts on it.
+ *   From the refusal until starkv_check_device_error has reported it, the state's
+ *   calls that change a pool (extend, fork, free, compact, store) are held back:
+ *   they leave every byte as it is, and the pool is found as the refused call found
+ *   it.  load and the attention calls run, on the rows as they are.  (A refusal
+ *   holds back the state's other pools too, and a store that runs at that moment on
+ *   another stream may be carried out in part: pools that must not depend on one
+ *   another take a state each.  starkv_pages_reset is not held back.)
  * - Supported: page_size 16, 32, 64, 128 or 256; 1 <= n_pages <= 2^20;
  *   1 <= n_rows <= 65536; max_pages * page_size <= 2^24.
  * ------------------------------------------------------------------------- */

@@ -26,6 +26,7 @@ constexpr uint32_t kErrMeta = 2u;
 constexpr uint32_t kErrIndex = 4u;
 constexpr uint32_t kErrRow = 8u;    // a page-table row, length or page number that does not fit the call
 constexpr uint32_t kErrPool = 16u;  // not enough free pages
+constexpr uint32_t kErrHeld = 32u;  // with one of the two: a bookkeeping call was refused, calls that change a pool are held back
 
 // Token metadata word (Sec. 3.1): bit 31 visual, 20..30 frame, 10..19 row, 0..9 col.
 __host__ __device__ __forceinline__ bool meta_visual(uint32_t m) { return (m >> 31) != 0; }

@@ -14,13 +14,16 @@
 // (lowest number first) belongs to the a-th need: results do not depend on the
 // order in which threads run.  The call is carried out as a whole or not at all: the
 // pages that its rows hold are looked at, an eighth of them per CTA, before anything
-// changes, and a CTA that finds a wrong one says so in the same exchange.
+// changes, and a CTA that finds a wrong one says so in the same exchange.  A refused
+// call sets kErrHeld, which holds back every call after it that changes a pool: a store
+// queued behind an extend that found no page would write over the row's last tokens.
 //
 // What bounds it is a chain of memory waits (row, length, table, count), two sums over
-// the block and the cluster barrier (0.7 us): 3.9 us a call of 64 rows for fork and free,
+// the block and the cluster barrier (0.7 us): 4 us a call of 64 rows for fork and free,
 // launches one after another (0.8 of it for looking at the held pages first).  extend and
-// compact read every count, through eight SMs: extend with its copies 4.8 us in a pool of
+// compact read every count, through eight SMs: extend with its copies 4.9 us in a pool of
 // 4,096 pages, 12 in 300,000, 30 in 2^20.
+//
 // The copies move 256-byte rows (d = 128 bf16) as k_compact does: a warp task is
 // 32 rows, whose places its lanes resolve; 16-byte accesses, eight per lane in
 // flight, past L1.  Bound by HBM: 28 layers of a 2,736-token row gathered, stored or
@@ -50,8 +53,9 @@ struct BookSmem {
   int before[kSliceWords];      // free pages before a word, in this CTA's part
   uint32_t seen[kMaxTableRows / 32];   // rows named so far
   int2 warp_sum[32];
-  int count[kBookCtas];         // free pages of each CTA's part; -1: a page there that no row can hold
+  int count[kBookCtas];         // free pages of each CTA's part; -1: a page there that no row can hold; -2 (CTA 0): held back
   int bad;
+  uint32_t hold;   // CTA 0: held back
 };
 
 // Exclusive sums over the block of two numbers at once (x, y: their sums fit 31 bits);
@@ -134,6 +138,10 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
   int count0 = 1;
   if (kTakes && warp < nw && ((w0 + warp) << 5) + lane < pg.n_pages) count0 = pg.refs[((w0 + warp) << 5) + lane];
 
+  // An earlier call was refused and nobody has asked yet: what was queued behind it counts on it, and is not carried
+  // out either.  One CTA asks for all (a call of another pool may be refused meanwhile).
+  const uint32_t latched = rank == 0 && tid == 0 ? *p.err : 0;
+
   // ---- the call's rows
   const int i = tid;
   int need = 0, held = 0, L = 0, after = 0, fill = 0;
@@ -190,6 +198,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
       need = held = 0;
     }
   }
+  if (tid == 0) s.hold = latched & kErrHeld;
   int2 totals;
   const int2 off = block_scan(make_int2(need, held), s.warp_sum, &totals);
   const int total = totals.x, held_total = totals.y;
@@ -236,7 +245,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
     mine = base;
   }
   cluster_wait();   // every CTA of the cluster runs: its shared memory may be written
-  if (tid < kBookCtas) dsmem_st_u32(dsmem_map(&s.count[rank], tid), static_cast<uint32_t>(odd ? -1 : mine));
+  if (tid < kBookCtas) dsmem_st_u32(dsmem_map(&s.count[rank], tid), static_cast<uint32_t>(s.hold ? -2 : odd ? -1 : mine));
   cluster_sync();   // from here on lengths, tables and counts change
 
   int before = 0, avail = 0;
@@ -248,7 +257,7 @@ __global__ void __cluster_dims__(kBookCtas, 1, 1) __launch_bounds__(kBookThreads
   }
   const bool ok = !wrong && (!kTakes || total <= avail);
   if (rank == 0 && tid == 0) {
-    if (!ok) atomicOr(p.err, wrong ? kErrRow : kErrPool);
+    if (!ok && s.count[0] != -2) atomicOr(p.err, (wrong ? kErrRow : kErrPool) | kErrHeld);
     if (p.plan) {
       p.plan->ok = ok;
       p.plan->n_copies = !ok ? 0 : OP == kBookExtend ? p.n : OP == kBookForkDeep ? total : 0;
@@ -501,6 +510,7 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveBlocksPerSm)
     k_page_move(const __grid_constant__ PagesView pg, const __grid_constant__ TokensView t, uint32_t* err) {
   griddep_launch_dependents();
   griddep_wait();
+  const uint32_t latched = STORE ? *err : 0;   // (looked at when the places are known: its way is as long as theirs)
   const int lane = threadIdx.x & 31;
   const int nblk = static_cast<int>((static_cast<int64_t>(t.T) * pg.G + kTaskRows - 1) / kTaskRows);
   const int tensors = t.v ? 2 : 1;
@@ -532,6 +542,7 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveBlocksPerSm)
       if (page < 0 || page >= pg.n_pages || (STORE && pg.refs[page] != 1)) atomicOr(err, kErrRow);
       else word = page << pg.shift | (at & ((1 << pg.shift) - 1));
     }
+    if (STORE && __any_sync(kFull, latched & kErrHeld)) return;   // a call was refused: nothing is written
     __nv_bfloat16* pool = (tensor ? pg.v : pg.k) + (t.layer0 + l) * pg.layer_stride;
     __nv_bfloat16* flat = (tensor ? t.v : t.k) + seq * t.seq_stride + l * t.layer_stride;
     const int half = lane >> 4, hl = lane & 15;

@@ -484,3 +484,83 @@ def test_extending_a_row_whose_last_page_nobody_holds_changes_nothing():
     assert _error(st) == sk.ERR_DEVICE
     c.check()
     st.close()
+
+
+def test_calls_behind_a_refused_one_are_held_back_until_it_is_reported():
+    """A store queued behind an extend that found no page would write over the row's last tokens; whatever else would
+    change the pool counts on the refused call just as much."""
+    st = PH.state(layers=2, heads=4, kv_heads=2, window=8, max_seqs=2)
+    c = PH.Pair(st, n_pages=8, P=16, n_rows=4, max_pages=6)
+    other = PH.Pair(st, n_pages=8, P=16, n_rows=2, max_pages=4)
+    c.extend([0, 1], [40, 50])       # 7 of 8 pages, none shared
+    k = torch.zeros((1, 2, 30, 2, PH.D), dtype=torch.bfloat16, device="cuda")
+    tok = sk.Tokens(k=k, v=k, rows=c.ids([0]))
+    keep = torch.arange(20, dtype=torch.int32, device="cuda").expand(2, 1, 20).contiguous()
+    sk.pages_extend(st, c.pages, c.ids([0]), c.ids([30]), c.ws)       # needs two pages
+    sk.pages_store(st, c.pages, 0, tok)
+    for call in (lambda: sk.pages_extend(st, c.pages, c.ids([2]), c.ids([3]), c.ws),      # each would do by itself
+                 lambda: sk.pages_fork(st, c.pages, c.ids([0]), c.ids([2]), c.ws),
+                 lambda: sk.pages_fork(st, c.pages, c.ids([0]), c.ids([2]), c.ws, deep=True),
+                 lambda: sk.pages_compact(st, c.pages, c.ids([0]), [sk.Seq(L=40, budget=20, idx=keep)], c.ws),
+                 lambda: sk.pages_free(st, c.pages, c.ids([1])),
+                 lambda: sk.pages_extend(st, other.pages, other.ids([1]), other.ids([3]), other.ws)):
+        call()
+        sk.pages_store(st, c.pages, 1, sk.Tokens(k=k[:, :1], v=k[:, :1], rows=c.ids([1])))
+    got = torch.empty((1, 2, 40, 2, PH.D), dtype=torch.bfloat16, device="cuda")
+    sk.pages_load(st, c.pages, 0, sk.Tokens(k=got, rows=c.ids([0])))          # reading goes on
+    assert _error(st) == sk.ERR_DEVICE
+    c.check()
+    other.check()
+    for layer in range(2):
+        want = c.ref.tokens(0, layer, c.ref.k).swapaxes(0, 1)
+        np.testing.assert_array_equal(got[0, layer].view(torch.int16).cpu().numpy(), want)
+    c.free([1])                      # reported: the pool is as the refused call found it, and the call may be made again
+    c.extend([0], [30])
+    sk.pages_store(st, c.pages, 0, tok)
+    for layer in range(2):
+        for x in (c.ref.k, c.ref.v):
+            c.ref.store(0, layer, x, np.zeros((30, 2, PH.D), np.int16))
+    c.check()
+    st.close()
+
+
+def test_captured_steps_stop_where_the_pool_is_full():
+    """extend and store of a token, replayed past the last free page: the row keeps every token that it took."""
+    st = PH.state(layers=1, heads=4, kv_heads=1, window=8)
+    c = PH.Pair(st, n_pages=3, P=16, n_rows=2, max_pages=6)
+    c.extend([0], [20])
+    rows, one = c.ids([0]), c.ids([1])
+    k = torch.zeros((1, 1, 1, 1, PH.D), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        sk.pages_extend(st, c.pages, rows, one, c.ws)
+        sk.pages_store(st, c.pages, 0, sk.Tokens(k=k, v=k, rows=rows))
+    for step in range(40):
+        k.fill_(float(step + 1))
+        g.replay()
+        if int(c.ref.len[0]) < 48:
+            c.ref.extend([0], [1])
+            word = torch.tensor(float(step + 1), dtype=torch.bfloat16).view(torch.int16).item()
+            for x in (c.ref.k, c.ref.v):
+                c.ref.store(0, 0, x, np.full((1, 1, PH.D), word, np.int16))
+        c.check(errors=False)
+    assert _error(st) == sk.ERR_DEVICE
+    c.check()
+    st.close()
+
+
+def test_errors_of_a_store_hold_nothing_back():
+    st = PH.state(heads=4, kv_heads=2)
+    c = PH.Pair(st, n_pages=12, P=16, n_rows=3, max_pages=4)
+    c.extend([0], [20])
+    c.fork([0], [1])
+    k = torch.zeros((1, 1, 6, 2, PH.D), dtype=torch.bfloat16, device="cuda")
+    sk.pages_store(st, c.pages, 0, sk.Tokens(k=k, v=k, rows=c.ids([1])))      # into a shared page: passed over
+    c.extend([1], [6])
+    sk.pages_store(st, c.pages, 0, sk.Tokens(k=k, v=k, rows=c.ids([1])))
+    for x in (c.ref.k, c.ref.v):
+        c.ref.store(1, 0, x, np.zeros((6, 2, PH.D), np.int16))
+    assert _error(st) == sk.ERR_DEVICE
+    c.check()
+    st.close()
