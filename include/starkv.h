@@ -464,7 +464,8 @@ starkv_status starkv_pages_compact(starkv_state* st, const starkv_pages* pages, 
 
 /* Bit copies of tokens into the pages (store) or out of them (load), layers
  * [layer0, layer0 + n_layers).  A page that more than one row holds is not
- * written to (device error). */
+ * written to, nor is a row that two sequences of a store with tokens name (device
+ * error).  load may name a row any number of times. */
 starkv_status starkv_pages_store(starkv_state* st, const starkv_pages* pages, int32_t layer0, int32_t n_layers,
                                  const starkv_tokens* tokens, void* stream);
 starkv_status starkv_pages_load(starkv_state* st, const starkv_pages* pages, int32_t layer0, int32_t n_layers,

@@ -564,3 +564,34 @@ def test_errors_of_a_store_hold_nothing_back():
     assert _error(st) == sk.ERR_DEVICE
     c.check()
     st.close()
+
+
+@pytest.mark.parametrize("n,twins", [(3, [(0, 2)]), (40, [(3, 39), (4, 5)]), (1024, [(0, 1023), (100, 101), (300, 900)])])
+def test_a_store_that_names_a_row_twice_leaves_that_row_alone(n, twins):
+    """Two sequences' tokens for the same places, far apart in the call or next to each other: neither is written and
+    it is reported; the others are.  A sequence that brings no tokens is no rival (a padded batch), and to load a row
+    twice is nothing wrong."""
+    st = PH.state(layers=2, heads=4, kv_heads=2)
+    c = PH.Pair(st, n_pages=2 * n + 3, P=16, n_rows=n, max_pages=3)
+    c.extend(range(n), [3 + i % 20 for i in range(n)])
+    T = 3
+    rows = [int(r) for r in np.random.default_rng(n).permutation(n)]
+    k = torch.from_numpy(np.random.default_rng(1).standard_normal((2, n, 2, T, 2, PH.D), dtype=np.float32)).to(torch.bfloat16).cuda()
+    for padded in (False, True):
+        named, counts = list(rows), [T] * n
+        for a, b in twins:
+            named[b] = named[a]
+            counts[b] = 0 if padded else T
+        sk.pages_store(st, c.pages, 0, sk.Tokens(k=k[0], v=k[1], rows=c.ids(named), n_tokens=c.ids(counts)))
+        assert _error(st) == (sk.OK if padded else sk.ERR_DEVICE)
+        lone = [i for i in range(n) if counts[i] and (padded or named.count(named[i]) == 1)]
+        for i in lone:
+            for layer in range(2):
+                for x, part in ((c.ref.k, k[0]), (c.ref.v, k[1])):
+                    c.ref.store(named[i], layer, x, part[i, layer].view(torch.int16).cpu().numpy())
+        c.check()
+        k = k.flip(0)
+    back = torch.empty((2, 2, T, 2, PH.D), dtype=torch.bfloat16, device="cuda")
+    sk.pages_load(st, c.pages, 0, sk.Tokens(k=back, rows=c.ids([rows[1], rows[1]])))
+    assert _error(st) == sk.OK and torch.equal(back[0], back[1])
+    st.close()
