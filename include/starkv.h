@@ -478,7 +478,8 @@ starkv_status starkv_pages_load(starkv_state* st, const starkv_pages* pages, int
  * not looked at).  With z_j = q . K[g(h), j] / sqrt(d) over the keys seen,
  *   o = sum_j softmax_j(z) V[g(h), j],   lse = log sum_j exp(z_j);
  * a query that sees none has o = 0 and lse = -inf.  K and V that a query does not
- * see do not reach its output, whatever they hold. */
+ * see do not reach its output, whatever they hold (V that is not finite and is
+ * seen by some queries only costs time: their rows are taken again key by key). */
 starkv_status starkv_tree_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
                                     void* workspace, size_t workspace_bytes, void* stream);
 
@@ -497,7 +498,8 @@ starkv_status starkv_check_device_error(starkv_state* st, void* stream);
  * kernels (default 1e9).  A wait that runs out stops its kernel early and
  * latches STARKV_ERR_TIMEOUT in the device error word; before it exits or
  * releases tensor memory the kernel still waits for the copies and MMAs it
- * has already issued, for max(limit, 2 s). */
+ * has already issued, for max(limit, 2 s).  (The paged attention's waits for rows
+ * that are taken key by key, see there, count from those rows' last unit of 64 keys.) */
 starkv_status starkv_set_wait_limit(starkv_state* st, uint64_t limit_ns);
 
 /* Self-test of the failure path that every bounded device wait shares: one

@@ -106,6 +106,7 @@ struct Ctl {
   uint64_t drain;
   uint32_t tmem_base;
   volatile int abort;
+  volatile int beat;                // grows while rows are taken key by key
   int warp_sum[kThreads / 32];
   int items;                        // of the launch: sequences in gangs, else query blocks
   int gang;                         // CTAs of a gang (1: none)
@@ -135,11 +136,17 @@ __device__ __forceinline__ void fail(Ctl* ctl, uint32_t* err) {
 // A wait of a warp-wide role: true when every lane's barrier completed and, where that
 // took time, no role had failed.  The one place where these roles learn of a failure, so
 // that a warp's lanes leave together: a barrier that a failed role should have
-// completed does not complete.
+// completed does not complete.  The limit counts from the last sign of life of rows that are
+// taken key by key (recompute_rows): these may take long, but come to an end.
 __device__ __forceinline__ bool warp_wait(const Ctl* ctl, uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
   if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
-  const bool aborted = ctl->abort;
-  return __all_sync(kFull, mbar_wait(bar, parity, limit_ns) && !aborted);
+  while (true) {
+    const bool aborted = ctl->abort;
+    const int beat = ctl->beat;
+    const bool there = mbar_wait(bar, parity, limit_ns);
+    if (__all_sync(kFull, there && !aborted)) return true;
+    if (!__all_sync(kFull, !aborted) || !__any_sync(kFull, ctl->beat != beat)) return false;
+  }
 }
 
 // Two of them, at the price of one where both are complete.  They may be looked at in
@@ -684,8 +691,9 @@ __device__ __forceinline__ float4 bf16x4(const __nv_bfloat16* p) {
 // Columns col .. col + 63 of the staged rows `which` (bits) of a warp's 32, from row r0 of
 // the block on, over the piece's keys: by the whole warp, one row and one key at a
 // time, skipping the keys that the row does not see.  Against the reference `top` of the
-// row (lane i: row i), times `norm` (the same).
-__device__ __noinline__ void recompute_rows(const PagedAttnParams& p, const Block& blk, int g, int j0, int n, int r0, int col, uint32_t which,
+// row (lane i: row i), times `norm` (the same).  Some microseconds a row and 64 keys, so that
+// every unit is a sign of life for the roles that wait.
+__device__ __noinline__ void recompute_rows(const PagedAttnParams& p, Ctl* ctl, const Block& blk, int g, int j0, int n, int r0, int col, uint32_t which,
                                             float top, float norm, float* stage) {
   const int lane = threadIdx.x & 31;
   const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
@@ -699,6 +707,7 @@ __device__ __noinline__ void recompute_rows(const PagedAttnParams& p, const Bloc
     float2 acc = make_float2(0.f, 0.f);
     for (int j = j0; j < j0 + n; ++j) {
       const int k0 = blk.key(j);
+      if (lane == 0) atomicAdd(const_cast<int*>(&ctl->beat), 1);
       for (uint64_t bits = see(k0); bits;) {
         float4 k[8];   // eight keys' loads at once: their latency is most of this path's time
         float2 v[8];
@@ -859,7 +868,7 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
 #pragma unroll
         for (int i = 0; i < 32; ++i) sum += __uint_as_float(a[0][i]) * 0.f + __uint_as_float(a[1][i]) * 0.f;   // 0, or NaN
         const uint32_t which = __ballot_sync(kFull, live && sum != 0.f);
-        if (which) recompute_rows(p, blk, c.g, c.j0, c.n, quad * 32, 64 * line, which, ref, norm, stage_o);
+        if (which) recompute_rows(p, ctl, blk, c.g, c.j0, c.n, quad * 32, 64 * line, which, ref, norm, stage_o);
       }
       __syncwarp();
       const int rows = min(32, blk.nrows - quad * 32);
@@ -922,7 +931,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
     mbar_init(&ctl->ml_full, kSoftWarps);
     mbar_init(&ctl->o_empty, kSoftWarps);
     mbar_init(&ctl->drain, 2);   // one commit per MMA issuer
-    ctl->abort = 0;
+    ctl->abort = ctl->beat = 0;
     ctl->gang = 1;
     ctl->sum[0] = ctl->sum[1] = 0;
     fence_mbar_init();

@@ -521,3 +521,30 @@ def test_offsets_past_32_bits():
     assert int(big.table[0, 0]) == big.refs.numel() - 5 and int(small.table[0, 0]) == 0
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
     st.close()
+
+
+def test_rows_taken_key_by_key_run_into_no_wait_limit():
+    """A value that is not finite before the first query's window in rows that are one piece each (as many rows as fill
+    the GPU): the other queries' rows are taken again key by key, for longer than the wait limit, and the short rows
+    that come after them in the same ranges are there too."""
+    T, W, n = 18, 5900, 44
+    lens = [6000 if i % 11 < 10 else 70 for i in range(n)]
+    c = filled(lens, P=64, seed=2)
+    clean = {r: c.cache(r, 0) for r in (0, 9, 10, 43)}
+    for r in range(n):
+        if lens[r] == 6000:
+            j = 6000 - T - W + 1
+            c.pages.v[0, int(c.ref.table[r, j // 64]), :, j % 64] = float("nan")
+    sk.set_wait_limit(c.st, 2_000_000)
+    qs = queries(c, n, T, seed=1)
+    sk.sink_attention(c.st, c.pages, 0, qs, 2, W, c.ws)
+    torch.cuda.synchronize()
+    sk.check_device_error(c.st)
+    o, lse, q = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy(), qs.q.float().cpu().numpy()
+    for r in range(n):
+        assert np.isnan(o[r, 0]).all() == (lens[r] == 6000) and np.isfinite(o[r, 1:]).all(), r
+    for r, (k, v) in clean.items():
+        seen = O.seen_sink(k.shape[1], T, 2, W)
+        for t in (1, T - 1):
+            PH.check_attention(o[r, t:t + 1], lse[r, t:t + 1], q[r, t:t + 1], k, v, seen[t:t + 1], what=f"{r} {t}")
+    c.st.close()
