@@ -44,7 +44,8 @@
 // slots behind the last token, which may hold anything, are zeroed in shared memory, and a
 // piece with masked units whose O has elements that are not finite takes those rows
 // again, key by key (recompute_rows): what a row does not see then has no part in it, and
-// what it sees has its due.  (Looking through V of every masked unit beforehand took 1,500
+// what it sees has its due.  In a piece without masked units such a column is settled by its
+// V alone (settle_columns).  (Looking through V of every masked unit beforehand took 1,500
 // cycles a unit.)
 //
 // What bounds it.  Few query rows: the stream of K and V (64 rows of one token, 4.2k keys
@@ -81,6 +82,7 @@ constexpr uint32_t kFull = 0xffffffffu;
 constexpr float kSumLimit = 16384.f;               // largest sum of a unit's 64 weights against a row's reference ...
 constexpr float kMoveThreshold = 8.f;              // ... a larger one holds a weight above 2^8
 constexpr uint64_t kDrainWaitNs = 2000000000ull;
+constexpr float kLeast = 1e-45f;                  // (2^-149)
 constexpr uint64_t kAll = ~uint64_t(0);
 
 // Tensor memory, in columns: O 128, S or P 5 x 64 (P: 32 hi, 32 lo), Q 64.
@@ -688,6 +690,49 @@ __device__ __forceinline__ float4 bf16x4(const __nv_bfloat16* p) {
                      __uint_as_float(w.y & 0xFFFF0000u));
 }
 
+__device__ __forceinline__ bool is_inf(float x) { return fabsf(x) == INFINITY; }
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
+
+// w x for a weight w >= 0 that stands for one above 0, however small
+__device__ __forceinline__ float weighted(float w, float x) { return is_inf(x) ? x : w * x; }
+
+// A piece that every row sees whole, where O has elements that are not finite: every weight is above 0,
+// so that a column with a V of infinity comes to infinity, with both or a NaN to NaN, whatever the weights
+// (products of their parts say otherwise where a part is 0: 0 * infinity).  Columns col .. col + 63 of the
+// staged rows `which`, by the whole warp, each lane two columns over all keys.
+__device__ __noinline__ void settle_columns(const PagedAttnParams& p, Ctl* ctl, const Block& blk, int g, int j0, int n, int col, uint32_t which,
+                                            float* stage) {
+  const int lane = threadIdx.x & 31;
+  const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
+  const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
+  float2 sum = make_float2(0.f, 0.f);   // of the column's infinities and NaNs: 0 where it has none
+  for (int j = j0; j < j0 + n; ++j) {
+    const int k0 = blk.key(j);
+    if (lane == 0) atomicAdd(const_cast<int*>(&ctl->beat), 1);
+#pragma unroll 1
+    for (int k1 = k0; k1 < k0 + kPagedUnitKeys; k1 += 16) {
+      const int page = entries[k1 >> p.shift];   // (a page has 16 slots or more)
+      if (page < 0 || page >= p.n_pages) continue;
+      const __nv_bfloat16* v =
+          p.v + page * p.page_stride + ((static_cast<int64_t>(g) << p.shift) + (k1 & ((1 << p.shift) - 1))) * kHeadDim + col + 2 * lane;
+      uint32_t w[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) w[u] = *reinterpret_cast<const uint32_t*>(v + u * kHeadDim);
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        const float x = __uint_as_float(w[u] << 16), y = __uint_as_float(w[u] & 0xFFFF0000u);
+        sum.x += is_finite(x) ? 0.f : x;
+        sum.y += is_finite(y) ? 0.f : y;
+      }
+    }
+  }
+  for (; which; which &= which - 1) {
+    float2* o = &reinterpret_cast<float2*>(staged(stage, __ffs(which) - 1, lane >> 1))[lane & 1];
+    if (sum.x != 0.f) o->x = sum.x;
+    if (sum.y != 0.f) o->y = sum.y;
+  }
+}
+
 // Columns col .. col + 63 of the staged rows `which` (bits) of a warp's 32, from row r0 of
 // the block on, over the piece's keys: by the whole warp, one row and one key at a
 // time, skipping the keys that the row does not see.  Against the reference `top` of the
@@ -733,7 +778,8 @@ __device__ __noinline__ void recompute_rows(const PagedAttnParams& p, Ctl* ctl, 
 #pragma unroll
           for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
           const float e = exp2f(z * p.scale2 - ref);
-          if (any[u]) acc = make_float2(acc.x + e * v[u].x, acc.y + e * v[u].y);
+          const float some = z > -INFINITY ? fmaxf(e, kLeast) : e;   // (a weight is 0 in fp32 only)
+          if (any[u]) acc = make_float2(acc.x + (is_inf(v[u].x) ? some : e) * v[u].x, acc.y + (is_inf(v[u].y) ? some : e) * v[u].y);
         }
       }
     }
@@ -863,12 +909,20 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
         *staged(stage_o, lane, i) = make_float4(__uint_as_float(x[0]) * norm, __uint_as_float(x[1]) * norm, __uint_as_float(x[2]) * norm,
                                                 __uint_as_float(x[3]) * norm);
       }
-      if (ctl->masked[pc & 1][0] | ctl->masked[pc & 1][1]) {   // (else every row sees every key)
-        float sum = 0.f;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};   // 0, or NaN where O is not finite
 #pragma unroll
-        for (int i = 0; i < 32; ++i) sum += __uint_as_float(a[0][i]) * 0.f + __uint_as_float(a[1][i]) * 0.f;   // 0, or NaN
-        const uint32_t which = __ballot_sync(kFull, live && sum != 0.f);
-        if (which) recompute_rows(p, ctl, blk, c.g, c.j0, c.n, quad * 32, 64 * line, which, ref, norm, stage_o);
+      for (int i = 0; i < 32; ++i) {
+        sum[i & 1] = fmaf(__uint_as_float(a[0][i]), 0.f, sum[i & 1]);
+        sum[2 + (i & 1)] = fmaf(__uint_as_float(a[1][i]), 0.f, sum[2 + (i & 1)]);
+      }
+      // (a logit that is NaN or infinite has all of its row's columns NaN already)
+      const uint32_t which = __ballot_sync(kFull, live && (sum[0] + sum[1]) + (sum[2] + sum[3]) != 0.f && L == L && M < INFINITY);
+      if (which) {
+        __syncwarp();   // (rows of other lanes)
+        if (ctl->masked[pc & 1][0] | ctl->masked[pc & 1][1])
+          recompute_rows(p, ctl, blk, c.g, c.j0, c.n, quad * 32, 64 * line, which, ref, norm, stage_o);
+        else
+          settle_columns(p, ctl, blk, c.g, c.j0, c.n, 64 * line, which, stage_o);
       }
       __syncwarp();
       const int rows = min(32, blk.nrows - quad * 32);
@@ -996,6 +1050,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
 // the first adds up what they found.  (paged_combine_launch chooses WARPS.)
 constexpr int kBatch = 4;
 
+__device__ __forceinline__ float4 scaled(float w, const float4& o) {
+  return make_float4(weighted(w, o.x), weighted(w, o.y), weighted(w, o.z), weighted(w, o.w));
+}
+__device__ __forceinline__ float4 sum_of(const float4& a, const float4& b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+
 template <int WARPS>
 __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ PagedAttnParams p) {
   __shared__ float2 s_ml[8];
@@ -1030,12 +1089,12 @@ __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ P
     const float ref = top == -INFINITY ? 0.f : top, keep = exp2f(M - ref);
     M = top;
     L *= keep;
-    acc = make_float4(acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep);
+    acc = scaled(keep, acc);
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const float w = exp2f(ml[k].x - ref);
       L += w * ml[k].y;
-      acc = make_float4(acc.x + w * o[k].x, acc.y + w * o[k].y, acc.z + w * o[k].z, acc.w + w * o[k].w);
+      acc = sum_of(acc, scaled(w, o[k]));
     }
   }
   if (WARPS > 1) {
@@ -1049,13 +1108,12 @@ __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ P
     const float ref = top == -INFINITY ? 0.f : top, keep = exp2f(M - ref);
     M = top;
     L *= keep;
-    acc = make_float4(acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep);
+    acc = scaled(keep, acc);
 #pragma unroll
     for (int k = 1; k < WARPS; ++k) {
       const float w = exp2f(s_ml[warp + k].x - ref);
-      const float4 o = s_o[warp + k][lane];
       L += w * s_ml[warp + k].y;
-      acc = make_float4(acc.x + w * o.x, acc.y + w * o.y, acc.z + w * o.z, acc.w + w * o.w);
+      acc = sum_of(acc, scaled(w, s_o[warp + k][lane]));
     }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;

@@ -548,3 +548,48 @@ def test_rows_taken_key_by_key_run_into_no_wait_limit():
         for t in (1, T - 1):
             PH.check_attention(o[r, t:t + 1], lse[r, t:t + 1], q[r, t:t + 1], k, v, seen[t:t + 1], what=f"{r} {t}")
     c.st.close()
+
+
+def same_where_not_finite(o, lse, q, k, v, clean, seen, what):
+    """The NaNs and infinities of the definition, and elsewhere what the clean values give (an infinite V of a key does
+    nothing to its other columns, nor to lse)."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        want, _ = O.attention(q, k, v, seen)
+    for kind in (np.isnan, np.isposinf, np.isneginf):
+        np.testing.assert_array_equal(kind(o), kind(want), err_msg=f"{what} {kind.__name__}")
+    rest, _ = O.attention(q, k, clean, seen)
+    PH.check_attention(np.where(np.isfinite(want), o, rest), lse, q, k, clean, seen, what=what)
+
+
+@pytest.mark.parametrize("scale", [1.0, 40.0])
+@pytest.mark.parametrize("n,L,T,window", [(1, 1500, 1, 1 << 20), (1, 1500, 6, 900), (45, 700, 3, 1 << 20), (45, 700, 2, 300), (1, 9000, 19, 1 << 20)])
+def test_seen_values_of_infinity(n, L, T, window, scale):
+    """A V of infinity gives infinity in its column to every query that sees it, however its row is cut into pieces and
+    whether every query sees all of a piece or not: at a row's largest weight (exactly 1, one part of it 0), at
+    weights that are 0 in fp32 (logits of some hundreds), and NaN where both infinities meet."""
+    c = filled([L] * n, P=64, seed=L)
+    qs = queries(c, n, T, seed=3, scale=scale)
+    pick = [0, n - 1] if n > 1 else [0]
+    q = qs.q.float().cpu().numpy()
+    clean = {r: c.cache(r, 0) for r in pick}
+    for r in pick:
+        k = clean[r][0]
+        put = []
+        for h, col, x in ((0, 17, np.inf), (8, 64, -np.inf), (27, 127, np.inf), (20, 3, np.nan)):
+            z = k[h // 7] @ q[r, T - 1, h]
+            z[:max(0, L - T - window + 1)] = -np.inf       # of the keys that every query sees
+            put.append((int(z.argmax()), h // 7, col, x))
+        put += [(L - T - 5, 0, 90, np.inf), (L - T - 70, 0, 90, -np.inf), (L - T - 100, 1, 40, -np.inf), (L - 1, 2, 0, np.inf)]
+        for j, g, col, x in put:
+            c.pages.v[0, int(c.ref.table[r, j // 64]), g, j % 64, col] = float(x)
+    c.ref.v = c.pages.v.view(torch.int16).cpu().numpy()
+    sk.sink_attention(c.st, c.pages, 0, qs, 0, window, c.ws)
+    torch.cuda.synchronize()
+    sk.check_device_error(c.st)
+    o, lse = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy()
+    for r in pick:
+        k, v = c.cache(r, 0)
+        at = range(T) if T < 7 else (0, T - 1)
+        for t in at:
+            same_where_not_finite(o[r, t:t + 1], lse[r, t:t + 1], q[r, t:t + 1], k, v, clean[r][1], O.seen_sink(L, T, 0, window)[t:t + 1], f"{r} {t}")
+    c.st.close()
