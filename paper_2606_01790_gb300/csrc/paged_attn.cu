@@ -787,6 +787,36 @@ __device__ __noinline__ void recompute_rows(const PagedAttnParams& p, Ctl* ctl, 
   }
 }
 
+// Rows `which` of a warp's 32 (from row r0 of the block on), whose largest logit is +inf: those with a logit
+// that is NaN among the piece's keys, as bits.  (Their sums are NaN either way: inf - inf.)
+__device__ __noinline__ uint32_t rows_with_nan(const PagedAttnParams& p, Ctl* ctl, const Block& blk, int g, int j0, int n, int r0, uint32_t which) {
+  const int lane = threadIdx.x & 31;
+  const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
+  const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
+  uint32_t found = 0;
+  for (; which; which &= which - 1) {
+    const int i = __ffs(which) - 1;
+    const int t = quotient(blk.row0 + r0 + i, p.inv_hg), h = g * p.hg + blk.row0 + r0 + i - t * p.hg;
+    const Seen see = blk.row(p, blk.L - blk.n + t, p.tree ? p.mask[static_cast<int64_t>(blk.seq) * p.T + t] : 0);
+    const float4 q = bf16x4(p.q + blk.seq * p.q_seq + t * p.q_token + h * p.q_head + 4 * lane);
+    for (int j = j0; j < j0 + n; ++j) {
+      const int k0 = blk.key(j);
+      if (lane == 0) atomicAdd(const_cast<int*>(&ctl->beat), 1);
+      for (uint64_t bits = see(k0); bits; bits &= bits - 1) {
+        const int key = k0 + __ffsll(static_cast<long long>(bits)) - 1;
+        const int page = entries[key >> p.shift];
+        if (page < 0 || page >= p.n_pages) continue;
+        const float4 k = bf16x4(p.k + page * p.page_stride + ((static_cast<int64_t>(g) << p.shift) + (key & ((1 << p.shift) - 1))) * kHeadDim + 4 * lane);
+        float z = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
+        if (z != z) found |= 1u << i;
+      }
+    }
+  }
+  return found;
+}
+
 // Softmax warps of a line (0: even units, 1: odd): one thread per query row (TMEM lane
 // quad * 32 + lane).
 __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, float* stage_o, uint32_t tmem, int line, int quad, int lane,
@@ -897,7 +927,12 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
       const bool whole = c.whole();
       const float2 other = ctl->ml[pc & 1][line ^ 1][r];
       const float M = fmaxf(m, other.x), ref = M == -INFINITY ? 0.f : M;   // (the last reference is the largest)
-      const float L = exp2f(m - ref) * l + exp2f(other.x - ref) * other.y;
+      float L = exp2f(m - ref) * l + exp2f(other.x - ref) * other.y;
+      const uint32_t infinite = __ballot_sync(kFull, live && M == INFINITY);
+      if (infinite) {
+        const uint32_t nan = rows_with_nan(p, ctl, blk, c.g, c.j0, c.n, quad * 32, infinite);
+        if (M == INFINITY) L = nan >> lane & 1 ? NAN : 1.f;   // lse is +inf (and every column NaN)
+      }
       const float norm = !whole ? 1.f : L == 0.f ? 0.f : 1.f / L;
       const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (c.j0 == 0);
       // this line's half of the columns by way of shared memory, for rows that are written whole
@@ -1050,6 +1085,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constan
 // the first adds up what they found.  (paged_combine_launch chooses WARPS.)
 constexpr int kBatch = 4;
 
+// 2^(m - ref) for m <= ref, also where both are infinite
+__device__ __forceinline__ float decay(float m, float ref) { return m == ref ? 1.f : exp2f(m - ref); }
+
 __device__ __forceinline__ float4 scaled(float w, const float4& o) {
   return make_float4(weighted(w, o.x), weighted(w, o.y), weighted(w, o.z), weighted(w, o.w));
 }
@@ -1086,13 +1124,13 @@ __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ P
     float top = M;
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) top = fmaxf(top, ml[k].x);
-    const float ref = top == -INFINITY ? 0.f : top, keep = exp2f(M - ref);
+    const float ref = top == -INFINITY ? 0.f : top, keep = decay(M, ref);
     M = top;
     L *= keep;
     acc = scaled(keep, acc);
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const float w = exp2f(ml[k].x - ref);
+      const float w = decay(ml[k].x, ref);
       L += w * ml[k].y;
       acc = sum_of(acc, scaled(w, o[k]));
     }
@@ -1105,13 +1143,13 @@ __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ P
     float top = M;
 #pragma unroll
     for (int k = 1; k < WARPS; ++k) top = fmaxf(top, s_ml[warp + k].x);
-    const float ref = top == -INFINITY ? 0.f : top, keep = exp2f(M - ref);
+    const float ref = top == -INFINITY ? 0.f : top, keep = decay(M, ref);
     M = top;
     L *= keep;
     acc = scaled(keep, acc);
 #pragma unroll
     for (int k = 1; k < WARPS; ++k) {
-      const float w = exp2f(s_ml[warp + k].x - ref);
+      const float w = decay(s_ml[warp + k].x, ref);
       L += w * s_ml[warp + k].y;
       acc = sum_of(acc, scaled(w, s_o[warp + k][lane]));
     }

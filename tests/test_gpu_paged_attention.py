@@ -593,3 +593,41 @@ def test_seen_values_of_infinity(n, L, T, window, scale):
         for t in at:
             same_where_not_finite(o[r, t:t + 1], lse[r, t:t + 1], q[r, t:t + 1], k, v, clean[r][1], O.seen_sink(L, T, 0, window)[t:t + 1], f"{r} {t}")
     c.st.close()
+
+
+@pytest.mark.parametrize("n,L,T,window", [(1, 1500, 1, 1 << 20), (1, 1500, 6, 900), (45, 700, 3, 1 << 20), (45, 700, 2, 300), (1, 9000, 19, 1 << 20)])
+def test_logits_of_infinity(n, L, T, window):
+    """K with an infinite element gives logits of +inf to some heads and -inf to the others: lse is +inf and o NaN
+    where a logit is +inf, unless one is NaN (lse NaN); a logit of -inf is a weight of 0."""
+    c = filled([L] * n, P=64, seed=L)
+    qs = queries(c, n, T, seed=4)
+    pick = [0, n - 1] if n > 1 else [0]
+    for r, at in zip(pick, ((L - T - 5, L - T - 150, L - 1), (L - T - 290,))):
+        for i, j in enumerate(at):
+            c.pages.k[0, int(c.ref.table[r, j // 64]), i % 4, j % 64, 7 + i] = float("inf")
+    j = L - T - 100
+    c.pages.k[0, int(c.ref.table[pick[-1], j // 64]), :2, j % 64, 99] = float("nan")
+    c.ref.k = c.pages.k.view(torch.int16).cpu().numpy()
+    sk.sink_attention(c.st, c.pages, 0, qs, 0, window, c.ws)
+    torch.cuda.synchronize()
+    sk.check_device_error(c.st)
+    o, lse, q = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy(), qs.q.float().cpu().numpy()
+    met = set()
+    for r in pick:
+        k, v = c.cache(r, 0)
+        seen = O.seen_sink(L, T, 0, window)
+        for t in range(T) if T < 7 else (0, T - 1):
+            for h in range(28):
+                z = k[h // 7, seen[t]] @ q[r, t, h]
+                if np.isnan(z).any() or np.isposinf(z).any():
+                    met.add("nan" if np.isnan(z).any() else "inf")
+                    assert np.isnan(o[r, t, h]).all() and (np.isnan(lse[r, t, h]) if np.isnan(z).any() else np.isposinf(lse[r, t, h])), (r, t, h)
+                    continue
+                met.add("-inf" if np.isneginf(z).any() else "finite")
+                see = seen[t:t + 1].copy()
+                see[0, np.flatnonzero(seen[t])[np.isneginf(z)]] = False
+                kk = np.where(np.isfinite(k), k, 0)
+                g = slice(h // 7, h // 7 + 1)
+                PH.check_attention(o[r, t:t + 1, h:h + 1], lse[r, t:t + 1, h:h + 1], q[r, t:t + 1, h:h + 1], kk[g], v[g], see, what=f"{r} {t} {h}")
+    assert {"inf", "nan", "-inf", "finite"} <= met
+    c.st.close()
