@@ -184,6 +184,7 @@ struct Seen {
   uint64_t bits;
   // all of the keys k0 .. k0 + 63 (apart from drafted tokens)
   __device__ __forceinline__ bool whole(int k0) const { return k0 + 64 <= first || (k0 >= lo && k0 + 64 <= hi); }
+  __device__ __forceinline__ bool none() const { return first <= 0 && hi <= lo && !bits; }
   // of the keys k0 .. k0 + 63
   __device__ __forceinline__ uint64_t operator()(int k0) const {
     return below(first - k0) | (below(hi - k0) & ~below(lo - k0)) | (bits ? shifted(bits, ctx - k0) : 0);
@@ -933,7 +934,7 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
         const uint32_t nan = rows_with_nan(p, ctl, blk, c.g, c.j0, c.n, quad * 32, infinite);
         if (M == INFINITY) L = nan >> lane & 1 ? NAN : 1.f;   // lse is +inf (and every column NaN)
       }
-      const float norm = !whole ? 1.f : L == 0.f ? 0.f : 1.f / L;
+      const float norm = !whole ? 1.f : L != 0.f ? 1.f / L : see.none() ? 0.f : NAN;   // (0 / 0 where every logit is -inf)
       const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (c.j0 == 0);
       // this line's half of the columns by way of shared memory, for rows that are written whole
       uint32_t a[2][32];
@@ -1154,8 +1155,12 @@ __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ P
       acc = sum_of(acc, scaled(w, s_o[warp + k][lane]));
     }
   }
-  const float inv = L == 0.f ? 0.f : 1.f / L;
   const int t = quotient(s.row0 + r, p.inv_hg), h = s.g * p.hg + s.row0 + r - t * p.hg;
+  float inv = 1.f / L;
+  if (L == 0.f) {   // no key seen, or every logit -inf
+    const Block blk(p, read_item(p, s.seq), s.seq, s.row0 / kPagedRows);
+    inv = blk.row(p, blk.L - blk.n + t, p.tree ? p.mask[static_cast<int64_t>(s.seq) * p.T + t] : 0).none() ? 0.f : NAN;
+  }
   const __nv_bfloat162 x[2] = {__floats2bfloat162_rn(acc.x * inv, acc.y * inv), __floats2bfloat162_rn(acc.z * inv, acc.w * inv)};
   *reinterpret_cast<uint2*>(p.o + s.seq * p.o_seq + t * p.o_token + h * p.o_head + lane * 4) = *reinterpret_cast<const uint2*>(x);
   if (p.lse && lane == 0)

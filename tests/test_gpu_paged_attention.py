@@ -631,3 +631,29 @@ def test_logits_of_infinity(n, L, T, window):
                 PH.check_attention(o[r, t:t + 1, h:h + 1], lse[r, t:t + 1, h:h + 1], q[r, t:t + 1, h:h + 1], kk[g], v[g], see, what=f"{r} {t} {h}")
     assert {"inf", "nan", "-inf", "finite"} <= met
     c.st.close()
+
+
+@pytest.mark.parametrize("n,L,T", [(1, 1500, 1), (1, 1500, 9), (45, 300, 3)])
+def test_logits_that_are_all_minus_infinity(n, L, T):
+    """o is 0 / 0 and lse -inf where a query sees keys and every logit is -inf; o is 0 where it sees none."""
+    c = filled([L] * n, P=64, seed=L)
+    qs = queries(c, n, T, seed=5)
+    c.pages.k[0, :, 2, :, 31] = float("-inf")
+    q = qs.q.float().cpu().numpy()
+    for n_sink, window in ((0, 1 << 20), (3, 150), (0, 0)):
+        sk.sink_attention(c.st, c.pages, 0, qs, n_sink, window, c.ws)
+        torch.cuda.synchronize()
+        sk.check_device_error(c.st)
+        o, lse = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy()
+        for r in range(n):
+            for t in range(T):
+                for h in range(14, 21):
+                    if window and q[r, t, h, 31] > 0:
+                        assert np.isnan(o[r, t, h]).all() and np.isneginf(lse[r, t, h]), (r, t, h)
+                    elif window:
+                        assert np.isnan(o[r, t, h]).all() and np.isposinf(lse[r, t, h]), (r, t, h)
+                if not window:
+                    assert np.all(o[r, t] == 0) and np.all(np.isneginf(lse[r, t]))
+                else:
+                    assert np.isfinite(o[r, t, :14]).all() and np.isfinite(o[r, t, 21:]).all()
+    c.st.close()
