@@ -457,7 +457,8 @@ starkv_status starkv_pages_free(starkv_state* st, const starkv_pages* pages, con
  * order, in pages of its own (numbers as for extend, taken before the old pages
  * are let go; other holders of those keep them): len = B + w.  Reads idx, L,
  * budget, meta and its strides of seqs (host values, fixed in a captured call), writes
- * meta_out where meta is given; the other buffers may be NULL.  In the per-KV-head mode
+ * meta_out where meta is given; the other buffers may be NULL, and slots are not
+ * looked at.  In the per-KV-head mode
  * group g keeps idx[g].  Error (device): an index outside the past tokens keeps token 0. */
 starkv_status starkv_pages_compact(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const starkv_seq* seqs,
                                    int32_t nseq, void* workspace, size_t workspace_bytes, void* stream);

@@ -204,7 +204,8 @@ starkv_status validate_config(const starkv_config& c) {
 }
 
 enum Need : unsigned {
-  kNeedK = 1, kNeedQ = 2, kNeedV = 4, kNeedMeta = 8, kNeedS = 16, kNeedIdx = 32, kNeedOut = 64
+  kNeedK = 1, kNeedQ = 2, kNeedV = 4, kNeedMeta = 8, kNeedS = 16, kNeedIdx = 32, kNeedOut = 64,
+  kNoSlots = 128   // the call touches no slot's state: any number of sequences, whatever their slots
 };
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -214,12 +215,15 @@ starkv_status validate_seqs(const starkv_state* st, const starkv_seq* seqs, int 
   if (!st) return set_error(STARKV_ERR_INVALID_ARG, "state is NULL");
   if (nseq < 0 || (nseq > 0 && !seqs)) return set_error(STARKV_ERR_INVALID_ARG, "bad sequence array");
   const starkv_config& c = st->cfg;
-  std::vector<char> used(c.max_seqs, 0);
+  const bool slots = !(need & kNoSlots);
+  std::vector<char> used(slots ? c.max_seqs : 0, 0);
   for (int i = 0; i < nseq; ++i) {
     const starkv_seq& s = seqs[i];
-    if (s.slot < 0 || s.slot >= c.max_seqs) return set_error(STARKV_ERR_INVALID_ARG, "seq %d: slot out of range", i);
-    if (used[s.slot]) return set_error(STARKV_ERR_INVALID_ARG, "seq %d: slot %d used twice in one call", i, s.slot);
-    used[s.slot] = 1;
+    if (slots) {
+      if (s.slot < 0 || s.slot >= c.max_seqs) return set_error(STARKV_ERR_INVALID_ARG, "seq %d: slot out of range", i);
+      if (used[s.slot]) return set_error(STARKV_ERR_INVALID_ARG, "seq %d: slot %d used twice in one call", i, s.slot);
+      used[s.slot] = 1;
+    }
     if (s.L < c.window) return set_error(STARKV_ERR_INVALID_ARG, "seq %d: L < window", i);
     if (s.L >= (1 << 24)) return set_error(STARKV_ERR_UNSUPPORTED, "seq %d: L >= 2^24", i);
     const int lp = s.L - c.window;
@@ -1480,11 +1484,11 @@ starkv_status starkv_pages_compact(starkv_state* st, const starkv_pages* pages, 
   if (s != STARKV_OK) return s;
   if ((s = check_rows(nseq)) != STARKV_OK) return s;
   if (!aligned4(rows)) return set_error(STARKV_ERR_INVALID_ARG, "rows not 4-byte aligned");
-  if ((s = validate_seqs(st, seqs, nseq, kNeedIdx)) != STARKV_OK) return s;
+  if ((s = validate_seqs(st, seqs, nseq, kNeedIdx | kNoSlots)) != STARKV_OK) return s;
   for (int i = 0; i < nseq; ++i) {
     if (!seqs[i].meta) continue;
     if (!seqs[i].meta_out) return set_error(STARKV_ERR_INVALID_ARG, "seq %d: meta without meta_out", i);
-    if ((s = validate_seqs(st, seqs + i, 1, kNeedMeta)) != STARKV_OK) return s;
+    if ((s = validate_seqs(st, seqs + i, 1, kNeedMeta | kNoSlots)) != STARKV_OK) return s;
   }
   if ((s = check_device(st)) != STARKV_OK) return s;
   if ((s = check_ws(st, workspace, workspace_bytes, book_ws(*pages, nseq).total)) != STARKV_OK) return s;

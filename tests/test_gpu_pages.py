@@ -595,3 +595,17 @@ def test_a_store_that_names_a_row_twice_leaves_that_row_alone(n, twins):
     sk.pages_load(st, c.pages, 0, sk.Tokens(k=back, rows=c.ids([rows[1], rows[1]])))
     assert _error(st) == sk.OK and torch.equal(back[0], back[1])
     st.close()
+
+
+def test_compaction_looks_at_no_slot():
+    """More rows than the state has slots, all with the default one: compaction touches no slot's state."""
+    w = 8
+    st = PH.state(heads=4, kv_heads=2, window=w, max_seqs=1)
+    c = PH.Pair(st, n_pages=40, P=16, n_rows=3, max_pages=8)
+    c.extend([0, 1, 2], [60, 33, 90])
+    idx = [np.arange(b, dtype=np.int32).reshape(1, 1, b) for b in (20, 5, 40)]
+    sk.pages_compact(st, c.pages, None, [sk.Seq(L=int(c.ref.len[i]), budget=x.size, idx=torch.from_numpy(x).cuda())
+                                         for i, x in enumerate(idx)], c.ws)
+    c.ref.compact([0, 1, 2], [60, 33, 90], idx, w)
+    c.check()
+    st.close()
