@@ -669,11 +669,32 @@ def pages_free(st: State, pages: Pages, rows: torch.Tensor, stream=None) -> None
     _check(lib().starkv_pages_free(st.handle, c, _ids(rows, n, "rows"), n, _stream_on(pages, stream)))
 
 
+def _check_kept(cfg: Config, i: int, s: Seq) -> None:
+    """What a compaction reads and writes of a sequence: 32-bit words, as many as the call goes through."""
+    rows, B, n = sel_rows(cfg), s.budget, s.budget + cfg.window
+    for name, t, kinds, last, need in (("idx", s.idx, (torch.int32,), B, cfg.n_layers * rows * B),
+                                       ("meta_out", s.meta_out, _WORDS, n, cfg.n_layers * rows * n),
+                                       ("meta", s.meta, _WORDS, None,
+                                        (cfg.n_layers - 1) * s.meta_layer_stride + (rows - 1) * s.meta_group_stride + s.L)):
+        if t is None:
+            continue
+        if t.dtype not in kinds:
+            raise ValueError(f"seq {i}: {name}: expected {kinds[0]}, got {t.dtype}")
+        if t.numel() < need or (last and t.dim() > 1 and t.shape[-1] != last):
+            raise ValueError(f"seq {i}: {name} of shape {tuple(t.shape)}: the call goes through {need} words"
+                             + ("" if last is None else f", {last} a row"))
+
+
+_WORDS = (torch.int32, torch.uint32)
+
+
 def pages_compact(st: State, pages: Pages, rows: Optional[torch.Tensor], seqs: Sequence[Seq], ws: torch.Tensor,
                   stream=None) -> None:
     """Every layer of ``rows[i]`` keeps the tokens ``seqs[i].idx`` and the window (``starkv_compact`` on pages)."""
     c = _c_pages(st, pages)
     _on(pages, rows, ws, *(t for s in seqs for t in (s.idx, s.meta, s.meta_out)))
+    for i, s in enumerate(seqs):
+        _check_kept(st.cfg, i, s)
     _check(lib().starkv_pages_compact(st.handle, c, _ids(rows, len(seqs), "rows"), _seq_array(seqs), len(seqs),
                                       ws.data_ptr(), ws.numel(), _stream_on(pages, stream)))
 

@@ -195,3 +195,23 @@ def test_the_two_cpu_definitions_agree():
         o, lse = O.attention(s["q"][i, :n].float().numpy(), k, v, O.seen_tree(L, n, s["mask"][i].tolist()))
         np.testing.assert_allclose(got["lse"][i, :n].numpy(), lse, rtol=2e-6)
         np.testing.assert_allclose(got["o"][i, :n].float().numpy(), o, rtol=2**-7, atol=1e-5)
+
+
+@pytest.mark.parametrize("over,what", [
+    (dict(idx=torch.zeros((2, 1, 3), dtype=torch.int64)), "idx"), (dict(idx=torch.zeros((1, 1, 3), dtype=torch.int32)), "idx"),
+    (dict(idx=torch.zeros((2, 1, 4), dtype=torch.int32)), "idx"), (dict(idx=torch.zeros((2, 1, 3))), "idx"),
+    (dict(meta_out=torch.zeros((2, 1, 10), dtype=torch.int32)), "meta_out"), (dict(meta_out=torch.zeros(21, dtype=torch.int32)), "meta_out"),
+    (dict(meta_out=torch.zeros((2, 1, 11), dtype=torch.int64)), "meta_out"), (dict(meta=torch.zeros(39, dtype=torch.int32)), "meta"),
+    (dict(meta=torch.zeros(79, dtype=torch.int32), meta_layer_stride=40), "meta"), (dict(meta=torch.zeros(40, dtype=torch.int64)), "meta")],
+    ids=lambda x: x if isinstance(x, str) else str(tuple(next(iter(x.values())).shape)))
+def test_the_binding_checks_what_a_compaction_keeps(over, what):
+    """idx as 64-bit words would be read as pairs of 32-bit ones, and a short meta_out be written past its end."""
+    st, pages = _State(), _pages()
+    st.cfg = sk.Config(n_layers=2, n_heads=8, n_kv_heads=4, window=8)
+    seq = dict(L=40, budget=3, idx=torch.zeros((2, 1, 3), dtype=torch.int32), meta=torch.zeros(40, dtype=torch.int32),
+               meta_out=torch.zeros((2, 1, 11), dtype=torch.int32))
+    ws = torch.zeros(256, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="pages on cpu"):     # all is well with it but the device
+        sk.pages_compact(st, pages, None, [sk.Seq(**seq)], ws)
+    with pytest.raises(ValueError, match=f"seq 1: {what}"):
+        sk.pages_compact(st, pages, None, [sk.Seq(**seq), sk.Seq(**{**seq, **over})], ws)
