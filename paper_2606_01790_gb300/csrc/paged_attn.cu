@@ -254,7 +254,8 @@ __device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
     // The flat order leaves none idle but takes about 1.2 times as long a unit, since it reads
     // each block's keys on its own.  Busy for all of the time, gangs took 124 us where the flat order
     // took 143 (32 trees of 36 over 6,000), for 0.76 of it 140 and 131 (ragged, 64), for 0.71 151
-    // and 145 (ragged, 26).
+    // and 145 (ragged, 26).  CTAs too few for a gang more are idle too: with 80 blocks of four
+    // rows of 20,000 gangs (one, 80 of 152 CTAs) took 635, the flat order 379; with 40 (three) 228 and 203.
     int64_t units = 0, work = 0;
     int most = 1;
     for (int seq = tid; seq < p.n; seq += kThreads) {
@@ -276,7 +277,10 @@ __device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
       atomicMax(&ctl->gang, most);
     }
     __syncthreads();
-    if (tid == 0 && (ctl->gang == 1 || 6 * ctl->sum[1] < 5 * ctl->sum[0] * ctl->gang)) ctl->gang = 1;
+    if (tid == 0) {
+      const int B = ctl->gang, used = gridDim.x / B * B;   // CTAs in gangs: none if B is more than all
+      if (B == 1 || 6 * ctl->sum[1] * used < 5 * ctl->sum[0] * B * static_cast<int64_t>(gridDim.x)) ctl->gang = 1;
+    }
     __syncthreads();
   }
   const bool gangs = ctl->gang > 1;

@@ -657,3 +657,23 @@ def test_logits_that_are_all_minus_infinity(n, L, T):
                 else:
                     assert np.isfinite(o[r, t, :14]).all() and np.isfinite(o[r, t, 21:]).all()
     c.st.close()
+
+
+@pytest.mark.parametrize("heads,T", [(160, 64), (128, 63), (256, 64)])
+def test_trees_of_many_query_blocks(heads, T):
+    """80 blocks of a sequence (no gang's worth of CTAs is left over by a second one), 63 (two gangs) and 128."""
+    c = filled([T + 90, T, 300], P=32, heads=heads, kv_heads=1, seed=heads)
+    rng = np.random.default_rng(T)
+    masks = [random_tree(rng, T) for _ in range(3)]
+    qs = queries(c, 3, T, mask=words(masks, T))
+    sk.tree_attention(c.st, c.pages, 0, qs, c.ws)
+    torch.cuda.synchronize()
+    sk.check_device_error(c.st)
+    o, lse, q = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy(), qs.q.float().cpu().numpy()
+    for i, L in enumerate((T + 90, T, 300)):
+        k, v = c.cache(i, 0)
+        seen = O.seen_tree(L, T, masks[i])
+        for t in sorted({0, 1, T // 2, T - 1}):
+            PH.check_attention(o[i, t:t + 1], lse[i, t:t + 1], q[i, t:t + 1], k, v, seen[t:t + 1], what=f"{i} {t}")
+    assert np.isfinite(o).all() and np.isfinite(lse).all()
+    c.st.close()
