@@ -1216,6 +1216,39 @@ BookParams book_params(starkv_state* st, const starkv_pages& p, const int32_t* r
   return b;
 }
 
+// Whether rows of d elements at sums of i_k * stride_k (0 <= i_k < n_k) can meet, that is, whether
+// differences d_k, |d_k| < n_k and not all 0, bring |sum d_k stride_k| below d.
+struct Axis {
+  int64_t n, stride, reach;   // reach: what the axes after it span, (n_k - 1) stride_k added up
+};
+
+// The differences from axis k on, largest stride first: few of an axis leave a sum that the axes
+// after it can still bring back.  `left`: sums to look at before the answer is yes for good.
+bool meet(const Axis* a, int k, int n, int64_t sum, bool moved, int* left) {
+  if (k == n) return moved && std::abs(sum) < kHeadDim;
+  if (--*left < 0) return true;
+  const int64_t within = a[k].reach + kHeadDim - 1, s = a[k].stride;
+  const int64_t lo = std::max(-(a[k].n - 1), (-sum - within) / s), hi = std::min(a[k].n - 1, (-sum + within) / s);
+  for (int64_t d = lo; d <= hi; ++d)
+    if (meet(a, k + 1, n, sum + d * s, moved || d != 0, left)) return true;
+  return false;
+}
+
+template <size_t N>
+bool rows_overlap(const int64_t (&sizes)[N], const int64_t (&strides)[N]) {
+  Axis a[N];
+  int n = 0;
+  for (size_t k = 0; k < N; ++k)
+    if (sizes[k] > 1) {
+      if (strides[k] < kHeadDim || strides[k] > (int64_t(1) << 58) / sizes[k]) return true;   // (or past any address)
+      a[n++] = {sizes[k], strides[k], 0};
+    }
+  std::sort(a, a + n, [](const Axis& x, const Axis& y) { return x.stride > y.stride; });
+  for (int k = n - 2; k >= 0; --k) a[k].reach = a[k + 1].reach + (a[k + 1].n - 1) * a[k + 1].stride;
+  int left = 1 << 14;
+  return meet(a, 0, n, 0, false, &left);
+}
+
 starkv_status validate_tokens(const starkv_state* st, bool store, int layer0, int nl, const starkv_tokens* t) {
   if (!t) return set_error(STARKV_ERR_INVALID_ARG, "tokens is NULL");
   starkv_status s = check_rows(t->n);
@@ -1231,8 +1264,9 @@ starkv_status validate_tokens(const starkv_state* st, bool store, int layer0, in
     return set_error(STARKV_ERR_INVALID_ARG, "tokens: rows or n_tokens not 4-byte aligned");
   for (int64_t x : {t->seq_stride, t->layer_stride, t->token_stride, t->head_stride})
     if (x < 0 || (x & 7)) return set_error(STARKV_ERR_INVALID_ARG, "tokens: strides must be multiples of 8 elements, not negative");
-  if (!store && ((t->n > 1 && t->seq_stride < kHeadDim) || (nl > 1 && t->layer_stride < kHeadDim) ||
-                 (t->T > 1 && t->token_stride < kHeadDim) || (st->cfg.n_kv_heads > 1 && t->head_stride < kHeadDim)))
+  if (store) return STARKV_OK;
+  if (t->k == t->v) return set_error(STARKV_ERR_INVALID_ARG, "tokens: k and v are the same");
+  if (rows_overlap({t->n, nl, t->T, st->cfg.n_kv_heads}, {t->seq_stride, t->layer_stride, t->token_stride, t->head_stride}))
     return set_error(STARKV_ERR_INVALID_ARG, "tokens: strides let the rows that are loaded overlap");
   return STARKV_OK;
 }
@@ -1285,8 +1319,7 @@ starkv_status validate_queries(const starkv_state* st, int layer, const starkv_q
     return set_error(STARKV_ERR_INVALID_ARG, "queries: mask NULL or not 8-byte aligned");
   for (int64_t x : {q->q_seq_stride, q->q_token_stride, q->q_head_stride, q->o_seq_stride, q->o_token_stride, q->o_head_stride})
     if (x < 0 || (x & 7)) return set_error(STARKV_ERR_INVALID_ARG, "queries: strides must be multiples of 8 elements, not negative");
-  if ((q->n > 1 && q->o_seq_stride < kHeadDim) || (q->T > 1 && q->o_token_stride < kHeadDim) ||
-      (c.n_heads > 1 && q->o_head_stride < kHeadDim))
+  if (rows_overlap({q->n, q->T, c.n_heads}, {q->o_seq_stride, q->o_token_stride, q->o_head_stride}))
     return set_error(STARKV_ERR_INVALID_ARG, "queries: strides of o let its rows overlap");
   return STARKV_OK;
 }

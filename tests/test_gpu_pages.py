@@ -609,3 +609,28 @@ def test_compaction_looks_at_no_slot():
     c.ref.compact([0, 1, 2], [60, 33, 90], idx, w)
     c.check()
     st.close()
+
+
+def test_outputs_whose_rows_meet_are_refused_on_the_host():
+    """Strides that each step over a row and still let two rows share elements; axes in any order, or interleaved without meeting, are taken."""
+    st = PH.state(layers=2, heads=8, kv_heads=4)
+    c = PH.Pair(st, n_pages=9, P=16, n_rows=2, max_pages=4)
+    c.extend([0, 1], [20, 20])
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    flat, D = torch.zeros(1 << 16, **bf), PH.D
+    q = torch.zeros((2, 3, 8, D), **bf)
+    for strides in ((3 * D, D, D), (8 * D, 8 * D, D), (24 * D, 7 * D, D), (23 * D, 8 * D, D), (D, 2 * D, 3 * D), (1 << 47, 1 << 62, D)):
+        with pytest.raises((sk.StarkvError, RuntimeError)):
+            sk.sink_attention(st, c.pages, 0, sk.Queries(q=q, o=flat.as_strided((2, 3, 8, D), (*strides, 1))), 1, 40, c.ws)
+    for strides in ((24 * D, 8 * D, D), (D, 2 * D, 6 * D), (3 * D, D, 6 * D), (50 * D, 9 * D, D), (3 * D, 2 * D, 8 * D)):
+        sk.sink_attention(st, c.pages, 0, sk.Queries(q=q, o=flat.as_strided((2, 3, 8, D), (*strides, 1))), 1, 40, c.ws)
+    for strides in ((D, D, D, D), (24 * D, 12 * D, 4 * D, 2 * D), (24 * D, 11 * D, 4 * D, D), (12 * D, 12 * D, 4 * D, D)):
+        with pytest.raises(sk.StarkvError):
+            sk.pages_load(st, c.pages, 0, sk.Tokens(k=flat.as_strided((2, 2, 3, 4, D), (*strides, 1))))
+    k = torch.zeros((2, 2, 3, 4, D), **bf)
+    with pytest.raises(sk.StarkvError):
+        sk.pages_load(st, c.pages, 0, sk.Tokens(k=k, v=k))
+    for strides in ((24 * D, 12 * D, 4 * D, D), (D, 24 * D, 8 * D, 2 * D), (24 * D, 12 * D, D, 3 * D)):
+        sk.pages_load(st, c.pages, 0, sk.Tokens(k=flat.as_strided((2, 2, 3, 4, D), (*strides, 1))))
+    c.check()
+    st.close()
