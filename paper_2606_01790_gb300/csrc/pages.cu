@@ -95,11 +95,14 @@ __device__ __forceinline__ int row_of(const int* off, int n, int a) {
   return lo;
 }
 
+// (Not the read-only path: a kernel here starts while the ones before it still write the pool, and copies
+// within it.)
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "l"(p));
+               : "l"(p)
+               : "memory");
   return v;
 }
 
