@@ -650,7 +650,7 @@ def pages_extend(st: State, pages: Pages, rows: Optional[torch.Tensor], n_new: t
     c, n = _c_pages(st, pages), n_new.numel()
     _on(pages, rows, n_new, ws)
     _check(lib().starkv_pages_extend(st.handle, c, _ids(rows, n, "rows"), _ids(n_new, n, "n_new"), n,
-                                     ws.data_ptr(), ws.numel(), _stream_on(pages, stream)))
+                                     _ptr(ws), ws.numel(), _stream_on(pages, stream)))
 
 
 def pages_fork(st: State, pages: Pages, src: torch.Tensor, dst: torch.Tensor, ws: torch.Tensor, deep: bool = False,
@@ -659,7 +659,7 @@ def pages_fork(st: State, pages: Pages, src: torch.Tensor, dst: torch.Tensor, ws
     c, n = _c_pages(st, pages), dst.numel()
     _on(pages, src, dst, ws)
     _check(lib().starkv_pages_fork(st.handle, c, _ids(src, n, "src"), _ids(dst, n, "dst"), n, int(deep),
-                                   ws.data_ptr(), ws.numel(), _stream_on(pages, stream)))
+                                   _ptr(ws), ws.numel(), _stream_on(pages, stream)))
 
 
 def pages_free(st: State, pages: Pages, rows: torch.Tensor, stream=None) -> None:
@@ -696,7 +696,7 @@ def pages_compact(st: State, pages: Pages, rows: Optional[torch.Tensor], seqs: S
     for i, s in enumerate(seqs):
         _check_kept(st.cfg, i, s)
     _check(lib().starkv_pages_compact(st.handle, c, _ids(rows, len(seqs), "rows"), _seq_array(seqs), len(seqs),
-                                      ws.data_ptr(), ws.numel(), _stream_on(pages, stream)))
+                                      _ptr(ws), ws.numel(), _stream_on(pages, stream)))
 
 
 def pages_store(st: State, pages: Pages, layer0: int, tokens: Tokens, stream=None) -> None:
@@ -715,7 +715,7 @@ def tree_attention(st: State, pages: Pages, layer: int, queries: Queries, ws: to
     """Attention of each row's last (drafted) tokens over its cache; ``queries.mask`` names the drafted ones seen."""
     c, q = _c_pages(st, pages), _c_queries(st, pages, queries)
     _on(pages, ws)
-    _check(lib().starkv_tree_attention(st.handle, c, layer, q, ws.data_ptr(), ws.numel(),
+    _check(lib().starkv_tree_attention(st.handle, c, layer, q, _ptr(ws), ws.numel(),
                                        _stream_on(pages, stream)))
 
 
@@ -724,5 +724,5 @@ def sink_attention(st: State, pages: Pages, layer: int, queries: Queries, n_sink
     """Causal attention over the first ``n_sink`` tokens and the last ``window``."""
     c, q = _c_pages(st, pages), _c_queries(st, pages, queries)
     _on(pages, ws)
-    _check(lib().starkv_sink_attention(st.handle, c, layer, q, n_sink, window, ws.data_ptr(),
+    _check(lib().starkv_sink_attention(st.handle, c, layer, q, n_sink, window, _ptr(ws),
                                        ws.numel(), _stream_on(pages, stream)))

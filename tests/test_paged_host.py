@@ -215,3 +215,16 @@ def test_the_binding_checks_what_a_compaction_keeps(over, what):
         sk.pages_compact(st, pages, None, [sk.Seq(**seq)], ws)
     with pytest.raises(ValueError, match=f"seq 1: {what}"):
         sk.pages_compact(st, pages, None, [sk.Seq(**seq), sk.Seq(**{**seq, **over})], ws)
+
+
+def test_the_binding_refuses_a_workspace_that_is_not_what_it_says():
+    """An expanded tensor has more elements than bytes behind it."""
+    st, pages = _State(), _pages()
+    ws, ids = torch.zeros(1, dtype=torch.uint8).expand(1 << 30), torch.zeros(2, dtype=torch.int32)
+    q = torch.zeros((1, 1, 8, 128), dtype=torch.bfloat16)
+    qs = sk.Queries(q=q, o=torch.zeros_like(q), mask=torch.zeros((1, 1), dtype=torch.int64))
+    for call in (lambda: sk.pages_extend(st, pages, None, ids, ws), lambda: sk.pages_fork(st, pages, ids, ids, ws),
+                 lambda: sk.pages_compact(st, pages, None, [sk.Seq(L=40)], ws), lambda: sk.tree_attention(st, pages, 0, qs, ws),
+                 lambda: sk.sink_attention(st, pages, 0, qs, 1, 1, ws)):
+        with pytest.raises(ValueError, match="contiguous"):
+            call()
