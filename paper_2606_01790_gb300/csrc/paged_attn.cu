@@ -139,16 +139,20 @@ __device__ __forceinline__ void fail(Ctl* ctl, uint32_t* err) {
 // took time, no role had failed.  The one place where these roles learn of a failure, so
 // that a warp's lanes leave together: a barrier that a failed role should have
 // completed does not complete.  The limit counts from the last sign of life of rows that are
-// taken key by key (recompute_rows): these may take long, but come to an end.
+// taken key by key (recompute_rows and the like): these may take long, but come to an end.
 __device__ __forceinline__ bool warp_wait(const Ctl* ctl, uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
   if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
-  while (true) {
-    const bool aborted = ctl->abort;
-    const int beat = ctl->beat;
-    const bool there = mbar_wait(bar, parity, limit_ns);
-    if (__all_sync(kFull, there && !aborted)) return true;
-    if (!__all_sync(kFull, !aborted) || !__any_sync(kFull, ctl->beat != beat)) return false;
+  const bool aborted = ctl->abort;
+  bool there = mbar_try_wait(bar, parity);   // (most waits end before a clock is read)
+  int beat = ctl->beat;
+  for (uint64_t t0 = global_timer_ns(); !there;) {
+    there = mbar_try_wait_sleep(bar, parity, 20000u);
+    if (there || global_timer_ns() - t0 <= limit_ns) continue;
+    if (ctl->beat == beat) break;
+    beat = ctl->beat;
+    t0 = global_timer_ns();
   }
+  return __all_sync(kFull, there && !aborted);
 }
 
 // Two of them, at the price of one where both are complete.  They may be looked at in
@@ -933,11 +937,6 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
       const float2 other = ctl->ml[pc & 1][line ^ 1][r];
       const float M = fmaxf(m, other.x), ref = M == -INFINITY ? 0.f : M;   // (the last reference is the largest)
       float L = exp2f(m - ref) * l + exp2f(other.x - ref) * other.y;
-      const uint32_t infinite = __ballot_sync(kFull, live && M == INFINITY);
-      if (infinite) {
-        const uint32_t nan = rows_with_nan(p, ctl, blk, c.g, c.j0, c.n, quad * 32, infinite);
-        if (M == INFINITY) L = nan >> lane & 1 ? NAN : 1.f;   // lse is +inf (and every column NaN)
-      }
       const float norm = !whole ? 1.f : L != 0.f ? 1.f / L : see.none() ? 0.f : NAN;   // (0 / 0 where every logit is -inf)
       const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (c.j0 == 0);
       // this line's half of the columns by way of shared memory, for rows that are written whole
@@ -955,13 +954,18 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
         sum[i & 1] = fmaf(__uint_as_float(a[0][i]), 0.f, sum[i & 1]);
         sum[2 + (i & 1)] = fmaf(__uint_as_float(a[1][i]), 0.f, sum[2 + (i & 1)]);
       }
-      // (a logit that is NaN or infinite has all of its row's columns NaN already)
-      const uint32_t which = __ballot_sync(kFull, live && (sum[0] + sum[1]) + (sum[2] + sum[3]) != 0.f && L == L && M < INFINITY);
-      if (which) {
-        __syncwarp();   // (rows of other lanes)
-        if (ctl->masked[pc & 1][0] | ctl->masked[pc & 1][1])
+      const bool odd = live && (sum[0] + sum[1]) + (sum[2] + sum[3]) != 0.f;
+      if (__any_sync(kFull, odd)) {
+        // (a logit that is NaN or +inf has all of its row's columns NaN, as they are to be, and L too)
+        const uint32_t infinite = __ballot_sync(kFull, odd && M == INFINITY && line == 0);   // (the line that writes L)
+        if (infinite) {
+          const uint32_t nan = rows_with_nan(p, ctl, blk, c.g, c.j0, c.n, quad * 32, infinite);
+          if (M == INFINITY) L = nan >> lane & 1 ? NAN : 1.f;   // lse is +inf where no logit is NaN
+        }
+        const uint32_t which = __ballot_sync(kFull, odd && L == L && M < INFINITY);
+        if (which && (ctl->masked[pc & 1][0] | ctl->masked[pc & 1][1]))
           recompute_rows(p, ctl, blk, c.g, c.j0, c.n, quad * 32, 64 * line, which, ref, norm, stage_o);
-        else
+        else if (which)
           settle_columns(p, ctl, blk, c.g, c.j0, c.n, 64 * line, which, stage_o);
       }
       __syncwarp();
