@@ -811,15 +811,26 @@ __device__ __noinline__ uint32_t rows_with_nan(const PagedAttnParams& p, Ctl* ct
     for (int j = j0; j < j0 + n; ++j) {
       const int k0 = blk.key(j);
       if (lane == 0) atomicAdd(const_cast<int*>(&ctl->beat), 1);
-      for (uint64_t bits = see(k0); bits; bits &= bits - 1) {
-        const int key = k0 + __ffsll(static_cast<long long>(bits)) - 1;
-        const int page = entries[key >> p.shift];
-        if (page < 0 || page >= p.n_pages) continue;
-        const float4 k = bf16x4(p.k + page * p.page_stride + ((static_cast<int64_t>(g) << p.shift) + (key & ((1 << p.shift) - 1))) * kHeadDim + 4 * lane);
-        float z = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
+      for (uint64_t bits = see(k0); bits;) {
+        float4 k[8];   // eight keys' loads at once
+        bool any[8];
 #pragma unroll
-        for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
-        if (z != z) found |= 1u << i;
+        for (int u = 0; u < 8; ++u) {
+          any[u] = bits != 0;
+          const int key = k0 + __ffsll(static_cast<long long>(bits)) - 1;
+          const int page = any[u] ? entries[key >> p.shift] : -1;
+          bits &= bits - 1;
+          k[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (page >= 0 && page < p.n_pages)
+            k[u] = bf16x4(p.k + page * p.page_stride + ((static_cast<int64_t>(g) << p.shift) + (key & ((1 << p.shift) - 1))) * kHeadDim + 4 * lane);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          float z = q.x * k[u].x + q.y * k[u].y + q.z * k[u].z + q.w * k[u].w;
+#pragma unroll
+          for (int o = 16; o; o >>= 1) z += __shfl_xor_sync(kFull, z, o);
+          if (any[u] && z != z) found |= 1u << i;
+        }
       }
     }
   }

@@ -677,3 +677,25 @@ def test_trees_of_many_query_blocks(heads, T):
             PH.check_attention(o[i, t:t + 1], lse[i, t:t + 1], q[i, t:t + 1], k, v, seen[t:t + 1], what=f"{i} {t}")
     assert np.isfinite(o).all() and np.isfinite(lse).all()
     c.st.close()
+
+
+def test_queries_of_infinity():
+    """Logits of both infinities from a query with an infinite element: lse +inf and o NaN; the other heads' are their own."""
+    c = filled([700, 75], P=64)
+    qs = queries(c, 2, 2, seed=6)
+    qs.q[:, 0, 3, 5], qs.q[:, 1, 20, 90] = float("inf"), float("-inf")
+    sk.sink_attention(c.st, c.pages, 0, qs, 0, 500, c.ws)
+    torch.cuda.synchronize()
+    sk.check_device_error(c.st)
+    o, lse, q = qs.o.float().cpu().numpy(), qs.lse.cpu().numpy(), qs.q.float().cpu().numpy()
+    for r in range(2):
+        k, v = c.cache(r, 0)
+        seen = O.seen_sink(k.shape[1], 2, 0, 500)
+        for t in range(2):
+            for h in range(28):
+                if (t, h) in ((0, 3), (1, 20)):
+                    assert np.isnan(o[r, t, h]).all() and np.isposinf(lse[r, t, h]), (r, t, h)
+                else:
+                    PH.check_attention(o[r, t:t + 1, h:h + 1], lse[r, t:t + 1, h:h + 1], q[r, t:t + 1, h:h + 1], k[h // 7:h // 7 + 1],
+                                       v[h // 7:h // 7 + 1], seen[t:t + 1], what=f"{r} {t} {h}")
+    c.st.close()
