@@ -479,8 +479,10 @@ starkv_status starkv_pages_load(starkv_state* st, const starkv_pages* pages, int
  * not looked at).  With z_j = q . K[g(h), j] / sqrt(d) over the keys seen,
  *   o = sum_j softmax_j(z) V[g(h), j],   lse = log sum_j exp(z_j);
  * a query that sees none has o = 0 and lse = -inf.  K and V that a query does not
- * see do not reach its output, whatever they hold (V that is not finite and is
- * seen by some queries only costs time: their rows are taken again key by key). */
+ * see do not reach its output, whatever they hold (V that is not finite and is seen by
+ * some queries only costs time: their rows are taken again key by key).  A seen V of
+ * infinity gives infinity, or NaN with its opposite.  Sums are held in fp32 against a
+ * weight of up to 2^8: values above 2^119 / L may overflow. */
 starkv_status starkv_tree_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
                                     void* workspace, size_t workspace_bytes, void* stream);
 

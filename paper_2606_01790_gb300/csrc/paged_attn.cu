@@ -49,15 +49,17 @@
 // cycles a unit.)
 //
 // What bounds it.  Few query rows: the stream of K and V (64 rows of one token, 4.2k keys
-// each in sight, 1.07 GB in 168 us: 94 % of the copy rate).  Many: shared memory and the
+// each in sight, 1.07 GB in 166 to 169 us: 94 % of the copy rate).  Many: shared memory and the
 // tensor pipe, which a unit keeps busy for 840 of its 1,000 cycles (K once, V twice, the
-// loads: 80 KB at some 91 B a cycle); four 56k caches with 64 drafted tokens 222 us, tensor
-// pipe 75 % busy, a chunk of 2,704 tokens under a window of 4,096 168 us, of which a sixth at
-// the ends of pieces.  Not kept: one softmax warpgroup for all units (344 and 278 us), two
-// with an O each and three places (232 and 185), one issuer for S and P V (291 and 275), waits
-// that spin (276 and 218), five or six stages (2 to 4 % slower), rows of O written by bulk copies
-// (5 % slower), range ends moved to the ends of (item, group)s (3 % faster for the chunk, 1 %
-// slower for decoding).
+// loads: 80 KB at some 91 B a cycle); four 56k caches with 64 drafted tokens 240 to 250 us (222
+// with the same inputs again and again), tensor pipe 76 % busy, a chunk of 2,704 tokens under a
+// window of 4,096 181 to 184 us (172), of which a sixth at the ends of pieces.  Measured when
+// these two took 222 and 168 with the same inputs, and not kept: one softmax warpgroup for
+// all units (344 and 278 us), two with an O each and three places (232 and 185), one issuer for
+// S and P V (291 and 275), waits that spin (276 and 218), five or six stages (2 to 4 % slower),
+// rows of O written by bulk copies (5 % slower), range ends moved to the ends of (item, group)s
+// (3 % faster for the chunk, 1 % slower for decoding).  The looks for values that are not finite
+// take 2 % of the chunk and 0.5 % of decoding; inside the softmax of a unit they took 8 %.
 //
 // Warp roles: 0 loads K, 3 loads V, 1 issues S and owns tensor memory, 2 issues P V,
 // 4..7 and 8..11 softmax.
