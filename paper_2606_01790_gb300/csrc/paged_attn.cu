@@ -969,6 +969,7 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
       }
       const bool odd = live && (sum[0] + sum[1]) + (sum[2] + sum[3]) != 0.f;
       if (__any_sync(kFull, odd)) {
+        __syncwarp();   // (rows that other lanes staged are written again)
         // (a logit that is NaN or +inf has all of its row's columns NaN, as they are to be, and L too)
         const uint32_t infinite = __ballot_sync(kFull, odd && M == INFINITY && line == 0);   // (the line that writes L)
         if (infinite) {
