@@ -493,6 +493,87 @@ starkv_status starkv_tree_attention(starkv_state* st, const starkv_pages* pages,
 starkv_status starkv_sink_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
                                     int32_t n_sink, int32_t window, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Attention mass: what each cached token has had of the queries' attention.
+ *
+ * One f32 per layer, row, KV head and token: token j of row r at mass + layer
+ * layer_stride + r row_stride + g group_stride + j, max_pages * page_size tokens a
+ * row, rows that do not overlap.  It belongs to the row, not to its pages: a branch
+ * takes a copy of its source's rows along, an emptied row leaves values that nothing
+ * reads. */
+typedef struct {
+  float* mass;            /* f32, device memory, 4-byte aligned                        */
+  int64_t layer_stride;   /* elements, not negative                                    */
+  int64_t row_stride;
+  int64_t group_stride;
+  float decay;            /* finite, >= 0: factor of what a token has had so far       */
+} starkv_mass;
+
+/* Adds the weights of an attention call, one layer: after starkv_tree_attention or
+ * starkv_sink_attention with the same queries (q, lse as it was written, mask, rows,
+ * n_tokens; o is not looked at), for row rows[i] of L tokens whose last n are the queries,
+ *   mass[g][j] = (j < L - n ? decay mass[g][j] : 0)
+ *                + sum_t sum_{h in g} [t sees j] exp(q[t, h] . K[g, j] / sqrt(d) - lse[t, h])
+ * for j < L, in fp32, the same from call to call.  A row's new tokens start at 0, so
+ * that rows need not be cleared; n = 0 leaves a row as it is.  Weights are what the
+ * formula has where q, a seen K or lse is not finite; what a query does not see adds
+ * nothing, whatever it holds.  A sequence that does not fit, or a row that two sequences
+ * with queries name, is left as it is (device error).  T and T * H / G as for the
+ * attention. */
+starkv_status starkv_tree_mass(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
+                               const starkv_mass* mass, void* workspace, size_t workspace_bytes, void* stream);
+starkv_status starkv_sink_mass(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
+                               int32_t n_sink, int32_t window, const starkv_mass* mass, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/* Eviction by mass: starkv_pages_compact, with the tokens chosen here.  Every layer of
+ * rows[i] keeps the budget past tokens (j < L - w) of greatest mass and the last w; in the
+ * per-KV-head mode group g by mass[g], else all groups by the sum over them (in 64 bits).
+ * Equal ones: the lower j; a NaN counts as +infinity.  Writes the chosen ones to idx
+ * (ascending), and moves the kept tokens' mass to their new places in the row (decay is
+ * not looked at).  A refused call changes nothing, idx and mass included. */
+starkv_status starkv_pages_evict(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const starkv_seq* seqs,
+                                 int32_t nseq, const starkv_mass* mass, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Bounds of pages, and attention over pages that each query chooses by them.
+ *
+ * Per layer, page and KV head the least and the greatest key of every channel: bf16
+ * [layer][page][G][2][d], the least ones first, strides of layer and page below.  They
+ * belong to the pages, as K and V do: rows that share a page share them. */
+typedef struct {
+  void* b;                /* bf16, device memory, 16-byte aligned                      */
+  int64_t layer_stride;   /* elements, multiples of 8, not negative                    */
+  int64_t page_stride;
+} starkv_bounds;
+
+/* Bounds of the pages that hold the last n_tokens[i] (0 .. T; NULL: T) tokens of row
+ * rows[i], layers [layer0, layer0 + n_layers), over the slots that hold tokens of that row:
+ * after tokens have been stored, and after a row has been compacted or its shared last page
+ * copied (extend), for the pages that changed.  What other pages have stays.  NaN where a
+ * key is NaN.  A sequence that does not fit, or a page that is none, is passed over (device
+ * error).  The pages' refs are not looked at, and a row may be named more than once. */
+starkv_status starkv_pages_bounds(starkv_state* st, const starkv_pages* pages, int32_t layer0, int32_t n_layers,
+                                  const starkv_bounds* bounds, const int32_t* rows, const int32_t* n_tokens, int32_t n, int32_t T,
+                                  void* stream);
+
+/* Bytes of workspace for a sparse attention call of n rows, T queries each and n_chosen pages. */
+starkv_status starkv_sparse_workspace_bytes(const starkv_state* st, const starkv_pages* pages, int32_t n, int32_t T, int32_t n_chosen,
+                                            size_t* bytes);
+
+/* Attention over chosen pages, one layer.  Query t (of n = n_tokens[i], as for
+ * starkv_sink_attention; mask is not looked at) is the token at position i = L - n + t of its
+ * row, in the row's page i / page_size.  For each KV head it attends over the tokens j <= i
+ * of n_chosen pages (of all pages up to its own, where they are not more): the first n_first,
+ * the last n_last up to its own, and of the others those with the greatest
+ *   score = sum_c (up_c hi_c + down_c lo_c),  up = sum_{h in g} max(q_h, 0),  down = sum_{h in g} min(q_h, 0),
+ * lo and hi the page's bounds: the most that the sum of the heads' logits with one of its keys
+ * can be.  Formed in 64 bits; equal ones: the lower page; a NaN counts as +infinity.
+ * n_first >= 0, n_last >= 1, n_first + n_last <= n_chosen.  chosen (i32 [n][T][G][n_chosen],
+ * or NULL) gets the pages' places in the row, ascending, -1 behind them.  o and lse are those of
+ * the keys attended over, as for the calls above. */
+starkv_status starkv_sparse_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
+                                      const starkv_bounds* bounds, int32_t n_first, int32_t n_last, int32_t n_chosen, int32_t* chosen,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
 /* Reads and clears the state's device error word (synchronises `stream`).
  * Returns STARKV_OK, STARKV_ERR_DEVICE or STARKV_ERR_TIMEOUT. */
 starkv_status starkv_check_device_error(starkv_state* st, void* stream);
@@ -529,9 +610,13 @@ enum {
   STARKV_KERNEL_PAGE_COPY = 8,    /* its page copies (extend, deep fork)                   */
   STARKV_KERNEL_PAGE_GATHER = 9,  /* its compaction (Eq. 11 on pages)                      */
   STARKV_KERNEL_PAGE_MOVE = 10,   /* tokens into and out of pages                          */
-  STARKV_KERNEL_PAGED_ATTENTION = 11,  /* tree and sink attention                          */
+  STARKV_KERNEL_PAGED_ATTENTION = 11,  /* tree, sink and sparse attention                  */
   STARKV_KERNEL_PAGED_COMBINE = 12,    /* merge of its parts                               */
-  STARKV_NUM_KERNELS = 13
+  STARKV_KERNEL_MASS = 13,             /* attention mass                                   */
+  STARKV_KERNEL_MASS_SELECT = 14,      /* tokens that stay by it                           */
+  STARKV_KERNEL_PAGE_BOUNDS = 15,      /* least and greatest keys of pages                 */
+  STARKV_KERNEL_PAGE_CHOOSE = 16,      /* pages that queries attend over                   */
+  STARKV_NUM_KERNELS = 17
 };
 
 /* Kernel timing, a profiling aid.  While `on` is non-zero every kernel launch

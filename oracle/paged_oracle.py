@@ -181,3 +181,51 @@ def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, seen: np.ndarray, spr
     if spread is not None:
         spread.append(size)
     return o, lse
+
+
+def mass(q: np.ndarray, k: np.ndarray, lse: np.ndarray, seen: np.ndarray, had: np.ndarray, decay: float,
+         slack: Optional[list] = None) -> np.ndarray:
+    """Attention mass [G][L] of a row of L tokens after n queries: q [n][H][d], k [G][L][d], lse [n][H], seen [n][L], had [G][L]
+    before.  `slack` takes sum of the weights times the error that each may carry in fp32 arithmetic."""
+    n, H, d = q.shape
+    G, L, _ = k.shape
+    out = had.astype(np.float64) * decay
+    out[:, L - n:] = 0
+    off = 2.0**-23 * np.abs(out)
+    for t in range(n):
+        at = np.flatnonzero(seen[t])
+        for h in range(H if len(at) else 0):
+            g = h * G // H
+            kk, qq = k[g, at].astype(np.float64), q[t, h].astype(np.float64)
+            z = kk @ qq / np.sqrt(d)
+            w = np.exp(z - float(lse[t, h]))
+            out[g, at] += w
+            # a logit's 128-term fp32 sum, its scale and the normaliser in base 2, exp2, and the sum over n H / G weights
+            dz = 130 * 2.0**-24 * (np.abs(kk) @ np.abs(qq)) / np.sqrt(d) + 2.0**-22 * (np.abs(z) + abs(float(lse[t, h])))
+            off[g, at] += w * (dz * (1 + dz) + 2.0**-21 + (n * H / G + 8) * 2.0**-24)
+    if slack is not None:
+        slack.append(off + 1e-37)
+    return out
+
+
+def heaviest(x: np.ndarray, budget: int) -> np.ndarray:
+    """The `budget` places of the greatest values, equal ones the lowest first, NaN as the greatest, in ascending order."""
+    x = np.where(np.isnan(x), np.inf, x.astype(np.float64))
+    return np.sort(np.argsort(-x, kind="stable")[:budget]).astype(np.int32)
+
+
+def page_scores(q: np.ndarray, lo: np.ndarray, hi: np.ndarray) -> np.ndarray:
+    """Most that the logits of a group's heads with one of a page's keys can add up to: q [heads][d], lo and hi [pages][d]."""
+    q, lo, hi = (x.astype(np.float64) for x in (q, lo, hi))
+    return np.maximum(q[None] * lo[:, None], q[None] * hi[:, None]).sum((1, 2))
+
+
+def choose_pages(score: np.ndarray, first: int, last: int, chosen: int) -> List[int]:
+    """Places of the pages taken of those up to a query's own (one score each), ascending."""
+    n = len(score)
+    if n <= chosen:
+        return list(range(n))
+    always = [j for j in range(n) if j < first or j >= n - last]
+    others = [j for j in range(n) if first <= j < n - last]
+    others.sort(key=lambda j: (-np.inf if np.isnan(score[j]) else -score[j], j))
+    return sorted(always + others[:chosen - len(always)])

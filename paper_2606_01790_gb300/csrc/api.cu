@@ -17,10 +17,12 @@
 #include "attn.cuh"
 #include "common.cuh"
 #include "compact.cuh"
+#include "mass.cuh"
 #include "paged_attn.cuh"
 #include "pages.cuh"
 #include "score.cuh"
 #include "select.cuh"
+#include "sparse.cuh"
 
 using namespace starkv;
 
@@ -146,6 +148,10 @@ const char* kernel_range_name(int kind) {
     case STARKV_KERNEL_PAGE_MOVE: return "starkv: tokens and pages";
     case STARKV_KERNEL_PAGED_ATTENTION: return "starkv: paged attention";
     case STARKV_KERNEL_PAGED_COMBINE: return "starkv: paged attention (combine)";
+    case STARKV_KERNEL_MASS: return "starkv: attention mass";
+    case STARKV_KERNEL_MASS_SELECT: return "starkv: choice by mass";
+    case STARKV_KERNEL_PAGE_BOUNDS: return "starkv: page bounds";
+    case STARKV_KERNEL_PAGE_CHOOSE: return "starkv: choice of pages";
     default: return "starkv: kernel";
   }
 }
@@ -1216,37 +1222,37 @@ BookParams book_params(starkv_state* st, const starkv_pages& p, const int32_t* r
   return b;
 }
 
-// Whether rows of d elements at sums of i_k * stride_k (0 <= i_k < n_k) can meet, that is, whether
-// differences d_k, |d_k| < n_k and not all 0, bring |sum d_k stride_k| below d.
+// Whether rows of `len` elements at sums of i_k * stride_k (0 <= i_k < n_k) can meet, that is, whether
+// differences d_k, |d_k| < n_k and not all 0, bring |sum d_k stride_k| below len.
 struct Axis {
   int64_t n, stride, reach;   // reach: what the axes after it span, (n_k - 1) stride_k added up
 };
 
 // The differences from axis k on, largest stride first: few of an axis leave a sum that the axes
 // after it can still bring back.  `left`: sums to look at before the answer is yes for good.
-bool meet(const Axis* a, int k, int n, int64_t sum, bool moved, int* left) {
-  if (k == n) return moved && std::abs(sum) < kHeadDim;
+bool meet(const Axis* a, int k, int n, int64_t sum, bool moved, int64_t len, int* left) {
+  if (k == n) return moved && std::abs(sum) < len;
   if (--*left < 0) return true;
-  const int64_t within = a[k].reach + kHeadDim - 1, s = a[k].stride;
+  const int64_t within = a[k].reach + len - 1, s = a[k].stride;
   const int64_t lo = std::max(-(a[k].n - 1), (-sum - within) / s), hi = std::min(a[k].n - 1, (-sum + within) / s);
   for (int64_t d = lo; d <= hi; ++d)
-    if (meet(a, k + 1, n, sum + d * s, moved || d != 0, left)) return true;
+    if (meet(a, k + 1, n, sum + d * s, moved || d != 0, len, left)) return true;
   return false;
 }
 
 template <size_t N>
-bool rows_overlap(const int64_t (&sizes)[N], const int64_t (&strides)[N]) {
+bool rows_overlap(const int64_t (&sizes)[N], const int64_t (&strides)[N], int64_t len = kHeadDim) {
   Axis a[N];
   int n = 0;
   for (size_t k = 0; k < N; ++k)
     if (sizes[k] > 1) {
-      if (strides[k] < kHeadDim || strides[k] > (int64_t(1) << 58) / sizes[k]) return true;   // (or past any address)
+      if (strides[k] < len || strides[k] > (int64_t(1) << 58) / sizes[k]) return true;   // (or past any address)
       a[n++] = {sizes[k], strides[k], 0};
     }
   std::sort(a, a + n, [](const Axis& x, const Axis& y) { return x.stride > y.stride; });
   for (int k = n - 2; k >= 0; --k) a[k].reach = a[k + 1].reach + (a[k + 1].n - 1) * a[k + 1].stride;
   int left = 1 << 14;
-  return meet(a, 0, n, 0, false, &left);
+  return meet(a, 0, n, 0, false, len, &left);
 }
 
 starkv_status validate_tokens(const starkv_state* st, bool store, int layer0, int nl, const starkv_tokens* t) {
@@ -1298,7 +1304,8 @@ starkv_status move_tokens(starkv_state* st, bool store, const starkv_pages* page
   return STARKV_OK;
 }
 
-starkv_status validate_queries(const starkv_state* st, int layer, const starkv_queries* q, bool tree) {
+// `weigh`: the queries of a mass call, which reads lse and does not look at o.
+starkv_status validate_queries(const starkv_state* st, int layer, const starkv_queries* q, bool tree, bool weigh = false) {
   if (!q) return set_error(STARKV_ERR_INVALID_ARG, "queries is NULL");
   starkv_status s = check_rows(q->n);
   if (s != STARKV_OK) return s;
@@ -1310,14 +1317,18 @@ starkv_status validate_queries(const starkv_state* st, int layer, const starkv_q
   if (static_cast<int64_t>(q->T) * hg > kPagedItems * kPagedRows)
     return set_error(STARKV_ERR_UNSUPPORTED, "queries: T * (H / G) > 2^17");
   if (q->n == 0 || q->T == 0) return STARKV_OK;
-  if (!q->q || !q->o || !aligned16(q->q) || !aligned16(q->o))
+  if (!q->q || !aligned16(q->q) || (!weigh && (!q->o || !aligned16(q->o))))
     return set_error(STARKV_ERR_INVALID_ARG, "queries: q or o NULL or not 16-byte aligned");
-  if (q->q == q->o) return set_error(STARKV_ERR_INVALID_ARG, "queries: q and o are the same");
+  if (weigh && !q->lse) return set_error(STARKV_ERR_INVALID_ARG, "queries: lse is NULL");
+  if (!weigh && q->q == q->o) return set_error(STARKV_ERR_INVALID_ARG, "queries: q and o are the same");
   if (!aligned4(q->lse) || !aligned4(q->rows) || !aligned4(q->n_tokens))
     return set_error(STARKV_ERR_INVALID_ARG, "queries: lse, rows or n_tokens not 4-byte aligned");
   if (tree && (!q->mask || (reinterpret_cast<uintptr_t>(q->mask) & 7)))
     return set_error(STARKV_ERR_INVALID_ARG, "queries: mask NULL or not 8-byte aligned");
-  for (int64_t x : {q->q_seq_stride, q->q_token_stride, q->q_head_stride, q->o_seq_stride, q->o_token_stride, q->o_head_stride})
+  for (int64_t x : {q->q_seq_stride, q->q_token_stride, q->q_head_stride})
+    if (x < 0 || (x & 7)) return set_error(STARKV_ERR_INVALID_ARG, "queries: strides must be multiples of 8 elements, not negative");
+  if (weigh) return STARKV_OK;
+  for (int64_t x : {q->o_seq_stride, q->o_token_stride, q->o_head_stride})
     if (x < 0 || (x & 7)) return set_error(STARKV_ERR_INVALID_ARG, "queries: strides must be multiples of 8 elements, not negative");
   if (rows_overlap({q->n, q->T, c.n_heads}, {q->o_seq_stride, q->o_token_stride, q->o_head_stride}))
     return set_error(STARKV_ERR_INVALID_ARG, "queries: strides of o let its rows overlap");
@@ -1354,6 +1365,46 @@ starkv_status encode_pages(CUtensorMap* map, const void* base, const PagesView& 
   return STARKV_OK;
 }
 
+uint32_t reciprocal(int n) { return n > 1 ? static_cast<uint32_t>(((uint64_t(1) << 32) + n - 1) / n) : 0u; }
+
+float attention_scale2() { return static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kHeadDim))); }
+
+// What the attention calls have in common (T, the strides and everything that does not change
+// from launch to launch but the query blocks and what is seen).
+starkv_status attn_params(starkv_state* st, const PagesView& pg, int layer, const starkv_queries* q, const PagedWs& w, char* ws,
+                          PagedAttnParams* p) {
+  starkv_status s;
+  if ((s = encode_pages(&p->tmk, pg.k + layer * pg.layer_stride, pg)) != STARKV_OK) return s;
+  if ((s = encode_pages(&p->tmv, pg.v + layer * pg.layer_stride, pg)) != STARKV_OK) return s;
+  p->k = pg.k + layer * pg.layer_stride;
+  p->v = pg.v + layer * pg.layer_stride;
+  p->page_stride = pg.page_stride;
+  p->table = pg.table;
+  p->len = pg.len;
+  p->n_pages = pg.n_pages;
+  p->n_rows = pg.n_rows;
+  p->max_pages = pg.max_pages;
+  p->shift = pg.shift;
+  p->T = q->T;
+  p->q_seq = q->q_seq_stride;
+  p->q_token = q->q_token_stride;
+  p->q_head = q->q_head_stride;
+  p->o_seq = q->o_seq_stride;
+  p->o_token = q->o_token_stride;
+  p->o_head = q->o_head_stride;
+  p->H = st->cfg.n_heads;
+  p->G = st->cfg.n_kv_heads;
+  p->hg = p->H / p->G;
+  p->inv_hg = reciprocal(p->hg);
+  p->scale2 = attention_scale2();
+  p->split = reinterpret_cast<PagedSplit*>(ws);
+  p->part_ml = reinterpret_cast<float2*>(ws + w.ml);
+  p->part_o = reinterpret_cast<float*>(ws + w.o);
+  p->err = st->dev.err;
+  p->wait_ns = st->wait_ns;
+  return STARKV_OK;
+}
+
 starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* q, bool tree,
                               int32_t n_sink, int32_t window, void* workspace, size_t workspace_bytes, void* stream) {
   starkv_status s = validate_pages(st, pages);
@@ -1365,45 +1416,15 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
   const PagedWs w = paged_attn_ws(st);
   if ((s = check_ws(st, workspace, workspace_bytes, w.total)) != STARKV_OK) return s;
   if ((s = get_encoder()) != STARKV_OK) return s;
-  const starkv_config& c = st->cfg;
   const PagesView pg = view_of(st, *pages);
-  char* ws = static_cast<char*>(workspace);
   PagedAttnParams p;
   memset(&p, 0, sizeof(p));
-  if ((s = encode_pages(&p.tmk, pg.k + layer * pg.layer_stride, pg)) != STARKV_OK) return s;
-  if ((s = encode_pages(&p.tmv, pg.v + layer * pg.layer_stride, pg)) != STARKV_OK) return s;
-  p.k = pg.k + layer * pg.layer_stride;
-  p.v = pg.v + layer * pg.layer_stride;
-  p.page_stride = pg.page_stride;
-  p.table = pg.table;
-  p.len = pg.len;
-  p.n_pages = pg.n_pages;
-  p.n_rows = pg.n_rows;
-  p.max_pages = pg.max_pages;
-  p.shift = pg.shift;
-  p.T = q->T;
-  p.q_seq = q->q_seq_stride;
-  p.q_token = q->q_token_stride;
-  p.q_head = q->q_head_stride;
-  p.o_seq = q->o_seq_stride;
-  p.o_token = q->o_token_stride;
-  p.o_head = q->o_head_stride;
-  p.H = c.n_heads;
-  p.G = c.n_kv_heads;
-  p.hg = p.H / p.G;
+  if ((s = attn_params(st, pg, layer, q, w, static_cast<char*>(workspace), &p)) != STARKV_OK) return s;
   p.nblk = (p.T * p.hg + kPagedRows - 1) / kPagedRows;
-  auto reciprocal = [](int n) { return n > 1 ? static_cast<uint32_t>(((uint64_t(1) << 32) + n - 1) / n) : 0u; };
-  p.inv_hg = reciprocal(p.hg);
   p.inv_nblk = reciprocal(p.nblk);
   p.tree = tree;
   p.n_sink = std::min(n_sink, 1 << 25);   // (more than any length)
   p.window = std::min(window, 1 << 25);
-  p.scale2 = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(kHeadDim)));
-  p.split = reinterpret_cast<PagedSplit*>(ws);
-  p.part_ml = reinterpret_cast<float2*>(ws + w.ml);
-  p.part_o = reinterpret_cast<float*>(ws + w.o);
-  p.err = st->dev.err;
-  p.wait_ns = st->wait_ns;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   // as many sequences a launch as it has room for query blocks
   const int per_launch = kPagedItems / p.nblk;
@@ -1421,6 +1442,160 @@ starkv_status paged_attention(starkv_state* st, const starkv_pages* pages, int32
     p.grid = static_cast<int>(std::min<int64_t>(st->num_sms, p.n * p.nblk * max_units * p.G));
     CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_ATTENTION, cs, [&] { return paged_attn_launch(p, cs); }));
     CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_COMBINE, cs, [&] { return paged_combine_launch(p, cs); }));
+  }
+  return STARKV_OK;
+}
+
+// ---- attention mass and page bounds
+
+starkv_status validate_mass(const starkv_state* st, const starkv_pages* pg, const starkv_mass* m) {
+  if (!m) return set_error(STARKV_ERR_INVALID_ARG, "mass is NULL");
+  if (!m->mass || !aligned4(m->mass)) return set_error(STARKV_ERR_INVALID_ARG, "mass: NULL or not 4-byte aligned");
+  if (!(m->decay >= 0.f) || std::isinf(m->decay)) return set_error(STARKV_ERR_INVALID_ARG, "mass: decay must be finite and >= 0");
+  if (m->layer_stride < 0 || m->row_stride < 0 || m->group_stride < 0)
+    return set_error(STARKV_ERR_INVALID_ARG, "mass: strides must not be negative");
+  if (rows_overlap({st->cfg.n_layers, pg->n_rows, st->cfg.n_kv_heads}, {m->layer_stride, m->row_stride, m->group_stride},
+                   static_cast<int64_t>(pg->max_pages) * pg->page_size))
+    return set_error(STARKV_ERR_INVALID_ARG, "mass: strides let rows of max_pages * page_size tokens overlap");
+  return STARKV_OK;
+}
+
+MassView mass_view(const starkv_mass& m) { return MassView{m.mass, m.layer_stride, m.row_stride, m.group_stride}; }
+
+starkv_status attention_mass(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* q, bool tree,
+                             int32_t n_sink, int32_t window, const starkv_mass* mass, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = validate_queries(st, layer, q, tree, true)) != STARKV_OK) return s;
+  if ((s = validate_mass(st, pages, mass)) != STARKV_OK) return s;
+  if (n_sink < 0 || window < 0) return set_error(STARKV_ERR_INVALID_ARG, "n_sink and window must be >= 0");
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if (q->n == 0 || q->T == 0) return STARKV_OK;
+  if ((s = check_ws(st, workspace, workspace_bytes, paged_attn_ws(st).total)) != STARKV_OK) return s;
+  const PagesView pg = view_of(st, *pages);
+  MassParams p;
+  memset(&p, 0, sizeof(p));
+  p.k = pg.k + layer * pg.layer_stride;
+  p.page_stride = pg.page_stride;
+  p.table = pg.table;
+  p.len = pg.len;
+  p.n_pages = pg.n_pages;
+  p.n_rows = pg.n_rows;
+  p.max_pages = pg.max_pages;
+  p.shift = pg.shift;
+  p.q = static_cast<const __nv_bfloat16*>(q->q);
+  p.lse = q->lse;
+  p.mask = q->mask;
+  p.rows = q->rows;
+  p.n_tokens = q->n_tokens;
+  p.n = q->n;
+  p.T = q->T;
+  p.q_seq = q->q_seq_stride;
+  p.q_token = q->q_token_stride;
+  p.q_head = q->q_head_stride;
+  p.H = st->cfg.n_heads;
+  p.G = st->cfg.n_kv_heads;
+  p.hg = p.H / p.G;
+  p.tree = tree;
+  p.n_sink = std::min(n_sink, 1 << 25);   // (more than any length)
+  p.window = std::min(window, 1 << 25);
+  p.scale2 = attention_scale2();
+  p.mass = mass_view(*mass);
+  p.mass.m += layer * mass->layer_stride;
+  p.decay = mass->decay;
+  p.err = st->dev.err;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  CUDA_TRY(launch(st, STARKV_KERNEL_MASS, cs, [&] { return mass_launch(p, st->num_sms, cs); }));
+  return STARKV_OK;
+}
+
+starkv_status validate_bounds(const starkv_state* st, const starkv_pages* pg, const starkv_bounds* b) {
+  if (!b) return set_error(STARKV_ERR_INVALID_ARG, "bounds is NULL");
+  if (!b->b || !aligned16(b->b)) return set_error(STARKV_ERR_INVALID_ARG, "bounds: NULL or not 16-byte aligned");
+  if (b->layer_stride < 0 || b->page_stride < 0 || (b->layer_stride & 7) || (b->page_stride & 7))
+    return set_error(STARKV_ERR_INVALID_ARG, "bounds: strides must be multiples of 8 elements, not negative");
+  if (rows_overlap({st->cfg.n_layers, pg->n_pages}, {b->layer_stride, b->page_stride}, int64_t(2) * st->cfg.n_kv_heads * kHeadDim))
+    return set_error(STARKV_ERR_INVALID_ARG, "bounds: strides let pages overlap");
+  return STARKV_OK;
+}
+
+// ---- attention over chosen pages
+
+// Workspace: that of the attention, then the list of the chosen pages and the scores of all, for as many queries
+// as a launch takes (a bounded share of memory, and the query blocks that the attention has room for).
+struct SparseWs {
+  PagedWs attn;
+  int per_launch, n_list;
+  size_t list, keys, total;
+};
+
+SparseWs sparse_ws(const starkv_state* st, const starkv_pages& p, int n, int T, int n_chosen) {
+  const starkv_config& c = st->cfg;
+  SparseWs w;
+  w.attn = paged_attn_ws(st);
+  w.n_list = std::min(n_chosen, p.max_pages);
+  const int nblk = (c.n_heads / c.n_kv_heads + kPagedRows - 1) / kPagedRows;
+  const int64_t each = static_cast<int64_t>(c.n_kv_heads) * (static_cast<int64_t>(w.n_list) * 4 + static_cast<int64_t>(p.max_pages) * 8);
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kPagedItems / nblk, (int64_t(256) << 20) / each));
+  w.per_launch = static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(1, static_cast<int64_t>(n) * T)));
+  w.list = w.attn.total;
+  w.keys = w.list + align256(static_cast<size_t>(w.per_launch) * c.n_kv_heads * w.n_list * sizeof(int32_t));
+  w.total = w.keys + align256(static_cast<size_t>(w.per_launch) * c.n_kv_heads * p.max_pages * sizeof(uint64_t));
+  return w;
+}
+
+starkv_status compact_pages(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const starkv_seq* seqs, int32_t nseq,
+                            const starkv_mass* mass, void* workspace, size_t workspace_bytes, void* stream) {
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = check_rows(nseq)) != STARKV_OK) return s;
+  if (!aligned4(rows)) return set_error(STARKV_ERR_INVALID_ARG, "rows not 4-byte aligned");
+  if ((s = validate_seqs(st, seqs, nseq, kNeedIdx | kNoSlots)) != STARKV_OK) return s;
+  for (int i = 0; i < nseq; ++i) {
+    if (!seqs[i].meta) continue;
+    if (!seqs[i].meta_out) return set_error(STARKV_ERR_INVALID_ARG, "seq %d: meta without meta_out", i);
+    if ((s = validate_seqs(st, seqs + i, 1, kNeedMeta | kNoSlots)) != STARKV_OK) return s;
+  }
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if ((s = check_ws(st, workspace, workspace_bytes, book_ws(*pages, nseq).total)) != STARKV_OK) return s;
+  const starkv_config& c = st->cfg;
+  const int per_head = c.select_mode == STARKV_SELECT_PER_HEAD;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  if (nseq == 0) return STARKV_OK;
+  const BookParams b = book_params(st, *pages, rows, nseq, static_cast<char*>(workspace));
+  static thread_local BookLens lens;   // 8 KB: kept off the stack
+  for (int i = 0; i < nseq; ++i) {
+    lens.L[i] = seqs[i].L;
+    lens.kept[i] = seqs[i].budget + c.window;
+  }
+  CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_BOOK, cs, [&] { return book_launch(kBookCompact, b, &lens, cs); }));
+  for (int i0 = 0; i0 < nseq; i0 += kMaxBatch) {
+    SeqBatch batch;
+    memset(&batch, 0, sizeof(batch));
+    batch.nseq = std::min(nseq - i0, kMaxBatch);
+    batch.nlayers = c.n_layers;
+    int rows_out = 0;
+    for (int i = 0; i < batch.nseq; ++i) {
+      const starkv_seq& q = seqs[i0 + i];
+      SeqView& v = batch.s[i];
+      v.meta = q.meta;
+      v.meta_layer_stride = q.meta_layer_stride;
+      v.meta_group_stride = q.meta_group_stride;
+      v.L = q.L;
+      v.Lp = q.L - c.window;
+      v.budget = q.budget;
+      v.meta_out = q.meta_out;
+      v.idx = q.idx;
+      rows_out = std::max(rows_out, q.budget + c.window);
+    }
+    if (mass)
+      CUDA_TRY(launch(st, STARKV_KERNEL_MASS_SELECT, cs, [&] {
+        return mass_select_launch(b.pg, batch, rows, i0, c.window, per_head, b.plan, mass_view(*mass), cs);
+      }));
+    CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_GATHER, cs, [&] {
+      return page_gather_launch(b.pg, batch, rows, i0, c.window, per_head, b.plan, b.old_table, rows_out, st->dev.err, cs);
+    }));
   }
   return STARKV_OK;
 }
@@ -1513,53 +1688,16 @@ starkv_status starkv_pages_free(starkv_state* st, const starkv_pages* pages, con
 starkv_status starkv_pages_compact(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const starkv_seq* seqs,
                                    int32_t nseq, void* workspace, size_t workspace_bytes, void* stream) {
   NvtxRange range("starkv_pages_compact");
+  return compact_pages(st, pages, rows, seqs, nseq, nullptr, workspace, workspace_bytes, stream);
+}
+
+starkv_status starkv_pages_evict(starkv_state* st, const starkv_pages* pages, const int32_t* rows, const starkv_seq* seqs,
+                                 int32_t nseq, const starkv_mass* mass, void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange range("starkv_pages_evict");
   starkv_status s = validate_pages(st, pages);
   if (s != STARKV_OK) return s;
-  if ((s = check_rows(nseq)) != STARKV_OK) return s;
-  if (!aligned4(rows)) return set_error(STARKV_ERR_INVALID_ARG, "rows not 4-byte aligned");
-  if ((s = validate_seqs(st, seqs, nseq, kNeedIdx | kNoSlots)) != STARKV_OK) return s;
-  for (int i = 0; i < nseq; ++i) {
-    if (!seqs[i].meta) continue;
-    if (!seqs[i].meta_out) return set_error(STARKV_ERR_INVALID_ARG, "seq %d: meta without meta_out", i);
-    if ((s = validate_seqs(st, seqs + i, 1, kNeedMeta | kNoSlots)) != STARKV_OK) return s;
-  }
-  if ((s = check_device(st)) != STARKV_OK) return s;
-  if ((s = check_ws(st, workspace, workspace_bytes, book_ws(*pages, nseq).total)) != STARKV_OK) return s;
-  const starkv_config& c = st->cfg;
-  cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  if (nseq == 0) return STARKV_OK;
-  const BookParams b = book_params(st, *pages, rows, nseq, static_cast<char*>(workspace));
-  static thread_local BookLens lens;   // 8 KB: kept off the stack
-  for (int i = 0; i < nseq; ++i) {
-    lens.L[i] = seqs[i].L;
-    lens.kept[i] = seqs[i].budget + c.window;
-  }
-  CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_BOOK, cs, [&] { return book_launch(kBookCompact, b, &lens, cs); }));
-  for (int i0 = 0; i0 < nseq; i0 += kMaxBatch) {
-    SeqBatch batch;
-    memset(&batch, 0, sizeof(batch));
-    batch.nseq = std::min(nseq - i0, kMaxBatch);
-    batch.nlayers = c.n_layers;
-    int rows_out = 0;
-    for (int i = 0; i < batch.nseq; ++i) {
-      const starkv_seq& q = seqs[i0 + i];
-      SeqView& v = batch.s[i];
-      v.meta = q.meta;
-      v.meta_layer_stride = q.meta_layer_stride;
-      v.meta_group_stride = q.meta_group_stride;
-      v.L = q.L;
-      v.Lp = q.L - c.window;
-      v.budget = q.budget;
-      v.meta_out = q.meta_out;
-      v.idx = q.idx;
-      rows_out = std::max(rows_out, q.budget + c.window);
-    }
-    CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_GATHER, cs, [&] {
-      return page_gather_launch(b.pg, batch, rows, i0, c.window, c.select_mode == STARKV_SELECT_PER_HEAD, b.plan, b.old_table,
-                                rows_out, st->dev.err, cs);
-    }));
-  }
-  return STARKV_OK;
+  if ((s = validate_mass(st, pages, mass)) != STARKV_OK) return s;
+  return compact_pages(st, pages, rows, seqs, nseq, mass, workspace, workspace_bytes, stream);
 }
 
 starkv_status starkv_pages_store(starkv_state* st, const starkv_pages* pages, int32_t layer0, int32_t n_layers,
@@ -1584,6 +1722,124 @@ starkv_status starkv_sink_attention(starkv_state* st, const starkv_pages* pages,
                                     int32_t n_sink, int32_t window, void* workspace, size_t workspace_bytes, void* stream) {
   NvtxRange range("starkv_sink_attention");
   return paged_attention(st, pages, layer, queries, false, n_sink, window, workspace, workspace_bytes, stream);
+}
+
+starkv_status starkv_tree_mass(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
+                               const starkv_mass* mass, void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange range("starkv_tree_mass");
+  return attention_mass(st, pages, layer, queries, true, 0, 0, mass, workspace, workspace_bytes, stream);
+}
+
+starkv_status starkv_sink_mass(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
+                               int32_t n_sink, int32_t window, const starkv_mass* mass, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  NvtxRange range("starkv_sink_mass");
+  return attention_mass(st, pages, layer, queries, false, n_sink, window, mass, workspace, workspace_bytes, stream);
+}
+
+starkv_status starkv_pages_bounds(starkv_state* st, const starkv_pages* pages, int32_t layer0, int32_t n_layers,
+                                  const starkv_bounds* bounds, const int32_t* rows, const int32_t* n_tokens, int32_t n, int32_t T,
+                                  void* stream) {
+  NvtxRange range("starkv_pages_bounds");
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = validate_bounds(st, pages, bounds)) != STARKV_OK) return s;
+  if ((s = check_rows(n)) != STARKV_OK) return s;
+  if (T < 0) return set_error(STARKV_ERR_INVALID_ARG, "T is negative");
+  if (T > (1 << 24)) return set_error(STARKV_ERR_UNSUPPORTED, "T > 2^24");
+  if (layer0 < 0 || n_layers < 0 || layer0 > st->cfg.n_layers - n_layers)
+    return set_error(STARKV_ERR_INVALID_ARG, "layer range out of range");
+  if (!aligned4(rows) || !aligned4(n_tokens)) return set_error(STARKV_ERR_INVALID_ARG, "rows or n_tokens not 4-byte aligned");
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if (n == 0 || T == 0 || n_layers == 0) return STARKV_OK;
+  const BoundsParams p{view_of(st, *pages), {static_cast<__nv_bfloat16*>(bounds->b), bounds->layer_stride, bounds->page_stride},
+                       rows, n_tokens, n, T, layer0, n_layers, st->dev.err};
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_BOUNDS, cs, [&] { return page_bounds_launch(p, st->num_sms, cs); }));
+  return STARKV_OK;
+}
+
+starkv_status starkv_sparse_workspace_bytes(const starkv_state* st, const starkv_pages* pages, int32_t n, int32_t T, int32_t n_chosen,
+                                            size_t* bytes) {
+  if (!bytes) return set_error(STARKV_ERR_INVALID_ARG, "bytes is NULL");
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = check_rows(n)) != STARKV_OK) return s;
+  if (T < 0) return set_error(STARKV_ERR_INVALID_ARG, "T is negative");
+  if (n_chosen < 1) return set_error(STARKV_ERR_INVALID_ARG, "n_chosen must be >= 1");
+  *bytes = sparse_ws(st, *pages, n, T, n_chosen).total;
+  return STARKV_OK;
+}
+
+starkv_status starkv_sparse_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* q,
+                                      const starkv_bounds* bounds, int32_t n_first, int32_t n_last, int32_t n_chosen, int32_t* chosen,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+  NvtxRange range("starkv_sparse_attention");
+  starkv_status s = validate_pages(st, pages);
+  if (s != STARKV_OK) return s;
+  if ((s = validate_queries(st, layer, q, false)) != STARKV_OK) return s;
+  if ((s = validate_bounds(st, pages, bounds)) != STARKV_OK) return s;
+  if (n_first < 0 || n_last < 1) return set_error(STARKV_ERR_INVALID_ARG, "n_first must be >= 0, n_last >= 1");
+  if (n_chosen < 1 || static_cast<int64_t>(n_first) + n_last > n_chosen)
+    return set_error(STARKV_ERR_INVALID_ARG, "n_chosen must be >= n_first + n_last");
+  if (!aligned4(chosen)) return set_error(STARKV_ERR_INVALID_ARG, "chosen not 4-byte aligned");
+  if ((s = check_device(st)) != STARKV_OK) return s;
+  if (q->n == 0 || q->T == 0) return STARKV_OK;
+  const SparseWs w = sparse_ws(st, *pages, q->n, q->T, n_chosen);
+  if ((s = check_ws(st, workspace, workspace_bytes, w.total)) != STARKV_OK) return s;
+  if ((s = get_encoder()) != STARKV_OK) return s;
+  const PagesView pg = view_of(st, *pages);
+  char* ws = static_cast<char*>(workspace);
+  SparseAttnParams p;
+  memset(&p, 0, sizeof(p));
+  if ((s = attn_params(st, pg, layer, q, w.attn, ws, &p)) != STARKV_OK) return s;
+  p.T = 1;
+  p.nblk = (p.hg + kPagedRows - 1) / kPagedRows;
+  p.inv_nblk = reciprocal(p.nblk);
+  p.window = 1 << 25;   // every token up to the query's own
+  p.q = static_cast<const __nv_bfloat16*>(q->q);
+  p.o = static_cast<__nv_bfloat16*>(q->o);
+  p.rows = q->rows;
+  p.n_tokens = q->n_tokens;
+  p.list = reinterpret_cast<const int32_t*>(ws + w.list);
+  p.n_list = w.n_list;
+  p.tokens = q->T;
+  ChooseParams ch;
+  memset(&ch, 0, sizeof(ch));
+  ch.pg = pg;
+  ch.bounds = static_cast<const __nv_bfloat16*>(bounds->b) + layer * bounds->layer_stride;
+  ch.bounds_page = bounds->page_stride;
+  ch.q = p.q;
+  ch.q_seq = p.q_seq;
+  ch.q_token = p.q_token;
+  ch.q_head = p.q_head;
+  ch.rows = q->rows;
+  ch.n_tokens = q->n_tokens;
+  ch.T = q->T;
+  ch.G = p.G;
+  ch.hg = p.hg;
+  ch.n_first = n_first;
+  ch.n_last = n_last;
+  ch.n_list = w.n_list;
+  ch.list = reinterpret_cast<int32_t*>(ws + w.list);
+  ch.chosen = chosen;
+  ch.n_chosen = n_chosen;
+  ch.keys = reinterpret_cast<uint64_t*>(ws + w.keys);
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  const int64_t items = static_cast<int64_t>(q->n) * q->T;
+  if (items >= (int64_t(1) << 31)) return set_error(STARKV_ERR_UNSUPPORTED, "queries: n * T >= 2^31");
+  const int64_t max_units = (static_cast<int64_t>(w.n_list) << pg.shift) / kPagedUnitKeys + 2;
+  for (int64_t i0 = 0; i0 < items; i0 += w.per_launch) {
+    const int m = static_cast<int>(std::min<int64_t>(items - i0, w.per_launch));
+    ch.item0 = p.item0 = static_cast<int>(i0);
+    ch.items = p.n = m;
+    p.lse = q->lse ? q->lse + i0 * p.H : nullptr;
+    p.grid = static_cast<int>(std::min<int64_t>(st->num_sms, m * p.nblk * max_units * p.G));
+    CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_CHOOSE, cs, [&] { return page_choose_launch(ch, cs); }));
+    CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_ATTENTION, cs, [&] { return paged_attn_launch(p, cs); }));
+    CUDA_TRY(launch(st, STARKV_KERNEL_PAGED_COMBINE, cs, [&] { return paged_combine_launch(p, cs); }));
+  }
+  return STARKV_OK;
 }
 
 }  // extern "C"

@@ -68,6 +68,7 @@
 #include "common.cuh"
 #include "paged_attn.cuh"
 #include "ptx.cuh"
+#include "sparse.cuh"
 
 namespace starkv {
 
@@ -236,6 +237,41 @@ struct Block {
   }
 };
 
+// Where a launch finds a sequence's pages, queries and outputs.  Attention over chosen pages
+// takes every query of the call as a sequence of one, with the pages chosen for it.
+__device__ __forceinline__ const int32_t* entries_of(const PagedAttnParams& p, int seq, int) {
+  const int row = p.rows ? p.rows[seq] : p.row0 + seq;
+  return p.table + static_cast<int64_t>(row) * p.max_pages;
+}
+__device__ __forceinline__ const int32_t* entries_of(const SparseAttnParams& p, int seq, int g) {
+  return p.list + (static_cast<int64_t>(seq) * p.G + g) * p.n_list;
+}
+
+__device__ __forceinline__ int64_t q_at(const PagedAttnParams& p, int seq, int t, int h) {
+  return seq * p.q_seq + t * p.q_token + h * p.q_head;
+}
+__device__ __forceinline__ int64_t o_at(const PagedAttnParams& p, int seq, int t, int h) {
+  return seq * p.o_seq + t * p.o_token + h * p.o_head;
+}
+__device__ __forceinline__ int64_t q_at(const SparseAttnParams& p, int item, int, int h) {
+  const int v = p.item0 + item, seq = v / p.tokens;
+  return seq * p.q_seq + (v - seq * p.tokens) * p.q_token + h * p.q_head;
+}
+__device__ __forceinline__ int64_t o_at(const SparseAttnParams& p, int item, int, int h) {
+  const int v = p.item0 + item, seq = v / p.tokens;
+  return seq * p.o_seq + (v - seq * p.tokens) * p.o_token + h * p.o_head;
+}
+
+// A query of a call over chosen pages: a sequence of the tokens that these hold up to its own.
+__device__ Item read_item(const SparseAttnParams& p, int item) {
+  const SparseQuery q = sparse_query(p.rows, p.n_tokens, p.len, p.n_rows, p.max_pages, p.shift, p.tokens, p.item0 + item);
+  if (q.wrong) atomicOr(p.err, kErrRow);
+  if (!q.live) return Item{-1, 0};
+  if (q.pos < 0) return Item{-1, 1};
+  const int pages = min((q.pos >> p.shift) + 1, p.n_list);
+  return Item{((pages - 1) << p.shift) + (q.pos & ((1 << p.shift) - 1)) + 1, 1};
+}
+
 // A sequence's length and queries (read by every CTA: the call may be replayed).
 __device__ Item read_item(const PagedAttnParams& p, int seq) {
   const int row = p.rows ? p.rows[seq] : p.row0 + seq;
@@ -253,7 +289,8 @@ __device__ Item read_item(const PagedAttnParams& p, int seq) {
 }
 
 // Whether the launch goes in gangs, and the units before each item.
-__device__ void count_units(const PagedAttnParams& p, Ctl* ctl) {
+template <class Params>
+__device__ void count_units(const Params& p, Ctl* ctl) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (p.tree && p.nblk > 1) {
     // A gang of B (the most blocks of a sequence) leaves CTAs idle at sequences with fewer.
@@ -407,7 +444,8 @@ struct Share {
 
 // K or V loader: the units' pages into a ring.  Lane l holds the number of page
 // base + l of the row, so that the table is read once in 32 pages.
-__device__ void load_loop(const PagedAttnParams& p, Ctl* ctl, const CUtensorMap* map, uint8_t* ring, uint64_t* full,
+template <class Params>
+__device__ void load_loop(const Params& p, Ctl* ctl, const CUtensorMap* map, uint8_t* ring, uint64_t* full,
                           uint64_t* empty, int lane, const Share& sh) {
   const uint64_t pol = policy_evict_first();   // a single query block reads K and V once
   const bool once = p.nblk == 1;
@@ -419,8 +457,7 @@ __device__ void load_loop(const PagedAttnParams& p, Ctl* ctl, const CUtensorMap*
   bool ok = true;
   for (PieceIter c(p, ctl, sh.member, sh.fb, sh.fe); ok && c.valid(); c.next(p, ctl)) {
     const Block blk = c.block(p, ctl);
-    const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
-    const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
+    const int32_t* entries = entries_of(p, blk.seq, c.g);
     const int held = blk.L < 0 ? 0 : (blk.L + P - 1) >> p.shift;
     int base = 0, have = 0, id = 0;
     for (int j = c.j0; ok && j < c.j0 + c.n; ++j) {
@@ -711,11 +748,11 @@ __device__ __forceinline__ float weighted(float w, float x) { return is_inf(x) ?
 // so that a column with a V of infinity comes to infinity, with both or a NaN to NaN, whatever the weights
 // (products of their parts say otherwise where a part is 0: 0 * infinity).  Columns col .. col + 63 of the
 // staged rows `which`, by the whole warp, each lane two columns over all keys.
-__device__ __noinline__ void settle_columns(const PagedAttnParams& p, Ctl* ctl, const Block& blk, int g, int j0, int n, int col, uint32_t which,
+template <class Params>
+__device__ __noinline__ void settle_columns(const Params& p, Ctl* ctl, const Block& blk, int g, int j0, int n, int col, uint32_t which,
                                             float* stage) {
   const int lane = threadIdx.x & 31;
-  const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
-  const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
+  const int32_t* entries = entries_of(p, blk.seq, g);
   float2 sum = make_float2(0.f, 0.f);   // of the column's infinities and NaNs: 0 where it has none
   for (int j = j0; j < j0 + n; ++j) {
     const int k0 = blk.key(j);
@@ -749,16 +786,16 @@ __device__ __noinline__ void settle_columns(const PagedAttnParams& p, Ctl* ctl, 
 // time, skipping the keys that the row does not see.  Against the reference `top` of the
 // row (lane i: row i), times `norm` (the same).  Some microseconds a row and 64 keys, so that
 // every unit is a sign of life for the roles that wait.
-__device__ __noinline__ void recompute_rows(const PagedAttnParams& p, Ctl* ctl, const Block& blk, int g, int j0, int n, int r0, int col, uint32_t which,
+template <class Params>
+__device__ __noinline__ void recompute_rows(const Params& p, Ctl* ctl, const Block& blk, int g, int j0, int n, int r0, int col, uint32_t which,
                                             float top, float norm, float* stage) {
   const int lane = threadIdx.x & 31;
-  const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
-  const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
+  const int32_t* entries = entries_of(p, blk.seq, g);
   for (; which; which &= which - 1) {
     const int i = __ffs(which) - 1;
     const int t = quotient(blk.row0 + r0 + i, p.inv_hg), h = g * p.hg + blk.row0 + r0 + i - t * p.hg;
     const Seen see = blk.row(p, blk.L - blk.n + t, p.tree ? p.mask[static_cast<int64_t>(blk.seq) * p.T + t] : 0);
-    const float4 q = bf16x4(p.q + blk.seq * p.q_seq + t * p.q_token + h * p.q_head + 4 * lane);
+    const float4 q = bf16x4(p.q + q_at(p, blk.seq, t, h) + 4 * lane);
     const float ref = __shfl_sync(kFull, top, i), scale = __shfl_sync(kFull, norm, i);
     float2 acc = make_float2(0.f, 0.f);
     for (int j = j0; j < j0 + n; ++j) {
@@ -800,16 +837,16 @@ __device__ __noinline__ void recompute_rows(const PagedAttnParams& p, Ctl* ctl, 
 
 // Rows `which` of a warp's 32 (from row r0 of the block on), whose largest logit is +inf: those with a logit
 // that is NaN among the piece's keys, as bits.  (Their sums are NaN either way: inf - inf.)
-__device__ __noinline__ uint32_t rows_with_nan(const PagedAttnParams& p, Ctl* ctl, const Block& blk, int g, int j0, int n, int r0, uint32_t which) {
+template <class Params>
+__device__ __noinline__ uint32_t rows_with_nan(const Params& p, Ctl* ctl, const Block& blk, int g, int j0, int n, int r0, uint32_t which) {
   const int lane = threadIdx.x & 31;
-  const int row = p.rows ? p.rows[blk.seq] : p.row0 + blk.seq;
-  const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
+  const int32_t* entries = entries_of(p, blk.seq, g);
   uint32_t found = 0;
   for (; which; which &= which - 1) {
     const int i = __ffs(which) - 1;
     const int t = quotient(blk.row0 + r0 + i, p.inv_hg), h = g * p.hg + blk.row0 + r0 + i - t * p.hg;
     const Seen see = blk.row(p, blk.L - blk.n + t, p.tree ? p.mask[static_cast<int64_t>(blk.seq) * p.T + t] : 0);
-    const float4 q = bf16x4(p.q + blk.seq * p.q_seq + t * p.q_token + h * p.q_head + 4 * lane);
+    const float4 q = bf16x4(p.q + q_at(p, blk.seq, t, h) + 4 * lane);
     for (int j = j0; j < j0 + n; ++j) {
       const int k0 = blk.key(j);
       if (lane == 0) atomicAdd(const_cast<int*>(&ctl->beat), 1);
@@ -841,7 +878,8 @@ __device__ __noinline__ uint32_t rows_with_nan(const PagedAttnParams& p, Ctl* ct
 
 // Softmax warps of a line (0: even units, 1: odd): one thread per query row (TMEM lane
 // quad * 32 + lane).
-__device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, float* stage_o, uint32_t tmem, int line, int quad, int lane,
+template <class Params>
+__device__ void softmax_loop(const Params& p, Ctl* ctl, uint8_t* sV, float* stage_o, uint32_t tmem, int line, int quad, int lane,
                              const Share& sh) {
   const int r = quad * 32 + lane;
   const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
@@ -853,7 +891,7 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
     if (quad * 32 < blk.nrows) {
       const bool live = r < blk.nrows;
       const int t = quotient(blk.row0 + r, p.inv_hg), h = c.g * p.hg + blk.row0 + r - t * p.hg;
-      const uint4* src = reinterpret_cast<const uint4*>(p.q + blk.seq * p.q_seq + t * p.q_token + h * p.q_head);
+      const uint4* src = reinterpret_cast<const uint4*>(p.q + q_at(p, blk.seq, t, h));
       uint4 w[16];   // every load before the first use
 #pragma unroll
       for (int i = 0; i < 16; ++i) w[i] = live ? src[i] : make_uint4(0u, 0u, 0u, 0u);
@@ -985,7 +1023,7 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
       __syncwarp();
       const int rows = min(32, blk.nrows - quad * 32);
       if (whole) {
-        const int64_t at = blk.seq * p.o_seq + t * p.o_token + h * p.o_head + 64 * line;   // this lane's row
+        const int64_t at = o_at(p, blk.seq, t, h) + 64 * line;   // this lane's row
 #pragma unroll 4
         for (int i = lane >> 3; i < 32; i += 4) {   // eight lanes a row, eight columns each
           const int64_t to = __shfl_sync(kFull, at, i);
@@ -1017,7 +1055,8 @@ __device__ void softmax_loop(const PagedAttnParams& p, Ctl* ctl, uint8_t* sV, fl
 
 }  // namespace
 
-__global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constant__ PagedAttnParams p) {
+template <class Params>
+__global__ void __launch_bounds__(kThreads, 1) k_paged_attn(const __grid_constant__ Params p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sK = smem;                           // [kStages][2 halves][64 keys][128 B]
@@ -1116,8 +1155,8 @@ __device__ __forceinline__ float4 scaled(float w, const float4& o) {
 }
 __device__ __forceinline__ float4 sum_of(const float4& a, const float4& b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 
-template <int WARPS>
-__global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ PagedAttnParams p) {
+template <int WARPS, class Params>
+__global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ Params p) {
   __shared__ float2 s_ml[8];
   __shared__ float4 s_o[8][32];
   griddep_launch_dependents();
@@ -1184,7 +1223,7 @@ __global__ void __launch_bounds__(256) k_paged_combine(const __grid_constant__ P
     inv = blk.row(p, blk.L - blk.n + t, p.tree ? p.mask[static_cast<int64_t>(s.seq) * p.T + t] : 0).none() ? 0.f : NAN;
   }
   const __nv_bfloat162 x[2] = {__floats2bfloat162_rn(acc.x * inv, acc.y * inv), __floats2bfloat162_rn(acc.z * inv, acc.w * inv)};
-  *reinterpret_cast<uint2*>(p.o + s.seq * p.o_seq + t * p.o_token + h * p.o_head + lane * 4) = *reinterpret_cast<const uint2*>(x);
+  *reinterpret_cast<uint2*>(p.o + o_at(p, s.seq, t, h) + lane * 4) = *reinterpret_cast<const uint2*>(x);
   if (p.lse && lane == 0)
     p.lse[(static_cast<int64_t>(s.seq) * p.T + t) * p.H + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
@@ -1210,16 +1249,22 @@ cudaLaunchConfig_t config(cudaLaunchAttribute* attr, dim3 grid, int threads, siz
 }  // namespace
 
 cudaError_t paged_attn_configure() {
-  return cudaFuncSetAttribute(k_paged_attn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  const cudaError_t e = cudaFuncSetAttribute(k_paged_attn<PagedAttnParams>, attr, static_cast<int>(kSmemBytes));
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(k_paged_attn<SparseAttnParams>, attr, static_cast<int>(kSmemBytes));
 }
 
-cudaError_t paged_attn_launch(const PagedAttnParams& p, cudaStream_t stream) {
+namespace {
+
+template <class Params>
+cudaError_t attn_launch(const Params& p, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
   cudaLaunchConfig_t cfg = config(attr, dim3(p.grid), kThreads, kSmemBytes, stream);
-  return cudaLaunchKernelEx(&cfg, k_paged_attn, p);
+  return cudaLaunchKernelEx(&cfg, k_paged_attn<Params>, p);
 }
 
-cudaError_t paged_combine_launch(const PagedAttnParams& p, cudaStream_t stream) {
+template <class Params>
+cudaError_t combine_launch(const Params& p, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
   // one warp a row, but four where few rows meet more than 16 parts: one tree of 8 tokens (56
   // rows, 38 parts) 16.9 us so, 19.8 with one; of 18 (126 rows) 23.3 with four, 21.5 with one; four
@@ -1228,7 +1273,14 @@ cudaError_t paged_combine_launch(const PagedAttnParams& p, cudaStream_t stream) 
   const bool many = p.n * p.nblk * p.G * 16 >= p.grid || rows > 64;
   const int per = many ? 8 : 2;
   cudaLaunchConfig_t cfg = config(attr, dim3(p.grid, (rows + per - 1) / per), 256, 0, stream);
-  return cudaLaunchKernelEx(&cfg, many ? k_paged_combine<1> : k_paged_combine<4>, p);
+  return cudaLaunchKernelEx(&cfg, many ? k_paged_combine<1, Params> : k_paged_combine<4, Params>, p);
 }
+
+}  // namespace
+
+cudaError_t paged_attn_launch(const PagedAttnParams& p, cudaStream_t stream) { return attn_launch(p, stream); }
+cudaError_t paged_attn_launch(const SparseAttnParams& p, cudaStream_t stream) { return attn_launch(p, stream); }
+cudaError_t paged_combine_launch(const PagedAttnParams& p, cudaStream_t stream) { return combine_launch(p, stream); }
+cudaError_t paged_combine_launch(const SparseAttnParams& p, cudaStream_t stream) { return combine_launch(p, stream); }
 
 }  // namespace starkv

@@ -49,8 +49,18 @@ struct PagedAttnParams {
   uint64_t wait_ns;
 };
 
+// Attention over chosen pages: query item0 + i of the call's n * tokens is sequence i of the
+// launch, of one token (n: queries of the launch, T = 1, strides and rows those of the call).
+struct SparseAttnParams : PagedAttnParams {
+  const int32_t* list;   // [n][G][n_list] page numbers, in the order of their tokens
+  int n_list;
+  int tokens, item0;
+};
+
 cudaError_t paged_attn_configure();
 cudaError_t paged_attn_launch(const PagedAttnParams& p, cudaStream_t stream);
+cudaError_t paged_attn_launch(const SparseAttnParams& p, cudaStream_t stream);
 cudaError_t paged_combine_launch(const PagedAttnParams& p, cudaStream_t stream);
+cudaError_t paged_combine_launch(const SparseAttnParams& p, cudaStream_t stream);
 
 }  // namespace starkv

@@ -9,6 +9,17 @@ constexpr int kMaxPages = 1 << 20;       // pages of a pool (the free-page bits 
 constexpr int kMaxTableRows = 1 << 16;   // rows of a page table
 constexpr int kMaxCallRows = 1024;       // rows of one call (one per thread of a bookkeeping block)
 
+// (Not the read-only path: the pages' kernels start while the ones before them still write the pool, and copies
+// within it.)
+__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p)
+               : "memory");
+  return v;
+}
+
 // The pool and its table as the kernels see them (starkv_pages).
 struct PagesView {
   __nv_bfloat16* k;

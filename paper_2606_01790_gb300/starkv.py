@@ -33,10 +33,13 @@ ABI_FUNCTIONS = [
     "starkv_pages_workspace_bytes", "starkv_pages_reset", "starkv_pages_extend", "starkv_pages_fork",
     "starkv_pages_free", "starkv_pages_compact", "starkv_pages_store", "starkv_pages_load",
     "starkv_tree_attention", "starkv_sink_attention",
+    "starkv_tree_mass", "starkv_sink_mass", "starkv_pages_evict", "starkv_pages_bounds",
+    "starkv_sparse_workspace_bytes", "starkv_sparse_attention",
 ]
 
 KERNELS = ["score_lse", "score_accum", "pool", "calibrate", "compact", "attention", "attn_combine",
-           "page_book", "page_copy", "page_gather", "page_move", "paged_attention", "paged_combine"]
+           "page_book", "page_copy", "page_gather", "page_move", "paged_attention", "paged_combine",
+           "mass", "mass_select", "page_bounds", "page_choose"]
 
 
 SELECT_GLOBAL, SELECT_PER_HEAD = 0, 1   # starkv_config.select_mode
@@ -84,6 +87,15 @@ class CQueries(C.Structure):
                 ("rows", C.c_void_p), ("n_tokens", C.c_void_p), ("n", C.c_int32), ("T", C.c_int32),
                 ("q_seq_stride", C.c_int64), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
                 ("o_seq_stride", C.c_int64), ("o_token_stride", C.c_int64), ("o_head_stride", C.c_int64)]
+
+
+class CMass(C.Structure):
+    _fields_ = [("mass", C.c_void_p), ("layer_stride", C.c_int64), ("row_stride", C.c_int64), ("group_stride", C.c_int64),
+                ("decay", C.c_float)]
+
+
+class CBounds(C.Structure):
+    _fields_ = [("b", C.c_void_p), ("layer_stride", C.c_int64), ("page_stride", C.c_int64)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -147,6 +159,14 @@ def lib() -> C.CDLL:
             getattr(L, name).argtypes = [st, pg, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]
         L.starkv_tree_attention.argtypes = [st, pg, C.c_int32, C.c_void_p] + ws
         L.starkv_sink_attention.argtypes = [st, pg, C.c_int32, C.c_void_p, C.c_int32, C.c_int32] + ws
+        L.starkv_tree_mass.argtypes = [st, pg, C.c_int32, C.c_void_p, C.c_void_p] + ws
+        L.starkv_sink_mass.argtypes = [st, pg, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p] + ws
+        L.starkv_pages_evict.argtypes = [st, pg, C.c_void_p, C.POINTER(CSeq), C.c_int32, C.c_void_p] + ws
+        L.starkv_pages_bounds.argtypes = [st, pg, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                          C.c_void_p]
+        L.starkv_sparse_workspace_bytes.argtypes = [st, pg, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        L.starkv_sparse_attention.argtypes = [st, pg, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                                              C.c_void_p] + ws
         L.starkv_last_error.argtypes = []
         L.starkv_last_error.restype = C.c_char_p
         for name in ABI_FUNCTIONS:
@@ -521,12 +541,12 @@ class Tokens:
 
 @dataclass
 class Queries:
-    """Queries of ``tree_attention`` and ``sink_attention`` (``starkv_queries``)."""
+    """Queries of the attention calls and of the mass calls (``starkv_queries``)."""
 
     q: torch.Tensor                          # bf16 [n][T][H][d], any strides with d contiguous
-    o: torch.Tensor                          # bf16, the same shape
-    lse: Optional[torch.Tensor] = None       # f32 [n][T][H]
-    mask: Optional[torch.Tensor] = None      # i64 [n][T] (the bits of the u64 words), tree attention only
+    o: Optional[torch.Tensor] = None         # bf16, the same shape (attention; the mass calls do not look at it)
+    lse: Optional[torch.Tensor] = None       # f32 [n][T][H] (the mass calls read it)
+    mask: Optional[torch.Tensor] = None      # i64 [n][T] (the bits of the u64 words), tree calls only
     rows: Optional[torch.Tensor] = None      # i32 [n], or None: rows 0, 1, ...
     n_tokens: Optional[torch.Tensor] = None  # i32 [n], or None: T each
 
@@ -586,9 +606,13 @@ def _c_tokens(st: State, pages: Pages, tok: Tokens) -> bytes:
                         s0 if n > 1 else d, s1 if nl > 1 else d, s2 if T > 1 else d, s3 if G > 1 else d)
 
 
-def _c_queries(st: State, pages: Pages, qs: Queries) -> bytes:
+def _c_queries(st: State, pages: Pages, qs: Queries, weigh: bool = False) -> bytes:
     q, o, lse, mask, rows, count = qs.q, qs.o, qs.lse, qs.mask, qs.rows, qs.n_tokens
-    if q.dim() != 4 or o.shape != q.shape:
+    if weigh:     # (a mass call does not look at o)
+        o = q
+        if lse is None:
+            raise ValueError("queries: lse is missing")
+    if q.dim() != 4 or o is None or o.shape != q.shape:
         raise ValueError("queries: q is [n, T, H, d], o of the same shape")
     n, T, H, d = q.shape
     s0, s1, s2, s3 = q.stride()
@@ -726,3 +750,116 @@ def sink_attention(st: State, pages: Pages, layer: int, queries: Queries, n_sink
     _on(pages, ws)
     _check(lib().starkv_sink_attention(st.handle, c, layer, q, n_sink, window, _ptr(ws),
                                        ws.numel(), _stream_on(pages, stream)))
+
+
+# ---------------------------------------------------------------- attention mass, chosen pages
+
+class Mass:
+    """What each cached token has had of the queries' attention (``starkv_mass``).
+
+    data   f32 [n_layers][n_rows][G][tokens], tokens contiguous, max_pages * page_size of them or more
+    decay  factor of what a token has had so far, when a call adds to it
+    """
+
+    __slots__ = ("data", "decay", "_packed")
+
+    def __init__(self, data: torch.Tensor, decay: float = 1.0):
+        if data.dim() != 4 or data.stride(3) != 1:
+            raise ValueError("mass: data is [n_layers, n_rows, G, tokens] with the tokens contiguous")
+        _expect(torch.float32, data)
+        self.data, self.decay = data, float(decay)
+        # (an axis of one entry is never stepped along: its stride may be any)
+        strides = [s if n > 1 else data.shape[3] for n, s in zip(data.shape[:3], data.stride()[:3])]
+        self._packed = bytes(CMass(data.data_ptr(), *strides, self.decay))
+
+
+def make_mass(st: State, pages: Pages, decay: float = 1.0) -> Mass:
+    """A mass for the rows of ``pages`` (the calls that add to it start new tokens at 0)."""
+    rows, max_pages = pages.table.shape
+    return Mass(torch.zeros((st.cfg.n_layers, rows, st.cfg.n_kv_heads, max_pages * pages.k.shape[3]), dtype=torch.float32,
+                            device=pages.k.device), decay)
+
+
+def _c_mass(st: State, pages: Pages, mass: Mass) -> bytes:
+    data = mass.data
+    if data.shape[:3] != (st.cfg.n_layers, pages.table.shape[0], st.cfg.n_kv_heads) \
+            or data.shape[3] < pages.table.shape[1] * pages.k.shape[3]:
+        raise ValueError("mass: data is [n_layers, n_rows, G, max_pages * page_size or more]")
+    _on(pages, data)
+    return mass._packed
+
+
+def tree_mass(st: State, pages: Pages, layer: int, queries: Queries, mass: Mass, ws: torch.Tensor, stream=None) -> None:
+    """Adds the weights of ``tree_attention`` with the same queries (their ``lse`` as it wrote it) to ``mass``."""
+    c, q, m = _c_pages(st, pages), _c_queries(st, pages, queries, True), _c_mass(st, pages, mass)
+    _on(pages, ws)
+    _check(lib().starkv_tree_mass(st.handle, c, layer, q, m, _ptr(ws), ws.numel(), _stream_on(pages, stream)))
+
+
+def sink_mass(st: State, pages: Pages, layer: int, queries: Queries, n_sink: int, window: int, mass: Mass, ws: torch.Tensor,
+              stream=None) -> None:
+    """Adds the weights of ``sink_attention`` with the same queries (their ``lse`` as it wrote it) to ``mass``."""
+    c, q, m = _c_pages(st, pages), _c_queries(st, pages, queries, True), _c_mass(st, pages, mass)
+    _on(pages, ws)
+    _check(lib().starkv_sink_mass(st.handle, c, layer, q, n_sink, window, m, _ptr(ws), ws.numel(), _stream_on(pages, stream)))
+
+
+def pages_evict(st: State, pages: Pages, rows: Optional[torch.Tensor], seqs: Sequence[Seq], mass: Mass, ws: torch.Tensor,
+                stream=None) -> None:
+    """Every layer of ``rows[i]`` keeps the ``seqs[i].budget`` past tokens of greatest mass (written to ``seqs[i].idx``) and
+    the window; their mass moves with them."""
+    c, m = _c_pages(st, pages), _c_mass(st, pages, mass)
+    _on(pages, rows, ws, *(t for s in seqs for t in (s.idx, s.meta, s.meta_out)))
+    for i, s in enumerate(seqs):
+        _check_kept(st.cfg, i, s)
+    _check(lib().starkv_pages_evict(st.handle, c, _ids(rows, len(seqs), "rows"), _seq_array(seqs), len(seqs), m,
+                                    _ptr(ws), ws.numel(), _stream_on(pages, stream)))
+
+
+def make_bounds(st: State, pages: Pages) -> torch.Tensor:
+    """Room for the bounds of every page: bf16 [n_layers][n_pages][G][2][d], least keys first."""
+    return torch.empty((st.cfg.n_layers, pages.k.shape[1], st.cfg.n_kv_heads, 2, st.cfg.head_dim), dtype=torch.bfloat16,
+                       device=pages.k.device)
+
+
+def _c_bounds(st: State, pages: Pages, bounds: torch.Tensor) -> bytes:
+    G, d = st.cfg.n_kv_heads, st.cfg.head_dim
+    if tuple(bounds.shape) != (st.cfg.n_layers, pages.k.shape[1], G, 2, d) or bounds.stride()[2:] != (2 * d, d, 1):
+        raise ValueError("bounds: [n_layers, n_pages, G, 2, d], a page of a layer contiguous")
+    _expect(torch.bfloat16, bounds)
+    _on(pages, bounds)
+    strides = [s if n > 1 else 2 * G * d for n, s in zip(bounds.shape[:2], bounds.stride()[:2])]
+    return bytes(CBounds(bounds.data_ptr(), *strides))
+
+
+def pages_bounds(st: State, pages: Pages, layer0: int, n_layers: int, bounds: torch.Tensor, T: int,
+                 rows: Optional[torch.Tensor] = None, n_tokens: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Bounds of the pages that hold the last ``n_tokens[i]`` (at most ``T``; None: ``T``) tokens of ``rows[i]`` (None: of
+    every row)."""
+    c, b = _c_pages(st, pages), _c_bounds(st, pages, bounds)
+    n = rows.numel() if rows is not None else n_tokens.numel() if n_tokens is not None else pages.table.shape[0]
+    _on(pages, rows, n_tokens)
+    _check(lib().starkv_pages_bounds(st.handle, c, layer0, n_layers, b, _ids(rows, n, "rows"), _ids(n_tokens, n, "n_tokens"), n, T,
+                                     _stream_on(pages, stream)))
+
+
+def sparse_workspace(st: State, pages: Pages, n: int, T: int, n_chosen: int) -> torch.Tensor:
+    """Workspace for ``sparse_attention`` over at most ``n`` rows, ``T`` queries of each and ``n_chosen`` pages."""
+    b = C.c_size_t()
+    _check(lib().starkv_sparse_workspace_bytes(st.handle, _c_pages(st, pages), n, T, n_chosen, C.byref(b)))
+    return torch.empty(int(b.value), dtype=torch.uint8, device=pages.k.device)
+
+
+def sparse_attention(st: State, pages: Pages, layer: int, queries: Queries, bounds: torch.Tensor, n_first: int, n_last: int,
+                     n_chosen: int, ws: torch.Tensor, chosen_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Causal attention of each query over ``n_chosen`` pages per KV head: the first ``n_first``, the last ``n_last`` and
+    the best of the others by their bounds (``chosen_out``, i32 [n][T][G][n_chosen]: their places in the row)."""
+    c, q, b = _c_pages(st, pages), _c_queries(st, pages, queries), _c_bounds(st, pages, bounds)
+    _on(pages, ws, chosen_out)
+    if chosen_out is not None:
+        _expect(torch.int32, chosen_out)
+        n, T = queries.q.shape[:2]
+        if tuple(chosen_out.shape) != (n, T, st.cfg.n_kv_heads, n_chosen):
+            raise ValueError("chosen_out: [n, T, G, n_chosen]")
+    _check(lib().starkv_sparse_attention(st.handle, c, layer, q, b, n_first, n_last, n_chosen, _ptr(chosen_out), _ptr(ws), ws.numel(),
+                                         _stream_on(pages, stream)))
