@@ -613,10 +613,11 @@ enum {
   STARKV_KERNEL_PAGED_ATTENTION = 11,  /* tree, sink and sparse attention                  */
   STARKV_KERNEL_PAGED_COMBINE = 12,    /* merge of its parts                               */
   STARKV_KERNEL_MASS = 13,             /* attention mass                                   */
-  STARKV_KERNEL_MASS_SELECT = 14,      /* tokens that stay by it                           */
-  STARKV_KERNEL_PAGE_BOUNDS = 15,      /* least and greatest keys of pages                 */
-  STARKV_KERNEL_PAGE_CHOOSE = 16,      /* pages that queries attend over                   */
-  STARKV_NUM_KERNELS = 17
+  STARKV_KERNEL_MASS_SUM = 14,         /* sum of its parts (many queries)                  */
+  STARKV_KERNEL_MASS_SELECT = 15,      /* tokens that stay by it                           */
+  STARKV_KERNEL_PAGE_BOUNDS = 16,      /* least and greatest keys of pages                 */
+  STARKV_KERNEL_PAGE_CHOOSE = 17,      /* pages that queries attend over                   */
+  STARKV_NUM_KERNELS = 18
 };
 
 /* Kernel timing, a profiling aid.  While `on` is non-zero every kernel launch

@@ -149,6 +149,7 @@ const char* kernel_range_name(int kind) {
     case STARKV_KERNEL_PAGED_ATTENTION: return "starkv: paged attention";
     case STARKV_KERNEL_PAGED_COMBINE: return "starkv: paged attention (combine)";
     case STARKV_KERNEL_MASS: return "starkv: attention mass";
+    case STARKV_KERNEL_MASS_SUM: return "starkv: attention mass (parts)";
     case STARKV_KERNEL_MASS_SELECT: return "starkv: choice by mass";
     case STARKV_KERNEL_PAGE_BOUNDS: return "starkv: page bounds";
     case STARKV_KERNEL_PAGE_CHOOSE: return "starkv: choice of pages";
@@ -643,6 +644,7 @@ starkv_status starkv_init_state(const starkv_config* cfg, starkv_state** out, vo
   if (e == cudaSuccess) e = select_configure();
   if (e == cudaSuccess) e = attn_configure();
   if (e == cudaSuccess) e = pages_configure();
+  if (e == cudaSuccess) e = mass_configure();
   if (e == cudaSuccess) e = paged_attn_configure();
   if (e != cudaSuccess) {
     delete st;
@@ -1472,12 +1474,13 @@ starkv_status attention_mass(starkv_state* st, const starkv_pages* pages, int32_
   if (n_sink < 0 || window < 0) return set_error(STARKV_ERR_INVALID_ARG, "n_sink and window must be >= 0");
   if ((s = check_device(st)) != STARKV_OK) return s;
   if (q->n == 0 || q->T == 0) return STARKV_OK;
-  if ((s = check_ws(st, workspace, workspace_bytes, paged_attn_ws(st).total)) != STARKV_OK) return s;
+  const size_t parts = align256(static_cast<size_t>(st->num_sms) * sizeof(MassSplit));
+  if ((s = check_ws(st, workspace, workspace_bytes, paged_attn_ws(st).total)) != STARKV_OK) return s;   // (more than it takes)
+  if ((s = get_encoder()) != STARKV_OK) return s;
   const PagesView pg = view_of(st, *pages);
   MassParams p;
   memset(&p, 0, sizeof(p));
-  p.k = pg.k + layer * pg.layer_stride;
-  p.page_stride = pg.page_stride;
+  if ((s = encode_pages(&p.tmk, pg.k + layer * pg.layer_stride, pg)) != STARKV_OK) return s;
   p.table = pg.table;
   p.len = pg.len;
   p.n_pages = pg.n_pages;
@@ -1497,6 +1500,13 @@ starkv_status attention_mass(starkv_state* st, const starkv_pages* pages, int32_
   p.H = st->cfg.n_heads;
   p.G = st->cfg.n_kv_heads;
   p.hg = p.H / p.G;
+  p.heads = std::min(p.hg, kMassTile);
+  p.chunks = (p.hg + kMassTile - 1) / kMassTile;
+  p.tpb = p.chunks > 1 ? 1 : kMassTile / p.hg;
+  const int blocks = (p.T + p.tpb - 1) / p.tpb * p.chunks;
+  p.cut = blocks > 2;
+  p.span = blocks > 1 ? kMassSpan : 1;
+  p.span_from = 8;
   p.tree = tree;
   p.n_sink = std::min(n_sink, 1 << 25);   // (more than any length)
   p.window = std::min(window, 1 << 25);
@@ -1504,9 +1514,15 @@ starkv_status attention_mass(starkv_state* st, const starkv_pages* pages, int32_
   p.mass = mass_view(*mass);
   p.mass.m += layer * mass->layer_stride;
   p.decay = mass->decay;
+  const int64_t max_units = (((static_cast<int64_t>(pg.max_pages) << pg.shift) + kMassTile - 1) / kMassTile) * blocks;
+  p.grid = static_cast<int>(std::min<int64_t>(st->num_sms, p.n * p.G * max_units));
+  p.split = reinterpret_cast<MassSplit*>(workspace);
+  p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + parts);
   p.err = st->dev.err;
+  p.wait_ns = st->wait_ns;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  CUDA_TRY(launch(st, STARKV_KERNEL_MASS, cs, [&] { return mass_launch(p, st->num_sms, cs); }));
+  CUDA_TRY(launch(st, STARKV_KERNEL_MASS, cs, [&] { return mass_launch(p, cs); }));
+  if (p.cut) CUDA_TRY(launch(st, STARKV_KERNEL_MASS_SUM, cs, [&] { return mass_sum_launch(p, cs); }));
   return STARKV_OK;
 }
 

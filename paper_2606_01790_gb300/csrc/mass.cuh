@@ -12,9 +12,16 @@ struct MassView {
   int64_t layer_stride, row_stride, group_stride;   // elements
 };
 
+constexpr int kMassTile = 128;   // keys of a tile, (token, head) pairs of a query block at most
+constexpr int kMassSpan = 4;     // tiles of a group, at most
+
+// The group that a CTA's range begins and does not finish: the ranges up to `last` hold the rest.
+struct MassSplit {
+  int valid, seq, g, k0, keys, last, pad_[2];
+};
+
 struct MassParams {
-  const __nv_bfloat16* k;   // of the layer
-  int64_t page_stride;      // elements
+  CUtensorMap tmk;          // the layer's pages: dims (d, P, G, n_pages), box (64, min(P, 64), 1, 1), 128B swizzle
   const int32_t* table;
   const int32_t* len;
   int n_pages, n_rows, max_pages, shift;
@@ -22,20 +29,30 @@ struct MassParams {
   const __nv_bfloat16* q;
   const float* lse;         // [n][T][H]
   const uint64_t* mask;     // tree: [n][T]
-  const int32_t* rows;      // [n], or NULL = 0, 1, ...
+  const int32_t* rows;      // [n], or NULL = row0, row0 + 1, ...
   const int32_t* n_tokens;  // [n], or NULL
-  int n, T;
+  int row0, n, T;
   int64_t q_seq, q_token, q_head;
   int H, G, hg;             // hg = H / G
+  int tpb, heads, chunks;   // tokens and heads of a block; blocks that the heads of a group take
+  int cut;                  // 1: a group's blocks may be cut between ranges (more than stay in shared memory)
+  int span, span_from;      // tiles of a group, where a launch has as many tiles a CTA (else 1)
   int tree;                 // 1: mask, 0: n_sink and window
   int n_sink, window;
   float scale2;             // log2(e) / sqrt(d)
   MassView mass;
   float decay;
+  int grid;                 // CTAs of the main kernel
+  MassSplit* split;         // [grid]
+  float* part;              // [2 * grid][span * 128]
   uint32_t* err;
+  uint64_t wait_ns;
 };
 
-cudaError_t mass_launch(const MassParams& p, int num_sms, cudaStream_t stream);
+cudaError_t mass_configure();
+cudaError_t mass_launch(const MassParams& p, cudaStream_t stream);
+// The parts of the groups that were cut: with p.cut only.
+cudaError_t mass_sum_launch(const MassParams& p, cudaStream_t stream);
 
 // Picks the tokens of an eviction whose bookkeeping (`plan`) was carried out, and moves their mass.
 cudaError_t mass_select_launch(const PagesView& pg, const SeqBatch& b, const int32_t* rows, int row0, int w, int per_head,

@@ -39,7 +39,7 @@ ABI_FUNCTIONS = [
 
 KERNELS = ["score_lse", "score_accum", "pool", "calibrate", "compact", "attention", "attn_combine",
            "page_book", "page_copy", "page_gather", "page_move", "paged_attention", "paged_combine",
-           "mass", "mass_select", "page_bounds", "page_choose"]
+           "mass", "mass_sum", "mass_select", "page_bounds", "page_choose"]
 
 
 SELECT_GLOBAL, SELECT_PER_HEAD = 0, 1   # starkv_config.select_mode
