@@ -1505,8 +1505,13 @@ starkv_status attention_mass(starkv_state* st, const starkv_pages* pages, int32_
   p.tpb = p.chunks > 1 ? 1 : kMassTile / p.hg;
   const int blocks = (p.T + p.tpb - 1) / p.tpb * p.chunks;
   p.cut = blocks > 2;
-  p.span = blocks > 1 ? kMassSpan : 1;
-  p.span_from = 8;
+  p.inv_tpb = reciprocal(p.tpb);
+  p.inv_heads = reciprocal(p.heads);
+  p.inv_chunks = reciprocal(p.chunks);
+  p.step_h = kMassQueryStep % p.heads;
+  p.step = kMassQueryStep / p.heads * p.q_token + p.step_h * p.q_head;
+  p.wrap = p.q_token - p.heads * p.q_head;
+  p.span_from = blocks == 1 ? INT64_MAX : p.cut ? 16 * int64_t(st->num_sms) / blocks : 8 * int64_t(st->num_sms);
   p.tree = tree;
   p.n_sink = std::min(n_sink, 1 << 25);   // (more than any length)
   p.window = std::min(window, 1 << 25);

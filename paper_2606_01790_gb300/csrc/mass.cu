@@ -29,17 +29,23 @@ cudaLaunchConfig_t config(cudaLaunchAttribute* attr, dim3 grid, int threads, cud
 
 // ---------------------------------------------------------------- mass: units and their order
 
-constexpr int kMassWarps = 22;
+constexpr int kMassWarps = 12;
 constexpr int kThreads = 32 * kMassWarps;
-constexpr int kQueryWarp = 2, kSoftWarp = 6;      // first of the query warps (4) and of the weighing warps (16)
+constexpr int kQueryWarp = 2, kSoftWarp = 4;      // first of the query warps (2) and of the weighing warps (8)
+constexpr int kQueryThreads = 32 * (kSoftWarp - kQueryWarp);
+static_assert(kQueryThreads / 16 == kMassQueryStep, "16 threads take a row of 256 bytes");
 constexpr int kTileBytes = kMassTile * 256;       // 128 keys x 128 bf16, or as many (token, head) pairs: 32 KB
 constexpr int kHalfBytes = kTileBytes / 2;
-constexpr int kKeySlots = 4, kQuerySlots = 2;     // rings; a tile of keys has an accumulator and a warpgroup of its own
+constexpr int kKeySlots = 4, kQuerySlots = 2;     // rings; a tile of keys has an accumulator of its own
 constexpr int kTmemCols = 512;
+constexpr int kTileShift = 7, kSpanShift = 2;
+static_assert(kMassTile == 1 << kTileShift && kMassSpan == 1 << kSpanShift, "");
 constexpr uint64_t kDrainWaitNs = 2000000000ull;
 
 struct Item {
-  int L, n;   // tokens of the row and queries; n = 0: nothing to do
+  int L, n;     // tokens of the row and queries; n = 0: nothing to do
+  int row;
+  int blocks;   // of its queries
 };
 
 // A block of (token, head) pairs as the weighing warps see it.
@@ -60,73 +66,95 @@ struct Ctl {
   uint64_t drain;
   uint32_t tmem_base;
   volatile int abort;
-  int span;             // tiles of a group
+  int span;             // log2 of the keys of a group
+  int ranges;
+  int64_t begin, end;   // this CTA's range
   Start start;
   Pairs pairs[kQuerySlots];
   int64_t before[kMaxCallRows + 1];   // units before a sequence
   Item item[kMaxCallRows];
 };
 
+// x / n by its reciprocal ceil(2^32 / n) (0 for n = 1), for x n < 2^32
+__device__ __forceinline__ int quotient(int x, uint32_t inv) {
+  return inv ? static_cast<int>(__umulhi(static_cast<uint32_t>(x), inv)) : x;
+}
+
 // The tiles of one group of a row and the query blocks that see some of it.
 struct Group {
   int k0, tiles, lo, hi;   // first key; tiles of 128; blocks lo .. hi - 1
 
   __device__ __forceinline__ Group(const MassParams& p, const Item& it, int span, int s) {
-    k0 = s * span * kMassTile;
-    const int end = min(it.L, k0 + span * kMassTile), ctx = it.L - it.n;
+    k0 = s << span;
+    const int end = min(it.L, k0 + (1 << span)), ctx = it.L - it.n;
     tiles = (end - k0 + kMassTile - 1) / kMassTile;
     int t0 = 0, t1 = it.n;
     if (!p.tree) {
       t0 = max(0, k0 - ctx);
       if (k0 >= p.n_sink) t1 = min(it.n, end - 1 + p.window - ctx);
     }
-    if (!p.cut && t0 < t1) t0 = 0, t1 = it.n;   // (blocks that stay in shared memory stay whole)
-    lo = t0 / p.tpb * p.chunks;
-    hi = t1 <= t0 ? lo : (t1 + p.tpb - 1) / p.tpb * p.chunks;
+    if (!p.cut) {   // blocks that stay in shared memory stay whole
+      lo = 0;
+      hi = t0 < t1 ? it.blocks : 0;
+    } else {
+      lo = quotient(t0, p.inv_tpb) * p.chunks;
+      hi = t1 <= t0 ? lo : quotient(t1 + p.tpb - 1, p.inv_tpb) * p.chunks;
+    }
   }
   // a group that nothing sees is a unit all the same: its mass may fade
   __device__ __forceinline__ int units(const MassParams& p) const { return p.cut ? max(1, hi - lo) : 1; }
 };
 
-__device__ __forceinline__ int groups_of(int L, int span) { return (L + span * kMassTile - 1) / (span * kMassTile); }
+__device__ __forceinline__ int groups_of(int L, int span) { return (L + (1 << span) - 1) >> span; }
 
-// Runs of blocks of one group, in the order of a CTA's range.
+// Runs of blocks of one group, in the order of a CTA's range.  (Every role steps through them, and a step is
+// a chain of dependent instructions: no divisions, and what a row does not change is kept.)
 struct PieceIter {
   int seq, g, s;
   int b0, b1;        // blocks b0 .. b1 - 1
+  int span, groups;  // log2 of the keys of a group; groups of the row
   int64_t rem;       // units of the range from here on
   Group grp;
   Item it;
-  __device__ __forceinline__ PieceIter(const MassParams& p, const Ctl* ctl, int64_t units)
-      : seq(ctl->start.seq), g(ctl->start.g), s(ctl->start.s), rem(units), grp(p, Item{0, 0}, 1, 0), it{0, 0} {
+  __device__ __forceinline__ PieceIter(const MassParams& p, const Ctl* ctl)
+      : seq(ctl->start.seq), g(ctl->start.g), s(ctl->start.s), span(ctl->span), rem(ctl->end - ctl->begin),
+        grp(p, Item{0, 0, 0, 0}, 7, 0), it{0, 0, 0, 0} {
     if (rem <= 0) return;
     it = ctl->item[seq];
-    take(p, ctl, ctl->start.b);
+    groups = groups_of(it.L, span);
+    take(p, ctl->start.b);
   }
   __device__ __forceinline__ bool valid() const { return rem > 0; }
   __device__ __forceinline__ bool whole() const { return b0 == grp.lo && b1 == grp.hi; }
-  __device__ __forceinline__ void take(const MassParams& p, const Ctl* ctl, int from) {
-    grp = Group(p, it, ctl->span, s);
+  __device__ __forceinline__ void take(const MassParams& p, int from) {
+    grp = Group(p, it, span, s);
     b0 = grp.lo + from;
     b1 = p.cut ? static_cast<int>(min(static_cast<int64_t>(grp.hi), b0 + rem)) : grp.hi;
   }
   // the last group of this row and KV head that the range has
-  __device__ __forceinline__ bool last_of_head(const Ctl* ctl) const {
-    return rem <= 1 || s + 1 == groups_of(it.L, ctl->span);
-  }
+  __device__ __forceinline__ bool last_of_head() const { return rem <= 1 || s + 1 == groups; }
   __device__ __forceinline__ void next(const MassParams& p, const Ctl* ctl) {
     rem -= p.cut ? max(1, b1 - b0) : 1;
     if (rem <= 0) return;
-    if (++s == groups_of(it.L, ctl->span)) {
-      s = 0;
-      if (++g == p.G) {
-        g = 0;
-        do ++seq;
-        while (ctl->before[seq + 1] == ctl->before[seq]);
-        it = ctl->item[seq];
-      }
+    if (++s == groups) head(p, ctl);
+    take(p, 0);
+  }
+  // p.cut is 0: on to the next row or KV head
+  __device__ __forceinline__ void skip_head(const MassParams& p, const Ctl* ctl) {
+    rem -= groups - s;
+    if (rem <= 0) return;
+    head(p, ctl);
+    take(p, 0);
+  }
+  __device__ __forceinline__ void head(const MassParams& p, const Ctl* ctl) {
+    s = 0;
+    if (++g == p.G) {
+      g = 0;
+      do ++seq;
+      while (ctl->before[seq + 1] == ctl->before[seq]);
+      it = ctl->item[seq];
+      groups = groups_of(it.L, span);
     }
-    take(p, ctl, 0);
   }
 };
 
@@ -137,8 +165,9 @@ __device__ __forceinline__ int ranges_of(int64_t T, int P) { return T < P ? max(
 __device__ __forceinline__ int range_of(int64_t f, int64_t T, int P) { return static_cast<int>(((f + 1) * P - 1) / T); }
 
 // Every sequence's length and queries, the groups' span, the units before each sequence and this CTA's
-// first unit.  `named`: 2 bits a row of the table (in shared memory), for rows that two sequences name.
-__device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named, int64_t* fb, int64_t* fe, int64_t* total, int* ranges) {
+// range.  `named`: 2 bits a row of the table (in shared memory), for rows that two sequences name.
+// (Runs once, and cold code costs its size: one pass a thread over the sequences, one warp for the rest.)
+__device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int words = (p.n_rows + 31) >> 5;
   const bool rivals = p.rows && p.n > 1;
@@ -146,51 +175,59 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named, int64_t* fb
     for (int i = tid; i < 2 * words; i += kThreads) named[i] = 0;
     __syncthreads();
   }
-  __shared__ unsigned long long tiles;
-  if (tid == 0) tiles = 0;
+  int64_t tiles = 0;
   for (int i = tid; i < p.n; i += kThreads) {
-    const int row = p.rows ? p.rows[i] : p.row0 + i;
     Item it;
+    it.row = p.rows ? p.rows[i] : p.row0 + i;
     it.n = p.n_tokens ? p.n_tokens[i] : p.T;
-    it.L = row >= 0 && row < p.n_rows ? p.len[row] : -1;
+    it.L = it.row >= 0 && it.row < p.n_rows ? p.len[it.row] : -1;
     if (it.n < 0 || it.n > p.T || (it.n > 0 && (it.L < it.n || it.L > static_cast<int64_t>(p.max_pages) << p.shift))) {
       it.n = 0;
       atomicOr(p.err, kErrRow);
     }
-    if (rivals && it.n > 0 && (atomicOr(&named[row >> 5], 1u << (row & 31)) & (1u << (row & 31))))
-      atomicOr(&named[words + (row >> 5)], 1u << (row & 31));
+    if (rivals && it.n > 0 && (atomicOr(&named[it.row >> 5], 1u << (it.row & 31)) & (1u << (it.row & 31))))
+      atomicOr(&named[words + (it.row >> 5)], 1u << (it.row & 31));
+    it.blocks = quotient(it.n + p.tpb - 1, p.inv_tpb) * p.chunks;
+    if (it.n > 0) tiles += groups_of(it.L, kTileShift);
     ctl->item[i] = it;
   }
+  if (tiles) atomicAdd(reinterpret_cast<unsigned long long*>(&ctl->end), static_cast<unsigned long long>(tiles));
   __syncthreads();
-  unsigned long long mine = 0;
-  for (int i = tid; i < p.n; i += kThreads) {
-    const int row = p.rows ? p.rows[i] : p.row0 + i;
-    if (rivals && ctl->item[i].n > 0 && (named[words + (row >> 5)] >> (row & 31) & 1)) {
-      ctl->item[i].n = 0;
-      atomicOr(p.err, kErrRow);
+  const int span = kTileShift + (ctl->end * p.G >= p.span_from ? kSpanShift : 0);
+  if (!p.cut) {
+    for (int i = tid; i < p.n; i += kThreads) {
+      const Item it = ctl->item[i];
+      if (rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1)) {
+        ctl->item[i].n = 0;
+        atomicOr(p.err, kErrRow);
+        ctl->before[i + 1] = 0;
+      } else {
+        ctl->before[i + 1] = it.n > 0 ? groups_of(it.L, span) : 0;
+      }
     }
-    if (ctl->item[i].n > 0) mine += groups_of(ctl->item[i].L, 1);
-  }
-  if (mine) atomicAdd(&tiles, mine);
-  __syncthreads();
-  const int span = p.span > 1 && static_cast<int64_t>(tiles) * p.G >= static_cast<int64_t>(p.span_from) * gridDim.x ? p.span : 1;
-  if (tid == 0) ctl->span = span;
-  for (int i = warp; i < p.n; i += kMassWarps) {
-    const Item it = ctl->item[i];
-    const int ng = it.n > 0 ? groups_of(it.L, span) : 0;
-    int64_t u = 0;
-    if (!p.cut) u = lane == 0 ? ng : 0;
-    else
+  } else {
+    for (int i = warp; i < p.n; i += kMassWarps) {
+      const Item it = ctl->item[i];
+      const bool twice = rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1);
+      const int ng = it.n > 0 && !twice ? groups_of(it.L, span) : 0;
+      int u = 0;   // (32,768 groups of 1,041 blocks at most)
       for (int s = lane; s < ng; s += 32) u += Group(p, it, span, s).units(p);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(kFull, u, o);
-    if (lane == 0) ctl->before[i + 1] = u * p.G;
+      u = __reduce_add_sync(kFull, u);
+      if (lane == 0) {
+        ctl->before[i + 1] = u;
+        if (twice) {
+          ctl->item[i].n = 0;
+          atomicOr(p.err, kErrRow);
+        }
+      }
+    }
   }
   __syncthreads();
   if (warp == 0) {
     int64_t at = 0;
+#pragma unroll 1
     for (int i0 = 0; i0 < p.n; i0 += 32) {
-      int64_t u = i0 + lane < p.n ? ctl->before[i0 + lane + 1] : 0;
+      int64_t u = i0 + lane < p.n ? ctl->before[i0 + lane + 1] * p.G : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int64_t x = __shfl_up_sync(kFull, u, o);
@@ -201,54 +238,53 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named, int64_t* fb
     }
     if (lane == 0) ctl->before[0] = 0;
     __syncwarp();
-    const int64_t T = ctl->before[p.n];
-    const int R = ranges_of(T, gridDim.x);
-    const int64_t f = range_begin(T, blockIdx.x, R);
-    if (f < range_begin(T, blockIdx.x + 1, R)) {
-      int a = 0, b = p.n;   // the last sequence with no more than f units before it
+    const int R = ranges_of(at, gridDim.x);
+    const int64_t f0 = range_begin(at, blockIdx.x + (lane & 1), R);   // (lanes 0 and 1: the range's ends)
+    const int64_t fb = __shfl_sync(kFull, f0, 0), fe = __shfl_sync(kFull, f0, 1);
+    Start st{0, 0, 0, 0};
+    if (fb < fe) {
+      int a = 0, b = p.n;   // the last sequence with no more than fb units before it
       while (b - a > 1) {
         const int mid = (a + b) >> 1;
-        if (ctl->before[mid] <= f) a = mid;
+        if (ctl->before[mid] <= fb) a = mid;
         else b = mid;
       }
-      while (ctl->before[a + 1] <= f) ++a;
-      const int64_t per = (ctl->before[a + 1] - ctl->before[a]) / p.G;
-      int64_t off = f - ctl->before[a];
-      Start st;
       st.seq = a;
-      st.g = static_cast<int>(off / per);
-      off -= st.g * per;
-      st.s = static_cast<int>(off);
-      st.b = 0;
-      if (p.cut) {
-        const Item it = ctl->item[a];
-        const int ng = groups_of(it.L, span);
-        for (int s0 = 0;; s0 += 32) {
+      const Item it = ctl->item[a];
+      const int ng = groups_of(it.L, span);
+      int64_t off = fb - ctl->before[a];
+      const int64_t heads = ctl->before[a + 1] - ctl->before[a];   // G times the units of one
+      while ((st.g + 1) * heads <= off * p.G) ++st.g;
+      off -= st.g * (heads / p.G);
+      if (!p.cut) st.s = static_cast<int>(off);
+      else
+        for (int left = static_cast<int>(off), s0 = 0;; s0 += 32) {
           const int u = s0 + lane < ng ? Group(p, it, span, s0 + lane).units(p) : 0;
-          int64_t inc = u;
+          int inc = u;
 #pragma unroll
           for (int o = 1; o < 32; o <<= 1) {
-            const int64_t x = __shfl_up_sync(kFull, inc, o);
+            const int x = __shfl_up_sync(kFull, inc, o);
             if (lane >= o) inc += x;
           }
-          const uint32_t past = __ballot_sync(kFull, inc > off);
+          const uint32_t past = __ballot_sync(kFull, inc > left);
           if (past || s0 + 32 >= ng) {
             const int l = past ? __ffs(past) - 1 : 31;
             st.s = s0 + l;
-            st.b = static_cast<int>(off - __shfl_sync(kFull, inc - u, l));
+            st.b = left - __shfl_sync(kFull, inc - u, l);
             break;
           }
-          off -= __shfl_sync(kFull, inc, 31);
+          left -= __shfl_sync(kFull, inc, 31);
         }
-      }
-      if (lane == 0) ctl->start = st;
+    }
+    if (lane == 0) {
+      ctl->start = st;
+      ctl->span = span;
+      ctl->ranges = R;
+      ctl->begin = fb;
+      ctl->end = fe;
     }
   }
   __syncthreads();
-  *total = ctl->before[p.n];
-  *ranges = ranges_of(*total, gridDim.x);
-  *fb = range_begin(*total, blockIdx.x, *ranges);
-  *fe = range_begin(*total, blockIdx.x + 1, *ranges);
 }
 
 // ---------------------------------------------------------------- mass: waits
@@ -265,7 +301,7 @@ __device__ __forceinline__ void fail(Ctl* ctl, uint32_t* err) {
 __device__ __forceinline__ bool warp_wait(const Ctl* ctl, uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
   if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
   const bool aborted = ctl->abort;
-  const bool there = mbar_wait(bar, parity, limit_ns);
+  const bool there = mbar_try_wait(bar, parity) || mbar_wait(bar, parity, limit_ns);   // (most waits end before a clock is read)
   return __all_sync(kFull, there && !aborted);
 }
 
@@ -282,23 +318,41 @@ struct Ring {
 // ---------------------------------------------------------------- mass: roles
 
 // Keys: the tiles' pages into the ring.  Lane l holds the number of page base + l of the row.
-__device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int lane, int64_t units) {
+__device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int lane) {
   const uint64_t pol = policy_evict_first();
   const int P = 1 << p.shift, rows = min(P, 64), boxes = kMassTile / rows;
   Ring<kKeySlots> st;
   uint32_t used = 0, last_par = 0;   // last_par: bit s = parity of the last load into slot s
   bool ok = true;
-  for (PieceIter c(p, ctl, units); ok && c.valid(); c.next(p, ctl)) {
+  int base = 0, held = 0;            // lane l: pages base + l and base + 32 + l of the row, on their way before they are due
+  int id = 0, id_next = 0;
+  const int32_t* entries = nullptr;
+  auto number = [&](int at) {        // outside the map: zeros
+    int x = p.n_pages;
+    if (at < held) {
+      x = entries[at];
+      if (x < 0 || x >= p.n_pages) {
+        x = p.n_pages;
+        atomicOr(p.err, kErrRow);
+      }
+    }
+    return x;
+  };
+  for (PieceIter c(p, ctl); ok && c.valid(); c.next(p, ctl)) {
     if (c.b0 == c.b1) continue;
-    const int row = p.rows ? p.rows[c.seq] : p.row0 + c.seq;
-    const int32_t* entries = p.table + static_cast<int64_t>(row) * p.max_pages;
-    const int held = (c.it.L + P - 1) >> p.shift;
-    const int base = c.grp.k0 >> p.shift;   // (a group has 512 keys: 32 pages at most)
-    int id = p.n_pages;                     // outside the map: zeros
-    if (base + lane < held && lane << p.shift < c.grp.tiles * kMassTile) {
-      const int x = entries[base + lane];
-      if (x >= 0 && x < p.n_pages) id = x;
-      else atomicOr(p.err, kErrRow);
+    const int32_t* mine = p.table + static_cast<int64_t>(c.it.row) * p.max_pages;
+    const int page0 = c.grp.k0 >> p.shift;   // (a group has 512 keys: 32 pages at most)
+    const int page1 = (c.grp.k0 + c.grp.tiles * kMassTile - 1) >> p.shift;
+    if (mine != entries || page0 < base || page1 >= base + 64) {
+      entries = mine;
+      held = (c.it.L + P - 1) >> p.shift;
+      base = page0;
+      id = number(base + lane);
+      id_next = number(base + 32 + lane);
+    } else if (page0 >= base + 32) {
+      base += 32;
+      id = id_next;
+      id_next = number(base + 32 + lane);
     }
     __syncwarp();
     for (int i = 0; i < c.grp.tiles; ++i) {
@@ -308,7 +362,9 @@ __device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int lane, i
       if (leader) mbar_arrive_expect_tx(&ctl->k_full[st.at], kTileBytes);
       for (int b = 0; b < boxes; ++b) {
         const int key = c.grp.k0 + i * kMassTile + b * rows;
-        const int page = __shfl_sync(kFull, id, (key >> p.shift) - base);
+        const int at = (key >> p.shift) - base;
+        const int near = __shfl_sync(kFull, id, at & 31), far = __shfl_sync(kFull, id_next, at & 31);
+        const int page = at < 32 ? near : far;
         if (leader)
           for (int h = 0; h < 2; ++h) {
             uint8_t* dst = sK + st.at * kTileBytes + h * kHalfBytes + b * rows * 128;
@@ -333,7 +389,7 @@ __device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int lane, i
 struct Block {
   int t0, h0, count;
   __device__ __forceinline__ Block(const MassParams& p, int n, int b) {
-    const int tb = b / p.chunks;
+    const int tb = quotient(b, p.inv_chunks);
     t0 = tb * p.tpb;
     h0 = (b - tb * p.chunks) * kMassTile;   // (0 unless the heads of a group are more than a block has columns)
     count = min(p.tpb, n - t0) * min(p.heads, p.hg - h0);
@@ -343,60 +399,77 @@ struct Block {
 
 // Queries: blocks into the ring, rows of 128 bytes with the chunks of 16 swizzled as the tensor core reads
 // them, zeros behind the last pair.
-__device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid, int64_t units) {
+__device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) {
   Ring<kQuerySlots> st;
   bool ok = true, there = false;   // there: the blocks of this row and KV head stay
+  int due = -1;                    // slot whose copies are under way
   const int lane = tid & 31, chunk = tid & 15;
-  for (PieceIter c(p, ctl, units); ok && c.valid(); c.next(p, ctl)) {
-    if (p.cut || !there)
-      for (int b = c.b0; ok && b < c.b1; ++b) {
-        ok = warp_wait(ctl, &ctl->q_empty[st.at], st.par ^ 1, p.wait_ns);
-        if (!ok) break;
+  auto hand_over = [&] {
+    if (due < 0) return;
+    cp_async_wait();
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&ctl->q_full[due]);
+    due = -1;
+  };
+  for (PieceIter c(p, ctl); ok && c.valid(); there ? c.skip_head(p, ctl) : c.next(p, ctl)) {
+    there = false;
+    for (int b = c.b0; ok && b < c.b1; ++b) {
+        if (!__all_sync(kFull, mbar_try_wait(&ctl->q_empty[st.at], st.par ^ 1))) {   // time to see to the block before
+          hand_over();
+          ok = warp_wait(ctl, &ctl->q_empty[st.at], st.par ^ 1, p.wait_ns);
+          if (!ok) break;
+        }
         const Block blk(p, c.it.n, b);
-        const int heads = min(p.heads, p.hg - blk.h0);
-        const __nv_bfloat16* q = p.q + c.seq * p.q_seq + (static_cast<int64_t>(c.g) * p.hg + blk.h0) * p.q_head + chunk * 8;
-        uint8_t* dst = sQ + st.at * kTileBytes + (chunk >> 3) * kHalfBytes;
-        for (int r0 = tid >> 4; r0 < blk.columns(); r0 += 64) {
-          uint4 x[8];
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int r = r0 + 8 * u, t = r / heads;
-            x[u] = r < blk.count ? *reinterpret_cast<const uint4*>(q + (blk.t0 + t) * p.q_token + (r - t * heads) * p.q_head)
-                                 : make_uint4(0u, 0u, 0u, 0u);
-          }
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int r = r0 + 8 * u;
-            if (r < blk.columns()) *reinterpret_cast<uint4*>(dst + r * 128 + (((chunk & 7) ^ (r & 7)) << 4)) = x[u];
+        const int columns = blk.columns();
+        int r = tid >> 4, t = quotient(r, p.inv_heads), h = r - t * p.heads;
+        const __nv_bfloat16* q = p.q + c.seq * p.q_seq + (static_cast<int64_t>(c.g) * p.hg + blk.h0 + h) * p.q_head +
+                                 (blk.t0 + t) * p.q_token + chunk * 8;
+        uint32_t dst = smem_u32(sQ) + st.at * kTileBytes + (chunk >> 3) * kHalfBytes + r * 128 + (((chunk & 7) ^ (r & 7)) << 4);
+#pragma unroll 4
+        for (; r < columns; r += kMassQueryStep) {
+          cp_async16(dst, r < blk.count ? q : p.q, r < blk.count);
+          dst = (dst + kMassQueryStep * 128) ^ 64;   // (four rows on, the swizzle differs by four chunks)
+          q += p.step;
+          h += p.step_h;
+          if (h >= p.heads) {
+            h -= p.heads;
+            q += p.wrap;
           }
         }
-        if (tid < blk.count) {
-          const int t = blk.t0 + tid / heads, h = c.g * p.hg + blk.h0 + tid % heads;
+        cp_async_commit();
+        for (int i = tid; i < blk.count; i += kQueryThreads) {
+          const int at_t = quotient(i, p.inv_heads), t = blk.t0 + at_t, h = c.g * p.hg + blk.h0 + i - at_t * p.heads;
           const int64_t at = static_cast<int64_t>(c.seq) * p.T + t;
           Pairs& pr = ctl->pairs[st.at];
-          pr.lse[tid] = -1.4426950408889634f * p.lse[at * p.H + h];
-          pr.pos[tid] = c.it.L - c.it.n + t;
-          if (p.tree) pr.bits[tid] = p.mask[at];
+          pr.lse[i] = -1.4426950408889634f * p.lse[at * p.H + h];
+          pr.pos[i] = c.it.L - c.it.n + t;
+          if (p.tree) pr.bits[i] = p.mask[at];
         }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl->q_full[st.at]);
+        const int slot = st.at;
+        if (due >= 0) {   // (its copies were under way before these)
+          cp_async_wait_1();
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctl->q_full[due]);
+        }
+        due = slot;
         st.next();
-        there = true;
+        there = !p.cut;
       }
-    if (c.last_of_head(ctl)) there = false;
   }
+  hand_over();
   if (!ok) fail(ctl, p.err);
 }
 
-__device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const uint8_t* sQ, uint32_t tmem, int64_t units) {
+__device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const uint8_t* sQ, uint32_t tmem) {
   const uint64_t dk0 = sdesc_k_sw128(smem_u32(sK)), dq0 = sdesc_k_sw128(smem_u32(sQ));
   Ring<kKeySlots> st;
   Ring<kQuerySlots> q;    // the next block to come
   uint32_t s_par = 0;     // bit a: parity of accumulator a's next use
   bool ok = true;
   int held = 0, first = 0;   // blocks of this row and KV head that stay, and the first one's slot
-  for (PieceIter c(p, ctl, units); ok && c.valid(); c.next(p, ctl)) {
+  for (PieceIter c(p, ctl); ok && c.valid(); c.next(p, ctl)) {
     const int nb = c.b1 - c.b0;
     const bool take = p.cut || held == 0;
     if (take) first = q.at;
@@ -435,7 +508,7 @@ __device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const
     st = at;
     if (!p.cut) {
       if (take) held = nb;
-      if (c.last_of_head(ctl)) {
+      if (c.last_of_head()) {
         if (ok && elect_one())
           for (int j = 0; j < held; ++j) mma_commit(&ctl->q_empty[(first + j) % kQuerySlots]);
         __syncwarp();
@@ -450,11 +523,10 @@ __device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const
   __syncwarp();
 }
 
-// Sum of 32 pairs' weights, all of them seen.
-__device__ __forceinline__ float weigh32(uint32_t addr, const float* lse, float c2) {
-  uint32_t z[32];
-  tmem_ld32_async(addr, z);
-  tmem_wait32(z);
+// Sum of 32 pairs' weights from column c on, all of them seen; TAIL: of those in front of `count` (behind
+// them an earlier block may have left anything).
+template <bool TAIL>
+__device__ __forceinline__ float weigh32(const uint32_t (&z)[32], const float* lse, float c2, int count) {
   const float2 sc = make_float2(c2, c2);
   float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
@@ -462,101 +534,139 @@ __device__ __forceinline__ float weigh32(uint32_t addr, const float* lse, float 
     const float4 l = *reinterpret_cast<const float4*>(lse + i);
     const float2 a = ffma2(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), sc, make_float2(l.x, l.y));
     const float2 b = ffma2(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), sc, make_float2(l.z, l.w));
-    acc[0] = fadd2(acc[0], make_float2(ex2_approx(a.x), ex2_approx(a.y)));
-    acc[1] = fadd2(acc[1], make_float2(ex2_approx(b.x), ex2_approx(b.y)));
+    float2 x = make_float2(ex2_approx(a.x), ex2_approx(a.y)), y = make_float2(ex2_approx(b.x), ex2_approx(b.y));
+    if (TAIL) {
+      x = make_float2(i < count ? x.x : 0.f, i + 1 < count ? x.y : 0.f);
+      y = make_float2(i + 2 < count ? y.x : 0.f, i + 3 < count ? y.y : 0.f);
+    }
+    acc[0] = fadd2(acc[0], x);
+    acc[1] = fadd2(acc[1], y);
   }
   const float2 s = fadd2(acc[0], acc[1]);
   return s.x + s.y;
 }
 
-// Of 16 pairs from column c on, those that see key j.
-__device__ __forceinline__ float weigh16(const MassParams& p, uint32_t addr, const Pairs& pr, int c, int count, int j, int ctx, int L) {
-  uint32_t z[16];
-  tmem_ld16_async(addr + c, z);
-  tmem_wait16(z);
+// A block that every key of the tile is seen by: 32 columns at a time, the next ones on their way.
+__device__ __forceinline__ float weigh_block(uint32_t addr, const float* lse, float c2, int count) {
+  uint32_t z[2][32];
   float sum = 0.f;
+  tmem_ld32_async(addr, z[0]);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    bool seen = c + i < count;   // (behind the last pair: whatever an earlier block left)
-    if (seen) {
-      if (p.tree) {
-        seen = j < ctx || (j < L && (pr.bits[c + i] >> (j - ctx) & 1));
-      } else {
-        const int pos = pr.pos[c + i];
-        seen = j <= pos && (j < p.n_sink || j > pos - p.window);
-      }
-    }
-    const float w = seen ? ex2_approx(fmaf(__uint_as_float(z[i]), p.scale2, pr.lse[c + i])) : 0.f;
-    sum += w;
+  for (int k = 0; k < kMassTile / 32; ++k) {
+    if (32 * k >= count) break;
+    tmem_wait32(z[k & 1]);
+    if (32 * (k + 1) < count) tmem_ld32_async(addr + 32 * (k + 1), z[(k + 1) & 1]);
+    sum += 32 * (k + 1) <= count ? weigh32<false>(z[k & 1], lse + 32 * k, c2, 0) : weigh32<true>(z[k & 1], lse + 32 * k, c2, count - 32 * k);
   }
   return sum;
 }
 
-// Weighing warpgroup `own`: the tiles whose accumulator it is, a key a thread.
-__device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own, int quad, int lane, int64_t units) {
+// A block that is not: of the pairs in front of `count` those that see key j.
+// (Values, not the parameters' address: a call that is not inlined would read them from memory at every use.)
+__device__ __noinline__ float weigh_masked(uint32_t addr, const Pairs* pairs, float c2, int tree, int n_sink, int window, int count, int j,
+                                           int ctx, int L) {
+  float sum = 0.f;
+  // sink: positions j .. j + reach - 1 see the key; tree: bit `shift` of the token's half word, `any` the cached ones
+  const uint32_t reach = j < n_sink ? 0x7fffffffu : static_cast<uint32_t>(window);
+  const int drafted = max(j - ctx, 0);
+  const uint32_t any = j < ctx ? ~0u : 0u;
+  const int shift = drafted & 31;
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(pairs->bits) + (drafted >> 5 & 1);
+  const bool real = j < L;
+#pragma unroll 1
+  for (int c = 0; c < count; c += 16) {
+    uint32_t z[16];
+    tmem_ld16_async(addr + c, z);
+    tmem_wait16(z);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const bool seen = tree ? ((words[2 * (c + i)] | any) >> shift & 1) : static_cast<uint32_t>(pairs->pos[c + i] - j) < reach;
+      const float w = ex2_approx(fmaf(__uint_as_float(z[i]), c2, pairs->lse[c + i]));
+      sum += seen && real && c + i < count ? w : 0.f;
+    }
+  }
+  return sum;
+}
+
+// Weighing warpgroup `own`: every other tile, a key a thread.
+__device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own, int quad, int lane) {
   const int r = quad * 32 + lane;
-  const uint32_t addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + own * kMassTile;
+  const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
   Ring<kQuerySlots> q;
-  int tile = 0;            // number (mod 4) of the next tile to come
-  uint32_t par = 0;        // of the accumulator's next use
+  uint32_t tile = 0;       // number of the next tile to come
+  uint32_t par = 0;        // bit a: parity of accumulator a's next use
   bool ok = true;
   int held = 0, slot0 = 0; // blocks of this row and KV head that stay, and the first one's slot
-  for (PieceIter c(p, ctl, units); ok && c.valid(); c.next(p, ctl)) {
+  for (PieceIter c(p, ctl); ok && c.valid(); c.next(p, ctl)) {
     const int nb = c.b1 - c.b0;
     const bool take = p.cut || held == 0;
     if (take) slot0 = q.at;
-    const int i = (own - (nb > 0 ? tile : 0)) & (kKeySlots - 1);   // which of the group's tiles is this one's
-    const bool mine = i < c.grp.tiles;
-    const int k0 = c.grp.k0 + i * kMassTile, j = k0 + r, ctx = c.it.L - c.it.n;
-    const int row = p.rows ? p.rows[c.seq] : p.row0 + c.seq;
-    float* mass = p.mass.m + row * p.mass.row_stride + c.g * p.mass.group_stride + j;
+    const int i0 = (own ^ tile) & 1;   // tiles i0 and i0 + 2 of the group are this warpgroup's
+    const int ctx = c.it.L - c.it.n, j0 = c.grp.k0 + i0 * kMassTile + r;
+    float* mass = p.mass.m + c.it.row * p.mass.row_stride + c.g * p.mass.group_stride + j0;
     const bool whole = c.whole();
-    float sum = 0.f, had = 0.f;
-    if (mine && whole && j < ctx) had = *mass;
+    float sum[2] = {0.f, 0.f}, had[2] = {0.f, 0.f};
+    if (whole) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (i0 + 2 * u < c.grp.tiles && j0 + 2 * u * kMassTile < ctx) had[u] = mass[2 * u * kMassTile];
+    }
     for (int b = 0; b < nb; ++b) {
       const int slot = (slot0 + b) % kQuerySlots;
       if (take) {
         ok = warp_wait(ctl, &ctl->q_full[q.at], q.par, p.wait_ns);
         q.next();
       }
-      ok = ok && (!mine || warp_wait(ctl, &ctl->s_full[own], par, p.wait_ns));
-      if (!ok) break;
-      if (mine) {
+      const Block blk(p, c.it.n, c.b0 + b);
+      const Pairs& pr = ctl->pairs[slot];
+      const int first = ctx + blk.t0, end = ctx + min(blk.t0 + p.tpb, c.it.n) - 1;   // positions of the block's tokens
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int i = i0 + 2 * u;
+        if (!ok || i >= c.grp.tiles) break;
+        const uint32_t a = (tile + i) & (kKeySlots - 1);
+        ok = warp_wait(ctl, &ctl->s_full[a], par >> a & 1, p.wait_ns);
+        if (!ok) break;
         tc_fence_after();
-        const Block blk(p, c.it.n, c.b0 + b);
-        const Pairs& pr = ctl->pairs[slot];
-        const int first = ctx + blk.t0, end = ctx + min(blk.t0 + p.tpb, c.it.n) - 1;   // positions of the block's tokens
-        const bool all = p.tree ? k0 + kMassTile <= ctx
-                                : k0 + kMassTile - 1 <= first && (k0 + kMassTile <= p.n_sink || k0 > end - p.window);
-        int col = 0;
-        if (all)
-          for (; col + 32 <= blk.count; col += 32) sum += weigh32(addr + col, pr.lse + col, p.scale2);
-#pragma unroll 1
-        for (; col < blk.count; col += 16) sum += weigh16(p, addr, pr, col, blk.count, j, ctx, c.it.L);
+        // by the warp's 32 keys: seen by all of the block, by none, or by some
+        const int k0 = c.grp.k0 + i * kMassTile + 32 * quad, k1 = k0 + 31;
+        bool all, none = k0 >= c.it.L;
+        if (p.tree) {
+          all = k1 < ctx;
+        } else {
+          all = k1 <= first && (k1 < p.n_sink || k0 > end - p.window);
+          none = none || k0 > end || (k0 >= p.n_sink && k1 <= first - p.window);
+        }
+        if (all) sum[u] += weigh_block(lanes + a * kMassTile, pr.lse, p.scale2, blk.count);
+        else if (!none)
+          sum[u] += weigh_masked(lanes + a * kMassTile, &pr, p.scale2, p.tree, p.n_sink, p.window, blk.count, k0 + lane, ctx, c.it.L);
         tc_fence_before();
-        par ^= 1;
+        par ^= 1u << a;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ctl->s_empty[a]);
       }
-      __syncwarp();
-      if (lane == 0) {
-        if (mine) mbar_arrive(&ctl->s_empty[own]);
-        if (p.cut) mbar_arrive(&ctl->q_empty[slot]);
-      }
+      if (!ok) break;
+      if (p.cut && lane == 0) mbar_arrive(&ctl->q_empty[slot]);
     }
     if (!ok) break;
     if (!p.cut) {
       if (take) held = nb;
-      if (c.last_of_head(ctl)) {
+      if (c.last_of_head()) {
         if (lane == 0)
           for (int b = 0; b < held; ++b) mbar_arrive(&ctl->q_empty[(slot0 + b) % kQuerySlots]);
         held = 0;
       }
     }
-    if (mine && whole) {
-      if (j < c.it.L) *mass = fmaf(p.decay, had, sum);
-    } else if (mine) {
-      p.part[(2 * static_cast<int64_t>(blockIdx.x) + (c.b0 == c.grp.lo)) * (kMassSpan * kMassTile) + i * kMassTile + r] = sum;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int i = i0 + 2 * u;
+      if (i >= c.grp.tiles) break;
+      if (!whole)
+        p.part[(2 * static_cast<int64_t>(blockIdx.x) + (c.b0 == c.grp.lo)) * (kMassSpan * kMassTile) + i * kMassTile + r] = sum[u];
+      else if (j0 + 2 * u * kMassTile < c.it.L)
+        mass[2 * u * kMassTile] = fmaf(p.decay, had[u], sum[u]);
     }
-    if (nb > 0) tile = (tile + c.grp.tiles) & (kKeySlots - 1);
+    if (nb > 0) tile += c.grp.tiles;
   }
   if (!ok) fail(ctl, p.err);
 }
@@ -578,11 +688,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
       mbar_init(&ctl->s_empty[i], 4);
     }
     for (int i = 0; i < kQuerySlots; ++i) {
-      mbar_init(&ctl->q_full[i], 4);
+      mbar_init(&ctl->q_full[i], kSoftWarp - kQueryWarp);
       mbar_init(&ctl->q_empty[i], 1 + kMassWarps - kSoftWarp);   // the products and every weighing warp
     }
     mbar_init(&ctl->drain, 1);
     ctl->abort = 0;
+    ctl->end = 0;
     fence_mbar_init();
   }
   if (warp == 1) {
@@ -595,30 +706,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
   griddep_launch_dependents();
   griddep_wait();
   const uint32_t tmem = ctl->tmem_base;
-  int64_t fb, fe, total;
-  int ranges;
-  plan(p, ctl, reinterpret_cast<uint32_t*>(sQ), &fb, &fe, &total, &ranges);
-  const int64_t units = fe - fb;
+  plan(p, ctl, reinterpret_cast<uint32_t*>(sQ));
   if (warp == 0) {
-    key_loop(p, ctl, sK, lane, units);
+    key_loop(p, ctl, sK, lane);
   } else if (warp == 1) {
-    mma_loop(p, ctl, sK, sQ, tmem, units);
+    mma_loop(p, ctl, sK, sQ, tmem);
   } else if (warp >= kSoftWarp) {
-    weigh_loop(p, ctl, tmem, (warp - kSoftWarp) >> 2, warp & 3, lane, units);
+    weigh_loop(p, ctl, tmem, (warp - kSoftWarp) >> 2, warp & 3, lane);
   } else if (warp >= kQueryWarp) {
-    query_loop(p, ctl, sQ, threadIdx.x - 32 * kQueryWarp, units);
+    query_loop(p, ctl, sQ, threadIdx.x - 32 * kQueryWarp);
   }
   if (threadIdx.x == 0 && p.cut) {   // what the sum of the parts has to know of this range's end
     MassSplit s;
     s.valid = 0;
-    for (PieceIter c(p, ctl, units); c.valid(); c.next(p, ctl))
+    for (PieceIter c(p, ctl); c.valid(); c.next(p, ctl))
       if (c.b0 == c.grp.lo && c.b1 < c.grp.hi) {
         s.valid = 1;
         s.seq = c.seq;
         s.g = c.g;
         s.k0 = c.grp.k0;
         s.keys = min(c.grp.tiles * kMassTile, c.it.L - c.grp.k0);
-        s.last = range_of(fe + (c.grp.hi - c.b1) - 1, total, ranges);
+        s.last = range_of(ctl->end + (c.grp.hi - c.b1) - 1, ctl->before[p.n], ctl->ranges);
       }
     p.split[blockIdx.x] = s;
   }

@@ -14,6 +14,7 @@ struct MassView {
 
 constexpr int kMassTile = 128;   // keys of a tile, (token, head) pairs of a query block at most
 constexpr int kMassSpan = 4;     // tiles of a group, at most
+constexpr int kMassQueryStep = 4;   // rows of a query block that are copied at a time
 
 // The group that a CTA's range begins and does not finish: the ranges up to `last` hold the rest.
 struct MassSplit {
@@ -36,7 +37,10 @@ struct MassParams {
   int H, G, hg;             // hg = H / G
   int tpb, heads, chunks;   // tokens and heads of a block; blocks that the heads of a group take
   int cut;                  // 1: a group's blocks may be cut between ranges (more than stay in shared memory)
-  int span, span_from;      // tiles of a group, where a launch has as many tiles a CTA (else 1)
+  uint32_t inv_tpb, inv_heads, inv_chunks;   // ceil(2^32 / n), 0 for n = 1
+  int64_t step, wrap;       // elements from a block's pair to the one kMassQueryStep on; more where that passes `heads` heads
+  int step_h;               // kMassQueryStep mod heads
+  int64_t span_from;        // tiles of a launch from which groups have kMassSpan of them (else 1)
   int tree;                 // 1: mask, 0: n_sink and window
   int n_sink, window;
   float scale2;             // log2(e) / sqrt(d)
