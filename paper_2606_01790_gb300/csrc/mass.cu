@@ -29,11 +29,11 @@ cudaLaunchConfig_t config(cudaLaunchAttribute* attr, dim3 grid, int threads, cud
 
 // ---------------------------------------------------------------- mass: units and their order
 
-constexpr int kMassWarps = 12;
+constexpr int kMassWarps = 16;
 constexpr int kThreads = 32 * kMassWarps;
-constexpr int kQueryWarp = 2, kSoftWarp = 4;      // first of the query warps (2) and of the weighing warps (8)
+constexpr int kMmaWarp = 2, kQueryWarp = 4, kSoftWarp = 8;   // (0 and 1: keys; 4 query warps, 8 weighing warps)
 constexpr int kQueryThreads = 32 * (kSoftWarp - kQueryWarp);
-static_assert(kQueryThreads / 16 == kMassQueryStep, "16 threads take a row of 256 bytes");
+static_assert(kQueryThreads / 16 == kMassQueryStep && kQueryThreads >= kMassTile, "16 threads take a row of 256 bytes");
 constexpr int kTileBytes = kMassTile * 256;       // 128 keys x 128 bf16, or as many (token, head) pairs: 32 KB
 constexpr int kHalfBytes = kTileBytes / 2;
 constexpr int kKeySlots = 4, kQuerySlots = 2;     // rings; a tile of keys has an accumulator of its own
@@ -317,8 +317,9 @@ struct Ring {
 
 // ---------------------------------------------------------------- mass: roles
 
-// Keys: the tiles' pages into the ring.  Lane l holds the number of page base + l of the row.
-__device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int lane) {
+// Keys: the tiles' pages into the ring, half of the channels a warp (one warp alone took 2,100 cycles a tile of four
+// pages, where the copy rate leaves 1,500).
+__device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int half, int lane) {
   const uint64_t pol = policy_evict_first();
   const int P = 1 << p.shift, rows = min(P, 64), boxes = kMassTile / rows;
   Ring<kKeySlots> st;
@@ -359,18 +360,17 @@ __device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int lane) {
       ok = warp_wait(ctl, &ctl->k_empty[st.at], st.par ^ 1, p.wait_ns);
       if (!ok) break;
       const bool leader = elect_one();
-      if (leader) mbar_arrive_expect_tx(&ctl->k_full[st.at], kTileBytes);
+      if (leader) mbar_arrive_expect_tx(&ctl->k_full[st.at], kHalfBytes);
       for (int b = 0; b < boxes; ++b) {
         const int key = c.grp.k0 + i * kMassTile + b * rows;
         const int at = (key >> p.shift) - base;
         const int near = __shfl_sync(kFull, id, at & 31), far = __shfl_sync(kFull, id_next, at & 31);
         const int page = at < 32 ? near : far;
-        if (leader)
-          for (int h = 0; h < 2; ++h) {
-            uint8_t* dst = sK + st.at * kTileBytes + h * kHalfBytes + b * rows * 128;
-            if (p.cut) tma_load_4d(dst, &p.tmk, &ctl->k_full[st.at], h * 64, key & (P - 1), c.g, page);
-            else tma_load_4d_hint(dst, &p.tmk, &ctl->k_full[st.at], h * 64, key & (P - 1), c.g, page, pol);
-          }
+        if (leader) {
+          uint8_t* dst = sK + st.at * kTileBytes + half * kHalfBytes + b * rows * 128;
+          if (p.cut) tma_load_4d(dst, &p.tmk, &ctl->k_full[st.at], half * 64, key & (P - 1), c.g, page);
+          else tma_load_4d_hint(dst, &p.tmk, &ctl->k_full[st.at], half * 64, key & (P - 1), c.g, page, pol);
+        }
       }
       __syncwarp();
       used |= 1u << st.at;
@@ -422,14 +422,24 @@ __device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) 
         }
         const Block blk(p, c.it.n, b);
         const int columns = blk.columns();
+        float lse = 0.f;
+        uint64_t bits = 0;
+        int tok = 0;   // (a pair a thread; on their way before the copies)
+        if (tid < blk.count) {
+          const int at_t = quotient(tid, p.inv_heads);
+          tok = blk.t0 + at_t;
+          const int64_t at = static_cast<int64_t>(c.seq) * p.T + tok;
+          lse = p.lse[at * p.H + c.g * p.hg + blk.h0 + tid - at_t * p.heads];
+          if (p.tree) bits = p.mask[at];
+        }
         int r = tid >> 4, t = quotient(r, p.inv_heads), h = r - t * p.heads;
         const __nv_bfloat16* q = p.q + c.seq * p.q_seq + (static_cast<int64_t>(c.g) * p.hg + blk.h0 + h) * p.q_head +
                                  (blk.t0 + t) * p.q_token + chunk * 8;
         uint32_t dst = smem_u32(sQ) + st.at * kTileBytes + (chunk >> 3) * kHalfBytes + r * 128 + (((chunk & 7) ^ (r & 7)) << 4);
 #pragma unroll 4
-        for (; r < columns; r += kMassQueryStep) {
+        for (; r < columns; r += kMassQueryStep) {   // (eight rows on, the swizzle is the same)
           cp_async16(dst, r < blk.count ? q : p.q, r < blk.count);
-          dst = (dst + kMassQueryStep * 128) ^ 64;   // (four rows on, the swizzle differs by four chunks)
+          dst += kMassQueryStep * 128;
           q += p.step;
           h += p.step_h;
           if (h >= p.heads) {
@@ -438,13 +448,11 @@ __device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) 
           }
         }
         cp_async_commit();
-        for (int i = tid; i < blk.count; i += kQueryThreads) {
-          const int at_t = quotient(i, p.inv_heads), t = blk.t0 + at_t, h = c.g * p.hg + blk.h0 + i - at_t * p.heads;
-          const int64_t at = static_cast<int64_t>(c.seq) * p.T + t;
+        if (tid < blk.count) {
           Pairs& pr = ctl->pairs[st.at];
-          pr.lse[i] = -1.4426950408889634f * p.lse[at * p.H + h];
-          pr.pos[i] = c.it.L - c.it.n + t;
-          if (p.tree) pr.bits[i] = p.mask[at];
+          pr.lse[tid] = -1.4426950408889634f * lse;
+          pr.pos[tid] = c.it.L - c.it.n + tok;
+          if (p.tree) pr.bits[tid] = bits;
         }
         const int slot = st.at;
         if (due >= 0) {   // (its copies were under way before these)
@@ -523,14 +531,13 @@ __device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const
   __syncwarp();
 }
 
-// Sum of 32 pairs' weights from column c on, all of them seen; TAIL: of those in front of `count` (behind
+// Sum of 16 pairs' weights from column c on, all of them seen; TAIL: of those in front of `count` (behind
 // them an earlier block may have left anything).
 template <bool TAIL>
-__device__ __forceinline__ float weigh32(const uint32_t (&z)[32], const float* lse, float c2, int count) {
+__device__ __forceinline__ float2 weigh16(const uint32_t (&z)[16], const float* lse, float c2, int count, float2 acc) {
   const float2 sc = make_float2(c2, c2);
-  float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-  for (int i = 0; i < 32; i += 4) {
+  for (int i = 0; i < 16; i += 4) {
     const float4 l = *reinterpret_cast<const float4*>(lse + i);
     const float2 a = ffma2(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), sc, make_float2(l.x, l.y));
     const float2 b = ffma2(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), sc, make_float2(l.z, l.w));
@@ -539,26 +546,25 @@ __device__ __forceinline__ float weigh32(const uint32_t (&z)[32], const float* l
       x = make_float2(i < count ? x.x : 0.f, i + 1 < count ? x.y : 0.f);
       y = make_float2(i + 2 < count ? y.x : 0.f, i + 3 < count ? y.y : 0.f);
     }
-    acc[0] = fadd2(acc[0], x);
-    acc[1] = fadd2(acc[1], y);
+    acc = fadd2(acc, fadd2(x, y));
   }
-  const float2 s = fadd2(acc[0], acc[1]);
-  return s.x + s.y;
+  return acc;
 }
 
-// A block that every key of the tile is seen by: 32 columns at a time, the next ones on their way.
+// A block that the warp's keys are seen by: 16 columns at a time, the next ones on their way.
 __device__ __forceinline__ float weigh_block(uint32_t addr, const float* lse, float c2, int count) {
-  uint32_t z[2][32];
-  float sum = 0.f;
-  tmem_ld32_async(addr, z[0]);
+  uint32_t z[2][16];
+  float2 acc = make_float2(0.f, 0.f);
+  tmem_ld16_async(addr, z[0]);
 #pragma unroll
-  for (int k = 0; k < kMassTile / 32; ++k) {
-    if (32 * k >= count) break;
-    tmem_wait32(z[k & 1]);
-    if (32 * (k + 1) < count) tmem_ld32_async(addr + 32 * (k + 1), z[(k + 1) & 1]);
-    sum += 32 * (k + 1) <= count ? weigh32<false>(z[k & 1], lse + 32 * k, c2, 0) : weigh32<true>(z[k & 1], lse + 32 * k, c2, count - 32 * k);
+  for (int k = 0; k < kMassTile / 16; ++k) {
+    if (16 * k >= count) break;
+    tmem_wait16(z[k & 1]);
+    if (16 * (k + 1) < count) tmem_ld16_async(addr + 16 * (k + 1), z[(k + 1) & 1]);
+    acc = 16 * (k + 1) <= count ? weigh16<false>(z[k & 1], lse + 16 * k, c2, 0, acc)
+                                : weigh16<true>(z[k & 1], lse + 16 * k, c2, count - 16 * k, acc);
   }
-  return sum;
+  return acc.x + acc.y;
 }
 
 // A block that is not: of the pairs in front of `count` those that see key j.
@@ -682,7 +688,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kKeySlots; ++i) {
-      mbar_init(&ctl->k_full[i], 1);
+      mbar_init(&ctl->k_full[i], 2);
       mbar_init(&ctl->k_empty[i], 1);
       mbar_init(&ctl->s_full[i], 1);
       mbar_init(&ctl->s_empty[i], 4);
@@ -696,7 +702,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
     ctl->end = 0;
     fence_mbar_init();
   }
-  if (warp == 1) {
+  if (warp == kMmaWarp) {
     tmem_alloc(&ctl->tmem_base, kTmemCols);
     tmem_relinquish();
   }
@@ -707,9 +713,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
   griddep_wait();
   const uint32_t tmem = ctl->tmem_base;
   plan(p, ctl, reinterpret_cast<uint32_t*>(sQ));
-  if (warp == 0) {
-    key_loop(p, ctl, sK, lane);
-  } else if (warp == 1) {
+  if (warp < kMmaWarp) {
+    key_loop(p, ctl, sK, warp, lane);
+  } else if (warp == kMmaWarp) {
     mma_loop(p, ctl, sK, sQ, tmem);
   } else if (warp >= kSoftWarp) {
     weigh_loop(p, ctl, tmem, (warp - kSoftWarp) >> 2, warp & 3, lane);
@@ -731,7 +737,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
     p.split[blockIdx.x] = s;
   }
   __syncthreads();
-  if (warp == 1) {
+  if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
   }

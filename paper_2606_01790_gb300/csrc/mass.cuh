@@ -14,7 +14,7 @@ struct MassView {
 
 constexpr int kMassTile = 128;   // keys of a tile, (token, head) pairs of a query block at most
 constexpr int kMassSpan = 4;     // tiles of a group, at most
-constexpr int kMassQueryStep = 4;   // rows of a query block that are copied at a time
+constexpr int kMassQueryStep = 8;   // rows of a query block that are copied at a time
 
 // The group that a CTA's range begins and does not finish: the ranges up to `last` hold the rest.
 struct MassSplit {
