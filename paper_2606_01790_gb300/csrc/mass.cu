@@ -402,71 +402,53 @@ struct Block {
 __device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) {
   Ring<kQuerySlots> st;
   bool ok = true, there = false;   // there: the blocks of this row and KV head stay
-  int due = -1;                    // slot whose copies are under way
   const int lane = tid & 31, chunk = tid & 15;
-  auto hand_over = [&] {
-    if (due < 0) return;
-    cp_async_wait();
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&ctl->q_full[due]);
-    due = -1;
-  };
   for (PieceIter c(p, ctl); ok && c.valid(); there ? c.skip_head(p, ctl) : c.next(p, ctl)) {
     there = false;
     for (int b = c.b0; ok && b < c.b1; ++b) {
-        if (!__all_sync(kFull, mbar_try_wait(&ctl->q_empty[st.at], st.par ^ 1))) {   // time to see to the block before
-          hand_over();
-          ok = warp_wait(ctl, &ctl->q_empty[st.at], st.par ^ 1, p.wait_ns);
-          if (!ok) break;
-        }
-        const Block blk(p, c.it.n, b);
-        const int columns = blk.columns();
-        float lse = 0.f;
-        uint64_t bits = 0;
-        int tok = 0;   // (a pair a thread; on their way before the copies)
-        if (tid < blk.count) {
-          const int at_t = quotient(tid, p.inv_heads);
-          tok = blk.t0 + at_t;
-          const int64_t at = static_cast<int64_t>(c.seq) * p.T + tok;
-          lse = p.lse[at * p.H + c.g * p.hg + blk.h0 + tid - at_t * p.heads];
-          if (p.tree) bits = p.mask[at];
-        }
-        int r = tid >> 4, t = quotient(r, p.inv_heads), h = r - t * p.heads;
-        const __nv_bfloat16* q = p.q + c.seq * p.q_seq + (static_cast<int64_t>(c.g) * p.hg + blk.h0 + h) * p.q_head +
-                                 (blk.t0 + t) * p.q_token + chunk * 8;
-        uint32_t dst = smem_u32(sQ) + st.at * kTileBytes + (chunk >> 3) * kHalfBytes + r * 128 + (((chunk & 7) ^ (r & 7)) << 4);
-#pragma unroll 4
-        for (; r < columns; r += kMassQueryStep) {   // (eight rows on, the swizzle is the same)
-          cp_async16(dst, r < blk.count ? q : p.q, r < blk.count);
-          dst += kMassQueryStep * 128;
-          q += p.step;
-          h += p.step_h;
-          if (h >= p.heads) {
-            h -= p.heads;
-            q += p.wrap;
-          }
-        }
-        cp_async_commit();
-        if (tid < blk.count) {
-          Pairs& pr = ctl->pairs[st.at];
-          pr.lse[tid] = -1.4426950408889634f * lse;
-          pr.pos[tid] = c.it.L - c.it.n + tok;
-          if (p.tree) pr.bits[tid] = bits;
-        }
-        const int slot = st.at;
-        if (due >= 0) {   // (its copies were under way before these)
-          cp_async_wait_1();
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&ctl->q_full[due]);
-        }
-        due = slot;
-        st.next();
-        there = !p.cut;
+      ok = warp_wait(ctl, &ctl->q_empty[st.at], st.par ^ 1, p.wait_ns);
+      if (!ok) break;
+      const Block blk(p, c.it.n, b);
+      const int columns = blk.columns();
+      float lse = 0.f;
+      uint64_t bits = 0;
+      int tok = 0;   // (a pair a thread; on their way before the copies)
+      if (tid < blk.count) {
+        const int at_t = quotient(tid, p.inv_heads);
+        tok = blk.t0 + at_t;
+        const int64_t at = static_cast<int64_t>(c.seq) * p.T + tok;
+        lse = p.lse[at * p.H + c.g * p.hg + blk.h0 + tid - at_t * p.heads];
+        if (p.tree) bits = p.mask[at];
       }
+      int r = tid >> 4, t = quotient(r, p.inv_heads), h = r - t * p.heads;
+      const __nv_bfloat16* q = p.q + c.seq * p.q_seq + (static_cast<int64_t>(c.g) * p.hg + blk.h0 + h) * p.q_head +
+                               (blk.t0 + t) * p.q_token + chunk * 8;
+      uint32_t dst = smem_u32(sQ) + st.at * kTileBytes + (chunk >> 3) * kHalfBytes + r * 128 + (((chunk & 7) ^ (r & 7)) << 4);
+#pragma unroll 4
+      for (; r < columns; r += kMassQueryStep) {   // (eight rows on, the swizzle is the same)
+        cp_async16(dst, r < blk.count ? q : p.q, r < blk.count);
+        dst += kMassQueryStep * 128;
+        q += p.step;
+        h += p.step_h;
+        if (h >= p.heads) {
+          h -= p.heads;
+          q += p.wrap;
+        }
+      }
+      if (tid < blk.count) {
+        Pairs& pr = ctl->pairs[st.at];
+        pr.lse[tid] = -1.4426950408889634f * lse;
+        pr.pos[tid] = c.it.L - c.it.n + tok;
+        if (p.tree) pr.bits[tid] = bits;
+      }
+      cp_async_wait();
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ctl->q_full[st.at]);
+      st.next();
+      there = !p.cut;
+    }
   }
-  hand_over();
   if (!ok) fail(ctl, p.err);
 }
 

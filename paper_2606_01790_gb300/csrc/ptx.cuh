@@ -125,14 +125,12 @@ __device__ __forceinline__ uint64_t policy_evict_first() {
 
 // ------------------------------------------------------------------ cp.async
 
-// 16 bytes into shared memory, or zeros; this thread's copies up to a commit are one group.
+// 16 bytes into shared memory, or zeros.
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// Until every group of this thread has landed, or every one but the last.
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
-__device__ __forceinline__ void cp_async_wait_1() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+// Until this thread's copies have landed.
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // ------------------------------------------------------------------ tcgen05
 
