@@ -513,11 +513,26 @@ __device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const
   __syncwarp();
 }
 
-// Sum of 16 pairs' weights from column c on, all of them seen; TAIL: of those in front of `count` (behind
-// them an earlier block may have left anything).
+// 16 accumulator columns, as tmem_ld16_async and tmem_wait16, but without their order against other memory: what
+// is read between them is read-only here, and may be read ahead.
+__device__ __forceinline__ void ld16(uint32_t addr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void wait16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;\n"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+
+// Sum of 16 pairs' weights, all of them seen; TAIL: of those in front of `count` (behind them an earlier block
+// may have left anything).
 template <bool TAIL>
-__device__ __forceinline__ float2 weigh16(const uint32_t (&z)[16], const float* lse, float c2, int count, float2 acc) {
-  const float2 sc = make_float2(c2, c2);
+__device__ __forceinline__ float2 weigh16(const uint32_t (&z)[16], const float* lse, float2 sc, int count, float2 acc) {
 #pragma unroll
   for (int i = 0; i < 16; i += 4) {
     const float4 l = *reinterpret_cast<const float4*>(lse + i);
@@ -533,18 +548,31 @@ __device__ __forceinline__ float2 weigh16(const uint32_t (&z)[16], const float* 
   return acc;
 }
 
-// A block that the warp's keys are seen by: 16 columns at a time, the next ones on their way.
+// A block that the warp's keys are seen by: 16 columns at a time, the next ones on their way.  (A short loop: unrolled
+// over the block, whose code is then longer than the innermost instruction caches, it took half as long again.)
 __device__ __forceinline__ float weigh_block(uint32_t addr, const float* lse, float c2, int count) {
-  uint32_t z[2][16];
+  const float2 sc = make_float2(c2, c2);
+  uint32_t z0[16], z1[16];
   float2 acc = make_float2(0.f, 0.f);
-  tmem_ld16_async(addr, z[0]);
-#pragma unroll
-  for (int k = 0; k < kMassTile / 16; ++k) {
-    if (16 * k >= count) break;
-    tmem_wait16(z[k & 1]);
-    if (16 * (k + 1) < count) tmem_ld16_async(addr + 16 * (k + 1), z[(k + 1) & 1]);
-    acc = 16 * (k + 1) <= count ? weigh16<false>(z[k & 1], lse + 16 * k, c2, 0, acc)
-                                : weigh16<true>(z[k & 1], lse + 16 * k, c2, count - 16 * k, acc);
+  ld16(addr, z0);
+#pragma unroll 1
+  for (; count >= 32; count -= 32) {
+    wait16(z0);
+    ld16(addr + 16, z1);
+    acc = weigh16<false>(z0, lse, sc, 0, acc);
+    wait16(z1);
+    if (count > 32) ld16(addr + 32, z0);
+    acc = weigh16<false>(z1, lse + 16, sc, 0, acc);
+    addr += 32;
+    lse += 32;
+  }
+#pragma unroll 1
+  for (; count > 0; count -= 16) {
+    wait16(z0);
+    acc = weigh16<true>(z0, lse, sc, count, acc);
+    addr += 16;
+    lse += 16;
+    if (count > 16) ld16(addr, z0);
   }
   return acc.x + acc.y;
 }
@@ -608,15 +636,13 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
       const Block blk(p, c.it.n, c.b0 + b);
       const Pairs& pr = ctl->pairs[slot];
       const int first = ctx + blk.t0, end = ctx + min(blk.t0 + p.tpb, c.it.n) - 1;   // positions of the block's tokens
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int i = i0 + 2 * u;
-        if (!ok || i >= c.grp.tiles) break;
+#pragma unroll 1
+      for (int i = i0; i < c.grp.tiles; i += 2) {
         const uint32_t a = (tile + i) & (kKeySlots - 1);
         ok = warp_wait(ctl, &ctl->s_full[a], par >> a & 1, p.wait_ns);
         if (!ok) break;
         tc_fence_after();
-        // by the warp's 32 keys: seen by all of the block, by none, or by some
+        float w = 0.f;   // by the warp's 32 keys: seen by all of the block, by none, or by some
         const int k0 = c.grp.k0 + i * kMassTile + 32 * quad, k1 = k0 + 31;
         bool all, none = k0 >= c.it.L;
         if (p.tree) {
@@ -625,9 +651,11 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
           all = k1 <= first && (k1 < p.n_sink || k0 > end - p.window);
           none = none || k0 > end || (k0 >= p.n_sink && k1 <= first - p.window);
         }
-        if (all) sum[u] += weigh_block(lanes + a * kMassTile, pr.lse, p.scale2, blk.count);
+        if (all) w = weigh_block(lanes + a * kMassTile, pr.lse, p.scale2, blk.count);
         else if (!none)
-          sum[u] += weigh_masked(lanes + a * kMassTile, &pr, p.scale2, p.tree, p.n_sink, p.window, blk.count, k0 + lane, ctx, c.it.L);
+          w = weigh_masked(lanes + a * kMassTile, &pr, p.scale2, p.tree, p.n_sink, p.window, blk.count, k0 + lane, ctx, c.it.L);
+        if (i < 2) sum[0] += w;
+        else sum[1] += w;
         tc_fence_before();
         par ^= 1u << a;
         __syncwarp();
