@@ -51,7 +51,6 @@ struct Item {
 // A block of (token, head) pairs as the weighing warps see it.
 struct Pairs {
   alignas(16) float lse[kMassTile];   // -lse in base 2
-  int pos[kMassTile];                 // position of the token
   uint64_t bits[kMassTile];           // tree: drafted tokens seen
 };
 
@@ -412,11 +411,9 @@ __device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) 
       const int columns = blk.columns();
       float lse = 0.f;
       uint64_t bits = 0;
-      int tok = 0;   // (a pair a thread; on their way before the copies)
-      if (tid < blk.count) {
+      if (tid < blk.count) {   // (a pair a thread; on their way before the copies)
         const int at_t = quotient(tid, p.inv_heads);
-        tok = blk.t0 + at_t;
-        const int64_t at = static_cast<int64_t>(c.seq) * p.T + tok;
+        const int64_t at = static_cast<int64_t>(c.seq) * p.T + blk.t0 + at_t;
         lse = p.lse[at * p.H + c.g * p.hg + blk.h0 + tid - at_t * p.heads];
         if (p.tree) bits = p.mask[at];
       }
@@ -438,7 +435,6 @@ __device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) 
       if (tid < blk.count) {
         Pairs& pr = ctl->pairs[st.at];
         pr.lse[tid] = -1.4426950408889634f * lse;
-        pr.pos[tid] = c.it.L - c.it.n + tok;
         if (p.tree) pr.bits[tid] = bits;
       }
       cp_async_wait();
@@ -577,28 +573,45 @@ __device__ __forceinline__ float weigh_block(uint32_t addr, const float* lse, fl
   return acc.x + acc.y;
 }
 
-// A block that is not: of the pairs in front of `count` those that see key j.
-// (Values, not the parameters' address: a call that is not inlined would read them from memory at every use.)
-__device__ __noinline__ float weigh_masked(uint32_t addr, const Pairs* pairs, float c2, int tree, int n_sink, int window, int count, int j,
-                                           int ctx, int L) {
+// A block under a window that is not: the tokens that see a key follow one another, so that their pairs are the columns
+// lo .. hi - 1 (of this thread's key).
+__device__ __forceinline__ float weigh_columns(uint32_t addr, const float* lse, float c2, int lo, int hi, int count) {
   float sum = 0.f;
-  // sink: positions j .. j + reach - 1 see the key; tree: bit `shift` of the token's half word, `any` the cached ones
-  const uint32_t reach = j < n_sink ? 0x7fffffffu : static_cast<uint32_t>(window);
-  const int drafted = max(j - ctx, 0);
-  const uint32_t any = j < ctx ? ~0u : 0u;
-  const int shift = drafted & 31;
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(pairs->bits) + (drafted >> 5 & 1);
-  const bool real = j < L;
 #pragma unroll 1
-  for (int c = 0; c < count; c += 16) {
+  for (; count > 0; count -= 16) {
     uint32_t z[16];
-    tmem_ld16_async(addr + c, z);
-    tmem_wait16(z);
+    ld16(addr, z);
+    wait16(z);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const bool seen = tree ? ((words[2 * (c + i)] | any) >> shift & 1) : static_cast<uint32_t>(pairs->pos[c + i] - j) < reach;
-      const float w = ex2_approx(fmaf(__uint_as_float(z[i]), c2, pairs->lse[c + i]));
-      sum += seen && real && c + i < count ? w : 0.f;
+      const float w = ex2_approx(fmaf(__uint_as_float(z[i]), c2, lse[i]));
+      sum += i >= lo && i < hi ? w : 0.f;
+    }
+    addr += 16;
+    lse += 16;
+    lo -= 16;
+    hi -= 16;
+  }
+  return sum;
+}
+
+// A block of a tree that is not: of the pairs in front of `count` those whose token has bit j - ctx, or all for a cached key.
+__device__ __forceinline__ float weigh_bits(uint32_t addr, const Pairs& pr, float c2, int count, int j, int ctx, int L) {
+  float sum = 0.f;
+  const int drafted = max(j - ctx, 0), shift = drafted & 31;
+  const uint32_t any = j < ctx ? ~0u : 0u;
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(pr.bits) + (drafted >> 5 & 1);
+  if (j >= L) count = 0;
+  const int most = __reduce_max_sync(kFull, count);
+#pragma unroll 1
+  for (int c = 0; c < most; c += 16) {
+    uint32_t z[16];
+    ld16(addr + c, z);
+    wait16(z);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float w = ex2_approx(fmaf(__uint_as_float(z[i]), c2, pr.lse[c + i]));
+      sum += ((words[2 * (c + i)] | any) >> shift & 1) && c + i < count ? w : 0.f;
     }
   }
   return sum;
@@ -651,9 +664,17 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
           all = k1 <= first && (k1 < p.n_sink || k0 > end - p.window);
           none = none || k0 > end || (k0 >= p.n_sink && k1 <= first - p.window);
         }
-        if (all) w = weigh_block(lanes + a * kMassTile, pr.lse, p.scale2, blk.count);
-        else if (!none)
-          w = weigh_masked(lanes + a * kMassTile, &pr, p.scale2, p.tree, p.n_sink, p.window, blk.count, k0 + lane, ctx, c.it.L);
+        const uint32_t at = lanes + a * kMassTile;
+        if (all) {
+          w = weigh_block(at, pr.lse, p.scale2, blk.count);
+        } else if (p.tree) {
+          if (!none) w = weigh_bits(at, pr, p.scale2, blk.count, k0 + lane, ctx, c.it.L);
+        } else if (!none) {
+          const int j = k0 + lane, nt = end - first + 1;
+          const int ta = min(max(j - first, 0), nt), tb = j < p.n_sink ? nt : min(max(j + p.window - first, 0), nt);
+          const int per = nt > 1 ? p.heads : blk.count;   // columns of a token
+          w = weigh_columns(at, pr.lse, p.scale2, ta * per, tb * per, blk.count);
+        }
         if (i < 2) sum[0] += w;
         else sum[1] += w;
         tc_fence_before();
