@@ -645,6 +645,7 @@ starkv_status starkv_init_state(const starkv_config* cfg, starkv_state** out, vo
   if (e == cudaSuccess) e = attn_configure();
   if (e == cudaSuccess) e = pages_configure();
   if (e == cudaSuccess) e = mass_configure();
+  if (e == cudaSuccess) e = page_choose_configure();
   if (e == cudaSuccess) e = paged_attn_configure();
   if (e != cudaSuccess) {
     delete st;
@@ -1548,7 +1549,7 @@ starkv_status validate_bounds(const starkv_state* st, const starkv_pages* pg, co
 struct SparseWs {
   PagedWs attn;
   int per_launch, n_list;
-  size_t list, keys, total;
+  size_t list, keys, scores, total;
 };
 
 SparseWs sparse_ws(const starkv_state* st, const starkv_pages& p, int n, int T, int n_chosen) {
@@ -1557,12 +1558,14 @@ SparseWs sparse_ws(const starkv_state* st, const starkv_pages& p, int n, int T, 
   w.attn = paged_attn_ws(st);
   w.n_list = std::min(n_chosen, p.max_pages);
   const int nblk = (c.n_heads / c.n_kv_heads + kPagedRows - 1) / kPagedRows;
-  const int64_t each = static_cast<int64_t>(c.n_kv_heads) * (static_cast<int64_t>(w.n_list) * 4 + static_cast<int64_t>(p.max_pages) * 8);
+  const int64_t each = static_cast<int64_t>(c.n_kv_heads) * (static_cast<int64_t>(w.n_list) * 4 + static_cast<int64_t>(p.max_pages) * 12);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kPagedItems / nblk, (int64_t(256) << 20) / each));
   w.per_launch = static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(1, static_cast<int64_t>(n) * T)));
   w.list = w.attn.total;
   w.keys = w.list + align256(static_cast<size_t>(w.per_launch) * c.n_kv_heads * w.n_list * sizeof(int32_t));
-  w.total = w.keys + align256(static_cast<size_t>(w.per_launch) * c.n_kv_heads * p.max_pages * sizeof(uint64_t));
+  const size_t pages = static_cast<size_t>(w.per_launch) * c.n_kv_heads * p.max_pages;
+  w.scores = w.keys + align256(pages * sizeof(uint64_t));
+  w.total = w.scores + (p.max_pages > kChoosePages ? align256(pages * sizeof(uint32_t)) : 0);
   return w;
 }
 
@@ -1846,6 +1849,7 @@ starkv_status starkv_sparse_attention(starkv_state* st, const starkv_pages* page
   ch.chosen = chosen;
   ch.n_chosen = n_chosen;
   ch.keys = reinterpret_cast<uint64_t*>(ws + w.keys);
+  ch.scores = reinterpret_cast<uint32_t*>(ws + w.scores);
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   const int64_t items = static_cast<int64_t>(q->n) * q->T;
   if (items >= (int64_t(1) << 31)) return set_error(STARKV_ERR_UNSUPPORTED, "queries: n * T >= 2^31");
@@ -1854,6 +1858,8 @@ starkv_status starkv_sparse_attention(starkv_state* st, const starkv_pages* page
     const int m = static_cast<int>(std::min<int64_t>(items - i0, w.per_launch));
     ch.item0 = p.item0 = static_cast<int>(i0);
     ch.items = p.n = m;
+    // CTAs of a cluster: as many as keep the SMs busy, with 64 pages of a row each or more
+    for (ch.ctas = 1; ch.ctas < kMaxCluster && m * p.G * ch.ctas < 2 * st->num_sms && ch.ctas * 128 <= pg.max_pages;) ch.ctas *= 2;
     p.lse = q->lse ? q->lse + i0 * p.H : nullptr;
     p.grid = static_cast<int>(std::min<int64_t>(st->num_sms, m * p.nblk * max_units * p.G));
     CUDA_TRY(launch(st, STARKV_KERNEL_PAGE_CHOOSE, cs, [&] { return page_choose_launch(ch, cs); }));

@@ -8,8 +8,8 @@
 //   up_c = sum_h max(q_hc, 0),  down_c = sum_h min(q_hc, 0),
 // so that the heads of a group cost one product of 256 terms a page.  A query takes the
 // first pages, the last ones up to its own and the best of the others; equal scores go to
-// the lower page.  Which of two pages is taken hangs on the last bit of their scores: the
-// products of two bf16 numbers and their sums are formed in 64 bits.
+// the lower page.  Which of two pages is taken hangs on the last bit of their scores, which
+// are those of 64 bits.
 #include <algorithm>
 
 #include "common.cuh"
@@ -135,125 +135,328 @@ namespace {
 
 constexpr int kChooseThreads = 256;
 constexpr int kChooseWarps = kChooseThreads / 32;
+constexpr int kPagesAtOnce = 8;        // of a warp
+constexpr int kFew = 256;              // close pages that are ranked by comparing each with each
 
-// Ascending order of the scores; a NaN (a bound that is none) comes with the greatest, so that
-// its page is not passed over.
-__device__ __forceinline__ uint64_t score_key(double s) {
-  if (s != s) s = INFINITY;
-  const uint64_t b = static_cast<uint64_t>(__double_as_longlong(s + 0.0));   // (-0 is 0)
+// Ascending order as unsigned numbers.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return b >> 31 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
+// (A NaN, of a bound that is none, comes with infinity, so that its page is not passed over; -0 is 0.)
+__device__ __forceinline__ uint64_t order_of(double x) {
+  if (x != x) x = INFINITY;
+  const uint64_t b = static_cast<uint64_t>(__double_as_longlong(x + 0.0));
   return b >> 63 ? ~b : b | (uint64_t(1) << 63);
 }
 
-// Sum over the block of 0 / 1 flags in front of this thread's, and all of them.
-__device__ int2 count_before(bool flag, int* warp_sum) {
+struct ChooseSmem {
+  uint32_t key[kChoosePages];
+  float up[kHeadDim], down[kHeadDim];
+  uint32_t size[kMaxCluster][kChooseWarps];   // largest sum of terms' sizes that a warp met
+  int hist[256];
+  int warp_sum[kChooseWarps];
+  uint64_t prefix;
+  int need, few;
+  uint64_t close[kFew];
+  int close_page[kFew];
+};
+
+// Sum over the block of a count per thread, in front of this thread's; the total to everybody.
+__device__ __forceinline__ int block_before(int x, int* warp_sum, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t m = __ballot_sync(kFull, flag);
-  if (lane == 0) warp_sum[warp] = __popc(m);
+  int inc = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(kFull, inc, o);
+    if (lane >= o) inc += y;
+  }
+  if (lane == 31) warp_sum[warp] = inc;
   __syncthreads();
-  int before = __popc(m & ((1u << lane) - 1)), all = 0;
+  int before = inc - x, all = 0;
 #pragma unroll
   for (int w = 0; w < kChooseWarps; ++w) {
     if (w < warp) before += warp_sum[w];
     all += warp_sum[w];
   }
   __syncthreads();
-  return make_int2(before, all);
+  *total = all;
+  return before;
+}
+
+// The k-th greatest of key(lo) .. key(hi - 1), eight bits at a time; *of_it: how many of those that have
+// it are among the k greatest.
+template <typename Key, typename F>
+__device__ Key kth_greatest(ChooseSmem& s, int lo, int hi, int k, F key, int* of_it) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  Key prefix = 0;
+  for (int bit = static_cast<int>(sizeof(Key)) * 8 - 8; bit >= 0; bit -= 8) {
+    s.hist[tid] = 0;
+    __syncthreads();
+    for (int j = lo + tid; j < hi; j += kChooseThreads) {
+      const Key x = key(j);
+      if (bit == static_cast<int>(sizeof(Key)) * 8 - 8 || (x ^ prefix) >> (bit + 8) == 0) atomicAdd(&s.hist[x >> bit & 255], 1);
+    }
+    __syncthreads();
+    if (tid < 32) {   // lane l: the digits 255 - 8 l downwards
+      int sum = 0, n[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += n[i] = s.hist[255 - 8 * lane - i];
+      int inc = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(kFull, inc, o);
+        if (lane >= o) inc += y;
+      }
+      int left = k - (inc - sum);
+      if (left > 0 && left <= sum) {
+        int i = 0;
+        while (i < 7 && n[i] < left) left -= n[i++];
+        s.prefix = prefix | static_cast<Key>(255 - 8 * lane - i) << bit;
+        s.need = left;
+      }
+    }
+    __syncthreads();
+    prefix = static_cast<Key>(s.prefix);
+    k = s.need;
+  }
+  *of_it = k;
+  return prefix;
 }
 
 }  // namespace
 
-// Block (item, KV head): scores, the threshold by eight bits at a time, the list in order.
+static_assert(kChooseThreads == 256, "a thread a digit");
+
+// Cluster (item, KV head): its CTAs score a share of the pages each, in fp32, into the first one's shared
+// memory (rows of more pages than it holds: into the workspace); the first CTA takes the best.
+//
+// A lane has 8 of the 256 terms; sums over the lanes are taken for eight pages together, halving the pages with every
+// step.  With u = 2^-24 a score is off by at most (8 + 5 + hg) u times the sum of its terms' sizes (the products' sums, the
+// sums over lanes, the weights' sums over heads), plus what underflows: at most E, with the lanes' largest sizes added up for
+// all pages.  With t the k-th greatest score, a page 2 E above t is among the k best and one 2 E below is not; those between are
+// scored again in 64 bits where they are more than the places left: usually none or a few, all of them where scores are equal
+// or sizes are past what 32 bits hold.
 __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_constant__ ChooseParams p) {
-  __shared__ double s_up[kHeadDim], s_down[kHeadDim];
-  __shared__ int hist[256], warp_sum[kChooseWarps];
-  __shared__ uint64_t s_prefix;
-  __shared__ int s_need;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  ChooseSmem& s = *reinterpret_cast<ChooseSmem*>(smem_raw);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = blockIdx.x & (p.ctas - 1), g = blockIdx.y, item = blockIdx.x / p.ctas, v = p.item0 + item;
+  cluster_arrive();   // waited for before the first write into the first CTA's shared memory
   griddep_launch_dependents();
   griddep_wait();
   const PagesView& pg = p.pg;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int item = blockIdx.x, g = blockIdx.y, v = p.item0 + item;
   const SparseQuery sq = sparse_query(p.rows, p.n_tokens, pg.len, pg.n_rows, pg.max_pages, pg.shift, p.T, v);
-  if (!sq.live) return;
-  int32_t* list = p.list + (static_cast<int64_t>(item) * p.G + g) * p.n_list;
-  int32_t* chosen = p.chosen ? p.chosen + (static_cast<int64_t>(v) * p.G + g) * p.n_chosen : nullptr;
-  const int pages = sq.pos < 0 ? 0 : (sq.pos >> pg.shift) + 1;
+  const int pages = !sq.live || sq.pos < 0 ? 0 : (sq.pos >> pg.shift) + 1;
   const int take = min(pages, p.n_list);
   const int32_t* entries = pg.table + static_cast<int64_t>(sq.row) * pg.max_pages;
-  if (chosen)
-    for (int i = take + tid; i < p.n_chosen; i += kChooseThreads) chosen[i] = -1;
   // pages lo .. hi - 1 compete for `need` places; the others are taken anyway
   const int lo = take == pages ? pages : p.n_first, hi = take == pages ? pages : pages - p.n_last;
-  int need = take - (pages - (hi - lo));
-  uint64_t* keys = p.keys + (static_cast<int64_t>(item) * p.G + g) * pg.max_pages;
-  uint64_t least = 0;   // pages with greater keys are taken, and `need` of those that have this one
+  const int need = take - (pages - (hi - lo));
+  const bool here = hi - lo <= kChoosePages;   // the scores fit shared memory
+  const int64_t place = (static_cast<int64_t>(item) * p.G + g) * pg.max_pages;
+  uint32_t* far = p.scores + place - lo;
+  const int seq = v / p.T, t = v - seq * p.T;
+  const __nv_bfloat16* q = p.q + seq * p.q_seq + t * p.q_token + static_cast<int64_t>(g) * p.hg * p.q_head;
   if (need > 0) {
-    const int seq = v / p.T, t = v - seq * p.T;
     if (tid < kHeadDim) {
-      const __nv_bfloat16* q = p.q + seq * p.q_seq + t * p.q_token + static_cast<int64_t>(g) * p.hg * p.q_head + tid;
-      double up = 0, down = 0;
+      float up = 0.f, down = 0.f;
       for (int h = 0; h < p.hg; ++h) {
-        const double x = __bfloat162float(q[h * p.q_head]);
-        up += x < 0 ? 0 : x;   // (a NaN goes into both)
-        down += x > 0 ? 0 : x;
+        const float x = __bfloat162float(q[h * p.q_head + tid]);
+        up += x < 0.f ? 0.f : x;   // (a NaN goes into both)
+        down += x > 0.f ? 0.f : x;
       }
-      s_up[tid] = up;
-      s_down[tid] = down;
+      s.up[tid] = up;
+      s.down[tid] = down;
     }
     __syncthreads();
-    for (int j = lo + warp; j < hi; j += kChooseWarps) {
-      const int page = entries[j];
-      double s = 0;
-      if (page >= 0 && page < pg.n_pages) {
-        const __nv_bfloat16* b = p.bounds + page * p.bounds_page + static_cast<int64_t>(g) * 2 * kHeadDim;
+    float w[8];   // this lane's terms: eight channels, the least keys (lanes 0 .. 15) or the greatest
 #pragma unroll
-        for (int c = lane; c < kHeadDim; c += 32)
-          s += s_down[c] * static_cast<double>(__bfloat162float(b[c])) + s_up[c] * static_cast<double>(__bfloat162float(b[kHeadDim + c]));
+    for (int i = 0; i < 8; ++i) w[i] = lane < 16 ? s.down[lane * 8 + i] : s.up[lane * 8 + i - kHeadDim];
+    uint32_t size = 0;
+    cluster_wait();
+    const uint32_t first_cta = dsmem_map(s.key, 0);
+    const int per = p.ctas * kChooseWarps * kPagesAtOnce;
+    const int own = (rank * kChooseWarps + warp) * kPagesAtOnce;
+    int id = lo + own + (lane & 7) < hi ? entries[lo + own + (lane & 7)] : -1;   // lane l: page l of the eight
+    for (int j0 = lo + own; j0 < hi; j0 += per) {
+      uint4 x[kPagesAtOnce];
+#pragma unroll
+      for (int u = 0; u < kPagesAtOnce; ++u) {
+        const int page = __shfl_sync(kFull, id, u);
+        x[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (page >= 0 && page < pg.n_pages)
+          x[u] = ld_stream(reinterpret_cast<const uint4*>(p.bounds + page * p.bounds_page + static_cast<int64_t>(g) * 2 * kHeadDim) + lane);
       }
+      const int next = j0 + per + (lane & 7);
+      id = next < hi ? entries[next] : -1;
+      float sum[kPagesAtOnce];
 #pragma unroll
-      for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-      if (lane == 0) keys[j] = score_key(s);
+      for (int u = 0; u < kPagesAtOnce; ++u) {
+        const uint32_t words[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+        float a = 0.f, b = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float y0 = __uint_as_float(words[i] << 16), y1 = __uint_as_float(words[i] & 0xFFFF0000u);
+          a = fmaf(w[2 * i], y0, a);
+          a = fmaf(w[2 * i + 1], y1, a);
+          b = fmaf(fabsf(w[2 * i]), fabsf(y0), b);
+          b = fmaf(fabsf(w[2 * i + 1]), fabsf(y1), b);
+        }
+        sum[u] = a;
+        size = max(size, __float_as_uint(b));   // (sizes are not negative; a NaN is above infinity)
+      }
+      // the sum of page (lane & 7), in every lane
+#pragma unroll
+      for (int o = 4; o; o >>= 1)
+#pragma unroll
+        for (int u = 0; u < o; ++u) {
+          const bool upper = lane & o;
+          const float mine = upper ? sum[u + o] : sum[u], theirs = upper ? sum[u] : sum[u + o];
+          sum[u] = mine + __shfl_xor_sync(kFull, theirs, o);
+        }
+      sum[0] += __shfl_xor_sync(kFull, sum[0], 8);
+      sum[0] += __shfl_xor_sync(kFull, sum[0], 16);
+      const int j = j0 + (lane & 7);
+      if (lane < 8 && j < hi) {
+        const uint32_t k = order_of(sum[0] + 0.f);   // (-0 is 0)
+        if (here) dsmem_st_u32(first_cta + (j - lo) * 4, k);
+        else far[j] = k;
+      }
     }
-    if (tid == 0) s_prefix = 0, s_need = need;
+    float total = __uint_as_float(size);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kFull, total, o);
+    if (lane == 0) dsmem_st_u32(dsmem_map(&s.size[rank][warp], 0), __float_as_uint(total));
+  } else {
+    cluster_wait();
+  }
+  cluster_sync();   // (every CTA of the cluster has the same `need`, or leaves from here as well)
+  if (rank != 0 || !sq.live) return;
+
+  int32_t* list = p.list + (static_cast<int64_t>(item) * p.G + g) * p.n_list;
+  int32_t* chosen = p.chosen ? p.chosen + (static_cast<int64_t>(v) * p.G + g) * p.n_chosen : nullptr;
+  if (chosen)
+    for (int i = take + tid; i < p.n_chosen; i += kChooseThreads) chosen[i] = -1;
+  uint32_t* keys = here ? s.key - lo : far;   // from here on: 0 (not taken) or 1
+  if (need > 0) {
+    int of_it;
+    const float at = value_of(kth_greatest<uint32_t>(s, lo, hi, need, [&](int j) { return keys[j]; }, &of_it));
+    uint32_t size = 0;
+    for (int i = lane; i < p.ctas * kChooseWarps; i += 32) size = max(size, s.size[i / kChooseWarps][i % kChooseWarps]);
+    const float E = __uint_as_float(__reduce_max_sync(kFull, size)) * ((16 + p.hg) * 1.001f * 0x1p-24f) + 0x1p-140f;
+    const float above = at + 2.1f * E, below = at - 2.1f * E;
+    if (tid == 0) s.few = 0;
+    int sure = 0, close = 0;
+    for (int j = lo + tid; j < hi; j += kChooseThreads) {
+      const float x = value_of(keys[j]);
+      const bool in = x > above, out = x < below;   // (where E is not a number: neither)
+      sure += in;
+      close += !in && !out;
+    }
+    int n_sure, n_close;
+    block_before(sure, s.warp_sum, &n_sure);
+    block_before(close, s.warp_sum, &n_close);
+    const int left = need - n_sure;
+    const bool all = left == n_close, few = n_close <= kFew;
+    uint64_t* wide = p.keys + place - lo;
+    for (int j = lo + tid; j < hi; j += kChooseThreads) {
+      const float x = value_of(keys[j]);
+      const bool in = x > above, near = !in && !(x < below);
+      if (few || all) {
+        if (near && !all) s.close_page[atomicAdd(&s.few, 1)] = j;
+        keys[j] = in || (near && all);
+      } else {
+        wide[j] = in ? ~uint64_t(0) : near ? 1 : 0;   // (scores are above 1, and below ~0)
+      }
+    }
     __syncthreads();
-    for (int bit = 56; bit >= 0; bit -= 8) {
-      hist[tid] = 0;
-      __syncthreads();
-      const uint64_t prefix = s_prefix;
-      for (int j = lo + tid; j < hi; j += kChooseThreads)
-        if (bit == 56 || (keys[j] ^ prefix) >> (bit + 8) == 0) atomicAdd(&hist[keys[j] >> bit & 255], 1);
-      __syncthreads();
-      if (tid == 0) {
-        int left = s_need, d = 255;
-        while (d > 0 && hist[d] < left) left -= hist[d--];
-        s_prefix = prefix | static_cast<uint64_t>(d) << bit;
-        s_need = left;
+    if (!all) {
+      double wd[8];   // the same terms in 64 bits
+#pragma unroll
+      for (int i = 0; i < 8; ++i) wd[i] = 0;
+      for (int h = 0; h < p.hg; ++h)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const double x = __bfloat162float(q[h * p.q_head + (lane & 15) * 8 + i]);
+          wd[i] += lane < 16 ? (x > 0 ? 0 : x) : (x < 0 ? 0 : x);
+        }
+      auto score = [&](int j) {   // by the whole warp
+        const int page = entries[j];
+        double a = 0;
+        if (page >= 0 && page < pg.n_pages) {
+          const uint4 x = ld_stream(reinterpret_cast<const uint4*>(p.bounds + page * p.bounds_page + static_cast<int64_t>(g) * 2 * kHeadDim) + lane);
+          const uint32_t words[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            a = fma(wd[2 * i], static_cast<double>(__uint_as_float(words[i] << 16)), a);
+            a = fma(wd[2 * i + 1], static_cast<double>(__uint_as_float(words[i] & 0xFFFF0000u)), a);
+          }
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(kFull, a, o);
+        return order_of(a);
+      };
+      if (few) {
+        for (int i = warp; i < n_close; i += kChooseWarps) {
+          const uint64_t k = score(s.close_page[i]);
+          if (lane == 0) s.close[i] = k;
+        }
+        __syncthreads();
+        if (tid < n_close) {
+          const uint64_t k = s.close[tid];
+          const int j = s.close_page[tid];
+          int better = 0;
+          for (int i = 0; i < n_close; ++i) better += s.close[i] > k || (s.close[i] == k && s.close_page[i] < j);
+          keys[j] = better < left;
+        }
+        __syncthreads();
+      } else {
+        for (int j = lo + warp; j < hi; j += kChooseWarps)
+          if (wide[j] == 1) {
+            const uint64_t k = score(j);
+            __syncwarp();
+            if (lane == 0) wide[j] = k;
+          }
+        __syncthreads();
+        const uint64_t least = kth_greatest<uint64_t>(s, lo, hi, need, [&](int j) { return wide[j]; }, &of_it);
+        // of the pages that have the least key the lowest `of_it`: every thread a run of pages
+        const int run = (hi - lo + kChooseThreads - 1) / kChooseThreads, b = min(lo + tid * run, hi), e = min(b + run, hi);
+        int equal = 0, total;
+        for (int j = b; j < e; ++j) equal += wide[j] == least;
+        int before = block_before(equal, s.warp_sum, &total);
+        for (int j = b; j < e; ++j) keys[j] = wide[j] > least || (wide[j] == least && before++ < of_it);
+        __syncthreads();
       }
-      __syncthreads();
     }
-    least = s_prefix;
-    need = s_need;
   }
-  int at = 0, equal = 0;   // taken so far, and of those that have the least key
-  for (int j0 = 0; j0 < pages; j0 += kChooseThreads) {
-    const int j = j0 + tid;
-    const bool rival = j >= lo && j < hi;
-    const uint64_t key = rival && need > 0 ? keys[j] : 0;
-    const int2 e = count_before(rival && need > 0 && key == least, warp_sum);
-    const bool in = j < pages && (!rival || (need > 0 && (key > least || (key == least && equal + e.x < need))));
-    const int2 n = count_before(in, warp_sum);
-    if (in) {
-      list[at + n.x] = entries[j];
-      if (chosen) chosen[at + n.x] = j;
+  // the list, in the order of the pages: every thread a run of them
+  const int run = (pages + kChooseThreads - 1) / kChooseThreads, b = min(tid * run, pages), e = min(b + run, pages);
+  auto taken = [&](int j) { return j < lo || j >= hi || (need > 0 && keys[j]); };
+  int mine = 0, total;
+  for (int j = b; j < e; ++j) mine += taken(j);
+  int at = block_before(mine, s.warp_sum, &total);
+  for (int j = b; j < e; ++j)
+    if (taken(j)) {
+      list[at] = entries[j];
+      if (chosen) chosen[at] = j;
+      ++at;
     }
-    equal += e.y;
-    at += n.y;
-  }
+}
+
+cudaError_t page_choose_configure() {
+  return cudaFuncSetAttribute(k_page_choose, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(ChooseSmem));
 }
 
 cudaError_t page_choose_launch(const ChooseParams& p, cudaStream_t stream) {
-  cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = config(attr, dim3(p.items, p.G), kChooseThreads, stream);
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = config(attr, dim3(p.items * p.ctas, p.G), kChooseThreads, stream);
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.numAttrs = 2;
+  cfg.dynamicSmemBytes = sizeof(ChooseSmem);
   return cudaLaunchKernelEx(&cfg, k_page_choose, p);
 }
 

@@ -61,9 +61,14 @@ struct ChooseParams {
   int32_t* list;                 // [items][G][n_list] page numbers
   int32_t* chosen;               // [n * T][G][n_chosen] places in the row, or NULL
   int n_chosen;
-  uint64_t* keys;                // [items][G][max_pages]
+  int ctas;                      // of a cluster: 1, 2, 4 or 8
+  uint64_t* keys;                // [items][G][max_pages]: scores in 64 bits, where many are close
+  uint32_t* scores;              // the same, in 32: rows of more than kChoosePages pages
 };
 
+constexpr int kChoosePages = 8192;   // scores that shared memory holds
+
+cudaError_t page_choose_configure();
 cudaError_t page_choose_launch(const ChooseParams& p, cudaStream_t stream);
 
 }  // namespace starkv
