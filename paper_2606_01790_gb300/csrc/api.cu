@@ -645,6 +645,7 @@ starkv_status starkv_init_state(const starkv_config* cfg, starkv_state** out, vo
   if (e == cudaSuccess) e = attn_configure();
   if (e == cudaSuccess) e = pages_configure();
   if (e == cudaSuccess) e = mass_configure();
+  if (e == cudaSuccess) e = mass_select_configure();
   if (e == cudaSuccess) e = page_choose_configure();
   if (e == cudaSuccess) e = paged_attn_configure();
   if (e != cudaSuccess) {

@@ -820,13 +820,16 @@ cudaError_t mass_sum_launch(const MassParams& p, cudaStream_t stream) {
 
 namespace {
 
-constexpr int kSelThreads = 1024;
+constexpr int kSelThreads = 512;
 constexpr int kSelWarps = kSelThreads / 32;
+constexpr int kSelKeys = 49152;    // keys that shared memory holds
+constexpr int kSelClose = 512;     // close tokens that are ranked by comparing each with each
 
-// Ascending order; a NaN (a mass that is none) comes with the greatest, infinity, so that its token stays.
+// Ascending order as unsigned numbers; a NaN (a mass that is none) comes with infinity, so that its token
+// stays, and -0 is 0.
 __device__ __forceinline__ uint32_t order_key(float x) {
   if (x != x) x = INFINITY;
-  const uint32_t b = __float_as_uint(x + 0.f);   // (-0 is 0)
+  const uint32_t b = __float_as_uint(x + 0.f);
   return b >> 31 ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ uint64_t order_key(double x) {
@@ -834,39 +837,101 @@ __device__ __forceinline__ uint64_t order_key(double x) {
   const uint64_t b = static_cast<uint64_t>(__double_as_longlong(x + 0.0));
   return b >> 63 ? ~b : b | (uint64_t(1) << 63);
 }
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 
-// Sum over the block of 0 / 1 flags in front of this thread's, and all of them.
-__device__ int2 count_before(bool flag, int* warp_sum) {
+struct SelSmem {
+  int hist[256];
+  int warp_sum[kSelWarps];
+  uint64_t digit;
+  int need, n_close;
+  uint32_t size, negative;
+  uint64_t close[kSelClose];
+  int close_at[kSelClose];
+  uint32_t key[1];   // as many as the launch asks for
+};
+
+// Sum over the block of a count per thread, in front of this thread's; the total to everybody.
+__device__ int sum_before(int x, int* warp_sum, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t m = __ballot_sync(kFull, flag);
-  if (lane == 0) warp_sum[warp] = __popc(m);
-  __syncthreads();
-  int s = warp_sum[lane];
+  int inc = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(kFull, s, o);
-    if (lane >= o) s += x;
+    const int y = __shfl_up_sync(kFull, inc, o);
+    if (lane >= o) inc += y;
   }
-  const int all = __shfl_sync(kFull, s, 31), in_front = __shfl_sync(kFull, s, max(warp - 1, 0));
+  if (lane == 31) warp_sum[warp] = inc;
   __syncthreads();
-  return make_int2((warp ? in_front : 0) + __popc(m & ((1u << lane) - 1)), all);
+  int before = inc - x, all = 0;
+#pragma unroll
+  for (int w = 0; w < kSelWarps; ++w) {
+    if (w < warp) before += warp_sum[w];
+    all += warp_sum[w];
+  }
+  __syncthreads();
+  *total = all;
+  return before;
+}
+
+// The k-th greatest of key(0) .. key(n - 1), eight bits at a time; *of_it: how many of those that have it are among the
+// k greatest.  (Keys share their first bits: a warp adds up those that meet before it goes to shared memory.)
+template <typename Key, typename F>
+__device__ Key kth_greatest(SelSmem& s, int n, int k, F key, int* of_it) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  constexpr int kTop = static_cast<int>(sizeof(Key)) * 8 - 8;
+  Key prefix = 0;
+#pragma unroll 1
+  for (int bit = kTop; bit >= 0; bit -= 8) {
+    if (tid < 256) s.hist[tid] = 0;
+    __syncthreads();
+    for (int j0 = 0; j0 < n; j0 += kSelThreads) {
+      const Key x = j0 + tid < n ? key(j0 + tid) : 0;
+      const bool counts = j0 + tid < n && (bit == kTop || (x ^ prefix) >> (bit + 8) == 0);
+      const int digit = counts ? static_cast<int>(x >> bit & 255) : -1;
+      const uint32_t same = __match_any_sync(kFull, digit);
+      if (counts && lane == __ffs(same) - 1) atomicAdd(&s.hist[digit], __popc(same));
+    }
+    __syncthreads();
+    if (tid < 32) {   // lane l: the digits 255 - 8 l downwards
+      int sum = 0, c[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += c[i] = s.hist[255 - 8 * lane - i];
+      int inc = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(kFull, inc, o);
+        if (lane >= o) inc += y;
+      }
+      int left = k - (inc - sum);
+      if (left > 0 && left <= sum) {
+        int i = 0;
+        while (i < 7 && c[i] < left) left -= c[i++];
+        s.digit = 255 - 8 * lane - i;
+        s.need = left;
+      }
+    }
+    __syncthreads();
+    prefix |= static_cast<Key>(s.digit) << bit;
+    k = s.need;
+  }
+  *of_it = k;
+  return prefix;
 }
 
 }  // namespace
 
-// Block (set, layer, sequence): the budget tokens j < L - w of greatest mass (PER_HEAD: of one
-// KV head, else of all of them added up in 64 bits, which 32-bit masses fill without a
-// rounding where they lie within 2^24 of each other), equal ones the lowest first, in ascending
-// order; then the mass of the kept ones and of the window moves to their new places.
+// Block (set, layer, sequence): the budget tokens j < L - w of greatest mass (PER_HEAD: of one KV head, else of
+// all of them added up), equal ones the lowest first, in ascending order; then the mass of the kept ones and of the window
+// moves to their new places.
+//
+// Sums are formed in 32 bits first.  Of G masses that are not negative one is off by at most (G - 1) 2^-24 of itself (of the
+// largest sum of sizes else): tokens further than that from the budget-th greatest are in or out, and the few between are
+// added up in 64 bits.  (In 64 bits throughout, and again for every digit, eight rows of 12,000 tokens in 28 layers took 560 us.)
 template <bool PER_HEAD>
 __global__ void __launch_bounds__(kSelThreads)
     k_mass_select(const __grid_constant__ PagesView pg, const __grid_constant__ SeqBatch b, const int32_t* rows, int row0, int w,
                   const PagePlan* plan, const __grid_constant__ MassView mv) {
-  using Value = typename std::conditional<PER_HEAD, float, double>::type;
-  using Key = typename std::conditional<PER_HEAD, uint32_t, uint64_t>::type;
-  __shared__ int hist[256], warp_sum[kSelWarps];
-  __shared__ Key s_prefix;
-  __shared__ int s_need;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  SelSmem& s = *reinterpret_cast<SelSmem*>(smem_raw);
   griddep_launch_dependents();
   griddep_wait();
   if (!plan->ok) return;
@@ -877,53 +942,146 @@ __global__ void __launch_bounds__(kSelThreads)
   const int g0 = PER_HEAD ? set : 0, g1 = PER_HEAD ? set + 1 : pg.G;
   float* mass = mv.m + layer * mv.layer_stride + row * mv.row_stride;
   int32_t* idx = sv.idx + (static_cast<int64_t>(layer) * (PER_HEAD ? pg.G : 1) + set) * B;
-  auto key_of = [&](int j) {
-    Value x = mass[g0 * mv.group_stride + j];
-    for (int g = g0 + 1; g < g1; ++g) x += static_cast<Value>(mass[g * mv.group_stride + j]);
-    return order_key(x);
+  const float* heads = mass + g0 * mv.group_stride;
+  auto sum_of = [&](int j, float* size) {
+    float x = heads[j], a = fabsf(x);
+    for (int g = g0 + 1; g < g1; ++g) {
+      const float y = mass[g * mv.group_stride + j];
+      x += y;
+      a += fabsf(y);
+    }
+    *size = a;
+    return x;
   };
-  if (tid == 0) s_prefix = 0, s_need = B;
-  __syncthreads();
-  if (B > 0 && B < Lp)
-    for (int bit = static_cast<int>(sizeof(Key)) * 8 - 8; bit >= 0; bit -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      const Key prefix = s_prefix;
-      for (int j = tid; j < Lp; j += kSelThreads) {
-        const Key key = key_of(j);
-        if (bit + 8 == static_cast<int>(sizeof(Key)) * 8 || (key ^ prefix) >> (bit + 8) == 0) atomicAdd(&hist[key >> bit & 255], 1);
+  const bool here = Lp <= kSelKeys;
+  auto key_of = [&](int j) {
+    float a;
+    return here ? s.key[j] : order_key(sum_of(j, &a));
+  };
+  if (B > 0 && B < Lp) {
+    if (tid == 0) s.size = s.negative = s.n_close = 0;
+    __syncthreads();
+    uint32_t size = 0;
+    bool negative = false;
+#pragma unroll 4
+    for (int j = tid; j < Lp; j += kSelThreads) {
+      float a;
+      const float x = sum_of(j, &a);
+      if (here) s.key[j] = order_key(x);
+      if (!PER_HEAD) {
+        size = max(size, __float_as_uint(a));   // (a NaN is above infinity)
+        negative = negative || a != x;          // (also where a sum is not a number)
       }
-      __syncthreads();
-      if (tid == 0) {
-        int left = s_need, d = 255;
-        while (d > 0 && hist[d] < left) left -= hist[d--];
-        s_prefix = prefix | static_cast<Key>(d) << bit;
-        s_need = left;
+    }
+    if (!PER_HEAD) {
+      size = __reduce_max_sync(kFull, size);
+      negative = __any_sync(kFull, negative);
+      if ((tid & 31) == 0) {
+        atomicMax(&s.size, size);
+        if (negative) s.negative = 1;
       }
-      __syncthreads();
     }
-  const Key least = s_prefix;
-  const int need = s_need;   // of the tokens that have the least key
-  int at = 0, equal = 0;
-  if (B > 0)
-    for (int j0 = 0; j0 < Lp; j0 += kSelThreads) {
-      const int j = j0 + tid;
-      const Key key = j < Lp ? key_of(j) : 0;
-      const int2 e = count_before(j < Lp && key == least, warp_sum);
-      const bool in = j < Lp && (B == Lp || key > least || (key == least && equal + e.x < need));
-      const int2 c = count_before(in, warp_sum);
-      if (in) idx[at + c.x] = j;
-      equal += e.y;
-      at += c.y;
+    __syncthreads();
+    int need;   // of the tokens that have the least key
+    const uint32_t least = kth_greatest<uint32_t>(s, Lp, B, key_of, &need);
+    uint32_t above = least, below = least;   // keys: in, out, and those between
+    if (!PER_HEAD) {
+      const float at = key_value(least), e = pg.G * 2.5f * 0x1p-24f;   // (twice the error, and roundings)
+      const float off = s.negative || !(fabsf(at) < INFINITY) ? __uint_as_float(s.size) * e : at * e;
+      above = order_key(at + off + 1e-44f);
+      below = order_key(at - off - 1e-44f);
+      if (!(off < INFINITY)) above = ~0u, below = 0;   // all of them
     }
+    // every thread a run of tokens
+    const int run = (Lp + kSelThreads - 1) / kSelThreads, from = min(tid * run, Lp), to = min(from + run, Lp);
+    int sure = 0, close = 0, n_sure, n_close;
+    for (int j = from; j < to; ++j) {
+      const uint32_t k = key_of(j);
+      sure += k > above;
+      close += k <= above && k >= below;
+    }
+    int at_sure = sum_before(sure, s.warp_sum, &n_sure), at_close = sum_before(close, s.warp_sum, &n_close);
+    const int left = B - n_sure;
+    if (PER_HEAD || left == n_close) {   // of the close ones the lowest
+      for (int j = from; j < to; ++j) {
+        const uint32_t k = key_of(j);
+        const bool near = k <= above && k >= below;
+        if (k > above || (near && at_close < left)) idx[at_sure + min(at_close, left)] = j;
+        at_sure += k > above;
+        at_close += near;
+      }
+    } else {
+      auto wide = [&](int j) {
+        double x = heads[j];
+        for (int g = g0 + 1; g < g1; ++g) x += static_cast<double>(mass[g * mv.group_stride + j]);
+        return order_key(x);
+      };
+      uint64_t border;     // close tokens with greater keys stay, and `equal` of those that have this one
+      int equal;
+      const bool few = n_close <= kSelClose;
+      if (few) {
+        int c = at_close;
+        for (int j = from; j < to; ++j) {
+          const uint32_t k = key_of(j);
+          if (k <= above && k >= below) s.close_at[c++] = j;
+        }
+        __syncthreads();
+        if (tid < n_close) s.close[tid] = wide(s.close_at[tid]);
+        __syncthreads();
+        border = kth_greatest<uint64_t>(s, n_close, left, [&](int i) { return s.close[i]; }, &equal);
+      } else {
+        border = kth_greatest<uint64_t>(s, Lp, left, [&](int j) {
+          const uint32_t k = key_of(j);
+          return k <= above && k >= below ? wide(j) : 0;
+        }, &equal);
+      }
+      int same = 0, total, c = at_close;
+      auto wide_key = [&](int j) { return few ? s.close[c] : wide(j); };
+      for (int j = from; j < to; ++j) {
+        const uint32_t k = key_of(j);
+        if (!(k <= above && k >= below)) continue;
+        same += wide_key(j) == border;
+        ++c;
+      }
+      int at_same = sum_before(same, s.warp_sum, &total);
+      int taken = 0;
+      c = at_close;
+      for (int j = from, e = at_same; j < to; ++j) {
+        const uint32_t k = key_of(j);
+        if (!(k <= above && k >= below)) {
+          taken += k > above;
+          continue;
+        }
+        const uint64_t x = wide_key(j);
+        taken += x > border || (x == border && e < equal);
+        e += x == border;
+        ++c;
+      }
+      int out = sum_before(taken, s.warp_sum, &total);
+      c = at_close;
+      for (int j = from, e = at_same; j < to; ++j) {
+        const uint32_t k = key_of(j);
+        bool in = k > above;
+        if (k <= above && k >= below) {
+          const uint64_t x = wide_key(j);
+          in = x > border || (x == border && e < equal);
+          e += x == border;
+          ++c;
+        }
+        if (in) idx[out++] = j;
+      }
+    }
+  } else {
+    for (int j = tid; j < B; j += kSelThreads) idx[j] = j;
+  }
   __syncthreads();   // the indices are written
   // A token's new place is never behind its old one: what a round writes has been read.
   for (int r0 = 0; r0 < B + w; r0 += kSelThreads) {
     const int r = r0 + tid;
-    const int from = r < B ? idx[r] : Lp + (r - B);
+    const int src = r < B ? idx[r] : Lp + (r - B);
     for (int g = g0; g < g1; ++g) {
       float* m = mass + g * mv.group_stride;
-      const float x = r < B + w ? m[from] : 0.f;
+      const float x = r < B + w ? m[src] : 0.f;
       __syncthreads();
       if (r < B + w) m[r] = x;
     }
@@ -931,10 +1089,21 @@ __global__ void __launch_bounds__(kSelThreads)
   }
 }
 
+cudaError_t mass_select_configure() {
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  const int most = sizeof(SelSmem) + kSelKeys * 4;
+  const cudaError_t e = cudaFuncSetAttribute(k_mass_select<true>, attr, most);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(k_mass_select<false>, attr, most);
+}
+
 cudaError_t mass_select_launch(const PagesView& pg, const SeqBatch& b, const int32_t* rows, int row0, int w, int per_head,
                                const PagePlan* plan, const MassView& mass, cudaStream_t stream) {
+  int keys = 0;
+  for (int i = 0; i < b.nseq; ++i)
+    if (b.s[i].Lp <= kSelKeys) keys = std::max(keys, b.s[i].Lp);
   cudaLaunchAttribute attr[1];
   cudaLaunchConfig_t cfg = config(attr, dim3(per_head ? pg.G : 1, b.nlayers, b.nseq), kSelThreads, stream);
+  cfg.dynamicSmemBytes = sizeof(SelSmem) + keys * 4;
   return cudaLaunchKernelEx(&cfg, per_head ? k_mass_select<true> : k_mass_select<false>, pg, b, rows, row0, w, plan, mass);
 }
 

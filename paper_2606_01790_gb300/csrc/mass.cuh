@@ -58,6 +58,7 @@ cudaError_t mass_launch(const MassParams& p, cudaStream_t stream);
 // The parts of the groups that were cut: with p.cut only.
 cudaError_t mass_sum_launch(const MassParams& p, cudaStream_t stream);
 
+cudaError_t mass_select_configure();
 // Picks the tokens of an eviction whose bookkeeping (`plan`) was carried out, and moves their mass.
 cudaError_t mass_select_launch(const PagesView& pg, const SeqBatch& b, const int32_t* rows, int row0, int w, int per_head,
                                const PagePlan* plan, const MassView& mass, cudaStream_t stream);

@@ -137,6 +137,8 @@ constexpr int kChooseThreads = 256;
 constexpr int kChooseWarps = kChooseThreads / 32;
 constexpr int kPagesAtOnce = 8;        // of a warp
 constexpr int kFew = 256;              // close pages that are ranked by comparing each with each
+constexpr int kRun = 4;                // competing pages of a thread, at most, where one pass over bins finds the border
+constexpr int kBins = 2048;
 
 // Ascending order as unsigned numbers.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -151,19 +153,31 @@ __device__ __forceinline__ uint64_t order_of(double x) {
   return b >> 63 ? ~b : b | (uint64_t(1) << 63);
 }
 
+// a + b rounded, with what the rounding left out (Knuth's two-sum) added to *rest
+__device__ __forceinline__ float sum_and_rest(float a, float b, float* rest) {
+  const float s = a + b, t = s - a;
+  *rest += (a - (s - t)) + (b - t);
+  return s;
+}
+
 struct ChooseSmem {
   uint32_t key[kChoosePages];
-  float up[kHeadDim], down[kHeadDim];
+  float up[kHeadDim], down[kHeadDim], up_rest[kHeadDim], down_rest[kHeadDim];
   uint32_t size[kMaxCluster][kChooseWarps];   // largest sum of terms' sizes that a warp met
   int hist[256];
   int warp_sum[kChooseWarps];
   uint64_t prefix;
   int need, few;
+  uint32_t least, most;
+  int bin, bin_sum[2][kChooseWarps];
+  int bins[kBins];
   uint64_t close[kFew];
   int close_page[kFew];
 };
 
-// Sum over the block of a count per thread, in front of this thread's; the total to everybody.
+// Sum over the block of a count per thread, in front of this thread's; the total to everybody.  AGAIN: warp_sum is
+// free for another use afterwards.
+template <bool AGAIN = true>
 __device__ __forceinline__ int block_before(int x, int* warp_sum, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int inc = x;
@@ -180,7 +194,7 @@ __device__ __forceinline__ int block_before(int x, int* warp_sum, int* total) {
     if (w < warp) before += warp_sum[w];
     all += warp_sum[w];
   }
-  __syncthreads();
+  if (AGAIN) __syncthreads();
   *total = all;
   return before;
 }
@@ -192,11 +206,14 @@ __device__ Key kth_greatest(ChooseSmem& s, int lo, int hi, int k, F key, int* of
   const int tid = threadIdx.x, lane = tid & 31;
   Key prefix = 0;
   for (int bit = static_cast<int>(sizeof(Key)) * 8 - 8; bit >= 0; bit -= 8) {
-    s.hist[tid] = 0;
+    if (tid < 256) s.hist[tid] = 0;
     __syncthreads();
-    for (int j = lo + tid; j < hi; j += kChooseThreads) {
-      const Key x = key(j);
-      if (bit == static_cast<int>(sizeof(Key)) * 8 - 8 || (x ^ prefix) >> (bit + 8) == 0) atomicAdd(&s.hist[x >> bit & 255], 1);
+    for (int j0 = lo; j0 < hi; j0 += kChooseThreads) {   // (scores share their first bits: one addition for all of a warp that meet)
+      const Key x = j0 + tid < hi ? key(j0 + tid) : 0;
+      const bool counts = j0 + tid < hi && (bit == static_cast<int>(sizeof(Key)) * 8 - 8 || (x ^ prefix) >> (bit + 8) == 0);
+      const int digit = counts ? static_cast<int>(x >> bit & 255) : -1;
+      const uint32_t same = __match_any_sync(kFull, digit);
+      if (counts && lane == __ffs(same) - 1) atomicAdd(&s.hist[digit], __popc(same));
     }
     __syncthreads();
     if (tid < 32) {   // lane l: the digits 255 - 8 l downwards
@@ -227,7 +244,7 @@ __device__ Key kth_greatest(ChooseSmem& s, int lo, int hi, int k, F key, int* of
 
 }  // namespace
 
-static_assert(kChooseThreads == 256, "a thread a digit");
+static_assert(kChooseThreads >= 256, "a thread a digit and a close page");
 
 // Cluster (item, KV head): its CTAs score a share of the pages each, in fp32, into the first one's shared
 // memory (rows of more pages than it holds: into the workspace); the first CTA takes the best.
@@ -235,7 +252,7 @@ static_assert(kChooseThreads == 256, "a thread a digit");
 // A lane has 8 of the 256 terms; sums over the lanes are taken for eight pages together, halving the pages with every
 // step.  With u = 2^-24 a score is off by at most (8 + 5 + hg) u times the sum of its terms' sizes (the products' sums, the
 // sums over lanes, the weights' sums over heads), plus what underflows: at most E, with the lanes' largest sizes added up for
-// all pages.  With t the k-th greatest score, a page 2 E above t is among the k best and one 2 E below is not; those between are
+// all pages.  With the k-th greatest score between t0 and t1, a page 2 E above t1 is among the k best and one 2 E below t0 is not; those between are
 // scored again in 64 bits where they are more than the places left: usually none or a few, all of them where scores are equal
 // or sizes are past what 32 bits hold.
 __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_constant__ ChooseParams p) {
@@ -259,16 +276,24 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
   uint32_t* far = p.scores + place - lo;
   const int seq = v / p.T, t = v - seq * p.T;
   const __nv_bfloat16* q = p.q + seq * p.q_seq + t * p.q_token + static_cast<int64_t>(g) * p.hg * p.q_head;
+  const int per = p.ctas * kChooseWarps * kPagesAtOnce, own = (rank * kChooseWarps + warp) * kPagesAtOnce;
+  if (tid == 0) s.least = ~0u, s.most = 0, s.few = 0;
+  if (rank == 0)
+    for (int i = tid; i < kBins; i += kChooseThreads) s.bins[i] = 0;
   if (need > 0) {
+    int id = lo + own + (lane & 7) < hi ? entries[lo + own + (lane & 7)] : -1;   // lane l: page l of the eight
     if (tid < kHeadDim) {
-      float up = 0.f, down = 0.f;
+      float up = 0.f, down = 0.f, up_rest = 0.f, down_rest = 0.f;
+#pragma unroll 4
       for (int h = 0; h < p.hg; ++h) {
         const float x = __bfloat162float(q[h * p.q_head + tid]);
-        up += x < 0.f ? 0.f : x;   // (a NaN goes into both)
-        down += x > 0.f ? 0.f : x;
+        up = sum_and_rest(up, x < 0.f ? 0.f : x, &up_rest);   // (a NaN goes into both)
+        down = sum_and_rest(down, x > 0.f ? 0.f : x, &down_rest);
       }
       s.up[tid] = up;
       s.down[tid] = down;
+      s.up_rest[tid] = fabsf(up) < INFINITY ? up_rest : 0.f;
+      s.down_rest[tid] = fabsf(down) < INFINITY ? down_rest : 0.f;
     }
     __syncthreads();
     float w[8];   // this lane's terms: eight channels, the least keys (lanes 0 .. 15) or the greatest
@@ -277,9 +302,6 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
     uint32_t size = 0;
     cluster_wait();
     const uint32_t first_cta = dsmem_map(s.key, 0);
-    const int per = p.ctas * kChooseWarps * kPagesAtOnce;
-    const int own = (rank * kChooseWarps + warp) * kPagesAtOnce;
-    int id = lo + own + (lane & 7) < hi ? entries[lo + own + (lane & 7)] : -1;   // lane l: page l of the eight
     for (int j0 = lo + own; j0 < hi; j0 += per) {
       uint4 x[kPagesAtOnce];
 #pragma unroll
@@ -342,13 +364,87 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
   uint32_t* keys = here ? s.key - lo : far;   // from here on: 0 (not taken) or 1
   if (need > 0) {
     int of_it;
-    const float at = value_of(kth_greatest<uint32_t>(s, lo, hi, need, [&](int j) { return keys[j]; }, &of_it));
+    const int n = hi - lo, run = (n + kChooseThreads - 1) / kChooseThreads;
+    const bool ranked = run <= kRun;   // (shared memory holds them)
+    uint32_t mine[kRun];               // pages lo + tid run ..
+    float top, bottom;                 // the k-th greatest score lies between them
+    if (ranked) {
+      // bins of equal width between the least key and the greatest: the one that the k-th greatest is in holds
+      // hardly any other (digits of eight bits took four rounds, 3 us)
+      uint32_t least = ~0u, most = 0;
+#pragma unroll
+      for (int r = 0; r < kRun; ++r) {
+        const bool real = r < run && tid * run + r < n;
+        mine[r] = real ? s.key[tid * run + r] : 0;
+        if (real) least = min(least, mine[r]), most = max(most, mine[r]);
+      }
+      least = __reduce_min_sync(kFull, least);
+      most = __reduce_max_sync(kFull, most);
+      if (lane == 0) {
+        atomicMin(&s.least, least);
+        atomicMax(&s.most, most);
+      }
+      __syncthreads();
+      least = s.least;
+      most = s.most;
+      const int shift = max(0, 32 - __clz(most - least) - 11);   // (kBins = 2^11)
+#pragma unroll
+      for (int r = 0; r < kRun; ++r)
+        if (r < run && tid * run + r < n) atomicAdd(&s.bins[(mine[r] - least) >> shift], 1);
+      __syncthreads();
+      constexpr int kOwn = kBins / kChooseThreads;   // bins of a thread, from the greatest down
+      int count[kOwn], sum = 0, total;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) sum += count[i] = s.bins[kBins - 1 - tid * kOwn - i];
+      int left = need - block_before<false>(sum, s.bin_sum[0], &total);
+      if (left > 0 && left <= sum) {
+        int i = 0;
+#pragma unroll
+        for (int u = 0; u < kOwn - 1; ++u)
+          if (i == u && count[u] < left) left -= count[u], ++i;
+        s.bin = kBins - 1 - tid * kOwn - i;
+      }
+      __syncthreads();
+      const uint32_t from = least + (static_cast<uint32_t>(s.bin) << shift);
+      bottom = value_of(from);
+      top = value_of(min(most, from + ((1u << shift) - 1)));
+    } else {
+      top = bottom = value_of(kth_greatest<uint32_t>(s, lo, hi, need, [&](int j) { return keys[j]; }, &of_it));
+    }
     uint32_t size = 0;
     for (int i = lane; i < p.ctas * kChooseWarps; i += 32) size = max(size, s.size[i / kChooseWarps][i % kChooseWarps]);
     const float E = __uint_as_float(__reduce_max_sync(kFull, size)) * ((16 + p.hg) * 1.001f * 0x1p-24f) + 0x1p-140f;
-    const float above = at + 2.1f * E, below = at - 2.1f * E;
-    if (tid == 0) s.few = 0;
+    const float above = top + 2.1f * E, below = bottom - 2.1f * E;
     int sure = 0, close = 0;
+    if (ranked) {
+#pragma unroll
+      for (int r = 0; r < kRun; ++r) {
+        const float x = value_of(mine[r]);
+        const bool real = r < run && tid * run + r < n, in = x > above;
+        sure += real && in;
+        close += real && !in && !(x < below);
+      }
+      int total;   // (both counts in one sum: neither passes 1,024)
+      const int before = block_before<false>(sure << 16 | close, s.bin_sum[1], &total);
+      if (need - (total >> 16) == (total & 0xffff)) {   // the usual case: as many as there are places
+        int to = (before >> 16) + (before & 0xffff) + lo;
+#pragma unroll
+        for (int r = 0; r < kRun; ++r)
+          if (r < run && tid * run + r < n && !(value_of(mine[r]) < below)) {
+            const int j = lo + tid * run + r;
+            list[to] = entries[j];
+            if (chosen) chosen[to] = j;
+            ++to;
+          }
+        for (int i = tid; i < lo + pages - hi; i += kChooseThreads) {   // the first pages and the last ones
+          const int j = i < lo ? i : hi + i - lo, to_j = i < lo ? i : lo + need + i - lo;
+          list[to_j] = entries[j];
+          if (chosen) chosen[to_j] = j;
+        }
+        return;
+      }
+      sure = close = 0;
+    }
     for (int j = lo + tid; j < hi; j += kChooseThreads) {
       const float x = value_of(keys[j]);
       const bool in = x > above, out = x < below;   // (where E is not a number: neither)
@@ -373,14 +469,15 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
     }
     __syncthreads();
     if (!all) {
-      double wd[8];   // the same terms in 64 bits
-#pragma unroll
-      for (int i = 0; i < 8; ++i) wd[i] = 0;
-      for (int h = 0; h < p.hg; ++h)
+      // the same terms in 64 bits (of which the weights have 47: what 32 left out is known), by the warps that have a page:
+      // the unit for them is slow, and all warps' weights from the queries again took 12 us
+      double wd[8];
+      if (!few || warp < n_close)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const double x = __bfloat162float(q[h * p.q_head + (lane & 15) * 8 + i]);
-          wd[i] += lane < 16 ? (x > 0 ? 0 : x) : (x < 0 ? 0 : x);
+          const int c = (lane & 15) * 8 + i;
+          wd[i] = lane < 16 ? static_cast<double>(s.down[c]) + static_cast<double>(s.down_rest[c])
+                            : static_cast<double>(s.up[c]) + static_cast<double>(s.up_rest[c]);
         }
       auto score = [&](int j) {   // by the whole warp
         const int page = entries[j];
@@ -433,6 +530,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
   }
   // the list, in the order of the pages: every thread a run of them
   const int run = (pages + kChooseThreads - 1) / kChooseThreads, b = min(tid * run, pages), e = min(b + run, pages);
+  __syncthreads();
   auto taken = [&](int j) { return j < lo || j >= hi || (need > 0 && keys[j]); };
   int mine = 0, total;
   for (int j = b; j < e; ++j) mine += taken(j);
