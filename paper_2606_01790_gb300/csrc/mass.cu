@@ -820,9 +820,10 @@ cudaError_t mass_sum_launch(const MassParams& p, cudaStream_t stream) {
 
 namespace {
 
-constexpr int kSelThreads = 512;
+constexpr int kSelThreads = 1024;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelKeys = 49152;    // keys that shared memory holds
+constexpr int kSelMoves = 4;       // masses of a thread on their way at once
 constexpr int kSelClose = 512;     // close tokens that are ranked by comparing each with each
 
 // Ascending order as unsigned numbers; a NaN (a mass that is none) comes with infinity, so that its token
@@ -886,6 +887,7 @@ __device__ Key kth_greatest(SelSmem& s, int n, int k, F key, int* of_it) {
     for (int j0 = 0; j0 < n; j0 += kSelThreads) {
       const Key x = j0 + tid < n ? key(j0 + tid) : 0;
       const bool counts = j0 + tid < n && (bit == kTop || (x ^ prefix) >> (bit + 8) == 0);
+      if (!__any_sync(kFull, counts)) continue;
       const int digit = counts ? static_cast<int>(x >> bit & 255) : -1;
       const uint32_t same = __match_any_sync(kFull, digit);
       if (counts && lane == __ffs(same) - 1) atomicAdd(&s.hist[digit], __popc(same));
@@ -963,7 +965,7 @@ __global__ void __launch_bounds__(kSelThreads)
     __syncthreads();
     uint32_t size = 0;
     bool negative = false;
-#pragma unroll 4
+#pragma unroll 8
     for (int j = tid; j < Lp; j += kSelThreads) {
       float a;
       const float x = sum_of(j, &a);
@@ -1076,14 +1078,22 @@ __global__ void __launch_bounds__(kSelThreads)
   }
   __syncthreads();   // the indices are written
   // A token's new place is never behind its old one: what a round writes has been read.
-  for (int r0 = 0; r0 < B + w; r0 += kSelThreads) {
-    const int r = r0 + tid;
-    const int src = r < B ? idx[r] : Lp + (r - B);
+  for (int r0 = 0; r0 < B + w; r0 += kSelMoves * kSelThreads) {
+    int src[kSelMoves];
+#pragma unroll
+    for (int u = 0; u < kSelMoves; ++u) {
+      const int r = r0 + u * kSelThreads + tid;
+      src[u] = r < B ? idx[r] : r < B + w ? Lp + (r - B) : -1;
+    }
     for (int g = g0; g < g1; ++g) {
       float* m = mass + g * mv.group_stride;
-      const float x = r < B + w ? m[src] : 0.f;
+      float x[kSelMoves];
+#pragma unroll
+      for (int u = 0; u < kSelMoves; ++u) x[u] = src[u] >= 0 ? m[src[u]] : 0.f;
       __syncthreads();
-      if (r < B + w) m[r] = x;
+#pragma unroll
+      for (int u = 0; u < kSelMoves; ++u)
+        if (src[u] >= 0) m[r0 + u * kSelThreads + tid] = x[u];
     }
     __syncthreads();
   }
