@@ -83,6 +83,8 @@ __device__ __forceinline__ int quotient(int x, uint32_t inv) {
 struct Group {
   int k0, tiles, lo, hi;   // first key; tiles of 128; blocks lo .. hi - 1
 
+  Group() = default;
+  // where blocks may be cut: those that see some of it
   __device__ __forceinline__ Group(const MassParams& p, const Item& it, int span, int s) {
     k0 = s << span;
     const int end = min(it.L, k0 + (1 << span)), ctx = it.L - it.n;
@@ -92,16 +94,19 @@ struct Group {
       t0 = max(0, k0 - ctx);
       if (k0 >= p.n_sink) t1 = min(it.n, end - 1 + p.window - ctx);
     }
-    if (!p.cut) {   // blocks that stay in shared memory stay whole
-      lo = 0;
-      hi = t0 < t1 ? it.blocks : 0;
-    } else {
-      lo = quotient(t0, p.inv_tpb) * p.chunks;
-      hi = t1 <= t0 ? lo : quotient(t1 + p.tpb - 1, p.inv_tpb) * p.chunks;
-    }
+    lo = quotient(t0, p.inv_tpb) * p.chunks;
+    hi = t1 <= t0 ? lo : quotient(t1 + p.tpb - 1, p.inv_tpb) * p.chunks;
+  }
+  // where they are not: all or none (keys from `seen` on are in some query's window)
+  __device__ __forceinline__ Group(int n_sink, const Item& it, int span, int s, int seen) {
+    k0 = s << span;
+    const int end = min(it.L, k0 + (1 << span));
+    tiles = (end - k0 + kMassTile - 1) / kMassTile;
+    lo = 0;
+    hi = k0 < n_sink || end > seen ? it.blocks : 0;
   }
   // a group that nothing sees is a unit all the same: its mass may fade
-  __device__ __forceinline__ int units(const MassParams& p) const { return p.cut ? max(1, hi - lo) : 1; }
+  __device__ __forceinline__ int units() const { return max(1, hi - lo); }
 };
 
 __device__ __forceinline__ int groups_of(int L, int span) { return (L + (1 << span) - 1) >> span; }
@@ -112,23 +117,33 @@ struct PieceIter {
   int seq, g, s;
   int b0, b1;        // blocks b0 .. b1 - 1
   int span, groups;  // log2 of the keys of a group; groups of the row
+  int seen;          // first key in a window
   int64_t rem;       // units of the range from here on
   Group grp;
   Item it;
   __device__ __forceinline__ PieceIter(const MassParams& p, const Ctl* ctl)
-      : seq(ctl->start.seq), g(ctl->start.g), s(ctl->start.s), span(ctl->span), rem(ctl->end - ctl->begin),
-        grp(p, Item{0, 0, 0, 0}, 7, 0), it{0, 0, 0, 0} {
+      : seq(ctl->start.seq), g(ctl->start.g), s(ctl->start.s), span(ctl->span), rem(ctl->end - ctl->begin) {
     if (rem <= 0) return;
+    row(p, ctl);
+    take(p, ctl->start.b);
+  }
+  __device__ __forceinline__ void row(const MassParams& p, const Ctl* ctl) {
     it = ctl->item[seq];
     groups = groups_of(it.L, span);
-    take(p, ctl->start.b);
+    seen = p.tree ? 0 : it.L - it.n - p.window + 1;
   }
   __device__ __forceinline__ bool valid() const { return rem > 0; }
   __device__ __forceinline__ bool whole() const { return b0 == grp.lo && b1 == grp.hi; }
   __device__ __forceinline__ void take(const MassParams& p, int from) {
-    grp = Group(p, it, span, s);
-    b0 = grp.lo + from;
-    b1 = p.cut ? static_cast<int>(min(static_cast<int64_t>(grp.hi), b0 + rem)) : grp.hi;
+    if (p.cut) {
+      grp = Group(p, it, span, s);
+      b0 = grp.lo + from;
+      b1 = static_cast<int>(min(static_cast<int64_t>(grp.hi), b0 + rem));
+    } else {
+      grp = Group(p.n_sink, it, span, s, seen);
+      b0 = 0;
+      b1 = grp.hi;
+    }
   }
   // the last group of this row and KV head that the range has
   __device__ __forceinline__ bool last_of_head() const { return rem <= 1 || s + 1 == groups; }
@@ -151,8 +166,7 @@ struct PieceIter {
       g = 0;
       do ++seq;
       while (ctl->before[seq + 1] == ctl->before[seq]);
-      it = ctl->item[seq];
-      groups = groups_of(it.L, span);
+      row(p, ctl);
     }
   }
 };
@@ -210,7 +224,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
       const bool twice = rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1);
       const int ng = it.n > 0 && !twice ? groups_of(it.L, span) : 0;
       int u = 0;   // (32,768 groups of 1,041 blocks at most)
-      for (int s = lane; s < ng; s += 32) u += Group(p, it, span, s).units(p);
+      for (int s = lane; s < ng; s += 32) u += Group(p, it, span, s).units();
       u = __reduce_add_sync(kFull, u);
       if (lane == 0) {
         ctl->before[i + 1] = u;
@@ -258,7 +272,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
       if (!p.cut) st.s = static_cast<int>(off);
       else
         for (int left = static_cast<int>(off), s0 = 0;; s0 += 32) {
-          const int u = s0 + lane < ng ? Group(p, it, span, s0 + lane).units(p) : 0;
+          const int u = s0 + lane < ng ? Group(p, it, span, s0 + lane).units() : 0;
           int inc = u;
 #pragma unroll
           for (int o = 1; o < 32; o <<= 1) {
@@ -327,6 +341,7 @@ __device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int half, i
   int base = 0, held = 0;            // lane l: pages base + l and base + 32 + l of the row, on their way before they are due
   int id = 0, id_next = 0;
   const int32_t* entries = nullptr;
+  int seq = -1;
   auto number = [&](int at) {        // outside the map: zeros
     int x = p.n_pages;
     if (at < held) {
@@ -340,11 +355,11 @@ __device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int half, i
   };
   for (PieceIter c(p, ctl); ok && c.valid(); c.next(p, ctl)) {
     if (c.b0 == c.b1) continue;
-    const int32_t* mine = p.table + static_cast<int64_t>(c.it.row) * p.max_pages;
     const int page0 = c.grp.k0 >> p.shift;   // (a group has 512 keys: 32 pages at most)
     const int page1 = (c.grp.k0 + c.grp.tiles * kMassTile - 1) >> p.shift;
-    if (mine != entries || page0 < base || page1 >= base + 64) {
-      entries = mine;
+    if (c.seq != seq || page0 < base || page1 >= base + 64) {
+      seq = c.seq;
+      entries = p.table + static_cast<int64_t>(c.it.row) * p.max_pages;
       held = (c.it.L + P - 1) >> p.shift;
       base = page0;
       id = number(base + lane);
@@ -358,18 +373,15 @@ __device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int half, i
     for (int i = 0; i < c.grp.tiles; ++i) {
       ok = warp_wait(ctl, &ctl->k_empty[st.at], st.par ^ 1, p.wait_ns);
       if (!ok) break;
-      const bool leader = elect_one();
-      if (leader) mbar_arrive_expect_tx(&ctl->k_full[st.at], kHalfBytes);
-      for (int b = 0; b < boxes; ++b) {
-        const int key = c.grp.k0 + i * kMassTile + b * rows;
-        const int at = (key >> p.shift) - base;
-        const int near = __shfl_sync(kFull, id, at & 31), far = __shfl_sync(kFull, id_next, at & 31);
+      if (elect_one()) mbar_arrive_expect_tx(&ctl->k_full[st.at], kHalfBytes);
+      // a box a lane (one after the other by one lane, each with its page number fetched, took 245 cycles a box)
+      const int key = c.grp.k0 + i * kMassTile + lane * rows, at = (key >> p.shift) - base;
+      const int near = __shfl_sync(kFull, id, at & 31), far = __shfl_sync(kFull, id_next, at & 31);
+      if (lane < boxes) {
+        uint8_t* dst = sK + st.at * kTileBytes + half * kHalfBytes + lane * rows * 128;
         const int page = at < 32 ? near : far;
-        if (leader) {
-          uint8_t* dst = sK + st.at * kTileBytes + half * kHalfBytes + b * rows * 128;
-          if (p.cut) tma_load_4d(dst, &p.tmk, &ctl->k_full[st.at], half * 64, key & (P - 1), c.g, page);
-          else tma_load_4d_hint(dst, &p.tmk, &ctl->k_full[st.at], half * 64, key & (P - 1), c.g, page, pol);
-        }
+        if (p.cut) tma_load_4d(dst, &p.tmk, &ctl->k_full[st.at], half * 64, key & (P - 1), c.g, page);
+        else tma_load_4d_hint(dst, &p.tmk, &ctl->k_full[st.at], half * 64, key & (P - 1), c.g, page, pol);
       }
       __syncwarp();
       used |= 1u << st.at;
