@@ -29,9 +29,8 @@ cudaLaunchConfig_t config(cudaLaunchAttribute* attr, dim3 grid, int threads, cud
 
 // ---------------------------------------------------------------- mass: units and their order
 
-constexpr int kMassWarps = 16;
-constexpr int kThreads = 32 * kMassWarps;
-constexpr int kMmaWarp = 2, kQueryWarp = 4, kSoftWarp = 8;   // (0 and 1: keys; 4 query warps, 8 weighing warps)
+constexpr int kMmaWarp = 2, kQueryWarp = 4, kSoftWarp = 8;   // (0 and 1: keys; 4 query warps; the weighing warps)
+__host__ __device__ constexpr int threads_of(int groups) { return 32 * (kSoftWarp + 4 * groups); }
 constexpr int kQueryThreads = 32 * (kSoftWarp - kQueryWarp);
 static_assert(kQueryThreads / 16 == kMassQueryStep && kQueryThreads >= kMassTile, "16 threads take a row of 256 bytes");
 constexpr int kTileBytes = kMassTile * 256;       // 128 keys x 128 bf16, or as many (token, head) pairs: 32 KB
@@ -146,16 +145,16 @@ struct PieceIter {
     }
   }
   // the last group of this row and KV head that the range has
-  __device__ __forceinline__ bool last_of_head() const { return rem <= 1 || s + 1 == groups; }
+  __device__ __forceinline__ bool last_of_head() const { return rem <= it.blocks + 1 || s + 1 == groups; }
   __device__ __forceinline__ void next(const MassParams& p, const Ctl* ctl) {
-    rem -= p.cut ? max(1, b1 - b0) : 1;
+    rem -= p.cut ? max(1, b1 - b0) : it.blocks + 1;
     if (rem <= 0) return;
     if (++s == groups) head(p, ctl);
     take(p, 0);
   }
   // p.cut is 0: on to the next row or KV head
   __device__ __forceinline__ void skip_head(const MassParams& p, const Ctl* ctl) {
-    rem -= groups - s;
+    rem -= static_cast<int64_t>(groups - s) * (it.blocks + 1);
     if (rem <= 0) return;
     head(p, ctl);
     take(p, 0);
@@ -185,11 +184,11 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
   const int words = (p.n_rows + 31) >> 5;
   const bool rivals = p.rows && p.n > 1;
   if (rivals) {
-    for (int i = tid; i < 2 * words; i += kThreads) named[i] = 0;
+    for (int i = tid; i < 2 * words; i += blockDim.x) named[i] = 0;
     __syncthreads();
   }
   int64_t tiles = 0;
-  for (int i = tid; i < p.n; i += kThreads) {
+  for (int i = tid; i < p.n; i += blockDim.x) {
     Item it;
     it.row = p.rows ? p.rows[i] : p.row0 + i;
     it.n = p.n_tokens ? p.n_tokens[i] : p.T;
@@ -208,18 +207,19 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
   __syncthreads();
   const int span = kTileShift + (ctl->end * p.G >= p.span_from ? kSpanShift : 0);
   if (!p.cut) {
-    for (int i = tid; i < p.n; i += kThreads) {
+    for (int i = tid; i < p.n; i += blockDim.x) {
       const Item it = ctl->item[i];
       if (rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1)) {
         ctl->item[i].n = 0;
         atomicOr(p.err, kErrRow);
         ctl->before[i + 1] = 0;
       } else {
-        ctl->before[i + 1] = it.n > 0 ? groups_of(it.L, span) : 0;
+        // (a tile takes about 1,500 cycles to load, and 1,100 for each block: whole groups of 2 or 3 units)
+        ctl->before[i + 1] = it.n > 0 ? static_cast<int64_t>(groups_of(it.L, span)) * (it.blocks + 1) : 0;
       }
     }
   } else {
-    for (int i = warp; i < p.n; i += kMassWarps) {
+    for (int i = warp; i < p.n; i += blockDim.x / 32) {
       const Item it = ctl->item[i];
       const bool twice = rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1);
       const int ng = it.n > 0 && !twice ? groups_of(it.L, span) : 0;
@@ -253,7 +253,8 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
     __syncwarp();
     const int R = ranges_of(at, gridDim.x);
     const int64_t f0 = range_begin(at, blockIdx.x + (lane & 1), R);   // (lanes 0 and 1: the range's ends)
-    const int64_t fb = __shfl_sync(kFull, f0, 0), fe = __shfl_sync(kFull, f0, 1);
+    const int64_t fe = __shfl_sync(kFull, f0, 1);
+    int64_t fb = __shfl_sync(kFull, f0, 0);
     Start st{0, 0, 0, 0};
     if (fb < fe) {
       int a = 0, b = p.n;   // the last sequence with no more than fb units before it
@@ -269,8 +270,19 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
       const int64_t heads = ctl->before[a + 1] - ctl->before[a];   // G times the units of one
       while ((st.g + 1) * heads <= off * p.G) ++st.g;
       off -= st.g * (heads / p.G);
-      if (!p.cut) st.s = static_cast<int>(off);
-      else
+      if (!p.cut) {   // the first group that begins in the range
+        const int each = it.blocks + 1, part = static_cast<int>(off % each);
+        st.s = static_cast<int>(off / each) + (part > 0);
+        fb += part ? each - part : 0;
+        if (st.s == ng) {
+          st.s = 0;
+          if (++st.g == p.G) {
+            st.g = 0;
+            do ++st.seq;
+            while (st.seq < p.n && ctl->before[st.seq + 1] == ctl->before[st.seq]);
+          }
+        }
+      } else {
         for (int left = static_cast<int>(off), s0 = 0;; s0 += 32) {
           const int u = s0 + lane < ng ? Group(p, it, span, s0 + lane).units() : 0;
           int inc = u;
@@ -288,6 +300,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
           }
           left -= __shfl_sync(kFull, inc, 31);
         }
+      }
     }
     if (lane == 0) {
       ctl->start = st;
@@ -629,7 +642,8 @@ __device__ __forceinline__ float weigh_bits(uint32_t addr, const Pairs& pr, floa
   return sum;
 }
 
-// Weighing warpgroup `own`: every other tile, a key a thread.
+// Weighing warpgroup `own` of GROUPS: tile number i is that of i modulo them, a key a thread.
+template <int GROUPS>
 __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own, int quad, int lane) {
   const int r = quad * 32 + lane;
   const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
@@ -642,15 +656,16 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
     const int nb = c.b1 - c.b0;
     const bool take = p.cut || held == 0;
     if (take) slot0 = q.at;
-    const int i0 = (own ^ tile) & 1;   // tiles i0 and i0 + 2 of the group are this warpgroup's
+    const int i0 = (own - tile) & (GROUPS - 1);   // tiles i0, i0 + GROUPS .. of the group are this warpgroup's
     const int ctx = c.it.L - c.it.n, j0 = c.grp.k0 + i0 * kMassTile + r;
     float* mass = p.mass.m + c.it.row * p.mass.row_stride + c.g * p.mass.group_stride + j0;
     const bool whole = c.whole();
+    constexpr int kOwn = kKeySlots / GROUPS;
     float sum[2] = {0.f, 0.f}, had[2] = {0.f, 0.f};
     if (whole) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (i0 + 2 * u < c.grp.tiles && j0 + 2 * u * kMassTile < ctx) had[u] = mass[2 * u * kMassTile];
+      for (int u = 0; u < kOwn; ++u)
+        if (i0 + GROUPS * u < c.grp.tiles && j0 + GROUPS * u * kMassTile < ctx) had[u] = mass[GROUPS * u * kMassTile];
     }
     for (int b = 0; b < nb; ++b) {
       const int slot = (slot0 + b) % kQuerySlots;
@@ -662,7 +677,7 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
       const Pairs& pr = ctl->pairs[slot];
       const int first = ctx + blk.t0, end = ctx + min(blk.t0 + p.tpb, c.it.n) - 1;   // positions of the block's tokens
 #pragma unroll 1
-      for (int i = i0; i < c.grp.tiles; i += 2) {
+      for (int i = i0; i < c.grp.tiles; i += GROUPS) {
         const uint32_t a = (tile + i) & (kKeySlots - 1);
         ok = warp_wait(ctl, &ctl->s_full[a], par >> a & 1, p.wait_ns);
         if (!ok) break;
@@ -687,7 +702,7 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
           const int per = nt > 1 ? p.heads : blk.count;   // columns of a token
           w = weigh_columns(at, pr.lse, p.scale2, ta * per, tb * per, blk.count);
         }
-        if (i < 2) sum[0] += w;
+        if (i < GROUPS) sum[0] += w;
         else sum[1] += w;
         tc_fence_before();
         par ^= 1u << a;
@@ -707,13 +722,13 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
       }
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int i = i0 + 2 * u;
+    for (int u = 0; u < kOwn; ++u) {
+      const int i = i0 + GROUPS * u;
       if (i >= c.grp.tiles) break;
       if (!whole)
         p.part[(2 * static_cast<int64_t>(blockIdx.x) + (c.b0 == c.grp.lo)) * (kMassSpan * kMassTile) + i * kMassTile + r] = sum[u];
-      else if (j0 + 2 * u * kMassTile < c.it.L)
-        mass[2 * u * kMassTile] = fmaf(p.decay, had[u], sum[u]);
+      else if (j0 + GROUPS * u * kMassTile < c.it.L)
+        mass[GROUPS * u * kMassTile] = fmaf(p.decay, had[u], sum[u]);
     }
     if (nb > 0) tile += c.grp.tiles;
   }
@@ -722,7 +737,8 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
 
 }  // namespace
 
-__global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ MassParams p) {
+template <int GROUPS>
+__global__ void __launch_bounds__(threads_of(GROUPS), 1) k_mass(const __grid_constant__ MassParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sK = smem;                            // [slots][2 halves][128 keys][128 B]
@@ -738,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
     }
     for (int i = 0; i < kQuerySlots; ++i) {
       mbar_init(&ctl->q_full[i], kSoftWarp - kQueryWarp);
-      mbar_init(&ctl->q_empty[i], 1 + kMassWarps - kSoftWarp);   // the products and every weighing warp
+      mbar_init(&ctl->q_empty[i], 1 + 4 * GROUPS);   // the products and every weighing warp
     }
     mbar_init(&ctl->drain, 1);
     ctl->abort = 0;
@@ -761,7 +777,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
   } else if (warp == kMmaWarp) {
     mma_loop(p, ctl, sK, sQ, tmem);
   } else if (warp >= kSoftWarp) {
-    weigh_loop(p, ctl, tmem, (warp - kSoftWarp) >> 2, warp & 3, lane);
+    weigh_loop<GROUPS>(p, ctl, tmem, (warp - kSoftWarp) >> 2, warp & 3, lane);
   } else if (warp >= kQueryWarp) {
     query_loop(p, ctl, sQ, threadIdx.x - 32 * kQueryWarp);
   }
@@ -812,14 +828,19 @@ static_assert(kMaxTableRows / 4 <= kQuerySlots * kTileBytes, "the rows' bits fit
 }  // namespace
 
 cudaError_t mass_configure() {
-  return cudaFuncSetAttribute(k_mass, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  const cudaError_t e = cudaFuncSetAttribute(k_mass<2>, attr, static_cast<int>(kSmemBytes));
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(k_mass<4>, attr, static_cast<int>(kSmemBytes));
 }
 
 cudaError_t mass_launch(const MassParams& p, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
-  cudaLaunchConfig_t cfg = config(attr, dim3(p.grid), kThreads, stream);
+  // four weighing warpgroups where a tile meets many blocks, two (and registers for the other roles) where it meets one or two:
+  // a chunk of 2,704 tokens 114 us and 131, one token of 64 rows 225 us and 205
+  const int groups = p.cut ? 4 : 2;
+  cudaLaunchConfig_t cfg = config(attr, dim3(p.grid), threads_of(groups), stream);
   cfg.dynamicSmemBytes = kSmemBytes;
-  return cudaLaunchKernelEx(&cfg, k_mass, p);
+  return cudaLaunchKernelEx(&cfg, groups == 4 ? k_mass<4> : k_mass<2>, p);
 }
 
 cudaError_t mass_sum_launch(const MassParams& p, cudaStream_t stream) {
