@@ -517,7 +517,8 @@ typedef struct {
  * that rows need not be cleared; n = 0 leaves a row as it is.  Weights are what the
  * formula has where q, a seen K or lse is not finite; what a query does not see adds
  * nothing, whatever it holds.  A sequence that does not fit, or a row that two sequences
- * with queries name, is left as it is (device error).  T and T * H / G as for the
+ * with queries name, is left as it is (device error), and so is every row behind a
+ * refused call (as for the calls that change a pool).  T and T * H / G as for the
  * attention. */
 starkv_status starkv_tree_mass(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
                                const starkv_mass* mass, void* workspace, size_t workspace_bytes, void* stream);
@@ -566,7 +567,7 @@ starkv_status starkv_sparse_workspace_bytes(const starkv_state* st, const starkv
  * the last n_last up to its own, and of the others those with the greatest
  *   score = sum_c (up_c hi_c + down_c lo_c),  up = sum_{h in g} max(q_h, 0),  down = sum_{h in g} min(q_h, 0),
  * lo and hi the page's bounds: the most that the sum of the heads' logits with one of its keys
- * can be.  Formed in 64 bits; equal ones: the lower page; a NaN counts as +infinity.
+ * can be.  Their order is that of 64 bits; equal ones: the lower page; a NaN counts as +infinity.
  * n_first >= 0, n_last >= 1, n_first + n_last <= n_chosen.  chosen (i32 [n][T][G][n_chosen],
  * or NULL) gets the pages' places in the row, ascending, -1 behind them.  o and lse are those of
  * the keys attended over, as for the calls above. */

@@ -183,6 +183,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int words = (p.n_rows + 31) >> 5;
   const bool rivals = p.rows && p.n > 1;
+  const uint32_t latched = tid == 0 ? *p.err : 0;   // (behind a refused call nothing is added)
   if (rivals) {
     for (int i = tid; i < 2 * words; i += blockDim.x) named[i] = 0;
     __syncthreads();
@@ -302,6 +303,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
         }
       }
     }
+    if (__shfl_sync(kFull, latched, 0) & kErrHeld) fb = fe;
     if (lane == 0) {
       ctl->start = st;
       ctl->span = span;
