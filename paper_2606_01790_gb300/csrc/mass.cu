@@ -29,7 +29,7 @@ cudaLaunchConfig_t config(cudaLaunchAttribute* attr, dim3 grid, int threads, cud
 
 // ---------------------------------------------------------------- mass: units and their order
 
-constexpr int kMmaWarp = 2, kQueryWarp = 4, kSoftWarp = 8;   // (0 and 1: keys; 4 query warps; the weighing warps)
+constexpr int kMmaWarp = 2, kQueryWarp = 4, kSoftWarp = 8;   // (0 and 1: keys; 2 issuers; 4 query warps; the weighing warps)
 __host__ __device__ constexpr int threads_of(int groups) { return 32 * (kSoftWarp + 4 * groups); }
 constexpr int kQueryThreads = 32 * (kSoftWarp - kQueryWarp);
 static_assert(kQueryThreads / 16 == kMassQueryStep && kQueryThreads >= kMassTile, "16 threads take a row of 256 bytes");
@@ -475,7 +475,9 @@ __device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) 
   if (!ok) fail(ctl, p.err);
 }
 
-__device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const uint8_t* sQ, uint32_t tmem) {
+// Products: issuer 0 or 1 has every other tile.  (One for all left the tensor pipe idle for 400 of 1,000 cycles a tile and
+// block, between the end of one's instructions and the start of the next one's.)
+__device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const uint8_t* sQ, uint32_t tmem, int issuer) {
   const uint64_t dk0 = sdesc_k_sw128(smem_u32(sK)), dq0 = sdesc_k_sw128(smem_u32(sQ));
   Ring<kKeySlots> st;
   Ring<kQuerySlots> q;    // the next block to come
@@ -497,7 +499,8 @@ __device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const
       const uint32_t idesc = idesc_bf16(kMassTile, blk.columns());
       const uint64_t dq = dq0 + static_cast<uint64_t>(slot * (kTileBytes >> 4));
       at = st;
-      for (int i = 0; ok && i < c.grp.tiles; ++i) {
+      for (int i = 0; ok && i < c.grp.tiles; ++i, at.next()) {
+        if ((at.at & 1) != issuer) continue;
         if (j == 0) ok = warp_wait(ctl, &ctl->k_full[at.at], at.par, p.wait_ns);
         ok = ok && warp_wait(ctl, &ctl->s_empty[at.at], (s_par >> at.at & 1) ^ 1, p.wait_ns);
         if (!ok) break;
@@ -511,11 +514,13 @@ __device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const
           }
           mma_commit(&ctl->s_full[at.at]);
           if (j == nb - 1) mma_commit(&ctl->k_empty[at.at]);
-          if (p.cut && i == c.grp.tiles - 1) mma_commit(&ctl->q_empty[slot]);
         }
         __syncwarp();
         s_par ^= 1u << at.at;
-        at.next();
+      }
+      if (p.cut) {   // (with no tile of its own as well: both issuers are counted)
+        if (ok && elect_one()) mma_commit(&ctl->q_empty[slot]);
+        __syncwarp();
       }
     }
     st = at;
@@ -756,9 +761,9 @@ __global__ void __launch_bounds__(threads_of(GROUPS), 1) k_mass(const __grid_con
     }
     for (int i = 0; i < kQuerySlots; ++i) {
       mbar_init(&ctl->q_full[i], kSoftWarp - kQueryWarp);
-      mbar_init(&ctl->q_empty[i], 1 + 4 * GROUPS);   // the products and every weighing warp
+      mbar_init(&ctl->q_empty[i], 2 + 4 * GROUPS);   // both issuers and every weighing warp
     }
-    mbar_init(&ctl->drain, 1);
+    mbar_init(&ctl->drain, 2);
     ctl->abort = 0;
     ctl->end = 0;
     fence_mbar_init();
@@ -776,8 +781,8 @@ __global__ void __launch_bounds__(threads_of(GROUPS), 1) k_mass(const __grid_con
   plan(p, ctl, reinterpret_cast<uint32_t*>(sQ));
   if (warp < kMmaWarp) {
     key_loop(p, ctl, sK, warp, lane);
-  } else if (warp == kMmaWarp) {
-    mma_loop(p, ctl, sK, sQ, tmem);
+  } else if (warp < kQueryWarp) {
+    mma_loop(p, ctl, sK, sQ, tmem, warp - kMmaWarp);
   } else if (warp >= kSoftWarp) {
     weigh_loop<GROUPS>(p, ctl, tmem, (warp - kSoftWarp) >> 2, warp & 3, lane);
   } else if (warp >= kQueryWarp) {
