@@ -36,6 +36,9 @@ static_assert(kQueryThreads / 16 == kMassQueryStep && kQueryThreads >= kMassTile
 constexpr int kTileBytes = kMassTile * 256;       // 128 keys x 128 bf16, or as many (token, head) pairs: 32 KB
 constexpr int kHalfBytes = kTileBytes / 2;
 constexpr int kKeySlots = 4, kQuerySlots = 2;     // rings; a tile of keys has an accumulator of its own
+constexpr int kExtraBytes = kMassTile * 32;       // 128 rows of 16 more elements: the step of the products that takes lse off
+constexpr int kOneBytes = 256;
+constexpr float kRootDim = 11.313708498984761f;   // sqrt(d)
 constexpr int kTmemCols = 512;
 constexpr int kTileShift = 7, kSpanShift = 2;
 static_assert(kMassTile == 1 << kTileShift && kMassSpan == 1 << kSpanShift, "");
@@ -47,11 +50,26 @@ struct Item {
   int blocks;   // of its queries
 };
 
-// A block of (token, head) pairs as the weighing warps see it.
-struct Pairs {
-  alignas(16) float lse[kMassTile];   // -lse in base 2
-  uint64_t bits[kMassTile];           // tree: drafted tokens seen
-};
+// x / n by its reciprocal ceil(2^32 / n) (0 for n = 1), for x n < 2^32
+__device__ __forceinline__ int quotient(int x, uint32_t inv) {
+  return inv ? static_cast<int>(__umulhi(static_cast<uint32_t>(x), inv)) : x;
+}
+
+// An item in 64 bits: a length of 25, a count of 18, a row of 16 (n > 0 only where they fit the call).
+__device__ __forceinline__ uint64_t packed(int L, int n, int row) {
+  return static_cast<uint64_t>(L) | static_cast<uint64_t>(n) << 25 | static_cast<uint64_t>(row) << 43;
+}
+__device__ __forceinline__ int packed_n(uint64_t x) { return static_cast<int>(x >> 25 & 0x3ffff); }
+__device__ __forceinline__ int packed_L(uint64_t x) { return static_cast<int>(x & 0x1ffffff); }
+__device__ __forceinline__ int packed_row(uint64_t x) { return static_cast<int>(x >> 43); }
+__device__ __forceinline__ Item item_of(const MassParams& p, uint64_t x) {
+  Item it;
+  it.L = packed_L(x);
+  it.n = packed_n(x);
+  it.row = packed_row(x);
+  it.blocks = quotient(it.n + p.tpb - 1, p.inv_tpb) * p.chunks;
+  return it;
+}
 
 struct Start {
   int seq, g, s, b;
@@ -68,15 +86,10 @@ struct Ctl {
   int ranges;
   int64_t begin, end;   // this CTA's range
   Start start;
-  Pairs pairs[kQuerySlots];
-  int64_t before[kMaxCallRows + 1];   // units before a sequence
-  Item item[kMaxCallRows];
+  uint64_t bits[kQuerySlots][kMassTile];   // tree: drafted tokens that the pairs of a block see
+  int64_t before[kMaxCallRows + 1];        // units before a sequence
+  uint64_t item[kMaxCallRows];             // packed
 };
-
-// x / n by its reciprocal ceil(2^32 / n) (0 for n = 1), for x n < 2^32
-__device__ __forceinline__ int quotient(int x, uint32_t inv) {
-  return inv ? static_cast<int>(__umulhi(static_cast<uint32_t>(x), inv)) : x;
-}
 
 // The tiles of one group of a row and the query blocks that see some of it.
 struct Group {
@@ -127,7 +140,7 @@ struct PieceIter {
     take(p, ctl->start.b);
   }
   __device__ __forceinline__ void row(const MassParams& p, const Ctl* ctl) {
-    it = ctl->item[seq];
+    it = item_of(p, ctl->item[seq]);
     groups = groups_of(it.L, span);
     seen = p.tree ? 0 : it.L - it.n - p.window + 1;
   }
@@ -200,18 +213,17 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
     }
     if (rivals && it.n > 0 && (atomicOr(&named[it.row >> 5], 1u << (it.row & 31)) & (1u << (it.row & 31))))
       atomicOr(&named[words + (it.row >> 5)], 1u << (it.row & 31));
-    it.blocks = quotient(it.n + p.tpb - 1, p.inv_tpb) * p.chunks;
     if (it.n > 0) tiles += groups_of(it.L, kTileShift);
-    ctl->item[i] = it;
+    ctl->item[i] = it.n > 0 ? packed(it.L, it.n, it.row) : 0;
   }
   if (tiles) atomicAdd(reinterpret_cast<unsigned long long*>(&ctl->end), static_cast<unsigned long long>(tiles));
   __syncthreads();
   const int span = kTileShift + (ctl->end * p.G >= p.span_from ? kSpanShift : 0);
   if (!p.cut) {
     for (int i = tid; i < p.n; i += blockDim.x) {
-      const Item it = ctl->item[i];
+      const Item it = item_of(p, ctl->item[i]);
       if (rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1)) {
-        ctl->item[i].n = 0;
+        ctl->item[i] = 0;
         atomicOr(p.err, kErrRow);
         ctl->before[i + 1] = 0;
       } else {
@@ -221,7 +233,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
     }
   } else {
     for (int i = warp; i < p.n; i += blockDim.x / 32) {
-      const Item it = ctl->item[i];
+      const Item it = item_of(p, ctl->item[i]);
       const bool twice = rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1);
       const int ng = it.n > 0 && !twice ? groups_of(it.L, span) : 0;
       int u = 0;   // (32,768 groups of 1,041 blocks at most)
@@ -230,7 +242,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
       if (lane == 0) {
         ctl->before[i + 1] = u;
         if (twice) {
-          ctl->item[i].n = 0;
+          ctl->item[i] = 0;
           atomicOr(p.err, kErrRow);
         }
       }
@@ -265,7 +277,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
         else b = mid;
       }
       st.seq = a;
-      const Item it = ctl->item[a];
+      const Item it = item_of(p, ctl->item[a]);
       const int ng = groups_of(it.L, span);
       int64_t off = fb - ctl->before[a];
       const int64_t heads = ctl->before[a + 1] - ctl->before[a];   // G times the units of one
@@ -425,7 +437,7 @@ struct Block {
 
 // Queries: blocks into the ring, rows of 128 bytes with the chunks of 16 swizzled as the tensor core reads
 // them, zeros behind the last pair.
-__device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) {
+__device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, uint8_t* sL, int tid) {
   Ring<kQuerySlots> st;
   bool ok = true, there = false;   // there: the blocks of this row and KV head stay
   const int lane = tid & 31, chunk = tid & 15;
@@ -459,10 +471,16 @@ __device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) 
           q += p.wrap;
         }
       }
-      if (tid < blk.count) {
-        Pairs& pr = ctl->pairs[st.at];
-        pr.lse[tid] = -1.4426950408889634f * lse;
-        if (p.tree) pr.bits[tid] = bits;
+      if (tid < columns) {
+        // -lse in units of the products, three bf16 parts (24 bits; one where it is not finite)
+        const float x = -lse * kRootDim;
+        const __nv_bfloat16 hi = __float2bfloat16_rn(x);
+        const float rest = fabsf(x) < INFINITY ? x - __bfloat162float(hi) : 0.f;
+        const __nv_bfloat16 mid = __float2bfloat16_rn(rest), lo = __float2bfloat16_rn(rest - __bfloat162float(mid));
+        uint4* row = reinterpret_cast<uint4*>(sL + st.at * kExtraBytes + (tid >> 3) * 256 + (tid & 7) * 16);
+        row[0] = make_uint4(__bfloat16_as_ushort(hi) | static_cast<uint32_t>(__bfloat16_as_ushort(mid)) << 16, __bfloat16_as_ushort(lo), 0u, 0u);
+        row[8] = make_uint4(0u, 0u, 0u, 0u);
+        if (p.tree) ctl->bits[st.at][tid] = bits;
       }
       cp_async_wait();
       fence_proxy_async_smem();
@@ -477,8 +495,10 @@ __device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, int tid) 
 
 // Products: issuer 0 or 1 has every other tile.  (One for all left the tensor pipe idle for 400 of 1,000 cycles a tile and
 // block, between the end of one's instructions and the start of the next one's.)
-__device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const uint8_t* sQ, uint32_t tmem, int issuer) {
+__device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const uint8_t* sQ, const uint8_t* sOne, const uint8_t* sL,
+                         uint32_t tmem, int issuer) {
   const uint64_t dk0 = sdesc_k_sw128(smem_u32(sK)), dq0 = sdesc_k_sw128(smem_u32(sQ));
+  const uint64_t one = sdesc_k_none(smem_u32(sOne), 128, 0), dl0 = sdesc_k_none(smem_u32(sL), 128, 256);
   Ring<kKeySlots> st;
   Ring<kQuerySlots> q;    // the next block to come
   uint32_t s_par = 0;     // bit a: parity of accumulator a's next use
@@ -512,6 +532,7 @@ __device__ void mma_loop(const MassParams& p, Ctl* ctl, const uint8_t* sK, const
             const uint64_t off = (kk >> 2) * (kHalfBytes >> 4) + (kk & 3) * 2;
             mma_bf16(tmem + at.at * kMassTile, dk + off, dq + off, idesc, kk > 0);
           }
+          mma_bf16(tmem + at.at * kMassTile, one, dl0 + static_cast<uint64_t>(slot * (kExtraBytes >> 4)), idesc, 1);
           mma_commit(&ctl->s_full[at.at]);
           if (j == nb - 1) mma_commit(&ctl->k_empty[at.at]);
         }
@@ -560,12 +581,11 @@ __device__ __forceinline__ void wait16(uint32_t (&r)[16]) {
 // Sum of 16 pairs' weights, all of them seen; TAIL: of those in front of `count` (behind them an earlier block
 // may have left anything).
 template <bool TAIL>
-__device__ __forceinline__ float2 weigh16(const uint32_t (&z)[16], const float* lse, float2 sc, int count, float2 acc) {
+__device__ __forceinline__ float2 weigh16(const uint32_t (&z)[16], float2 sc, int count, float2 acc) {
 #pragma unroll
   for (int i = 0; i < 16; i += 4) {
-    const float4 l = *reinterpret_cast<const float4*>(lse + i);
-    const float2 a = ffma2(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), sc, make_float2(l.x, l.y));
-    const float2 b = ffma2(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), sc, make_float2(l.z, l.w));
+    const float2 a = fmul2(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), sc);
+    const float2 b = fmul2(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), sc);
     float2 x = make_float2(ex2_approx(a.x), ex2_approx(a.y)), y = make_float2(ex2_approx(b.x), ex2_approx(b.y));
     if (TAIL) {
       x = make_float2(i < count ? x.x : 0.f, i + 1 < count ? x.y : 0.f);
@@ -578,7 +598,7 @@ __device__ __forceinline__ float2 weigh16(const uint32_t (&z)[16], const float* 
 
 // A block that the warp's keys are seen by: 16 columns at a time, the next ones on their way.  (A short loop: unrolled
 // over the block, whose code is then longer than the innermost instruction caches, it took half as long again.)
-__device__ __forceinline__ float weigh_block(uint32_t addr, const float* lse, float c2, int count) {
+__device__ __forceinline__ float weigh_block(uint32_t addr, float c2, int count) {
   const float2 sc = make_float2(c2, c2);
   uint32_t z0[16], z1[16];
   float2 acc = make_float2(0.f, 0.f);
@@ -587,19 +607,17 @@ __device__ __forceinline__ float weigh_block(uint32_t addr, const float* lse, fl
   for (; count >= 32; count -= 32) {
     wait16(z0);
     ld16(addr + 16, z1);
-    acc = weigh16<false>(z0, lse, sc, 0, acc);
+    acc = weigh16<false>(z0, sc, 0, acc);
     wait16(z1);
     if (count > 32) ld16(addr + 32, z0);
-    acc = weigh16<false>(z1, lse + 16, sc, 0, acc);
+    acc = weigh16<false>(z1, sc, 0, acc);
     addr += 32;
-    lse += 32;
   }
 #pragma unroll 1
   for (; count > 0; count -= 16) {
     wait16(z0);
-    acc = weigh16<true>(z0, lse, sc, count, acc);
+    acc = weigh16<true>(z0, sc, count, acc);
     addr += 16;
-    lse += 16;
     if (count > 16) ld16(addr, z0);
   }
   return acc.x + acc.y;
@@ -607,7 +625,7 @@ __device__ __forceinline__ float weigh_block(uint32_t addr, const float* lse, fl
 
 // A block under a window that is not: the tokens that see a key follow one another, so that their pairs are the columns
 // lo .. hi - 1 (of this thread's key).
-__device__ __forceinline__ float weigh_columns(uint32_t addr, const float* lse, float c2, int lo, int hi, int count) {
+__device__ __forceinline__ float weigh_columns(uint32_t addr, float c2, int lo, int hi, int count) {
   float sum = 0.f;
 #pragma unroll 1
   for (; count > 0; count -= 16) {
@@ -616,11 +634,10 @@ __device__ __forceinline__ float weigh_columns(uint32_t addr, const float* lse, 
     wait16(z);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float w = ex2_approx(fmaf(__uint_as_float(z[i]), c2, lse[i]));
+      const float w = ex2_approx(__uint_as_float(z[i]) * c2);
       sum += i >= lo && i < hi ? w : 0.f;
     }
     addr += 16;
-    lse += 16;
     lo -= 16;
     hi -= 16;
   }
@@ -628,11 +645,11 @@ __device__ __forceinline__ float weigh_columns(uint32_t addr, const float* lse, 
 }
 
 // A block of a tree that is not: of the pairs in front of `count` those whose token has bit j - ctx, or all for a cached key.
-__device__ __forceinline__ float weigh_bits(uint32_t addr, const Pairs& pr, float c2, int count, int j, int ctx, int L) {
+__device__ __forceinline__ float weigh_bits(uint32_t addr, const uint64_t* bits, float c2, int count, int j, int ctx, int L) {
   float sum = 0.f;
   const int drafted = max(j - ctx, 0), shift = drafted & 31;
   const uint32_t any = j < ctx ? ~0u : 0u;
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(pr.bits) + (drafted >> 5 & 1);
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(bits) + (drafted >> 5 & 1);
   if (j >= L) count = 0;
   const int most = __reduce_max_sync(kFull, count);
 #pragma unroll 1
@@ -642,7 +659,7 @@ __device__ __forceinline__ float weigh_bits(uint32_t addr, const Pairs& pr, floa
     wait16(z);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float w = ex2_approx(fmaf(__uint_as_float(z[i]), c2, pr.lse[c + i]));
+      const float w = ex2_approx(__uint_as_float(z[i]) * c2);
       sum += ((words[2 * (c + i)] | any) >> shift & 1) && c + i < count ? w : 0.f;
     }
   }
@@ -681,7 +698,6 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
         q.next();
       }
       const Block blk(p, c.it.n, c.b0 + b);
-      const Pairs& pr = ctl->pairs[slot];
       const int first = ctx + blk.t0, end = ctx + min(blk.t0 + p.tpb, c.it.n) - 1;   // positions of the block's tokens
 #pragma unroll 1
       for (int i = i0; i < c.grp.tiles; i += GROUPS) {
@@ -700,14 +716,14 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
         }
         const uint32_t at = lanes + a * kMassTile;
         if (all) {
-          w = weigh_block(at, pr.lse, p.scale2, blk.count);
+          w = weigh_block(at, p.scale2, blk.count);
         } else if (p.tree) {
-          if (!none) w = weigh_bits(at, pr, p.scale2, blk.count, k0 + lane, ctx, c.it.L);
+          if (!none) w = weigh_bits(at, ctl->bits[slot], p.scale2, blk.count, k0 + lane, ctx, c.it.L);
         } else if (!none) {
           const int j = k0 + lane, nt = end - first + 1;
           const int ta = min(max(j - first, 0), nt), tb = j < p.n_sink ? nt : min(max(j + p.window - first, 0), nt);
           const int per = nt > 1 ? p.heads : blk.count;   // columns of a token
-          w = weigh_columns(at, pr.lse, p.scale2, ta * per, tb * per, blk.count);
+          w = weigh_columns(at, p.scale2, ta * per, tb * per, blk.count);
         }
         if (i < GROUPS) sum[0] += w;
         else sum[1] += w;
@@ -750,7 +766,9 @@ __global__ void __launch_bounds__(threads_of(GROUPS), 1) k_mass(const __grid_con
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sK = smem;                            // [slots][2 halves][128 keys][128 B]
   uint8_t* sQ = sK + kKeySlots * kTileBytes;     // [slots][2 halves][128 pairs][128 B]
-  Ctl* ctl = reinterpret_cast<Ctl*>(sQ + kQuerySlots * kTileBytes);
+  uint8_t* sOne = sQ + kQuerySlots * kTileBytes; // [8][16]: 1, 1, 1, 0 ..., for every eight keys of a tile
+  uint8_t* sL = sOne + kOneBytes;                // [slots][128 pairs][16]: the parts of -lse, 0 ...
+  Ctl* ctl = reinterpret_cast<Ctl*>(sL + kQuerySlots * kExtraBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < kKeySlots; ++i) {
@@ -768,6 +786,12 @@ __global__ void __launch_bounds__(threads_of(GROUPS), 1) k_mass(const __grid_con
     ctl->end = 0;
     fence_mbar_init();
   }
+  if (threadIdx.x < 8) {
+    uint4* row = reinterpret_cast<uint4*>(sOne + threadIdx.x * 16);
+    row[0] = make_uint4(0x3F803F80u, 0x3F80u, 0u, 0u);
+    row[8] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
+  }
   if (warp == kMmaWarp) {
     tmem_alloc(&ctl->tmem_base, kTmemCols);
     tmem_relinquish();
@@ -782,11 +806,11 @@ __global__ void __launch_bounds__(threads_of(GROUPS), 1) k_mass(const __grid_con
   if (warp < kMmaWarp) {
     key_loop(p, ctl, sK, warp, lane);
   } else if (warp < kQueryWarp) {
-    mma_loop(p, ctl, sK, sQ, tmem, warp - kMmaWarp);
+    mma_loop(p, ctl, sK, sQ, sOne, sL, tmem, warp - kMmaWarp);
   } else if (warp >= kSoftWarp) {
     weigh_loop<GROUPS>(p, ctl, tmem, (warp - kSoftWarp) >> 2, warp & 3, lane);
   } else if (warp >= kQueryWarp) {
-    query_loop(p, ctl, sQ, threadIdx.x - 32 * kQueryWarp);
+    query_loop(p, ctl, sQ, sL, threadIdx.x - 32 * kQueryWarp);
   }
   if (threadIdx.x == 0 && p.cut) {   // what the sum of the parts has to know of this range's end
     MassSplit s;
@@ -828,7 +852,8 @@ __global__ void __launch_bounds__(kMassSpan * kMassTile) k_mass_sum(const __grid
 
 namespace {
 
-constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kKeySlots + kQuerySlots) * kTileBytes + sizeof(Ctl);
+constexpr size_t kSmemBytes =
+    1024 + static_cast<size_t>(kKeySlots + kQuerySlots) * kTileBytes + kOneBytes + kQuerySlots * kExtraBytes + sizeof(Ctl);
 static_assert(kSmemBytes <= 227 * 1024, "the rings and the control block fit an SM");
 static_assert(kMaxTableRows / 4 <= kQuerySlots * kTileBytes, "the rows' bits fit the queries' ring");
 

@@ -362,6 +362,8 @@ __device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c) { return _
 
 __device__ __forceinline__ float2 fadd2(float2 a, float2 b) { return __fadd2_rn(a, b); }
 
+__device__ __forceinline__ float2 fmul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
+
 // ------------------------------------------------------------------ programmatic dependent launch
 
 // Lets the next kernel of the stream be scheduled before this one ends (it
