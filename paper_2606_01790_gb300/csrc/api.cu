@@ -1550,7 +1550,7 @@ starkv_status validate_bounds(const starkv_state* st, const starkv_pages* pg, co
 struct SparseWs {
   PagedWs attn;
   int per_launch, n_list;
-  size_t list, keys, scores, total;
+  size_t found, list, keys, scores, total;
 };
 
 SparseWs sparse_ws(const starkv_state* st, const starkv_pages& p, int n, int T, int n_chosen) {
@@ -1562,7 +1562,8 @@ SparseWs sparse_ws(const starkv_state* st, const starkv_pages& p, int n, int T, 
   const int64_t each = static_cast<int64_t>(c.n_kv_heads) * (static_cast<int64_t>(w.n_list) * 4 + static_cast<int64_t>(p.max_pages) * 12);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kPagedItems / nblk, (int64_t(256) << 20) / each));
   w.per_launch = static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(1, static_cast<int64_t>(n) * T)));
-  w.list = w.attn.total;
+  w.found = w.attn.total;
+  w.list = w.found + align256(static_cast<size_t>(w.per_launch) * sizeof(int2));
   w.keys = w.list + align256(static_cast<size_t>(w.per_launch) * c.n_kv_heads * w.n_list * sizeof(int32_t));
   const size_t pages = static_cast<size_t>(w.per_launch) * c.n_kv_heads * p.max_pages;
   w.scores = w.keys + align256(pages * sizeof(uint64_t));
@@ -1827,6 +1828,7 @@ starkv_status starkv_sparse_attention(starkv_state* st, const starkv_pages* page
   p.rows = q->rows;
   p.n_tokens = q->n_tokens;
   p.list = reinterpret_cast<const int32_t*>(ws + w.list);
+  p.found = reinterpret_cast<const int2*>(ws + w.found);
   p.n_list = w.n_list;
   p.tokens = q->T;
   ChooseParams ch;
@@ -1847,6 +1849,8 @@ starkv_status starkv_sparse_attention(starkv_state* st, const starkv_pages* page
   ch.n_last = n_last;
   ch.n_list = w.n_list;
   ch.list = reinterpret_cast<int32_t*>(ws + w.list);
+  ch.tokens = reinterpret_cast<int2*>(ws + w.found);
+  ch.err = st->dev.err;
   ch.chosen = chosen;
   ch.n_chosen = n_chosen;
   ch.keys = reinterpret_cast<uint64_t*>(ws + w.keys);

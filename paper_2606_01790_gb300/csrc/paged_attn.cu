@@ -68,7 +68,6 @@
 #include "common.cuh"
 #include "paged_attn.cuh"
 #include "ptx.cuh"
-#include "sparse.cuh"
 
 namespace starkv {
 
@@ -264,12 +263,8 @@ __device__ __forceinline__ int64_t o_at(const SparseAttnParams& p, int item, int
 
 // A query of a call over chosen pages: a sequence of the tokens that these hold up to its own.
 __device__ Item read_item(const SparseAttnParams& p, int item) {
-  const SparseQuery q = sparse_query(p.rows, p.n_tokens, p.len, p.n_rows, p.max_pages, p.shift, p.tokens, p.item0 + item);
-  if (q.wrong) atomicOr(p.err, kErrRow);
-  if (!q.live) return Item{-1, 0};
-  if (q.pos < 0) return Item{-1, 1};
-  const int pages = min((q.pos >> p.shift) + 1, p.n_list);
-  return Item{((pages - 1) << p.shift) + (q.pos & ((1 << p.shift) - 1)) + 1, 1};
+  const int2 x = p.found[item];
+  return Item{x.x, x.y};
 }
 
 // A sequence's length and queries (read by every CTA: the call may be replayed).

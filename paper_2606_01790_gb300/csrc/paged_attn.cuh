@@ -53,6 +53,7 @@ struct PagedAttnParams {
 // launch, of one token (n: queries of the launch, T = 1, strides and rows those of the call).
 struct SparseAttnParams : PagedAttnParams {
   const int32_t* list;   // [n][G][n_list] page numbers, in the order of their tokens
+  const int2* found;     // [n] tokens of such a sequence (-1: its row does not fit), and 1 for a query that there is
   int n_list;
   int tokens, item0;
 };

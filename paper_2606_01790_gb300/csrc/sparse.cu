@@ -264,6 +264,18 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
   griddep_launch_dependents();
   griddep_wait();
   const PagesView& pg = p.pg;
+  const int seq = v / p.T, t = v - seq * p.T;
+  const __nv_bfloat16* q = p.q + seq * p.q_seq + t * p.q_token + static_cast<int64_t>(g) * p.hg * p.q_head;
+  // the weights of the terms, on their way with the row's length (a query that is none is not read)
+  const int count = p.n_tokens ? p.n_tokens[seq] : p.T;
+  float up = 0.f, down = 0.f, up_rest = 0.f, down_rest = 0.f;
+  if (tid < kHeadDim && t < count && count <= p.T)
+#pragma unroll 4
+    for (int h = 0; h < p.hg; ++h) {
+      const float x = __bfloat162float(q[h * p.q_head + tid]);
+      up = sum_and_rest(up, x < 0.f ? 0.f : x, &up_rest);   // (a NaN goes into both)
+      down = sum_and_rest(down, x > 0.f ? 0.f : x, &down_rest);
+    }
   const SparseQuery sq = sparse_query(p.rows, p.n_tokens, pg.len, pg.n_rows, pg.max_pages, pg.shift, p.T, v);
   const int pages = !sq.live || sq.pos < 0 ? 0 : (sq.pos >> pg.shift) + 1;
   const int take = min(pages, p.n_list);
@@ -274,8 +286,11 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
   const bool here = hi - lo <= kChoosePages;   // the scores fit shared memory
   const int64_t place = (static_cast<int64_t>(item) * p.G + g) * pg.max_pages;
   uint32_t* far = p.scores + place - lo;
-  const int seq = v / p.T, t = v - seq * p.T;
-  const __nv_bfloat16* q = p.q + seq * p.q_seq + t * p.q_token + static_cast<int64_t>(g) * p.hg * p.q_head;
+  if (tid == 0 && g == 0 && rank == 0) {   // what the attention has to know of the query
+    if (sq.wrong) atomicOr(p.err, kErrRow);
+    const int last = sq.pos & ((1 << pg.shift) - 1);
+    p.tokens[item] = make_int2(sq.live && sq.pos >= 0 ? ((take - 1) << pg.shift) + last + 1 : -1, sq.live);
+  }
   const int per = p.ctas * kChooseWarps * kPagesAtOnce, own = (rank * kChooseWarps + warp) * kPagesAtOnce;
   if (tid == 0) s.least = ~0u, s.most = 0, s.few = 0;
   if (rank == 0)
@@ -283,13 +298,6 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
   if (need > 0) {
     int id = lo + own + (lane & 7) < hi ? entries[lo + own + (lane & 7)] : -1;   // lane l: page l of the eight
     if (tid < kHeadDim) {
-      float up = 0.f, down = 0.f, up_rest = 0.f, down_rest = 0.f;
-#pragma unroll 4
-      for (int h = 0; h < p.hg; ++h) {
-        const float x = __bfloat162float(q[h * p.q_head + tid]);
-        up = sum_and_rest(up, x < 0.f ? 0.f : x, &up_rest);   // (a NaN goes into both)
-        down = sum_and_rest(down, x > 0.f ? 0.f : x, &down_rest);
-      }
       s.up[tid] = up;
       s.down[tid] = down;
       s.up_rest[tid] = fabsf(up) < INFINITY ? up_rest : 0.f;
@@ -367,6 +375,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
     const int n = hi - lo, run = (n + kChooseThreads - 1) / kChooseThreads;
     const bool ranked = run <= kRun;   // (shared memory holds them)
     uint32_t mine[kRun];               // pages lo + tid run ..
+    int number[kRun];                  // and theirs in the pool, on their way
     float top, bottom;                 // the k-th greatest score lies between them
     if (ranked) {
       // bins of equal width between the least key and the greatest: the one that the k-th greatest is in holds
@@ -376,6 +385,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
       for (int r = 0; r < kRun; ++r) {
         const bool real = r < run && tid * run + r < n;
         mine[r] = real ? s.key[tid * run + r] : 0;
+        number[r] = real ? entries[lo + tid * run + r] : 0;
         if (real) least = min(least, mine[r]), most = max(most, mine[r]);
       }
       least = __reduce_min_sync(kFull, least);
@@ -432,7 +442,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
         for (int r = 0; r < kRun; ++r)
           if (r < run && tid * run + r < n && !(value_of(mine[r]) < below)) {
             const int j = lo + tid * run + r;
-            list[to] = entries[j];
+            list[to] = number[r];
             if (chosen) chosen[to] = j;
             ++to;
           }

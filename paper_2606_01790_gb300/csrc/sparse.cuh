@@ -59,6 +59,8 @@ struct ChooseParams {
   int G, hg;
   int n_first, n_last, n_list;   // n_list: pages taken, at most max_pages
   int32_t* list;                 // [items][G][n_list] page numbers
+  int2* tokens;                  // [items] tokens that the chosen pages hold up to the query (-1: the row does not fit), 1 for a query
+  uint32_t* err;
   int32_t* chosen;               // [n * T][G][n_chosen] places in the row, or NULL
   int n_chosen;
   int ctas;                      // of a cluster: 1, 2, 4 or 8
