@@ -889,6 +889,7 @@ constexpr int kSelThreads = 1024;
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelKeys = 49152;    // keys that shared memory holds
 constexpr int kSelMoves = 4;       // masses of a thread on their way at once
+constexpr int kSelBins = 2048;
 constexpr int kSelClose = 512;     // close tokens that are ranked by comparing each with each
 
 // Ascending order as unsigned numbers; a NaN (a mass that is none) comes with infinity, so that its token
@@ -909,10 +910,12 @@ struct SelSmem {
   int hist[256];
   int warp_sum[kSelWarps];
   uint64_t digit;
-  int need, n_close;
-  uint32_t size, negative;
+  int need, bin;
+  uint32_t least, most, size, negative;
+  int bins[kSelBins];
   uint64_t close[kSelClose];
   int close_at[kSelClose];
+  uint8_t stays[kSelClose];
   uint32_t key[1];   // as many as the launch asks for
 };
 
@@ -1026,117 +1029,154 @@ __global__ void __launch_bounds__(kSelThreads)
     return here ? s.key[j] : order_key(sum_of(j, &a));
   };
   if (B > 0 && B < Lp) {
-    if (tid == 0) s.size = s.negative = s.n_close = 0;
+    if (tid == 0) s.size = s.negative = s.most = 0, s.least = ~0u;
+    for (int i = tid; i < kSelBins; i += kSelThreads) s.bins[i] = 0;
     __syncthreads();
-    uint32_t size = 0;
+    uint32_t size = 0, least = ~0u, most = 0;
     bool negative = false;
 #pragma unroll 8
     for (int j = tid; j < Lp; j += kSelThreads) {
       float a;
       const float x = sum_of(j, &a);
-      if (here) s.key[j] = order_key(x);
+      const uint32_t k = order_key(x);
+      if (here) s.key[j] = k;
+      least = min(least, k);
+      most = max(most, k);
       if (!PER_HEAD) {
         size = max(size, __float_as_uint(a));   // (a NaN is above infinity)
         negative = negative || a != x;          // (also where a sum is not a number)
       }
     }
+    least = __reduce_min_sync(kFull, least);
+    most = __reduce_max_sync(kFull, most);
     if (!PER_HEAD) {
       size = __reduce_max_sync(kFull, size);
       negative = __any_sync(kFull, negative);
-      if ((tid & 31) == 0) {
-        atomicMax(&s.size, size);
-        if (negative) s.negative = 1;
-      }
+    }
+    if ((tid & 31) == 0) {
+      atomicMin(&s.least, least);
+      atomicMax(&s.most, most);
+      if (!PER_HEAD) atomicMax(&s.size, size);
+      if (negative) s.negative = 1;
     }
     __syncthreads();
-    int need;   // of the tokens that have the least key
-    const uint32_t least = kth_greatest<uint32_t>(s, Lp, B, key_of, &need);
-    uint32_t above = least, below = least;   // keys: in, out, and those between
-    if (!PER_HEAD) {
-      const float at = key_value(least), e = pg.G * 2.5f * 0x1p-24f;   // (twice the error, and roundings)
-      const float off = s.negative || !(fabsf(at) < INFINITY) ? __uint_as_float(s.size) * e : at * e;
-      above = order_key(at + off + 1e-44f);
-      below = order_key(at - off - 1e-44f);
-      if (!(off < INFINITY)) above = ~0u, below = 0;   // all of them
+    least = s.least;
+    most = s.most;
+    // the bin of keys (of equal width between the least and the greatest) that the budget-th greatest is in
+    const int shift = max(0, 32 - __clz(most - least) - 11);   // (kSelBins = 2^11)
+    for (int j = tid; j < Lp; j += kSelThreads) atomicAdd(&s.bins[(key_of(j) - least) >> shift], 1);
+    __syncthreads();
+    {
+      constexpr int kOwn = kSelBins / kSelThreads;   // bins of a thread, from the greatest down
+      int count[kOwn], sum = 0, total;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) sum += count[i] = s.bins[kSelBins - 1 - tid * kOwn - i];
+      int left = B - sum_before(sum, s.warp_sum, &total);
+      if (left > 0 && left <= sum) {
+        int i = 0;
+#pragma unroll
+        for (int u = 0; u < kOwn - 1; ++u)
+          if (i == u && count[u] < left) left -= count[u], ++i;
+        s.bin = kSelBins - 1 - tid * kOwn - i;
+      }
+      __syncthreads();
     }
-    // every thread a run of tokens
-    const int run = (Lp + kSelThreads - 1) / kSelThreads, from = min(tid * run, Lp), to = min(from + run, Lp);
-    int sure = 0, close = 0, n_sure, n_close;
-    for (int j = from; j < to; ++j) {
-      const uint32_t k = key_of(j);
-      sure += k > above;
-      close += k <= above && k >= below;
-    }
-    int at_sure = sum_before(sure, s.warp_sum, &n_sure), at_close = sum_before(close, s.warp_sum, &n_close);
-    const int left = B - n_sure;
-    if (PER_HEAD || left == n_close) {   // of the close ones the lowest
+    const uint32_t first = least + (static_cast<uint32_t>(s.bin) << shift);
+    uint32_t bottom = first, top = min(most, first + ((1u << shift) - 1));   // keys that the budget-th greatest lies between
+    const int run = (Lp + kSelThreads - 1) / kSelThreads, from = min(tid * run, Lp), to = min(from + run, Lp);   // of a thread
+    // A second round, with the budget-th greatest itself, where the bin holds more tokens than are compared one by one.
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+      int need;   // of the tokens that have the key
+      if (again) top = bottom = kth_greatest<uint32_t>(s, Lp, B, key_of, &need);
+      uint32_t above = top, below = bottom;   // greater keys are in, lower ones out
+      if (!PER_HEAD) {
+        const float t = key_value(top), e = pg.G * 2.5f * 0x1p-24f;   // (twice the error, and roundings)
+        const float off = s.negative || !(fabsf(t) < INFINITY) ? __uint_as_float(s.size) * e : t * e;
+        above = order_key(t + off + 1e-44f);
+        below = order_key(key_value(bottom) - off - 1e-44f);
+        if (!(off < INFINITY)) above = ~0u, below = 0;   // all of them are between
+      }
+      int sure = 0, close = 0, n_sure, n_close;
       for (int j = from; j < to; ++j) {
         const uint32_t k = key_of(j);
-        const bool near = k <= above && k >= below;
-        if (k > above || (near && at_close < left)) idx[at_sure + min(at_close, left)] = j;
-        at_sure += k > above;
-        at_close += near;
+        sure += k > above;
+        close += k <= above && k >= below;
       }
-    } else {
-      auto wide = [&](int j) {
+      int at_sure = sum_before(sure, s.warp_sum, &n_sure), at_close = sum_before(close, s.warp_sum, &n_close);
+      const int left = B - n_sure;
+      if (left == n_close || (PER_HEAD && top == bottom)) {   // of the close ones the lowest
+        for (int j = from; j < to; ++j) {
+          const uint32_t k = key_of(j);
+          const bool near = k <= above && k >= below;
+          if (k > above || (near && at_close < left)) idx[at_sure + min(at_close, left)] = j;
+          at_sure += k > above;
+          at_close += near;
+        }
+        break;
+      }
+      auto exact = [&](int j) -> uint64_t {
+        if (PER_HEAD) return key_of(j);
         double x = heads[j];
         for (int g = g0 + 1; g < g1; ++g) x += static_cast<double>(mass[g * mv.group_stride + j]);
         return order_key(x);
       };
-      uint64_t border;     // close tokens with greater keys stay, and `equal` of those that have this one
-      int equal;
-      const bool few = n_close <= kSelClose;
-      if (few) {
+      if (n_close <= kSelClose) {   // each compared with each
         int c = at_close;
         for (int j = from; j < to; ++j) {
           const uint32_t k = key_of(j);
           if (k <= above && k >= below) s.close_at[c++] = j;
         }
         __syncthreads();
-        if (tid < n_close) s.close[tid] = wide(s.close_at[tid]);
+        if (tid < n_close) s.close[tid] = exact(s.close_at[tid]);
         __syncthreads();
-        border = kth_greatest<uint64_t>(s, n_close, left, [&](int i) { return s.close[i]; }, &equal);
-      } else {
-        border = kth_greatest<uint64_t>(s, Lp, left, [&](int j) {
+        int stays = 0, total;
+        if (tid < n_close) {
+          const uint64_t k = s.close[tid];
+          int better = 0;
+          for (int i = 0; i < n_close; ++i) better += s.close[i] > k || (s.close[i] == k && i < tid);
+          stays = better < left;
+          s.stays[tid] = stays;
+        }
+        __syncthreads();
+        c = at_close;
+        int taken = sure;
+        for (int j = from; j < to; ++j) {
           const uint32_t k = key_of(j);
-          return k <= above && k >= below ? wide(j) : 0;
-        }, &equal);
+          if (k <= above && k >= below) taken += s.stays[c++];
+        }
+        int out = sum_before(taken, s.warp_sum, &total);
+        c = at_close;
+        for (int j = from; j < to; ++j) {
+          const uint32_t k = key_of(j);
+          if (k > above || (k <= above && k >= below && s.stays[c++])) idx[out++] = j;
+        }
+        break;
       }
-      int same = 0, total, c = at_close;
-      auto wide_key = [&](int j) { return few ? s.close[c] : wide(j); };
+      if (!again) continue;
+      // too many of them: digits of the sums in 64 bits
+      int equal, total;
+      const uint64_t border = kth_greatest<uint64_t>(s, Lp, left, [&](int j) {
+        const uint32_t k = key_of(j);
+        return k <= above && k >= below ? exact(j) : 0;
+      }, &equal);
+      int same = 0, taken = 0;
       for (int j = from; j < to; ++j) {
         const uint32_t k = key_of(j);
-        if (!(k <= above && k >= below)) continue;
-        same += wide_key(j) == border;
-        ++c;
+        if (k <= above && k >= below) same += exact(j) == border;
       }
-      int at_same = sum_before(same, s.warp_sum, &total);
-      int taken = 0;
-      c = at_close;
-      for (int j = from, e = at_same; j < to; ++j) {
+      const int at_same = sum_before(same, s.warp_sum, &total);
+      auto stays = [&](int j, int* e) {
         const uint32_t k = key_of(j);
-        if (!(k <= above && k >= below)) {
-          taken += k > above;
-          continue;
-        }
-        const uint64_t x = wide_key(j);
-        taken += x > border || (x == border && e < equal);
-        e += x == border;
-        ++c;
-      }
+        if (k > above || k < below) return k > above;
+        const uint64_t x = exact(j);
+        return x > border || (x == border && (*e)++ < equal);
+      };
+      for (int j = from, e = at_same; j < to; ++j) taken += stays(j, &e);
       int out = sum_before(taken, s.warp_sum, &total);
-      c = at_close;
-      for (int j = from, e = at_same; j < to; ++j) {
-        const uint32_t k = key_of(j);
-        bool in = k > above;
-        if (k <= above && k >= below) {
-          const uint64_t x = wide_key(j);
-          in = x > border || (x == border && e < equal);
-          e += x == border;
-          ++c;
-        }
-        if (in) idx[out++] = j;
-      }
+      for (int j = from, e = at_same; j < to; ++j)
+        if (stays(j, &e)) idx[out++] = j;
+      break;
     }
   } else {
     for (int j = tid; j < B; j += kSelThreads) idx[j] = j;
