@@ -1559,7 +1559,7 @@ SparseWs sparse_ws(const starkv_state* st, const starkv_pages& p, int n, int T, 
   w.attn = paged_attn_ws(st);
   w.n_list = std::min(n_chosen, p.max_pages);
   const int nblk = (c.n_heads / c.n_kv_heads + kPagedRows - 1) / kPagedRows;
-  const int64_t each = static_cast<int64_t>(c.n_kv_heads) * (static_cast<int64_t>(w.n_list) * 4 + static_cast<int64_t>(p.max_pages) * 12);
+  const int64_t each = static_cast<int64_t>(c.n_kv_heads) * p.max_pages * 16;   // (of any n_chosen: a workspace for more serves fewer)
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kPagedItems / nblk, (int64_t(256) << 20) / each));
   w.per_launch = static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(1, static_cast<int64_t>(n) * T)));
   w.found = w.attn.total;

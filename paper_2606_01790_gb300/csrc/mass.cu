@@ -441,10 +441,12 @@ __device__ void query_loop(const MassParams& p, Ctl* ctl, uint8_t* sQ, uint8_t* 
   Ring<kQuerySlots> st;
   bool ok = true, there = false;   // there: the blocks of this row and KV head stay
   const int lane = tid & 31, chunk = tid & 15;
+  // (a slot whose blocks stay is free when the CTA is through with a row and KV head: microseconds a group)
+  const uint64_t wait_ns = p.wait_ns + (p.cut ? 0 : static_cast<uint64_t>(ctl->end - ctl->begin) * 5000);
   for (PieceIter c(p, ctl); ok && c.valid(); there ? c.skip_head(p, ctl) : c.next(p, ctl)) {
     there = false;
     for (int b = c.b0; ok && b < c.b1; ++b) {
-      ok = warp_wait(ctl, &ctl->q_empty[st.at], st.par ^ 1, p.wait_ns);
+      ok = warp_wait(ctl, &ctl->q_empty[st.at], st.par ^ 1, wait_ns);
       if (!ok) break;
       const Block blk(p, c.it.n, b);
       const int columns = blk.columns();

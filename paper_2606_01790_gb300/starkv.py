@@ -755,22 +755,26 @@ def sink_attention(st: State, pages: Pages, layer: int, queries: Queries, n_sink
 # ---------------------------------------------------------------- attention mass, chosen pages
 
 class Mass:
-    """What each cached token has had of the queries' attention (``starkv_mass``).
+    """What each cached token has had of the queries' attention (``starkv_mass``).  The tensor is checked once, when the
+    object is made, and stays its own.
 
     data   f32 [n_layers][n_rows][G][tokens], tokens contiguous, max_pages * page_size of them or more
     decay  factor of what a token has had so far, when a call adds to it
     """
 
-    __slots__ = ("data", "decay", "_packed")
+    __slots__ = ("_data", "_decay", "_packed")
 
     def __init__(self, data: torch.Tensor, decay: float = 1.0):
         if data.dim() != 4 or data.stride(3) != 1:
             raise ValueError("mass: data is [n_layers, n_rows, G, tokens] with the tokens contiguous")
         _expect(torch.float32, data)
-        self.data, self.decay = data, float(decay)
+        self._data, self._decay = data, float(decay)
         # (an axis of one entry is never stepped along: its stride may be any)
         strides = [s if n > 1 else data.shape[3] for n, s in zip(data.shape[:3], data.stride()[:3])]
-        self._packed = bytes(CMass(data.data_ptr(), *strides, self.decay))
+        self._packed = bytes(CMass(data.data_ptr(), *strides, self._decay))
+
+    data = property(lambda self: self._data)
+    decay = property(lambda self: self._decay)
 
 
 def make_mass(st: State, pages: Pages, decay: float = 1.0) -> Mass:
@@ -781,7 +785,7 @@ def make_mass(st: State, pages: Pages, decay: float = 1.0) -> Mass:
 
 
 def _c_mass(st: State, pages: Pages, mass: Mass) -> bytes:
-    data = mass.data
+    data = mass._data
     if data.shape[:3] != (st.cfg.n_layers, pages.table.shape[0], st.cfg.n_kv_heads) \
             or data.shape[3] < pages.table.shape[1] * pages.k.shape[3]:
         raise ValueError("mass: data is [n_layers, n_rows, G, max_pages * page_size or more]")

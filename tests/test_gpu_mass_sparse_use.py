@@ -358,3 +358,20 @@ def test_calls_that_do_not_fit_are_refused_on_the_host():
     assert torch.equal(mass.data, before)
     c.check()
     st.close()
+
+
+def test_a_workspace_for_more_serves_fewer():
+    """Of rows, queries or pages; also where the scores of all queries would not fit one launch's share of it."""
+    st = PH.state(layers=1, heads=8, kv_heads=8)
+    c = PH.Pair(st, n_pages=300, P=16, n_rows=4, max_pages=100_000)
+    c.extend([0, 1], [2000, 600])
+    bounds = bounded(c)
+    ws = sk.sparse_workspace(st, c.pages, 4, 40, 5000)
+    for n, T, n_chosen in ((4, 40, 5000), (2, 40, 7), (1, 3, 5000), (2, 40, 3)):
+        assert sk.sparse_workspace(st, c.pages, n, T, n_chosen).numel() <= ws.numel()
+        qs = queries(c, min(n, 2), T, rows=c.ids([0, 1][:n]))
+        sk.sparse_attention(st, c.pages, 0, qs, bounds, 1, 1, n_chosen, ws)
+        torch.cuda.synchronize()
+        sk.check_device_error(st)
+        assert torch.isfinite(qs.o).all()
+    st.close()

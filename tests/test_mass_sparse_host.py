@@ -203,3 +203,13 @@ def test_the_two_cpu_definitions_agree():
                 o, lse = O.attention(q[None], k[g:g + 1], v[g:g + 1], seen)
                 np.testing.assert_allclose(got["lse"][i, t, 2 * g:2 * g + 2].numpy(), lse[0], rtol=2e-6)
                 np.testing.assert_allclose(got["o"][i, t, 2 * g:2 * g + 2].float().numpy(), o[0], rtol=2**-7, atol=1e-5)
+
+
+def test_a_masss_tensor_is_checked_once_and_stays_its_own():
+    m = sk.Mass(torch.zeros((2, 3, 4, 64)), 0.5)
+    with pytest.raises(AttributeError):
+        m.data = torch.zeros((2, 3, 4, 64))
+    with pytest.raises(AttributeError):
+        m.decay = 1.0
+    got = sk.CMass.from_buffer_copy(sk._c_mass(_State(), _pages(), m))
+    assert (got.mass, got.layer_stride, got.row_stride, got.group_stride, got.decay) == (m.data.data_ptr(), 768, 256, 64, 0.5)
