@@ -3,6 +3,29 @@
 // Mass: token j of a row, KV head g, after a call whose queries (the row's last n tokens)
 // have normalisers lse:
 //   mass_j = (j < L - n ? decay mass_j : 0) + sum_t sum_{h in g} [t sees j] exp(q_th . k_j / sqrt(d) - lse_th).
+//
+// Keys lie on the lanes of tensor memory and (token, head) pairs in its columns, so that a key's sum is a thread's own, no
+// sum crosses lanes, and a key that holds NaN or garbage touches nothing but its own.  A tile of 128 keys (A) meets blocks of up
+// to 128 pairs (B), nine K = 16 steps: eight of q . k, and one of three ones against -lse sqrt(d) in three bf16 parts (24 bits),
+// after which a weight is exp2 of the accumulator times one constant: no normaliser has to be fetched for each
+// element (from shared memory they took as much of its path as the accumulators: 112 us for 99 below).
+//
+// Work split.  A group is one tile or four (512 keys) of one row and KV head.  Where a call has one or two blocks of queries
+// they stay in shared memory while a row's keys pass once; groups go whole to contiguous ranges, one a CTA (persistent
+// grid), and are written by their CTA.  Where it has more, a group's keys stay and the blocks that see them pass; (group, block)
+// units are cut into ranges, and the parts of a group that is cut (at most the first and the last of a range) are added up by
+// k_mass_sum in the order of the ranges: no atomics, the same sums every time.
+//
+// What bounds it.  Few queries: the stream of K (64 rows of one token over 14k ragged keys, 8 KV heads: 1.2 GB in 183 us, 97 % of
+// the copy rate).  26 drafted tokens of 32 rows: 64 to 66 us for a stream of 45, half of the SMs' time in weighing two blocks a tile.
+// Many: the products' operands (8 KB a step through shared memory, 64 cycles) and the accumulators' way out of tensor
+// memory; a chunk of 2,704 tokens under a window of 4,096, 81 GFLOP, 99 us, tensor pipe 52 % busy; without the weighing 67, with
+// everything in it but the exponentials 93.  Not kept: exponentials in part as polynomials on the FMA pipe (an eighth of them 104,
+// a quarter 109); one key loader (246 for 205 us in the first case) and one issuer of products (205 for 183); a look through the
+// ring for the queries' next slot before their last block is handed over (230 for 218 in an earlier state of the chunk, since
+// asking a barrier may wait); weights unrolled over a block (212 for 162).
+//
+// Warp roles: 0 and 1 load keys, 2 and 3 issue products, 4 to 7 copy queries, the others weigh.
 #include <algorithm>
 
 #include "common.cuh"

@@ -10,6 +10,11 @@
 // first pages, the last ones up to its own and the best of the others; equal scores go to
 // the lower page.  Which of two pages is taken hangs on the last bit of their scores, which
 // are those of 64 bits.
+//
+// What bounds them.  Bounds: the keys' bytes, read once (28 layers of 14,032 tokens, 415 MB, 67 us: 90 % of the copy rate; one new
+// token of 64 rows in 28 layers 15 us, of which the pages' 68 MB 10).  Choice: the bounds' bytes (64 rows of 14k ragged
+// tokens in pages of 32: 72 MB of them in 12 us), and behind them a chain of about 6 us (row, length, query, numbers and bounds
+// of pages, the border, the list).  Scores in 64 bits throughout took 590 us there.
 #include <algorithm>
 
 #include "common.cuh"
