@@ -1513,7 +1513,9 @@ starkv_status attention_mass(starkv_state* st, const starkv_pages* pages, int32_
   p.step_h = kMassQueryStep % p.heads;
   p.step = kMassQueryStep / p.heads * p.q_token + p.step_h * p.q_head;
   p.wrap = p.q_token - p.heads * p.q_head;
-  p.span_from = blocks == 1 ? INT64_MAX : p.cut ? 16 * int64_t(st->num_sms) / blocks : 8 * int64_t(st->num_sms);
+  // Groups of four tiles, where every CTA then has two or more (blocks that stay) or four units (blocks that pass): the roles step
+  // from group to group (64 rows of one token 176 us, with a tile a group 183; 126 pairs 53 and 68)
+  p.span_from = p.cut ? 16 * int64_t(st->num_sms) / blocks : 8 * int64_t(st->num_sms);
   p.tree = tree;
   p.n_sink = std::min(n_sink, 1 << 25);   // (more than any length)
   p.window = std::min(window, 1 << 25);

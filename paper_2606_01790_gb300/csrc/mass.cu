@@ -16,12 +16,12 @@
 // units are cut into ranges, and the parts of a group that is cut (at most the first and the last of a range) are added up by
 // k_mass_sum in the order of the ranges: no atomics, the same sums every time.
 //
-// What bounds it.  Few queries: the stream of K (64 rows of one token over 14k ragged keys, 8 KV heads: 1.2 GB in 183 us, 97 % of
-// the copy rate).  26 drafted tokens of 32 rows: 64 to 66 us for a stream of 45, half of the SMs' time in weighing two blocks a tile.
+// What bounds it.  Few queries: the stream of K (64 rows of one token over 14k ragged keys, 8 KV heads: 1.2 GB in 176 us, the
+// copy rate).  26 drafted tokens of 32 rows: 63 us for a stream of 45, half of the SMs' time in weighing two blocks a tile.
 // Many: the products' operands (8 KB a step through shared memory, 64 cycles) and the accumulators' way out of tensor
 // memory; a chunk of 2,704 tokens under a window of 4,096, 81 GFLOP, 99 us, tensor pipe 52 % busy; without the weighing 67, with
 // everything in it but the exponentials 93.  Not kept: exponentials in part as polynomials on the FMA pipe (an eighth of them 104,
-// a quarter 109); one key loader (246 for 205 us in the first case) and one issuer of products (205 for 183); a look through the
+// a quarter 109); one key loader (246 for 205 us in the first case) and one issuer of products (205 for 183); groups of a tile each (183 for 176); a look through the
 // ring for the queries' next slot before their last block is handed over (230 for 218 in an earlier state of the chunk, since
 // asking a barrier may wait); weights unrolled over a block (212 for 162).
 //
@@ -93,6 +93,10 @@ __device__ __forceinline__ Item item_of(const MassParams& p, uint64_t x) {
   it.blocks = quotient(it.n + p.tpb - 1, p.inv_tpb) * p.chunks;
   return it;
 }
+
+// Units of a group whose blocks stay (one or two): what a launch of either took (4 and 7: 62.7 us for 32 rows of 13 to 26
+// drafted tokens, 2 and 3: 66.4).
+__device__ __forceinline__ int weight_of(int blocks) { return 3 * blocks + 1; }
 
 struct Start {
   int seq, g, s, b;
@@ -181,16 +185,16 @@ struct PieceIter {
     }
   }
   // the last group of this row and KV head that the range has
-  __device__ __forceinline__ bool last_of_head() const { return rem <= it.blocks + 1 || s + 1 == groups; }
+  __device__ __forceinline__ bool last_of_head() const { return rem <= weight_of(it.blocks) || s + 1 == groups; }
   __device__ __forceinline__ void next(const MassParams& p, const Ctl* ctl) {
-    rem -= p.cut ? max(1, b1 - b0) : it.blocks + 1;
+    rem -= p.cut ? max(1, b1 - b0) : weight_of(it.blocks);
     if (rem <= 0) return;
     if (++s == groups) head(p, ctl);
     take(p, 0);
   }
   // p.cut is 0: on to the next row or KV head
   __device__ __forceinline__ void skip_head(const MassParams& p, const Ctl* ctl) {
-    rem -= static_cast<int64_t>(groups - s) * (it.blocks + 1);
+    rem -= static_cast<int64_t>(groups - s) * weight_of(it.blocks);
     if (rem <= 0) return;
     head(p, ctl);
     take(p, 0);
@@ -250,8 +254,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
         atomicOr(p.err, kErrRow);
         ctl->before[i + 1] = 0;
       } else {
-        // (a tile takes about 1,500 cycles to load, and 1,100 for each block: whole groups of 2 or 3 units)
-        ctl->before[i + 1] = it.n > 0 ? static_cast<int64_t>(groups_of(it.L, span)) * (it.blocks + 1) : 0;
+        ctl->before[i + 1] = it.n > 0 ? static_cast<int64_t>(groups_of(it.L, span)) * weight_of(it.blocks) : 0;
       }
     }
   } else {
@@ -307,7 +310,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
       while ((st.g + 1) * heads <= off * p.G) ++st.g;
       off -= st.g * (heads / p.G);
       if (!p.cut) {   // the first group that begins in the range
-        const int each = it.blocks + 1, part = static_cast<int>(off % each);
+        const int each = weight_of(it.blocks), part = static_cast<int>(off % each);
         st.s = static_cast<int>(off / each) + (part > 0);
         fb += part ? each - part : 0;
         if (st.s == ng) {
