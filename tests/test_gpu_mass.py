@@ -323,3 +323,100 @@ def test_a_refused_eviction_changes_nothing():
     np.testing.assert_array_equal(mass.data.cpu().numpy(), data)
     c.check()
     st.close()
+
+
+def verify_on_device(c, qs, rows, counts, before, mass, seen_of):
+    """``verify`` with the definition in 64 bits on the device, for calls whose oracle would take minutes: seen_of(i, L, n) is [n][L]
+    there.  The same error is allowed."""
+    torch.cuda.synchronize()
+    sk.check_device_error(c.st)
+    G, hg, P = c.st.cfg.n_kv_heads, c.st.cfg.n_heads // c.st.cfg.n_kv_heads, c.ref.P
+    untouched = torch.from_numpy(before).cuda()
+    for i, (r, n) in enumerate(zip(rows, counts)):
+        L = int(c.ref.len[r])
+        if n == 0:
+            continue
+        untouched[0, r, :, :L] = mass.data[0, r, :, :L]
+        seen = seen_of(i, L, n)
+        pages = c.pages.table[r, :-(-L // P)].long()
+        for g in range(G):
+            k = c.pages.k[0, pages, g].reshape(-1, PH.D)[:L].double()
+            want = torch.from_numpy(before[0, r, g, :L]).cuda().double() * mass.decay
+            want[L - n:] = 0
+            off = 2.0**-23 * want.abs() + 1e-37
+            for h in range(g * hg, (g + 1) * hg):
+                q, lse = qs.q[i, :n, h].double(), qs.lse[i, :n, h].double()[:, None]
+                z = q @ k.T / np.sqrt(PH.D)
+                w = torch.where(seen, torch.exp(z - lse), 0.0)
+                dz = 130 * 2.0**-24 * (q.abs() @ k.abs().T) / np.sqrt(PH.D) + 2.0**-22 * (z.abs() + lse.abs())
+                want += w.sum(0)
+                off += (w * (dz * (1 + dz) + 2.0**-21 + (n * hg + 8) * 2.0**-24)).sum(0)
+            err = (mass.data[0, r, g, :L].double() - want).abs()
+            assert bool((err <= off).all()), (i, g, float((err / off).max()), int((err / off).argmax()))
+    assert torch.equal(untouched, mass.data)
+
+
+def normalisers_on_device(c, qs, rows, counts, seen_of):
+    G, hg, P = c.st.cfg.n_kv_heads, c.st.cfg.n_heads // c.st.cfg.n_kv_heads, c.ref.P
+    for i, (r, n) in enumerate(zip(rows, counts)):
+        L = int(c.ref.len[r])
+        if n:
+            seen = seen_of(i, L, n)
+            pages = c.pages.table[r, :-(-L // P)].long()
+            for g in range(G):
+                k = c.pages.k[0, pages, g].reshape(-1, PH.D)[:L].double()
+                z = torch.einsum("thd,jd->htj", qs.q[i, :n, g * hg:(g + 1) * hg].double(), k) / np.sqrt(PH.D)
+                qs.lse[i, :n, g * hg:(g + 1) * hg] = torch.where(seen, z, -torch.inf).logsumexp(-1).T.float()
+
+
+def sink_on_device(n_sink, window):
+    def seen(i, L, n):
+        j, pos = torch.arange(L, device="cuda"), torch.arange(L - n, L, device="cuda")[:, None]
+        return (j <= pos) & ((j < n_sink) | (j > pos - window))
+    return seen
+
+
+@pytest.mark.parametrize("P,heads,kv_heads,T,n_sink,window", [
+    (64, 28, 4, 1, 0, 1 << 20), (16, 28, 4, 1, 5, 700), (128, 28, 4, 18, 0, 1 << 20), (32, 28, 4, 30, 200, 900), (256, 8, 8, 3, 0, 100),
+    (64, 28, 4, 90, 3, 1 << 20), (16, 32, 8, 300, 1000, 200), (64, 12, 1, 700, 0, 64)])
+def test_mass_of_calls_with_many_tiles(P, heads, kv_heads, T, n_sink, window):
+    """Groups of four tiles, whole and cut, that begin and end anywhere in a range: rows of one to 23 tiles, some of whose groups no
+    token sees."""
+    rng = np.random.default_rng(T)
+    n = 120 // kv_heads
+    lens = [int(x) for x in rng.integers(max(T, 100), 3000, n)]
+    c = filled(lens, P=P, heads=heads, kv_heads=kv_heads, seed=T)
+    rows = [int(r) for r in rng.permutation(n)]
+    counts = [int(rng.integers(T // 2, T + 1)) if i else T for i in range(n)]
+    qs = queries(c, n, T, rows=c.ids(rows), n_tokens=c.ids(counts), scale=1.5)
+    seen = sink_on_device(n_sink, window)
+    normalisers_on_device(c, qs, rows, counts, seen)
+    before, mass = make_mass(c, 0.5)
+    sk.sink_mass(c.st, c.pages, 0, qs, n_sink, window, mass, c.ws)
+    verify_on_device(c, qs, rows, counts, before, mass, seen)
+    again = sk.Mass(torch.from_numpy(before).cuda(), 0.5)
+    sk.sink_mass(c.st, c.pages, 0, qs, n_sink, window, again, c.ws)
+    assert torch.equal(again.data, mass.data)
+    c.st.close()
+
+
+@pytest.mark.parametrize("P,heads,kv_heads,T", [(64, 28, 4, 26), (16, 28, 4, 64), (128, 8, 2, 9)])
+def test_mass_of_many_trees(P, heads, kv_heads, T):
+    rng = np.random.default_rng(T)
+    n = 30
+    lens = [int(x) for x in rng.integers(T, 3000, n)]
+    c = filled(lens, P=P, heads=heads, kv_heads=kv_heads, seed=T)
+    rows = [int(r) for r in rng.permutation(n)]
+    counts = [int(rng.integers(0, T + 1)) if i else T for i in range(n)]
+    masks = [random_tree(rng, m) for m in counts]
+    qs = queries(c, n, T, mask=words(masks, T), rows=c.ids(rows), n_tokens=c.ids(counts))
+
+    def seen(i, L, m):
+        out = torch.ones((m, L), dtype=torch.bool, device="cuda")
+        out[:, L - m:] = torch.tensor([[x >> j & 1 for j in range(m)] for x in masks[i]], device="cuda").bool()
+        return out
+    normalisers_on_device(c, qs, rows, counts, seen)
+    before, mass = make_mass(c, 0.9)
+    sk.tree_mass(c.st, c.pages, 0, qs, mass, c.ws)
+    verify_on_device(c, qs, rows, counts, before, mass, seen)
+    c.st.close()
