@@ -294,3 +294,45 @@ def test_sequences_that_do_not_fit_have_zero_outputs():
     some = sk.Queries(q=qs.q[good], o=qs.o[good], lse=qs.lse[good])
     verify(c, some, bounds, [0, 3], [5, 2], 1, 1, 3, chosen[good])
     c.st.close()
+
+
+@pytest.mark.parametrize("n_pages", [255, 257, 1026, 1027, 3000, 8194, 8195, 9500])
+@pytest.mark.parametrize("kind", ["spread", "equal", "steps", "odd"])
+def test_the_choice_among_many_pages(n_pages, kind):
+    """On either side of what a thread, a pass over bins and shared memory hold; scores apart, all equal, in a few steps, with
+    infinities and NaN among them."""
+    P, first, last, n_chosen = 16, 1, 1, 70
+    st = PH.state(layers=1, heads=4, kv_heads=2)
+    pages = sk.Pages(k=torch.zeros((1, n_pages, 2, P, PH.D), dtype=torch.bfloat16, device="cuda"),
+                     v=torch.zeros((1, n_pages, 2, P, PH.D), dtype=torch.bfloat16, device="cuda"),
+                     table=torch.randperm(n_pages, generator=torch.Generator().manual_seed(1)).to(torch.int32).cuda()[None],
+                     len=torch.tensor([n_pages * P - 3], dtype=torch.int32, device="cuda"),
+                     refs=torch.ones(n_pages, dtype=torch.int32, device="cuda"))
+    rng = np.random.default_rng(n_pages)
+    b = rng.standard_normal((n_pages, 2, 2, PH.D)).astype(np.float32)
+    if kind == "equal":
+        b[:] = b[:1]
+    if kind == "steps":
+        b[:] = b[:1]
+        b[:, :, 1, 3] = rng.integers(0, 3, (n_pages, 2))
+    if kind == "odd":
+        b[rng.integers(0, n_pages, 5), 0, 1, 7] = np.nan
+        b[rng.integers(0, n_pages, 5), 1, 1, 7] = np.inf
+        b[rng.integers(0, n_pages, 5), 1, 0, 8] = -np.inf
+    bounds = torch.from_numpy(b)[None].to(torch.bfloat16).cuda()
+    q = torch.from_numpy(rng.standard_normal((1, 1, 4, PH.D)).astype(np.float32)).to(torch.bfloat16).cuda()
+    q[..., 7:9] = 0.5
+    q[:, :, 0, 8] = -0.5
+    qs = sk.Queries(q=q, o=torch.empty_like(q))
+    chosen = torch.full((1, 1, 2, n_chosen), -5, dtype=torch.int32, device="cuda")
+    ws = sk.sparse_workspace(st, pages, 1, 1, n_chosen)
+    sk.sparse_attention(st, pages, 0, qs, bounds, first, last, n_chosen, ws, chosen_out=chosen)
+    torch.cuda.synchronize()
+    sk.check_device_error(st)
+    bf, order, x = bounds[0].float().cpu().numpy(), pages.table[0].cpu().numpy(), q.float().cpu().numpy()[0, 0]
+    for g in range(2):
+        up, down = (f(x[2 * g:2 * g + 2], 0).astype(np.float64).sum(0) for f in (np.maximum, np.minimum))
+        with np.errstate(invalid="ignore"):
+            score = bf[order, g, 1].astype(np.float64) @ up + bf[order, g, 0].astype(np.float64) @ down
+        assert chosen[0, 0, g].tolist() == O.choose_pages(score, first, last, n_chosen), g
+    st.close()
