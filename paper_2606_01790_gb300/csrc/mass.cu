@@ -17,13 +17,14 @@
 // k_mass_sum in the order of the ranges: no atomics, the same sums every time.
 //
 // What bounds it.  Few queries: the stream of K (64 rows of one token over 14k ragged keys, 8 KV heads: 1.2 GB in 176 us, the
-// copy rate).  26 drafted tokens of 32 rows: 63 us for a stream of 45, half of the SMs' time in weighing two blocks a tile.
+// copy rate).  26 drafted tokens of 32 rows: 59 us for a stream of 45, half of the SMs' time in weighing two blocks a tile.
 // Many: the products' operands (8 KB a step through shared memory, 64 cycles) and the accumulators' way out of tensor
 // memory; a chunk of 2,704 tokens under a window of 4,096, 81 GFLOP, 99 us, tensor pipe 52 % busy; without the weighing 67, with
 // everything in it but the exponentials 93.  Not kept: exponentials in part as polynomials on the FMA pipe (an eighth of them 104,
-// a quarter 109); one key loader (246 for 205 us in the first case) and one issuer of products (205 for 183); groups of a tile each (183 for 176); a look through the
-// ring for the queries' next slot before their last block is handed over (230 for 218 in an earlier state of the chunk, since
-// asking a barrier may wait); weights unrolled over a block (212 for 162).
+// a quarter 109); one key loader (246 for 205 us in the first case) and one issuer of products (205 for 183); groups of a tile
+// each (183 for 176); two weighing warpgroups (63 for 59 in the second case, 112 for 99 in the chunk, 175 for 176 in the first);
+// a look through the ring for the queries' next slot before their last block is handed over (230 for 218 in an earlier state of
+// the chunk, since asking a barrier may wait); weights unrolled over a block (212 for 162).
 //
 // Warp roles: 0 and 1 load keys, 2 and 3 issue products, 4 to 7 copy queries, the others weigh.
 #include <algorithm>
@@ -52,13 +53,13 @@ cudaLaunchConfig_t config(cudaLaunchAttribute* attr, dim3 grid, int threads, cud
 
 // ---------------------------------------------------------------- mass: units and their order
 
+constexpr int kKeySlots = 4, kQuerySlots = 2;     // rings; a tile of keys has an accumulator and a weighing warpgroup of its own
 constexpr int kMmaWarp = 2, kQueryWarp = 4, kSoftWarp = 8;   // (0 and 1: keys; 2 issuers; 4 query warps; the weighing warps)
-__host__ __device__ constexpr int threads_of(int groups) { return 32 * (kSoftWarp + 4 * groups); }
+constexpr int kWarps = kSoftWarp + 4 * kKeySlots, kThreads = 32 * kWarps;
 constexpr int kQueryThreads = 32 * (kSoftWarp - kQueryWarp);
 static_assert(kQueryThreads / 16 == kMassQueryStep && kQueryThreads >= kMassTile, "16 threads take a row of 256 bytes");
 constexpr int kTileBytes = kMassTile * 256;       // 128 keys x 128 bf16, or as many (token, head) pairs: 32 KB
 constexpr int kHalfBytes = kTileBytes / 2;
-constexpr int kKeySlots = 4, kQuerySlots = 2;     // rings; a tile of keys has an accumulator of its own
 constexpr int kExtraBytes = kMassTile * 32;       // 128 rows of 16 more elements: the step of the products that takes lse off
 constexpr int kOneBytes = 256;
 constexpr float kRootDim = 11.313708498984761f;   // sqrt(d)
@@ -225,11 +226,11 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
   const bool rivals = p.rows && p.n > 1;
   const uint32_t latched = tid == 0 ? *p.err : 0;   // (behind a refused call nothing is added)
   if (rivals) {
-    for (int i = tid; i < 2 * words; i += blockDim.x) named[i] = 0;
+    for (int i = tid; i < 2 * words; i += kThreads) named[i] = 0;
     __syncthreads();
   }
   int64_t tiles = 0;
-  for (int i = tid; i < p.n; i += blockDim.x) {
+  for (int i = tid; i < p.n; i += kThreads) {
     Item it;
     it.row = p.rows ? p.rows[i] : p.row0 + i;
     it.n = p.n_tokens ? p.n_tokens[i] : p.T;
@@ -247,7 +248,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
   __syncthreads();
   const int span = kTileShift + (ctl->end * p.G >= p.span_from ? kSpanShift : 0);
   if (!p.cut) {
-    for (int i = tid; i < p.n; i += blockDim.x) {
+    for (int i = tid; i < p.n; i += kThreads) {
       const Item it = item_of(p, ctl->item[i]);
       if (rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1)) {
         ctl->item[i] = 0;
@@ -258,7 +259,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
       }
     }
   } else {
-    for (int i = warp; i < p.n; i += blockDim.x / 32) {
+    for (int i = warp; i < p.n; i += kWarps) {
       const Item it = item_of(p, ctl->item[i]);
       const bool twice = rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1);
       const int ng = it.n > 0 && !twice ? groups_of(it.L, span) : 0;
@@ -694,47 +695,39 @@ __device__ __forceinline__ float weigh_bits(uint32_t addr, const uint64_t* bits,
   return sum;
 }
 
-// Weighing warpgroup `own` of GROUPS: tile number i is that of i modulo them, a key a thread.
-template <int GROUPS>
+// Weighing warpgroup `own`: every fourth tile, a key a thread.
 __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own, int quad, int lane) {
   const int r = quad * 32 + lane;
-  const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+  const uint32_t at = tmem + (static_cast<uint32_t>(quad * 32) << 16) + own * kMassTile;   // this warp's part of the accumulator
   Ring<kQuerySlots> q;
   uint32_t tile = 0;       // number of the next tile to come
-  uint32_t par = 0;        // bit a: parity of accumulator a's next use
+  uint32_t par = 0;        // parity of the accumulator's next use
   bool ok = true;
   int held = 0, slot0 = 0; // blocks of this row and KV head that stay, and the first one's slot
   for (PieceIter c(p, ctl); ok && c.valid(); c.next(p, ctl)) {
     const int nb = c.b1 - c.b0;
     const bool take = p.cut || held == 0;
     if (take) slot0 = q.at;
-    const int i0 = (own - tile) & (GROUPS - 1);   // tiles i0, i0 + GROUPS .. of the group are this warpgroup's
-    const int ctx = c.it.L - c.it.n, j0 = c.grp.k0 + i0 * kMassTile + r;
-    float* mass = p.mass.m + c.it.row * p.mass.row_stride + c.g * p.mass.group_stride + j0;
+    const int i = (own - tile) & (kKeySlots - 1);   // the group's tile that is this warpgroup's, if it has as many
+    const bool mine = i < c.grp.tiles;
+    const int ctx = c.it.L - c.it.n, k0 = c.grp.k0 + i * kMassTile + 32 * quad, k1 = k0 + 31, j = k0 + lane;
+    float* mass = p.mass.m + c.it.row * p.mass.row_stride + c.g * p.mass.group_stride + j;
     const bool whole = c.whole();
-    constexpr int kOwn = kKeySlots / GROUPS;
-    float sum[2] = {0.f, 0.f}, had[2] = {0.f, 0.f};
-    if (whole) {
-#pragma unroll
-      for (int u = 0; u < kOwn; ++u)
-        if (i0 + GROUPS * u < c.grp.tiles && j0 + GROUPS * u * kMassTile < ctx) had[u] = mass[GROUPS * u * kMassTile];
-    }
+    float sum = 0.f, had = 0.f;
+    if (mine && whole && j < ctx) had = *mass;
     for (int b = 0; b < nb; ++b) {
       const int slot = (slot0 + b) % kQuerySlots;
       if (take) {
         ok = warp_wait(ctl, &ctl->q_full[q.at], q.par, p.wait_ns);
         q.next();
       }
-      const Block blk(p, c.it.n, c.b0 + b);
-      const int first = ctx + blk.t0, end = ctx + min(blk.t0 + p.tpb, c.it.n) - 1;   // positions of the block's tokens
-#pragma unroll 1
-      for (int i = i0; i < c.grp.tiles; i += GROUPS) {
-        const uint32_t a = (tile + i) & (kKeySlots - 1);
-        ok = warp_wait(ctl, &ctl->s_full[a], par >> a & 1, p.wait_ns);
-        if (!ok) break;
+      ok = ok && (!mine || warp_wait(ctl, &ctl->s_full[own], par, p.wait_ns));
+      if (!ok) break;
+      if (mine) {
         tc_fence_after();
-        float w = 0.f;   // by the warp's 32 keys: seen by all of the block, by none, or by some
-        const int k0 = c.grp.k0 + i * kMassTile + 32 * quad, k1 = k0 + 31;
+        // by the warp's 32 keys: seen by all of the block, by none, or by some
+        const Block blk(p, c.it.n, c.b0 + b);
+        const int first = ctx + blk.t0, end = ctx + min(blk.t0 + p.tpb, c.it.n) - 1;   // positions of the block's tokens
         bool all, none = k0 >= c.it.L;
         if (p.tree) {
           all = k1 < ctx;
@@ -742,26 +735,24 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
           all = k1 <= first && (k1 < p.n_sink || k0 > end - p.window);
           none = none || k0 > end || (k0 >= p.n_sink && k1 <= first - p.window);
         }
-        const uint32_t at = lanes + a * kMassTile;
         if (all) {
-          w = weigh_block(at, p.scale2, blk.count);
+          sum += weigh_block(at, p.scale2, blk.count);
         } else if (p.tree) {
-          if (!none) w = weigh_bits(at, ctl->bits[slot], p.scale2, blk.count, k0 + lane, ctx, c.it.L);
+          if (!none) sum += weigh_bits(at, ctl->bits[slot], p.scale2, blk.count, j, ctx, c.it.L);
         } else if (!none) {
-          const int j = k0 + lane, nt = end - first + 1;
+          const int nt = end - first + 1;
           const int ta = min(max(j - first, 0), nt), tb = j < p.n_sink ? nt : min(max(j + p.window - first, 0), nt);
           const int per = nt > 1 ? p.heads : blk.count;   // columns of a token
-          w = weigh_columns(at, p.scale2, ta * per, tb * per, blk.count);
+          sum += weigh_columns(at, p.scale2, ta * per, tb * per, blk.count);
         }
-        if (i < GROUPS) sum[0] += w;
-        else sum[1] += w;
         tc_fence_before();
-        par ^= 1u << a;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctl->s_empty[a]);
+        par ^= 1;
       }
-      if (!ok) break;
-      if (p.cut && lane == 0) mbar_arrive(&ctl->q_empty[slot]);
+      __syncwarp();
+      if (lane == 0) {
+        if (mine) mbar_arrive(&ctl->s_empty[own]);
+        if (p.cut) mbar_arrive(&ctl->q_empty[slot]);
+      }
     }
     if (!ok) break;
     if (!p.cut) {
@@ -772,15 +763,10 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
         held = 0;
       }
     }
-#pragma unroll
-    for (int u = 0; u < kOwn; ++u) {
-      const int i = i0 + GROUPS * u;
-      if (i >= c.grp.tiles) break;
-      if (!whole)
-        p.part[(2 * static_cast<int64_t>(blockIdx.x) + (c.b0 == c.grp.lo)) * (kMassSpan * kMassTile) + i * kMassTile + r] = sum[u];
-      else if (j0 + GROUPS * u * kMassTile < c.it.L)
-        mass[GROUPS * u * kMassTile] = fmaf(p.decay, had[u], sum[u]);
-    }
+    if (mine && !whole)
+      p.part[(2 * static_cast<int64_t>(blockIdx.x) + (c.b0 == c.grp.lo)) * (kMassSpan * kMassTile) + i * kMassTile + r] = sum;
+    else if (mine && j < c.it.L)
+      *mass = fmaf(p.decay, had, sum);
     if (nb > 0) tile += c.grp.tiles;
   }
   if (!ok) fail(ctl, p.err);
@@ -788,8 +774,7 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
 
 }  // namespace
 
-template <int GROUPS>
-__global__ void __launch_bounds__(threads_of(GROUPS), 1) k_mass(const __grid_constant__ MassParams p) {
+__global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ MassParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sK = smem;                            // [slots][2 halves][128 keys][128 B]
@@ -807,7 +792,7 @@ __global__ void __launch_bounds__(threads_of(GROUPS), 1) k_mass(const __grid_con
     }
     for (int i = 0; i < kQuerySlots; ++i) {
       mbar_init(&ctl->q_full[i], kSoftWarp - kQueryWarp);
-      mbar_init(&ctl->q_empty[i], 2 + 4 * GROUPS);   // both issuers and every weighing warp
+      mbar_init(&ctl->q_empty[i], 2 + kWarps - kSoftWarp);   // both issuers and every weighing warp
     }
     mbar_init(&ctl->drain, 2);
     ctl->abort = 0;
@@ -836,7 +821,7 @@ __global__ void __launch_bounds__(threads_of(GROUPS), 1) k_mass(const __grid_con
   } else if (warp < kQueryWarp) {
     mma_loop(p, ctl, sK, sQ, sOne, sL, tmem, warp - kMmaWarp);
   } else if (warp >= kSoftWarp) {
-    weigh_loop<GROUPS>(p, ctl, tmem, (warp - kSoftWarp) >> 2, warp & 3, lane);
+    weigh_loop(p, ctl, tmem, (warp - kSoftWarp) >> 2, warp & 3, lane);
   } else if (warp >= kQueryWarp) {
     query_loop(p, ctl, sQ, sL, threadIdx.x - 32 * kQueryWarp);
   }
@@ -888,19 +873,14 @@ static_assert(kMaxTableRows / 4 <= kQuerySlots * kTileBytes, "the rows' bits fit
 }  // namespace
 
 cudaError_t mass_configure() {
-  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  const cudaError_t e = cudaFuncSetAttribute(k_mass<2>, attr, static_cast<int>(kSmemBytes));
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(k_mass<4>, attr, static_cast<int>(kSmemBytes));
+  return cudaFuncSetAttribute(k_mass, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
 }
 
 cudaError_t mass_launch(const MassParams& p, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
-  // four weighing warpgroups where a tile meets many blocks, two (and registers for the other roles) where it meets one or two:
-  // a chunk of 2,704 tokens 114 us and 131, one token of 64 rows 225 us and 205
-  const int groups = p.cut ? 4 : 2;
-  cudaLaunchConfig_t cfg = config(attr, dim3(p.grid), threads_of(groups), stream);
+  cudaLaunchConfig_t cfg = config(attr, dim3(p.grid), kThreads, stream);
   cfg.dynamicSmemBytes = kSmemBytes;
-  return cudaLaunchKernelEx(&cfg, groups == 4 ? k_mass<4> : k_mass<2>, p);
+  return cudaLaunchKernelEx(&cfg, k_mass, p);
 }
 
 cudaError_t mass_sum_launch(const MassParams& p, cudaStream_t stream) {
