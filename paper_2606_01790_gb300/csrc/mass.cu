@@ -16,8 +16,8 @@
 // units are cut into ranges, and the parts of a group that is cut (at most the first and the last of a range) are added up by
 // k_mass_sum in the order of the ranges: no atomics, the same sums every time.
 //
-// What bounds it.  Few queries: the stream of K (64 rows of one token over 14k ragged keys, 8 KV heads: 1.2 GB in 176 us, the
-// copy rate).  26 drafted tokens of 32 rows: 59 us for a stream of 45, half of the SMs' time in weighing two blocks a tile.
+// What bounds it.  Few queries: the stream of K (64 rows of one token over 14k ragged keys, 8 KV heads: 1.2 GB in 175 us, the
+// copy rate).  13 to 26 drafted tokens of 32 rows: 57 us for a stream of 45 (their exponentials, 16 a clock, 35).
 // Many: the products' operands (8 KB a step through shared memory, 64 cycles) and the accumulators' way out of tensor
 // memory; a chunk of 2,704 tokens under a window of 4,096, 81 GFLOP, 99 us, tensor pipe 52 % busy; without the weighing 67, with
 // everything in it but the exponentials 93.  Not kept: exponentials in part as polynomials on the FMA pipe (an eighth of them 104,
@@ -95,9 +95,9 @@ __device__ __forceinline__ Item item_of(const MassParams& p, uint64_t x) {
   return it;
 }
 
-// Units of a group whose blocks stay (one or two): what a launch of either took (4 and 7: 62.7 us for 32 rows of 13 to 26
-// drafted tokens, 2 and 3: 66.4).
-__device__ __forceinline__ int weight_of(int blocks) { return 3 * blocks + 1; }
+// Units of a group whose blocks stay (one or two), by what it takes.  32 rows of 13 to 26 drafted tokens: 6 and 11 56.6 us,
+// 1 and 2 57.0, 4 and 7 57.9, 2 and 3 62.5, 3 and 7 60.5.
+__device__ __forceinline__ int weight_of(int blocks) { return 5 * blocks + 1; }
 
 struct Start {
   int seq, g, s, b;
