@@ -893,12 +893,15 @@ cudaError_t mass_sum_launch(const MassParams& p, cudaStream_t stream) {
 
 namespace {
 
-constexpr int kSelThreads = 1024;
+constexpr int kSelThreads = 512;   // (1,024: one block an SM, 41 us for 35 in the 224 blocks of eight rows in 28 layers; 21 for 22 in
+                                   // the 112 of one row)
 constexpr int kSelWarps = kSelThreads / 32;
 constexpr int kSelKeys = 49152;    // keys that shared memory holds
+constexpr int kSelLoads = 8;       // masses of a thread and KV head on their way at once (one: 48 us for 41 there)
 constexpr int kSelMoves = 4;       // masses of a thread on their way at once
 constexpr int kSelBins = 2048;
 constexpr int kSelClose = 512;     // close tokens that are ranked by comparing each with each
+static_assert(kSelThreads >= kSelClose && kSelThreads >= 256 && kSelBins % kSelThreads == 0, "a thread a close token and a digit");
 
 // Ascending order as unsigned numbers; a NaN (a mass that is none) comes with infinity, so that its token
 // stays, and -0 is 0.
@@ -1042,17 +1045,32 @@ __global__ void __launch_bounds__(kSelThreads)
     __syncthreads();
     uint32_t size = 0, least = ~0u, most = 0;
     bool negative = false;
-#pragma unroll 8
-    for (int j = tid; j < Lp; j += kSelThreads) {
-      float a;
-      const float x = sum_of(j, &a);
-      const uint32_t k = order_key(x);
-      if (here) s.key[j] = k;
-      least = min(least, k);
-      most = max(most, k);
-      if (!PER_HEAD) {
-        size = max(size, __float_as_uint(a));   // (a NaN is above infinity)
-        negative = negative || a != x;          // (also where a sum is not a number)
+    for (int j0 = tid; j0 < Lp; j0 += kSelLoads * kSelThreads) {
+      float x[kSelLoads], a[kSelLoads];
+#pragma unroll
+      for (int u = 0; u < kSelLoads; ++u) {
+        x[u] = heads[min(j0 + u * kSelThreads, Lp - 1)];   // (behind the last token: the last one again)
+        a[u] = fabsf(x[u]);
+      }
+      if (!PER_HEAD)
+#pragma unroll 1
+        for (int g = 1; g < pg.G; ++g) {
+          float y[kSelLoads];
+#pragma unroll
+          for (int u = 0; u < kSelLoads; ++u) y[u] = mass[g * mv.group_stride + min(j0 + u * kSelThreads, Lp - 1)];
+#pragma unroll
+          for (int u = 0; u < kSelLoads; ++u) x[u] += y[u], a[u] += fabsf(y[u]);
+        }
+#pragma unroll
+      for (int u = 0; u < kSelLoads; ++u) {
+        const uint32_t k = order_key(x[u]);
+        if (here && j0 + u * kSelThreads < Lp) s.key[j0 + u * kSelThreads] = k;
+        least = min(least, k);
+        most = max(most, k);
+        if (!PER_HEAD) {
+          size = max(size, __float_as_uint(a[u]));   // (a NaN is above infinity)
+          negative = negative || a[u] != x[u];       // (also where a sum is not a number)
+        }
       }
     }
     least = __reduce_min_sync(kFull, least);
@@ -1091,7 +1109,8 @@ __global__ void __launch_bounds__(kSelThreads)
     }
     const uint32_t first = least + (static_cast<uint32_t>(s.bin) << shift);
     uint32_t bottom = first, top = min(most, first + ((1u << shift) - 1));   // keys that the budget-th greatest lies between
-    const int run = (Lp + kSelThreads - 1) / kSelThreads, from = min(tid * run, Lp), to = min(from + run, Lp);   // of a thread
+    const int run = ((Lp + kSelThreads - 1) / kSelThreads) | 1;   // tokens of a thread (odd: no two of a warp in one bank)
+    const int from = min(tid * run, Lp), to = min(from + run, Lp);
     // A second round, with the budget-th greatest itself, where the bin holds more tokens than are compared one by one.
 #pragma unroll 1
     for (bool again = false;; again = true) {
