@@ -616,7 +616,7 @@ def _c_queries(st: State, pages: Pages, qs: Queries, weigh: bool = False) -> byt
         raise ValueError("queries: q is [n, T, H, d], o of the same shape")
     n, T, H, d = q.shape
     s0, s1, s2, s3 = q.stride()
-    o0, o1, o2, o3 = o.stride()
+    o0, o1, o2, o3 = (s0, s1, s2, s3) if weigh else o.stride()
     if H != st.cfg.n_heads or d != st.cfg.head_dim or s3 != 1 or o3 != 1:
         raise ValueError("queries: q and o are [n, T, H, d] with d contiguous")
     if q.dtype is not torch.bfloat16 or o.dtype is not torch.bfloat16:
@@ -754,6 +754,10 @@ def sink_attention(st: State, pages: Pages, layer: int, queries: Queries, n_sink
 
 # ---------------------------------------------------------------- attention mass, chosen pages
 
+_MASS = struct.Struct("@P3qf4x")
+assert _MASS.size == C.sizeof(CMass)
+
+
 class Mass:
     """What each cached token has had of the queries' attention (``starkv_mass``).  The tensor is checked once, when the
     object is made, and stays its own.
@@ -762,16 +766,22 @@ class Mass:
     decay  factor of what a token has had so far, when a call adds to it
     """
 
-    __slots__ = ("_data", "_decay", "_packed")
+    __slots__ = ("_data", "_decay", "_packed", "_shape")
 
     def __init__(self, data: torch.Tensor, decay: float = 1.0):
         if data.dim() != 4 or data.stride(3) != 1:
             raise ValueError("mass: data is [n_layers, n_rows, G, tokens] with the tokens contiguous")
         _expect(torch.float32, data)
         self._data, self._decay = data, float(decay)
+        layers, rows, groups, tokens = data.shape
+        self._shape = layers, rows, groups, tokens
+        s0, s1, s2, _ = data.stride()
         # (an axis of one entry is never stepped along: its stride may be any)
-        strides = [s if n > 1 else data.shape[3] for n, s in zip(data.shape[:3], data.stride()[:3])]
-        self._packed = bytes(CMass(data.data_ptr(), *strides, self._decay))
+        words = (data.data_ptr(), s0 if layers > 1 else tokens, s1 if rows > 1 else tokens, s2 if groups > 1 else tokens)
+        try:
+            self._packed = _MASS.pack(*words, self._decay)
+        except OverflowError:      # (past 32 bits: infinity, which the calls refuse)
+            self._packed = bytes(CMass(*words, self._decay))
 
     data = property(lambda self: self._data)
     decay = property(lambda self: self._decay)
@@ -785,11 +795,11 @@ def make_mass(st: State, pages: Pages, decay: float = 1.0) -> Mass:
 
 
 def _c_mass(st: State, pages: Pages, mass: Mass) -> bytes:
-    data = mass._data
-    if data.shape[:3] != (st.cfg.n_layers, pages.table.shape[0], st.cfg.n_kv_heads) \
-            or data.shape[3] < pages.table.shape[1] * pages.k.shape[3]:
+    layers, rows, groups, tokens = mass._shape
+    n_rows, max_pages = pages.table.shape
+    if layers != st.cfg.n_layers or rows != n_rows or groups != st.cfg.n_kv_heads or tokens < max_pages * pages.k.shape[3]:
         raise ValueError("mass: data is [n_layers, n_rows, G, max_pages * page_size or more]")
-    _on(pages, data)
+    _on(pages, mass._data)
     return mass._packed
 
 

@@ -213,3 +213,13 @@ def test_a_masss_tensor_is_checked_once_and_stays_its_own():
         m.decay = 1.0
     got = sk.CMass.from_buffer_copy(sk._c_mass(_State(), _pages(), m))
     assert (got.mass, got.layer_stride, got.row_stride, got.group_stride, got.decay) == (m.data.data_ptr(), 768, 256, 64, 0.5)
+
+
+@pytest.mark.parametrize("decay", [0, 0.98, float("inf"), 1e300])
+def test_a_packed_mass_is_the_struct(decay):
+    data = torch.zeros((2, 3, 4, 70))[:, 1:]
+    c = sk.CMass.from_buffer_copy(sk.Mass(data, decay)._packed)
+    assert (c.mass, c.layer_stride, c.row_stride, c.group_stride) == (data.data_ptr(), 3 * 4 * 70, 4 * 70, 70)
+    assert c.decay == ctypes.c_float(decay).value      # (past 32 bits: infinity, which the calls refuse)
+    one = sk.CMass.from_buffer_copy(sk.Mass(torch.zeros((1, 1, 1, 70)).expand(1, 1, 1, 70), decay)._packed)
+    assert (one.layer_stride, one.row_stride, one.group_stride) == (70, 70, 70)
