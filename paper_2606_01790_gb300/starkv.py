@@ -754,8 +754,8 @@ def sink_attention(st: State, pages: Pages, layer: int, queries: Queries, n_sink
 
 # ---------------------------------------------------------------- attention mass, chosen pages
 
-_MASS = struct.Struct("@P3qf4x")
-assert _MASS.size == C.sizeof(CMass)
+_MASS, _BOUNDS = struct.Struct("@P3qf4x"), struct.Struct("@P2q")
+assert _MASS.size == C.sizeof(CMass) and _BOUNDS.size == C.sizeof(CBounds)
 
 
 class Mass:
@@ -837,13 +837,15 @@ def make_bounds(st: State, pages: Pages) -> torch.Tensor:
 
 
 def _c_bounds(st: State, pages: Pages, bounds: torch.Tensor) -> bytes:
-    G, d = st.cfg.n_kv_heads, st.cfg.head_dim
-    if tuple(bounds.shape) != (st.cfg.n_layers, pages.k.shape[1], G, 2, d) or bounds.stride()[2:] != (2 * d, d, 1):
+    layers, n_pages, G, _, d = shape = (st.cfg.n_layers, pages.k.shape[1], st.cfg.n_kv_heads, 2, st.cfg.head_dim)
+    strides = bounds.stride()
+    if bounds.shape != shape or strides[2:] != (2 * d, d, 1):
         raise ValueError("bounds: [n_layers, n_pages, G, 2, d], a page of a layer contiguous")
     _expect(torch.bfloat16, bounds)
     _on(pages, bounds)
-    strides = [s if n > 1 else 2 * G * d for n, s in zip(bounds.shape[:2], bounds.stride()[:2])]
-    return bytes(CBounds(bounds.data_ptr(), *strides))
+    # (an axis of one entry is never stepped along: its stride may be any)
+    page = 2 * G * d
+    return _BOUNDS.pack(bounds.data_ptr(), strides[0] if layers > 1 else page, strides[1] if n_pages > 1 else page)
 
 
 def pages_bounds(st: State, pages: Pages, layer0: int, n_layers: int, bounds: torch.Tensor, T: int,
@@ -872,8 +874,8 @@ def sparse_attention(st: State, pages: Pages, layer: int, queries: Queries, boun
     _on(pages, ws, chosen_out)
     if chosen_out is not None:
         _expect(torch.int32, chosen_out)
-        n, T = queries.q.shape[:2]
-        if tuple(chosen_out.shape) != (n, T, st.cfg.n_kv_heads, n_chosen):
+        n, T, _, _ = queries.q.shape
+        if chosen_out.shape != (n, T, st.cfg.n_kv_heads, n_chosen):
             raise ValueError("chosen_out: [n, T, G, n_chosen]")
     _check(lib().starkv_sparse_attention(st.handle, c, layer, q, b, n_first, n_last, n_chosen, _ptr(chosen_out), _ptr(ws), ws.numel(),
                                          _stream_on(pages, stream)))
