@@ -420,3 +420,35 @@ def test_mass_of_many_trees(P, heads, kv_heads, T):
     sk.tree_mass(c.st, c.pages, 0, qs, mass, c.ws)
     verify_on_device(c, qs, rows, counts, before, mass, seen)
     c.st.close()
+
+
+@pytest.mark.parametrize("per_head", [False, True])
+def test_eviction_of_many_lengths_at_once(per_head):
+    """Lengths about a block's threads and rounds, and about what it keeps of its keys, in one call."""
+    past = [2, 511, 512, 513, 1024, 4095, 4096, 4097, 16384, 49151, 49152, 49153]
+    P, window = 128, 4
+    budgets = [1, 510, 256, 512, 1, 2047, 2048, 4096, 5000, 20000, 49151, 700]
+    lens = [x + window for x in past]
+    need = [-(-x // P) for x in lens]
+    st = PH.state(layers=1, heads=4, kv_heads=2, window=window, select_mode=int(per_head))
+    c = PH.Pair(st, n_pages=sum(need) + sum(-(-(b + window) // P) for b in budgets), P=P, n_rows=len(past), max_pages=max(need))
+    c.extend(list(range(len(past))), lens)
+    rng = np.random.default_rng(7)
+    data, mass = make_mass(c, 1.0)
+    data[:] = rng.random(data.shape)
+    data[:, ::2] = np.round(data[:, ::2] * 256) / 256       # (many equal ones in every other row)
+    mass.data.copy_(torch.from_numpy(data))
+    n = 2 if per_head else 1
+    idx = [torch.full((1, n, b), -7, dtype=torch.int32, device="cuda") for b in budgets]
+    sk.pages_evict(st, c.pages, None, [sk.Seq(L=L, budget=b, idx=i) for L, b, i in zip(lens, budgets, idx)], mass, c.ws)
+    keep, want = [], data.copy()
+    for r, (x, b, L) in enumerate(zip(past, budgets, lens)):
+        m = data[0, r, :, :x].astype(np.float64)
+        keep.append(np.stack([[O.heaviest(y, b) for y in (m if per_head else m.sum(0, keepdims=True))]]))
+        at = np.concatenate([keep[-1][0], np.broadcast_to(np.arange(x, L), (n, window))], -1)
+        want[0, r, :, :b + window] = np.take_along_axis(data[0, r], np.broadcast_to(at, (2, b + window)), -1)
+        np.testing.assert_array_equal(idx[r].cpu().numpy(), keep[-1], err_msg=str(x))
+    np.testing.assert_array_equal(mass.data.cpu().numpy(), want)
+    c.ref.compact(list(range(len(past))), lens, keep, window)
+    c.check()
+    st.close()
