@@ -17,6 +17,7 @@
 // of pages, the border, the list).  Scores in 64 bits throughout took 590 us there.
 #include <algorithm>
 
+#include "bounds_task.cuh"
 #include "common.cuh"
 #include "ptx.cuh"
 #include "sparse.cuh"
@@ -65,15 +66,12 @@ __global__ void __launch_bounds__(kBoundsThreads) k_page_bounds(const __grid_con
   const PagesView& pg = p.pg;
   const int lane = threadIdx.x & 31, half = lane >> 4, hl = lane & 15;
   const int P = 1 << pg.shift;
-  const int most = ((p.T + P - 2) >> pg.shift) + 1;   // pages that T tokens may lie in
-  const int64_t per_seq = static_cast<int64_t>(most) * p.nlayers * pg.G, ntask = per_seq * p.n;
+  const int most = bounds_pages(p.T, pg.shift, pg.max_pages);
+  const int64_t ntask = static_cast<int64_t>(most) * p.nlayers * pg.G * p.n;
   for (int64_t task = static_cast<int64_t>(blockIdx.x) * kBoundsWarps + (threadIdx.x >> 5); task < ntask;
        task += static_cast<int64_t>(gridDim.x) * kBoundsWarps) {
-    const int seq = static_cast<int>(task / per_seq);
-    int rem = static_cast<int>(task - seq * per_seq);
-    const int g = rem % pg.G;
-    rem /= pg.G;
-    const int j = rem % most, l = rem / most;
+    const BoundsTask of(task, most, p.nlayers, pg.G);
+    const int seq = of.seq, g = of.g, l = of.layer;
     const int row = p.rows ? p.rows[seq] : seq;
     const int count = p.n_tokens ? p.n_tokens[seq] : p.T;
     const int L = row >= 0 && row < pg.n_rows ? pg.len[row] : -1;
@@ -81,7 +79,7 @@ __global__ void __launch_bounds__(kBoundsThreads) k_page_bounds(const __grid_con
       if (lane == 0) atomicOr(p.err, kErrRow);
       continue;
     }
-    const int at = ((L - count) >> pg.shift) + j;   // the page's place in the row
+    const int at = ((L - count) >> pg.shift) + of.page;   // the page's place in the row
     const int fill = min(P, L - (at << pg.shift));
     if (count == 0 || fill <= 0) continue;
     const int page = pg.table[static_cast<int64_t>(row) * pg.max_pages + at];
@@ -125,8 +123,7 @@ __global__ void __launch_bounds__(kBoundsThreads) k_page_bounds(const __grid_con
 }
 
 cudaError_t page_bounds_launch(const BoundsParams& p, int num_sms, cudaStream_t stream) {
-  const int P = 1 << p.pg.shift;
-  const int64_t tasks = static_cast<int64_t>(((p.T + P - 2) >> p.pg.shift) + 1) * p.nlayers * p.pg.G * p.n;
+  const int64_t tasks = static_cast<int64_t>(bounds_pages(p.T, p.pg.shift, p.pg.max_pages)) * p.nlayers * p.pg.G * p.n;
   if (tasks <= 0) return cudaSuccess;
   const int64_t blocks = (tasks + kBoundsWarps - 1) / kBoundsWarps;
   cudaLaunchAttribute attr[1];
