@@ -695,6 +695,11 @@ __device__ __forceinline__ float weigh_bits(uint32_t addr, const uint64_t* bits,
   return sum;
 }
 
+// Whether token j of a row lies in a page that is one.  (Keys of another are loaded as zeros, and their tokens' mass is left alone.)
+__device__ __forceinline__ bool in_a_page(const MassParams& p, int row, int j) {
+  return static_cast<uint32_t>(p.table[static_cast<int64_t>(row) * p.max_pages + (j >> p.shift)]) < static_cast<uint32_t>(p.n_pages);
+}
+
 // Weighing warpgroup `own`: every fourth tile, a key a thread.
 __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own, int quad, int lane) {
   const int r = quad * 32 + lane;
@@ -714,7 +719,11 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
     float* mass = p.mass.m + c.it.row * p.mass.row_stride + c.g * p.mass.group_stride + j;
     const bool whole = c.whole();
     float sum = 0.f, had = 0.f;
-    if (mine && whole && j < ctx) had = *mass;
+    bool paged = true;
+    if (mine && whole && j < c.it.L) {
+      paged = in_a_page(p, c.it.row, j);
+      if (j < ctx) had = *mass;
+    }
     for (int b = 0; b < nb; ++b) {
       const int slot = (slot0 + b) % kQuerySlots;
       if (take) {
@@ -765,8 +774,10 @@ __device__ void weigh_loop(const MassParams& p, Ctl* ctl, uint32_t tmem, int own
     }
     if (mine && !whole)
       p.part[(2 * static_cast<int64_t>(blockIdx.x) + (c.b0 == c.grp.lo)) * (kMassSpan * kMassTile) + i * kMassTile + r] = sum;
-    else if (mine && j < c.it.L)
-      *mass = fmaf(p.decay, had, sum);
+    else if (mine && j < c.it.L) {
+      if (paged) *mass = fmaf(p.decay, had, sum);
+      else atomicOr(p.err, kErrRow);
+    }
     if (nb > 0) tile += c.grp.tiles;
   }
   if (!ok) fail(ctl, p.err);
@@ -855,6 +866,7 @@ __global__ void __launch_bounds__(kMassSpan * kMassTile) k_mass_sum(const __grid
   const int row = p.rows ? p.rows[s.seq] : p.row0 + s.seq;
   const int n = p.n_tokens ? p.n_tokens[s.seq] : p.T;
   const int L = p.len[row], j = s.k0 + threadIdx.x;
+  if (!in_a_page(p, row, j)) return;   // (reported when its keys were loaded)
   float* mass = p.mass.m + row * p.mass.row_stride + s.g * p.mass.group_stride + j;
   const float had = j < L - n ? *mass : 0.f;
   float sum = 0.f;
