@@ -570,7 +570,8 @@ starkv_status starkv_sparse_workspace_bytes(const starkv_state* st, const starkv
  * can be.  Their order is that of 64 bits; equal ones: the lower page; a NaN counts as +infinity.
  * n_first >= 0, n_last >= 1, n_first + n_last <= n_chosen.  chosen (i32 [n][T][G][n_chosen],
  * or NULL) gets the pages' places in the row, ascending, -1 behind them.  o and lse are those of
- * the keys attended over, as for the calls above. */
+ * the keys attended over, as for the calls above.  A page that is none (device error) scores 0,
+ * and its K and V count as zeros where it is taken. */
 starkv_status starkv_sparse_attention(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
                                       const starkv_bounds* bounds, int32_t n_first, int32_t n_last, int32_t n_chosen, int32_t* chosen,
                                       void* workspace, size_t workspace_bytes, void* stream);

@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_page_choose(const __grid_con
     cluster_wait();
     const uint32_t first_cta = dsmem_map(s.key, 0);
     for (int j0 = lo + own; j0 < hi; j0 += per) {
+      if (j0 + (lane & 7) < hi && (id < 0 || id >= pg.n_pages)) atomicOr(p.err, kErrRow);   // (its score is 0)
       uint4 x[kPagesAtOnce];
 #pragma unroll
       for (int u = 0; u < kPagesAtOnce; ++u) {
