@@ -519,7 +519,8 @@ typedef struct {
  * nothing, whatever it holds.  A sequence that does not fit, or a row that two sequences
  * with queries name, is left as it is (device error), and so are the tokens of a page
  * that is none; also every row behind a refused call (as for the calls that change a
- * pool).  T and T * H / G as for the attention. */
+ * pool).  After STARKV_ERR_TIMEOUT some tokens of the layer have their mass after the call
+ * and the others that before it.  T and T * H / G as for the attention. */
 starkv_status starkv_tree_mass(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,
                                const starkv_mass* mass, void* workspace, size_t workspace_bytes, void* stream);
 starkv_status starkv_sink_mass(starkv_state* st, const starkv_pages* pages, int32_t layer, const starkv_queries* queries,

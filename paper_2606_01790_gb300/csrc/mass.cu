@@ -848,9 +848,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
         s.keys = min(c.grp.tiles * kMassTile, c.it.L - c.grp.k0);
         s.last = range_of(ctl->end + (c.grp.hi - c.b1) - 1, ctl->before[p.n], ctl->ranges);
       }
+    s.failed = 0;
     p.split[blockIdx.x] = s;
   }
   __syncthreads();
+  if (threadIdx.x == 0 && p.cut && ctl->abort) p.split[blockIdx.x].failed = 1;
   if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
@@ -858,6 +860,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
 }
 
 // Adds up the parts of the groups that ranges cut, in the order of the ranges: block c has the one that range c began.
+// Where one of these ranges was given up, the group's tokens keep their mass (a part that was not written holds anything).
 __global__ void __launch_bounds__(kMassSpan * kMassTile) k_mass_sum(const __grid_constant__ MassParams p) {
   griddep_launch_dependents();
   griddep_wait();
@@ -870,9 +873,12 @@ __global__ void __launch_bounds__(kMassSpan * kMassTile) k_mass_sum(const __grid
   float* mass = p.mass.m + row * p.mass.row_stride + s.g * p.mass.group_stride + j;
   const float had = j < L - n ? *mass : 0.f;
   float sum = 0.f;
-  for (int c = blockIdx.x; c <= s.last; ++c)
+  int failed = 0;
+  for (int c = blockIdx.x; c <= s.last; ++c) {
     sum += p.part[(2 * static_cast<int64_t>(c) + (c == static_cast<int>(blockIdx.x))) * (kMassSpan * kMassTile) + threadIdx.x];
-  *mass = fmaf(p.decay, had, sum);
+    failed |= p.split[c].failed;
+  }
+  if (!failed) *mass = fmaf(p.decay, had, sum);
 }
 
 namespace {
