@@ -112,6 +112,7 @@ struct Ctl {
   volatile int abort;
   int span;             // log2 of the keys of a group
   int ranges;
+  int held;             // 1: a call was refused before this CTA looked (on another stream CTAs may differ), its range is empty
   int64_t begin, end;   // this CTA's range
   Start start;
   uint64_t bits[kQuerySlots][kMassTile];   // tree: drafted tokens that the pairs of a block see
@@ -342,8 +343,10 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
         }
       }
     }
-    if (__shfl_sync(kFull, latched, 0) & kErrHeld) fb = fe;
+    const bool held = __shfl_sync(kFull, latched, 0) & kErrHeld;
+    if (held) fb = fe;
     if (lane == 0) {
+      ctl->held = held;
       ctl->start = st;
       ctl->span = span;
       ctl->ranges = R;
@@ -848,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_mass(const __grid_constant__ Ma
         s.keys = min(c.grp.tiles * kMassTile, c.it.L - c.grp.k0);
         s.last = range_of(ctl->end + (c.grp.hi - c.b1) - 1, ctl->before[p.n], ctl->ranges);
       }
-    s.failed = 0;
+    s.failed = ctl->held;
     p.split[blockIdx.x] = s;
   }
   __syncthreads();

@@ -17,7 +17,7 @@ constexpr int kMassSpan = 4;     // tiles of a group, at most
 constexpr int kMassQueryStep = 8;   // rows of a query block that are copied at a time
 
 // The group that a CTA's range begins and does not finish: the ranges up to `last` hold the rest.  `failed`: a wait of this
-// CTA ran out, and its parts may not be there.
+// CTA ran out, or it was held back, and its parts may not be there.
 struct MassSplit {
   int valid, seq, g, k0, keys, last, failed, pad_;
 };
