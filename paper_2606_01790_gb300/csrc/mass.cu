@@ -8,7 +8,7 @@
 // sum crosses lanes, and a key that holds NaN or garbage touches nothing but its own.  A tile of 128 keys (A) meets blocks of up
 // to 128 pairs (B), nine K = 16 steps: eight of q . k, and one of three ones against -lse sqrt(d) in three bf16 parts (24 bits),
 // after which a weight is exp2 of the accumulator times one constant: no normaliser has to be fetched for each
-// element (from shared memory they took as much of its path as the accumulators: 112 us for 99 below).
+// element (from shared memory they took as much of its path as the accumulators: a chunk, see below, 112 us for 99).
 //
 // Work split.  A group is one tile or four (512 keys) of one row and KV head.  Where a call has one or two blocks of queries
 // they stay in shared memory while a row's keys pass once; groups go whole to contiguous ranges, one a CTA (persistent
@@ -16,12 +16,13 @@
 // units are cut into ranges, and the parts of a group that is cut (at most the first and the last of a range) are added up by
 // k_mass_sum in the order of the ranges: no atomics, the same sums every time.
 //
-// What bounds it.  Few queries: the stream of K (64 rows of one token over 14k ragged keys, 8 KV heads: 1.2 GB in 175 us, the
-// copy rate).  13 to 26 drafted tokens of 32 rows: 57 us for a stream of 45 (their exponentials, 16 a clock, 35).
-// Many: the products' operands (8 KB a step through shared memory, 64 cycles) and the accumulators' way out of tensor
-// memory; a chunk of 2,704 tokens under a window of 4,096, 81 GFLOP, 99 us, tensor pipe 52 % busy; without the weighing 67, with
-// everything in it but the exponentials 93.  Not kept: exponentials in part as polynomials on the FMA pipe (an eighth of them 104,
-// a quarter 109); one key loader (246 for 205 us in the first case) and one issuer of products (205 for 183); groups of a tile
+// What bounds it.  Few queries: the stream of K (64 rows of one token over 14k ragged keys, 8 KV heads: 1.2 GB in 176 to 184 us,
+// the copy rate).  13 to 26 drafted tokens of 32 rows: 57 us for a stream of 45, beside the weighing (its exponentials, of which
+// an SM takes 32 a clock, 17).  Many: the products' operands (8 KB a step, 90 to 97 cycles at what shared memory delivers, where
+// the tensor core takes 64), and the weighing between them, since a tile has one accumulator, which its next products wait
+// for.  A chunk of 2,704 tokens under a window of 4,096, 81 GFLOP: 97 us, tensor pipe 54 % busy (at 99 us: without the weighing 67,
+// with everything in it but the exponentials 93).  Not kept: exponentials in part as polynomials on the FMA pipe (an eighth of them
+// 104, a quarter 109); one key loader (246 for 205 us in the first case) and one issuer of products (205 for 183); groups of a tile
 // each (183 for 176); two weighing warpgroups (63 for 59 in the second case, 112 for 99 in the chunk, 175 for 176 in the first);
 // a look through the ring for the queries' next slot before their last block is handed over (230 for 218 in an earlier state of
 // the chunk, since asking a barrier may wait); weights unrolled over a block (212 for 162).
@@ -96,7 +97,7 @@ __device__ __forceinline__ Item item_of(const MassParams& p, uint64_t x) {
 }
 
 // Units of a group whose blocks stay (one or two), by what it takes.  32 rows of 13 to 26 drafted tokens: 6 and 11 56.6 us,
-// 1 and 2 57.0, 4 and 7 57.9, 2 and 3 62.5, 3 and 7 60.5.
+// 1 and 2 57.0, 4 and 7 57.9, 2 and 3 62.5, 3 and 7 60.5 (of one case: between the first two it decides nothing).
 __device__ __forceinline__ int weight_of(int blocks) { return 5 * blocks + 1; }
 
 struct Start {
@@ -233,7 +234,7 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
   int64_t tiles = 0;
   for (int i = tid; i < p.n; i += kThreads) {
     Item it;
-    it.row = p.rows ? p.rows[i] : p.row0 + i;
+    it.row = p.rows ? p.rows[i] : i;
     it.n = p.n_tokens ? p.n_tokens[i] : p.T;
     it.L = it.row >= 0 && it.row < p.n_rows ? p.len[it.row] : -1;
     if (it.n < 0 || it.n > p.T || (it.n > 0 && (it.L < it.n || it.L > static_cast<int64_t>(p.max_pages) << p.shift))) {
@@ -264,7 +265,9 @@ __device__ void plan(const MassParams& p, Ctl* ctl, uint32_t* named) {
       const Item it = item_of(p, ctl->item[i]);
       const bool twice = rivals && it.n > 0 && (named[words + (it.row >> 5)] >> (it.row & 31) & 1);
       const int ng = it.n > 0 && !twice ? groups_of(it.L, span) : 0;
-      int u = 0;   // (32,768 groups of 1,041 blocks at most)
+      // (below 2^26: 2^15 groups of four tiles at most, of one tile only where all units are few, and 2,032 blocks, of 1,016 tokens
+      // with 129 heads a group; T H / G is no more than 2^17)
+      int u = 0;
       for (int s = lane; s < ng; s += 32) u += Group(p, it, span, s).units();
       u = __reduce_add_sync(kFull, u);
       if (lane == 0) {
@@ -869,7 +872,7 @@ __global__ void __launch_bounds__(kMassSpan * kMassTile) k_mass_sum(const __grid
   griddep_wait();
   const MassSplit s = p.split[blockIdx.x];
   if (!s.valid || static_cast<int>(threadIdx.x) >= s.keys) return;
-  const int row = p.rows ? p.rows[s.seq] : p.row0 + s.seq;
+  const int row = p.rows ? p.rows[s.seq] : s.seq;
   const int n = p.n_tokens ? p.n_tokens[s.seq] : p.T;
   const int L = p.len[row], j = s.k0 + threadIdx.x;
   if (!in_a_page(p, row, j)) return;   // (reported when its keys were loaded)

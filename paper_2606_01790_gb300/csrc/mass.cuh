@@ -31,9 +31,9 @@ struct MassParams {
   const __nv_bfloat16* q;
   const float* lse;         // [n][T][H]
   const uint64_t* mask;     // tree: [n][T]
-  const int32_t* rows;      // [n], or NULL = row0, row0 + 1, ...
+  const int32_t* rows;      // [n], or NULL = 0, 1, ...
   const int32_t* n_tokens;  // [n], or NULL
-  int row0, n, T;
+  int n, T;
   int64_t q_seq, q_token, q_head;
   int H, G, hg;             // hg = H / G
   int tpb, heads, chunks;   // tokens and heads of a block; blocks that the heads of a group take

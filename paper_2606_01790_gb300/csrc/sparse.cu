@@ -11,9 +11,9 @@
 // the lower page.  Which of two pages is taken hangs on the last bit of their scores, which
 // are those of 64 bits.
 //
-// What bounds them.  Bounds: the keys' bytes, read once (28 layers of 14,032 tokens, 415 MB, 67 us: 90 % of the copy rate; one new
+// What bounds them.  Bounds: the keys' bytes, read once (28 layers of 14,032 tokens, 415 MB, 66 us: 93 % of the copy rate; one new
 // token of 64 rows in 28 layers 15 us, of which the pages' 68 MB 10).  Choice: the bounds' bytes (64 rows of 14k ragged
-// tokens in pages of 32: 72 MB of them in 12 us), and behind them a chain of about 6 us (row, length, query, numbers and bounds
+// tokens in pages of 32: 72 MB of them in 12 us), and behind them a chain of about 10 us (row, length, query, numbers and bounds
 // of pages, the border, the list).  Scores in 64 bits throughout took 590 us there.
 #include <algorithm>
 
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kBoundsThreads) k_page_bounds(const __grid_con
   }
 }
 
-cudaError_t page_bounds_launch(const BoundsParams& p, int num_sms, cudaStream_t stream) {
+cudaError_t page_bounds_launch(const BoundsParams& p, cudaStream_t stream) {
   const int64_t tasks = static_cast<int64_t>(bounds_pages(p.T, p.pg.shift, p.pg.max_pages)) * p.nlayers * p.pg.G * p.n;
   if (tasks <= 0) return cudaSuccess;
   const int64_t blocks = (tasks + kBoundsWarps - 1) / kBoundsWarps;

@@ -22,7 +22,7 @@ struct BoundsParams {
   uint32_t* err;
 };
 
-cudaError_t page_bounds_launch(const BoundsParams& p, int num_sms, cudaStream_t stream);
+cudaError_t page_bounds_launch(const BoundsParams& p, cudaStream_t stream);
 
 // Query v of a call's n * T: its position in its row.
 struct SparseQuery {
