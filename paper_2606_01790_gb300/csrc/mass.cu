@@ -450,9 +450,11 @@ __device__ void key_loop(const MassParams& p, Ctl* ctl, uint8_t* sK, int half, i
     }
   }
   if (!ok) fail(ctl, p.err);
-  // every issued copy completes before the CTA can exit
+  // Every issued copy completes before the CTA can exit.  (Where the other key warp gave up first, its share of a slot never
+  // comes and the barrier does not complete: once the limit has passed all copies have had that time.)
+  bool in_time = true;
   for (int i = 0; i < kKeySlots; ++i)
-    if (used >> i & 1) mbar_wait(&ctl->k_full[i], last_par >> i & 1, drain_limit(p.wait_ns));
+    if (in_time && (used >> i & 1)) in_time = mbar_wait(&ctl->k_full[i], last_par >> i & 1, drain_limit(p.wait_ns));
   __syncwarp();
 }
 

@@ -46,7 +46,7 @@ def test_masses_of_a_call_whose_waits_run_out():
     torch.cuda.synchronize()
     took = time.perf_counter() - t0
     assert sk.device_error_status(st) == sk.ERR_TIMEOUT
-    assert took < 30                     # (the copies in flight at the end are waited for: 2 s each at most)
+    assert took < 6                      # (the copies in flight at the end of a CTA are waited for, 2 s at most)
     was, new = mass.data == before, mass.data == after
     assert bool((was | new).all()), int((~(was | new)).sum())
     assert not bool(new.all())

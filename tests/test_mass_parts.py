@@ -18,3 +18,9 @@ def test_a_cta_that_gave_up_says_so_when_its_roles_are_done():
     assert body.index("p.split[blockIdx.x] = s;") < body.rindex("__syncthreads();") < body.index(after)
     total = functions("mass.cu")["k_mass_sum"]
     assert total.index("failed |= p.split[c].failed;") < total.index("if (!failed) *mass")
+
+
+def test_the_key_loaders_wait_for_all_of_their_copies_together():
+    """A slot whose other half never comes has no end to wait for: the limit is one for all slots, as the header says."""
+    body = functions("mass.cu")["key_loop"]
+    assert "if (in_time && (used >> i & 1)) in_time = mbar_wait(&ctl->k_full[i]," in body
